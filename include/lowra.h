@@ -321,6 +321,48 @@ lowra_status lowra_lora_forward_adapters(const lowra_layout* layout, const uint8
                                          int32_t r, float s, uint16_t* Y_dev, void* workspace_dev, size_t workspace_bytes,
                                          void* stream);
 
+/*
+ * (No counterpart in the paper.)  The layer as it stands in a model: what follows the product is applied to its fp32 sums, in the kernel that forms them.
+ *     Z = X . deq(Wq)^T + s * (X . A) . B + bias;    H = act(Z);    Y = H * multiply + residual
+ * Everything in fp32; Y is rounded to bf16 once, and so is the copy of Z that lowra_epilogue_backward reads.
+ *   bias_dev      [N], bf16 (bias_bf16 != 0) or fp32, or NULL
+ *   activation    lowra_activation
+ *   multiply_dev  bf16 [M, N], or NULL: the other factor of a gated layer (the up projection's output, for a gate with SiLU)
+ *   residual_dev  bf16 [M, N], or NULL
+ *   pre_dev       bf16 [M, N] (out), or NULL: Z
+ * Arrays 16-byte aligned, row-major, without gaps, rows as in Y.  Y may be the residual itself (the residual stream, added to in place) or the multiplied
+ * array; else Y and pre overlap nothing that the call reads or writes (a pre that is Y, multiply or residual -> LOWRA_ERR_SHAPE).
+ * One epilogue belongs to one member; the array of epilogues is host memory and is read before the call returns.
+ *   lowra_lora_forward_epilogue           as lowra_lora_forward (few tokens included)
+ *   lowra_lora_forward_batch_epilogue     as lowra_lora_forward_batch: epilogues_host[count], one for every member
+ *   lowra_lora_forward_adapters_epilogue  as lowra_lora_forward_adapters: one epilogue for all M rows (the bias is the base model's)
+ * Errors: as those calls; a NULL epilogue -> LOWRA_ERR_NULL, an activation that is none -> LOWRA_ERR_SHAPE, an array not 16-byte aligned -> LOWRA_ERR_ALIGN.
+ */
+typedef enum {
+    LOWRA_ACT_NONE = 0,
+    LOWRA_ACT_RELU = 1,
+    LOWRA_ACT_GELU = 2,        /* z Phi(z) */
+    LOWRA_ACT_GELU_TANH = 3,   /* z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) */
+    LOWRA_ACT_SILU = 4         /* z / (1 + exp(-z)) */
+} lowra_activation;
+typedef struct {
+    const void* bias_dev;
+    const uint16_t* multiply_dev;
+    const uint16_t* residual_dev;
+    uint16_t* pre_dev;
+    int32_t activation;
+    int32_t bias_bf16;
+} lowra_epilogue;
+lowra_status lowra_lora_forward_epilogue(const lowra_layout* layout, const uint8_t* packed_dev, const float* absmax_dev, const float* maps_dev,
+                                         const uint16_t* X_dev, int32_t M, const uint16_t* A_dev, const uint16_t* B_dev, int32_t r, float s,
+                                         const lowra_epilogue* epilogue_host, uint16_t* Y_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+lowra_status lowra_lora_forward_batch_epilogue(const lowra_member* members_host, const lowra_epilogue* epilogues_host, int32_t count, int32_t M, int32_t r,
+                                               float s, void* workspace_dev, size_t workspace_bytes, void* stream);
+lowra_status lowra_lora_forward_adapters_epilogue(const lowra_layout* layout, const uint8_t* packed_dev, const float* absmax_dev, const float* maps_dev,
+                                                  int32_t n_adapters, const uint16_t* X_dev, int32_t M, const int32_t* group_start_host,
+                                                  const uint16_t* A_dev, const uint16_t* B_dev, int32_t r, float s, const lowra_epilogue* epilogue_host,
+                                                  uint16_t* Y_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+
 /* Bytes of device scratch that lowra_lora_backward_adapters needs for M tokens and rank r (0 if the
  * arguments are invalid).  The first 256 bytes hold the device status word. */
 size_t lowra_adapter_workspace_bytes(int32_t M, int32_t r);

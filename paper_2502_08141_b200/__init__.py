@@ -39,7 +39,8 @@ EXPORTS = (
     "lowra_learn_codebooks_all", "lowra_lora_forward_adapters", "lowra_batch_workspace_bytes",
     "lowra_lora_forward_batch", "lowra_lora_backward_input_batch", "lowra_lora_backward_adapters_reuse",
     "lowra_workspace_projection", "lowra_set_wait_limit", "lowra_diag_wait_expiry", "lowra_diag_drop_t_flags",
-    "lowra_encode_group", "lowra_decode_group", "lowra_diag_choose",
+    "lowra_encode_group", "lowra_decode_group", "lowra_diag_choose", "lowra_lora_forward_epilogue",
+    "lowra_lora_forward_batch_epilogue", "lowra_lora_forward_adapters_epilogue",
 )
 
 
@@ -75,6 +76,11 @@ class _CMember(ctypes.Structure):
                 ("B_dev", ctypes.c_void_p), ("out_dev", ctypes.c_void_p)]
 
 
+class _CEpilogue(ctypes.Structure):
+    _fields_ = [("bias_dev", ctypes.c_void_p), ("multiply_dev", ctypes.c_void_p), ("residual_dev", ctypes.c_void_p), ("pre_dev", ctypes.c_void_p),
+                ("activation", ctypes.c_int32), ("bias_bf16", ctypes.c_int32)]
+
+
 _lib = None
 _py_calls = None    # the products' and the gradients' native way (csrc/py_calls.cpp), loaded with the library
 
@@ -93,7 +99,7 @@ def _load_py_calls(L: ctypes.CDLL):
     address = lambda fn: ctypes.cast(fn, ctypes.c_void_p).value  # noqa: E731
     module.bind(*(address(fn) for fn in (L.lowra_lora_forward, L.lowra_lora_backward_input, L.lowra_workspace_bytes, L.lowra_workspace_init, L.lowra_lora_forward_batch,
                                          L.lowra_lora_backward_input_batch, L.lowra_lora_backward_adapters, L.lowra_lora_backward_adapters_reuse,
-                                         L.lowra_adapter_workspace_bytes, L.lowra_workspace_projection)))
+                                         L.lowra_adapter_workspace_bytes, L.lowra_workspace_projection, L.lowra_lora_forward_epilogue)))
     return module
 
 
@@ -142,6 +148,13 @@ def lib() -> ctypes.CDLL:
         L.lowra_lora_forward_batch.restype = ctypes.c_int
         L.lowra_lora_backward_input_batch.argtypes = batch_args
         L.lowra_lora_backward_input_batch.restype = ctypes.c_int
+        ep = ctypes.POINTER(_CEpilogue)
+        L.lowra_lora_forward_epilogue.argtypes = gemm_args[:10] + [ep] + gemm_args[10:]
+        L.lowra_lora_forward_epilogue.restype = ctypes.c_int
+        L.lowra_lora_forward_batch_epilogue.argtypes = batch_args[:1] + [ep] + batch_args[1:]
+        L.lowra_lora_forward_batch_epilogue.restype = ctypes.c_int
+        L.lowra_lora_forward_adapters_epilogue.argtypes = [lp, vp, vp, vp, i32, vp, i32, vp, vp, vp, i32, ctypes.c_float, ep, vp, vp, ctypes.c_size_t, vp]
+        L.lowra_lora_forward_adapters_epilogue.restype = ctypes.c_int
         L.lowra_lora_forward_static.argtypes = [lp, vp, vp, vp, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp, vp]
         L.lowra_lora_forward_static.restype = ctypes.c_int
         L.lowra_learn_codebooks.argtypes = [lp, vp, vp, vp, i32, vp, vp, vp]
@@ -563,13 +576,75 @@ def lowra_lora_forward(layout: Layout, packed, absmax, maps, X, A, B, s: float,
     return Y
 
 
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _activation(name: str) -> int:
+    number = ACTIVATIONS.get(name)
+    if number is None:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}, got {name!r}")
+    return number
+
+
+def _epilogue(M: int, N: int, bias, activation, multiply, residual, pre, to: Optional[_CEpilogue] = None) -> _CEpilogue:
+    """The C description of what stands behind a product of M tokens and N channels, its arrays checked."""
+    e = _CEpilogue() if to is None else to
+    if bias is not None:
+        _here(bias, "bias")
+        if bias.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"bias must be {torch.bfloat16} or {torch.float32}, got {bias.dtype}")
+        if tuple(bias.shape) != (N,) or not bias.is_contiguous():
+            raise ValueError(f"bias must be a contiguous [{N}], got {tuple(bias.shape)}")
+    for t, name in ((multiply, "multiply"), (residual, "residual"), (pre, "pre")):
+        if t is not None:
+            _dev(t, _BF16, name)
+            if tuple(t.shape) != (M, N):
+                raise ValueError(f"{name} must be [{M}, {N}], got {tuple(t.shape)}")
+    e.bias_dev, e.multiply_dev, e.residual_dev, e.pre_dev = _ptr(bias), _ptr(multiply), _ptr(residual), _ptr(pre)
+    e.activation, e.bias_bf16 = _activation(activation), int(bias is not None and bias.dtype == _BF16)
+    return e
+
+
+def lowra_lora_forward_epilogue(layout: Layout, packed, absmax, maps, X, A, B, s: float, bias: Optional[torch.Tensor] = None, activation: str = "none",
+                                multiply: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None,
+                                Y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The layer as it stands in a model: Z = X . deq(Wq)^T + s (X . A) . B + bias, Y = act(Z) * multiply + residual, in the kernels that form the product.
+    bias bf16 or fp32 [N]; activation "none", "relu", "gelu", "gelu_tanh" or "silu"; multiply (a gated layer's other factor) and residual bf16 [M, N], the
+    latter may be Y itself; pre: bf16 [M, N] that receives Z, for lowra_epilogue_backward."""
+    number = _activation(activation)
+    if stream is None and _py_calls is not None:
+        done = _py_calls.forward_epilogue(layout.address, layout.device_index, packed, absmax, maps, X, A, B, s, Y, workspace, bias, number, multiply, residual, pre)
+        if done is not None:
+            if done.__class__ is int:
+                _check(done, "lowra_lora_forward_epilogue")
+            return done
+    _dev(X, _BF16, "X")
+    _dev(A, _BF16, "A")
+    _dev(B, _BF16, "B")
+    M, r = X.shape[0], A.shape[1]
+    if X.shape != (M, layout.K) or A.shape != (layout.K, r) or B.shape != (r, layout.N):
+        raise ValueError("shape mismatch")
+    _weight_arrays(layout, packed, absmax, maps)
+    _extent(Y, M * layout.N, "Y", _BF16)
+    _extent(workspace, 0, "workspace")
+    behind = _epilogue(M, layout.N, bias, activation, multiply, residual, pre)
+    if Y is None:
+        Y = X.new_empty((M, layout.N))
+    if workspace is None:
+        workspace = _workspace(layout, M, r, X.device, stream)
+    code = lib().lowra_lora_forward_epilogue(layout.ref, _ptr(packed), _ptr(absmax), _ptr(maps), _ptr(X), M, _ptr(A), _ptr(B), r, s, ctypes.byref(behind),
+                                             _ptr(Y), _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(code, "lowra_lora_forward_epilogue")
+    return Y
+
+
 def lowra_batch_workspace_bytes(layout: Layout, count: int, M: int, r: int) -> int:
     return int(lib().lowra_batch_workspace_bytes(layout.ref, int(count), int(M), int(r)))
 
 
-def _batch(fn_name: str, members, s: float, workspace: torch.Tensor, backward: bool, stream=None):
-    """members: sequence of dicts with layout, packed, absmax, maps, act, A, B, out (device tensors)."""
-    if stream is None and _py_calls is not None:
+def _batch(fn_name: str, members, s: float, workspace: torch.Tensor, backward: bool, stream=None, epilogue: bool = False):
+    """members: sequence of dicts with layout, packed, absmax, maps, act, A, B, out (device tensors), and with an epilogue those of _epilogue."""
+    if stream is None and _py_calls is not None and not epilogue:
         done = _py_calls.batch(backward, members, s, workspace)
         if done is not None:
             if done.__class__ is int:
@@ -577,6 +652,7 @@ def _batch(fn_name: str, members, s: float, workspace: torch.Tensor, backward: b
             return done
     n = len(members)
     arr = (_CMember * n)()
+    behind = (_CEpilogue * n)()
     M = int(members[0]["act"].shape[0])
     r = int(members[0]["A"].shape[1])
     for i, m in enumerate(members):
@@ -591,11 +667,13 @@ def _batch(fn_name: str, members, s: float, workspace: torch.Tensor, backward: b
         if (tuple(m["act"].shape) != (M, act_cols) or tuple(m["out"].shape) != (M, out_cols) or
                 tuple(m["A"].shape) != (lay.K, r) or tuple(m["B"].shape) != (r, lay.N)):
             raise ValueError("shape mismatch in member %d" % i)
+        if epilogue:
+            _epilogue(M, lay.N, m.get("bias"), m.get("activation", "none"), m.get("multiply"), m.get("residual"), m.get("pre"), behind[i])
         arr[i].layout = ctypes.pointer(lay.c)
         arr[i].packed_dev, arr[i].absmax_dev, arr[i].maps_dev = m["packed"].data_ptr(), m["absmax"].data_ptr(), m["maps"].data_ptr()
         arr[i].act_dev, arr[i].A_dev, arr[i].B_dev, arr[i].out_dev = (m["act"].data_ptr(), m["A"].data_ptr(), m["B"].data_ptr(),
                                                                      m["out"].data_ptr())
-    code = getattr(lib(), fn_name)(arr, n, M, r, s, _ptr(workspace), workspace.numel(), _stream(stream))
+    code = getattr(lib(), fn_name)(arr, *((behind,) if epilogue else ()), n, M, r, s, _ptr(workspace), workspace.numel(), _stream(stream))
     _check(code, fn_name)
     return [m["out"] for m in members]
 
@@ -604,6 +682,12 @@ def lowra_lora_forward_batch(members, s: float, workspace: torch.Tensor, stream=
     """Several weights of one shape in one launch: Y_i = X_i deq(Wq_i)^T + s (X_i A_i) B_i.  `members`: dicts with
     layout (carrying a deal), packed, absmax, maps, act (X_i), A, B, out (Y_i).  Returns the outputs."""
     return _batch("lowra_lora_forward_batch", members, s, workspace, False, stream)
+
+
+def lowra_lora_forward_batch_epilogue(members, s: float, workspace: torch.Tensor, stream=None):
+    """lowra_lora_forward_batch with what stands behind each product: the members' dicts may also have bias, activation, multiply, residual and pre, as the
+    arguments of lowra_lora_forward_epilogue."""
+    return _batch("lowra_lora_forward_batch_epilogue", members, s, workspace, False, stream, True)
 
 
 def lowra_lora_backward_input_batch(members, s: float, workspace: torch.Tensor, stream=None):
@@ -616,6 +700,18 @@ def lowra_lora_forward_adapters(layout: Layout, packed, absmax, maps, X, group_s
                                 stream=None) -> torch.Tensor:
     """Several adapters on one quantised base weight: maps fp32 [n, N, 16], A bf16 [n, K, r], B bf16 [n, r, N];
     adapter a owns the token rows group_start[a] .. group_start[a + 1] of X (host sequence of n + 1 ints)."""
+    return _adapters(layout, packed, absmax, maps, X, group_start, A, B, s, Y, workspace, stream, None)
+
+
+def lowra_lora_forward_adapters_epilogue(layout: Layout, packed, absmax, maps, X, group_start, A, B, s: float, bias: Optional[torch.Tensor] = None,
+                                         activation: str = "none", multiply: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                                         pre: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
+                                         workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """lowra_lora_forward_adapters with what stands behind the product (the base model's bias, the same for all), as in lowra_lora_forward_epilogue."""
+    return _adapters(layout, packed, absmax, maps, X, group_start, A, B, s, Y, workspace, stream, (bias, activation, multiply, residual, pre))
+
+
+def _adapters(layout: Layout, packed, absmax, maps, X, group_start, A, B, s: float, Y, workspace, stream, behind) -> torch.Tensor:
     n, M, r = int(maps.shape[0]), int(X.shape[0]), int(A.shape[2])
     if not _fits(layout.device_index, X, "h", 0, A, "h", 0, B, "h", 0, maps, "f", 0, packed, "B", layout.packed_bytes, absmax, "f", layout.n_absmax,
                  Y, "h", M * layout.N, workspace, "B", 0):
@@ -635,10 +731,11 @@ def lowra_lora_forward_adapters(layout: Layout, packed, absmax, maps, X, group_s
         Y = X.new_empty((M, layout.N))
     if workspace is None:
         workspace = _workspace(layout, M, r, X.device, stream)
-    code = lib().lowra_lora_forward_adapters(layout.ref, _ptr(packed), _ptr(absmax), _ptr(maps), n, _ptr(X), M,
-                                             gs.ctypes.data_as(ctypes.c_void_p), _ptr(A), _ptr(B), r, s,
-                                             _ptr(Y), _ptr(workspace), workspace.numel(), _stream(stream))
-    _check(code, "lowra_lora_forward_adapters")
+    name = "lowra_lora_forward_adapters" if behind is None else "lowra_lora_forward_adapters_epilogue"
+    epilogue = () if behind is None else (ctypes.byref(_epilogue(M, layout.N, *behind)),)
+    code = getattr(lib(), name)(layout.ref, _ptr(packed), _ptr(absmax), _ptr(maps), n, _ptr(X), M, gs.ctypes.data_as(ctypes.c_void_p), _ptr(A), _ptr(B), r, s,
+                                *epilogue, _ptr(Y), _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(code, name)
     return Y
 
 

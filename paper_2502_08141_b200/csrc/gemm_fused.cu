@@ -166,7 +166,8 @@ struct Seg {
 // share (t_split or w_split above one), which long calls have none of: their loops pay for the code (512-token tiles by 1.5 to 2 % in the forward pass).
 template <int MODE, int NB, bool SHARED>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMaps<NB> TM) {
+fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMaps<NB> TM, const __grid_constant__ KEpilogues<MODE, NB> EP) {
+    constexpr bool kForward = MODE == kModeForward || MODE == kModeEpilogue;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     constexpr int CL = kCluster;
     constexpr uint32_t SW = kSlotsW, SX = kSlotsX;
@@ -382,9 +383,9 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                                 } else if (t.is_t) {
                                     // this CTA's 64 ranks (zeros past the rank): forward 64 features x 64 ranks from A [K, r],
                                     // backward 64 ranks x 64 channels from B [r, N]
-                                    if (MODE == kModeForward) ptx::tma_load_2d_pair(w_s, &tm.tmFt, (int)crank * 64, c0, bar);
+                                    if (kForward) ptx::tma_load_2d_pair(w_s, &tm.tmFt, (int)crank * 64, c0, bar);
                                     else ptx::tma_load_2d_pair(w_s, &tm.tmFt, c0, (int)crank * 64, bar);
-                                } else if (MODE == kModeForward) {   // channels x ranks from B [r, N]: two 64-channel boxes
+                                } else if (kForward) {   // channels x ranks from B [r, N]: two 64-channel boxes
                                     ptx::tma_load_2d_pair(w_s, &tm.tmFl, r0, c0, bar);
                                     ptx::tma_load_2d_pair(w_s + 8192, &tm.tmFl, r0 + 64, c0, bar);
                                 } else {                             // features x ranks from A [K, r], K-major: one 64 x 128 box
@@ -452,7 +453,7 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                             // factor tiles, fetched from A [K, r] (T tiles) and B [r, N] (LoRA blocks); backward - the
                             // dequantised weights.  16 contraction indices are 32 bytes further in a K-major tile, 2 KB in
                             // an MN-major one.
-                            const bool mn = MODE != kModeDense && (MODE == kModeForward ? !weights : weights);
+                            const bool mn = MODE != kModeDense && (kForward ? !weights : weights);
                             const uint64_t adesc = adesc0 + here * (kSmemSlot >> 4);
                             const uint64_t bdesc = (mn ? wmn0 : wk0) + ws * (kSmemSlot >> 4);
                             const uint32_t bstep = mn ? 128u : 2u, id = idesc | (mn ? kIdescBmn : 0u);
@@ -539,6 +540,31 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
                         if (j < left) dst[j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+                }
+            };
+            // 16 rows of one token from the tile's row c0 on, with what stands behind the product.  (16, not 32: the sums, a row of the residual and the
+            // activation's intermediate values have 72 registers between them.)
+            auto put16 = [&](int tok, int c0, uint32_t (&v)[16]) {
+                if constexpr (MODE == kModeEpilogue) {
+                    const size_t at = (size_t)tok * P.ld_out + r0 + c0;
+                    uint32_t o[8];
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        if (8 * g >= cols - c0) break;
+                        float z[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(v[8 * g + j]);
+                        const uint4 y = finish8(EP.m[t.prob], r0 + c0 + 8 * g, at + 8 * g, z);
+                        o[4 * g] = y.x; o[4 * g + 1] = y.y; o[4 * g + 2] = y.z; o[4 * g + 3] = y.w;
+                    }
+                    uint16_t* dst = P.mem[t.prob].out + at;
+                    if (P.out_align == 32 && cols - c0 >= 16) {
+                        ptx::st_global_v8(dst, o);
+                    } else {
+#pragma unroll
+                        for (int g = 0; g < 2; ++g)
+                            if (8 * g < cols - c0) *reinterpret_cast<uint4*>(dst + 8 * g) = make_uint4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+                    }
                 }
             };
             // publish this CTA's tokens of T, resp. its half of the cluster's partial tile: the writers meet, and one thread's
@@ -629,20 +655,35 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                             const int u = k + (2 * st + ch) * S, h = u / per_half, c0 = (u - h * per_half) * width;
                             const int tok = t.m0 + h * kHalfT + (int)crank * 128 + my_tok;
                             const float* ring = reinterpret_cast<const float*>(x_ring) + (size_t)(((st % ahead) * 2 + ch) * (S - 1)) * (kSmemSlot / 4) + my_tok;
-                            uint32_t v[32];
-                            ptx::tmem_ld_32x32(tmem_lane + ((hc + (uint32_t)h) & 1u) * (uint32_t)kPairR + (uint32_t)c0, v);
-                            ptx::tmem_ld_wait();
-                            for (int c = 1; c < S; ++c, ring += kSmemSlot / 4) {
+                            if (MODE == kModeEpilogue && !t.is_t) {
+#pragma unroll 1
+                                for (int e = 0; e < 32; e += 16) {
+                                    uint32_t v[16];
+                                    ptx::tmem_ld_32x16(tmem_lane + ((hc + (uint32_t)h) & 1u) * (uint32_t)kPairR + (uint32_t)(c0 + e), v);
+                                    ptx::tmem_ld_wait();
+                                    const float* from = ring + e * 128;
+                                    for (int c = 1; c < S; ++c, from += kSmemSlot / 4) {
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[j * 128]);
-                                if (width == 32) {
-#pragma unroll
-                                    for (int j = 16; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[j * 128]);
+                                        for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + from[j * 128]);
+                                    }
+                                    if (tok < M && c0 + e < cols) put16(tok, c0 + e, v);
                                 }
-                            }
-                            if (tok < M) {
-                                if (t.is_t) put_t(tok, c0, 16, v);
-                                else put(P.mem[t.prob].out + (size_t)tok * P.ld_out + r0 + c0, cols - c0, v);
+                            } else {
+                                uint32_t v[32];
+                                ptx::tmem_ld_32x32(tmem_lane + ((hc + (uint32_t)h) & 1u) * (uint32_t)kPairR + (uint32_t)c0, v);
+                                ptx::tmem_ld_wait();
+                                for (int c = 1; c < S; ++c, ring += kSmemSlot / 4) {
+#pragma unroll
+                                    for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[j * 128]);
+                                    if (width == 32) {
+#pragma unroll
+                                        for (int j = 16; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[j * 128]);
+                                    }
+                                }
+                                if (tok < M) {
+                                    if (t.is_t) put_t(tok, c0, 16, v);
+                                    else put(P.mem[t.prob].out + (size_t)tok * P.ld_out + r0 + c0, cols - c0, v);
+                                }
                             }
                         }
                         if (st + ahead < steps) {
@@ -690,15 +731,30 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                     const int h = s / 4, c0 = ch * 128 + (s & 3) * 32;
                     const int tok = t.m0 + h * kHalfT + (int)crank * 128 + my_tok;
                     if (!ptx::mbar_wait_warp(&bars->part_full[s % kPartSteps], (uint32_t)(s / kPartSteps) & 1u, abort_flag, wait_ns)) bars->abort = 1u;
-                    uint32_t v[32];
-                    ptx::tmem_ld_32x32(tmem_lane + ((hc + (uint32_t)h) & 1u) * (uint32_t)kPairR + (uint32_t)c0, v);
-                    ptx::tmem_ld_wait();
                     const float* ring = reinterpret_cast<const float*>(x_ring) + (size_t)((s % ahead) * pieces + ch) * (kSmemSlot / 4) + my_tok;
-                    for (int c = 0; c < nc; ++c) {
+                    const uint32_t from = tmem_lane + ((hc + (uint32_t)h) & 1u) * (uint32_t)kPairR + (uint32_t)c0;
+                    if constexpr (MODE == kModeEpilogue) {
+#pragma unroll 1
+                        for (int e = 0; e < 32; e += 16) {
+                            uint32_t v[16];
+                            ptx::tmem_ld_32x16(from + (uint32_t)e, v);
+                            ptx::tmem_ld_wait();
+                            for (int c = 0; c < nc; ++c) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[(size_t)(2 * c) * (kSmemSlot / 4) + j * 128]);
+                                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[(size_t)(2 * c) * (kSmemSlot / 4) + (e + j) * 128]);
+                            }
+                            if (tok < M && c0 + e < cols) put16(tok, c0 + e, v);
+                        }
+                    } else {
+                        uint32_t v[32];
+                        ptx::tmem_ld_32x32(from, v);
+                        ptx::tmem_ld_wait();
+                        for (int c = 0; c < nc; ++c) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[(size_t)(2 * c) * (kSmemSlot / 4) + j * 128]);
+                        }
+                        if (tok < M && c0 < cols) put(P.mem[t.prob].out + (size_t)tok * P.ld_out + r0 + c0, cols - c0, v);
                     }
-                    if (tok < M && c0 < cols) put(P.mem[t.prob].out + (size_t)tok * P.ld_out + r0 + c0, cols - c0, v);
                     if (s + ahead < steps) {
                         if (agree_abort()) { failed = true; break; }     // everybody has read the step's pieces: their place is filled again
                         if (et == 0) fetch(s + ahead);
@@ -715,6 +771,19 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                 if (!ptx::mbar_wait_warp(&bars->tmem_full[acc], (hc >> 1) & 1u, abort_flag, wait_ns)) bars->abort = 1u;
                 if (agree_abort()) { failed = true; break; }
                 ptx::tc_fence_after();
+                if constexpr (MODE == kModeEpilogue) {
+                    if (!t.is_t && !t.part) {
+#pragma unroll 1
+                        for (int c0 = c_first; c0 < c_last && any; c0 += 16) {
+                            uint32_t v[16];
+                            ptx::tmem_ld_32x16(taddr + (uint32_t)c0, v);
+                            ptx::tmem_ld_wait();
+                            if (tok < M) put16(tok, c0, v);
+                        }
+                        release(acc);
+                        continue;
+                    }
+                }
 #pragma unroll 1
                 for (int c0 = c_first; c0 < c_last && any; c0 += c_step) {
                     uint32_t v[32];
@@ -795,7 +864,7 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                     if (!stage_free(it)) { failed = true; bars->abort = 1u; break; }
                     publish(it % SW);
                 }
-            } else if (MODE == kModeForward) {
+            } else if (kForward) {
                 // ---------------------------------------------------------------- forward
                 // The operand tile of a stage is [128 channels][64 input features], K-major: a channel's
                 // 64-element absmax block is one 128-byte row.  Warp q of a group holds rows 32 q .. 32 q + 31
@@ -1072,7 +1141,7 @@ static lowra_status prepare_fused(cudaLaunchConfig_t& cfg, int* max_clusters) {
 }
 
 template <int MODE, int NB>
-static lowra_status launch_mode(const GemmParams& G, const BatchMaps& TM, cudaStream_t stream) {
+static lowra_status launch_mode(const GemmParams& G, const BatchMaps& TM, const Epilogue* epilogues, cudaStream_t stream) {
     constexpr int CL = kCluster;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
@@ -1106,17 +1175,23 @@ static lowra_status launch_mode(const GemmParams& G, const BatchMaps& TM, cudaSt
     KMaps<NB> QM;
     static_cast<GemmCommon&>(QP) = static_cast<const GemmCommon&>(Q);
     for (int i = 0; i < NB; ++i) { QP.mem[i] = Q.mem[i]; QM.m[i] = TM.m[i]; }
+    KEpilogues<MODE, NB> QE;
+    if constexpr (MODE == kModeEpilogue) {
+        for (int i = 0; i < NB; ++i) QE.m[i] = epilogues[i < Q.count ? i : 0];
+    }
     const bool shared = Q.t_split > 1 || Q.w_split > 1;
-    const cudaError_t rc = shared ? cudaLaunchKernelEx(&cfg, fused_kernel<MODE, NB, MODE != kModeDense>, QP, QM)
-                                  : cudaLaunchKernelEx(&cfg, fused_kernel<MODE, NB, false>, QP, QM);
+    const cudaError_t rc = shared ? cudaLaunchKernelEx(&cfg, fused_kernel<MODE, NB, MODE != kModeDense>, QP, QM, QE)
+                                  : cudaLaunchKernelEx(&cfg, fused_kernel<MODE, NB, false>, QP, QM, QE);
     return rc == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
 }
 
-lowra_status launch_fused(int mode, const GemmParams& G, const BatchMaps& TM, cudaStream_t stream) {
-    if (mode == kModeDense) return launch_mode<kModeDense, 1>(G, TM, stream);
+lowra_status launch_fused(int mode, const GemmParams& G, const BatchMaps& TM, const Epilogue* epilogues, cudaStream_t stream) {
+    if (mode == kModeDense) return launch_mode<kModeDense, 1>(G, TM, nullptr, stream);
     if (mode == kModeForward)
-        return G.count == 1 ? launch_mode<kModeForward, 1>(G, TM, stream) : launch_mode<kModeForward, kMaxBatch>(G, TM, stream);
-    return G.count == 1 ? launch_mode<kModeBackward, 1>(G, TM, stream) : launch_mode<kModeBackward, kMaxBatch>(G, TM, stream);
+        return G.count == 1 ? launch_mode<kModeForward, 1>(G, TM, nullptr, stream) : launch_mode<kModeForward, kMaxBatch>(G, TM, nullptr, stream);
+    if (mode == kModeEpilogue)
+        return G.count == 1 ? launch_mode<kModeEpilogue, 1>(G, TM, epilogues, stream) : launch_mode<kModeEpilogue, kMaxBatch>(G, TM, epilogues, stream);
+    return G.count == 1 ? launch_mode<kModeBackward, 1>(G, TM, nullptr, stream) : launch_mode<kModeBackward, kMaxBatch>(G, TM, nullptr, stream);
 }
 
 }  // namespace lowra

@@ -138,7 +138,19 @@ struct MemberArgs {
     const uint16_t* B;
     uint16_t* out;
     int32_t M;             // tokens of this member
+    Epilogue epilogue;     // in the calls that have one
 };
+
+// The caller's description of what stands behind a product, checked.
+lowra_status take_epilogue(const lowra_epilogue* e, const uint16_t* Y, Epilogue* out) {
+    if (!e) return LOWRA_ERR_NULL;
+    if (e->activation < LOWRA_ACT_NONE || e->activation > LOWRA_ACT_SILU) return LOWRA_ERR_SHAPE;
+    // (the copy of Z is written before the other arrays are read)
+    if (e->pre_dev && (e->pre_dev == Y || e->pre_dev == e->multiply_dev || e->pre_dev == e->residual_dev)) return LOWRA_ERR_SHAPE;
+    if (!aligned16(e->bias_dev) || !aligned16(e->multiply_dev) || !aligned16(e->residual_dev) || !aligned16(e->pre_dev)) return LOWRA_ERR_ALIGN;
+    *out = Epilogue{e->bias_dev, e->multiply_dev, e->residual_dev, e->pre_dev, e->activation, e->bias_bf16 != 0 ? 1 : 0};
+    return LOWRA_OK;
+}
 
 // Checks the arguments of a fused call for `count` weights of one shape.
 lowra_status check_members(const MemberArgs* mem, int count, int32_t r, const void* workspace, size_t workspace_bytes,
@@ -176,7 +188,7 @@ int out_alignment(const MemberArgs* mem, int count, int R) {
     return wide ? 32 : 16;
 }
 
-lowra_status run_small(const MemberArgs* mem, uint16_t* const* T_of, int count, int32_t r, float s, bool one_weight, void* workspace, cudaStream_t stream);
+lowra_status run_small(const MemberArgs* mem, uint16_t* const* T_of, int count, int32_t r, float s, bool one_weight, void* workspace, cudaStream_t stream, bool epilogue);
 // The diagnostic lowra_diag_drop_t_flags is about flags, which the path for few tokens has none of: it leaves that path out.
 bool dropping_flags() { return g_drop_t_flags.load(std::memory_order_relaxed) != 0; }
 // Up to 16 tokens it is always taken.  From 33 on it dequantises every weight twice, which many channels with short contractions do not repay, and
@@ -232,8 +244,9 @@ public:
 
 // Forward / backward-input for `count` weights of one shape in one launch (count == 1: the plain calls).  The members
 // may have different token counts (several adapters on one weight: one member per token group).  few_tokens: the path for few tokens is open.
+// epilogue (forward): the members have one.
 lowra_status run_members(bool backward, const MemberArgs* mem, int count, int32_t r, float s, void* workspace,
-                         size_t workspace_bytes, void* stream_v, bool stream_k = true, bool few_tokens = true) {
+                         size_t workspace_bytes, void* stream_v, bool stream_k = true, bool few_tokens = true, bool epilogue = false) {
     lowra_status st = check_members(mem, count, r, workspace, workspace_bytes, stream_k);
     if (st != LOWRA_OK) return st;
     const int N = mem[0].layout->N, K = mem[0].layout->K;
@@ -260,7 +273,7 @@ lowra_status run_members(bool backward, const MemberArgs* mem, int count, int32_
     if (few_tokens && !dropping_flags() && takes_small_path(backward, counts, K, M, r)) {   // (M: the largest member's tokens)
         uint16_t* T_of[kMaxBatch];
         for (int i = 0; i < count; ++i) T_of[i] = reinterpret_cast<uint16_t*>(ws + w.off_T[i]);
-        return run_small(mem, T_of, count, r, s, count == 1, workspace, stream);
+        return run_small(mem, T_of, count, r, s, count == 1, workspace, stream, epilogue);
     }
     if (w.t_flag_bytes > 0 && cudaMemsetAsync(t_flags, 0, w.t_flag_bytes, stream) != cudaSuccess) return LOWRA_ERR_CUDA;
 
@@ -349,13 +362,15 @@ lowra_status run_members(bool backward, const MemberArgs* mem, int count, int32_
             if (!make_map(&t.tmFl, m.A, (uint64_t)K, (uint64_t)r, (uint64_t)r, kTileR)) return LOWRA_ERR_CUDA;
         }
     }
-    return launch_fused(backward ? kModeBackward : kModeForward, G, TM, stream);
+    Epilogue epilogues[kMaxBatch];
+    for (int i = 0; i < count; ++i) epilogues[i] = mem[i].epilogue;
+    return launch_fused(backward ? kModeBackward : epilogue ? kModeEpilogue : kModeForward, G, TM, epilogues, stream);
 }
 
 // Forward pass of members of few tokens each (any number of them, one shape): two launches for every kSmallMembers.
 // Their arguments have been checked as run_members does.  T_of: where member i's down-projected tokens go.  one_weight: they share layout, codes
 // and absmax.
-lowra_status run_small(const MemberArgs* mem, uint16_t* const* T_of, int count, int32_t r, float s, bool one_weight, void* workspace, cudaStream_t stream) {
+lowra_status run_small(const MemberArgs* mem, uint16_t* const* T_of, int count, int32_t r, float s, bool one_weight, void* workspace, cudaStream_t stream, bool epilogue) {
     SmallParams<kSmallMembers> P;
     P.N = mem[0].layout->N;
     P.K = mem[0].layout->K;
@@ -371,7 +386,9 @@ lowra_status run_small(const MemberArgs* mem, uint16_t* const* T_of, int count, 
             const MemberArgs& m = mem[first + i];
             P.m[i] = SmallMember{make_row_layout(m.layout), m.packed, m.absmax, m.maps, m.act, m.A, m.B, m.out, T_of[first + i], m.M};
         }
-        const lowra_status st = launch_small(P, stream);
+        Epilogue epilogues[kSmallMembers];
+        for (int i = 0; i < P.count; ++i) epilogues[i] = mem[first + i].epilogue;
+        const lowra_status st = launch_small(P, epilogue ? epilogues : nullptr, stream);
         if (st != LOWRA_OK) return st;
     }
     return LOWRA_OK;
@@ -381,7 +398,7 @@ lowra_status run_lora(bool backward, const lowra_layout* layout, const uint8_t* 
                       const float* maps, const uint16_t* act, int32_t M, const uint16_t* A, const uint16_t* B,
                       int32_t r, float s, uint16_t* out, void* workspace, size_t workspace_bytes, void* stream_v,
                       bool stream_k = true) {
-    const MemberArgs m = {layout, packed, absmax, maps, act, A, B, out, M};
+    const MemberArgs m = {layout, packed, absmax, maps, act, A, B, out, M, {}};
     return run_members(backward, &m, 1, r, s, workspace, workspace_bytes, stream_v, stream_k);
 }
 
@@ -523,39 +540,59 @@ extern "C" size_t lowra_batch_workspace_bytes(const lowra_layout* layout, int32_
 
 namespace lowra {
 namespace {
-lowra_status run_batch(bool backward, const lowra_member* members, int32_t count, int32_t M, int32_t r, float s,
+lowra_status run_batch(bool backward, const lowra_member* members, const lowra_epilogue* epilogues, int32_t count, int32_t M, int32_t r, float s,
                        void* workspace, size_t workspace_bytes, void* stream) {
     if (!members) return LOWRA_ERR_NULL;
     if (count < 1 || count > kMaxBatch) return LOWRA_ERR_SHAPE;
     MemberArgs mem[kMaxBatch];
     for (int i = 0; i < count; ++i) {
         const lowra_member& m = members[i];
-        mem[i] = MemberArgs{m.layout, m.packed_dev, m.absmax_dev, m.maps_dev, m.act_dev, m.A_dev, m.B_dev, m.out_dev, M};
+        mem[i] = MemberArgs{m.layout, m.packed_dev, m.absmax_dev, m.maps_dev, m.act_dev, m.A_dev, m.B_dev, m.out_dev, M, {}};
+        if (epilogues != nullptr) {
+            const lowra_status st = take_epilogue(&epilogues[i], m.out_dev, &mem[i].epilogue);
+            if (st != LOWRA_OK) return st;
+        }
         if (m.layout != nullptr && m.layout->deal_dev == nullptr) return LOWRA_ERR_NULL;   // also for a batch of one
     }
-    return run_members(backward, mem, count, r, s, workspace, workspace_bytes, stream);
+    return run_members(backward, mem, count, r, s, workspace, workspace_bytes, stream, true, true, epilogues != nullptr);
 }
 }  // namespace
 }  // namespace lowra
 
 extern "C" lowra_status lowra_lora_forward_batch(const lowra_member* members_host, int32_t count, int32_t M, int32_t r,
                                                  float s, void* workspace_dev, size_t workspace_bytes, void* stream) {
-    return lowra::run_batch(false, members_host, count, M, r, s, workspace_dev, workspace_bytes, stream);
+    return lowra::run_batch(false, members_host, nullptr, count, M, r, s, workspace_dev, workspace_bytes, stream);
 }
 
 extern "C" lowra_status lowra_lora_backward_input_batch(const lowra_member* members_host, int32_t count, int32_t M,
                                                         int32_t r, float s, void* workspace_dev, size_t workspace_bytes,
                                                         void* stream) {
-    return lowra::run_batch(true, members_host, count, M, r, s, workspace_dev, workspace_bytes, stream);
+    return lowra::run_batch(true, members_host, nullptr, count, M, r, s, workspace_dev, workspace_bytes, stream);
 }
 
-extern "C" lowra_status lowra_lora_forward_adapters(const lowra_layout* layout, const uint8_t* packed_dev,
-                                                    const float* absmax_dev, const float* maps_dev, int32_t n_adapters,
-                                                    const uint16_t* X_dev, int32_t M, const int32_t* group_start_host,
-                                                    const uint16_t* A_dev, const uint16_t* B_dev, int32_t r, float s,
-                                                    uint16_t* Y_dev, void* workspace_dev, size_t workspace_bytes,
+extern "C" lowra_status lowra_lora_forward_batch_epilogue(const lowra_member* members_host, const lowra_epilogue* epilogues_host, int32_t count, int32_t M,
+                                                          int32_t r, float s, void* workspace_dev, size_t workspace_bytes, void* stream) {
+    if (!epilogues_host) return LOWRA_ERR_NULL;
+    return lowra::run_batch(false, members_host, epilogues_host, count, M, r, s, workspace_dev, workspace_bytes, stream);
+}
+
+extern "C" lowra_status lowra_lora_forward_epilogue(const lowra_layout* layout, const uint8_t* packed_dev, const float* absmax_dev, const float* maps_dev,
+                                                    const uint16_t* X_dev, int32_t M, const uint16_t* A_dev, const uint16_t* B_dev, int32_t r, float s,
+                                                    const lowra_epilogue* epilogue_host, uint16_t* Y_dev, void* workspace_dev, size_t workspace_bytes,
                                                     void* stream) {
     using namespace lowra;
+    MemberArgs m = {layout, packed_dev, absmax_dev, maps_dev, X_dev, A_dev, B_dev, Y_dev, M, {}};
+    const lowra_status st = take_epilogue(epilogue_host, Y_dev, &m.epilogue);
+    if (st != LOWRA_OK) return st;
+    return run_members(false, &m, 1, r, s, workspace_dev, workspace_bytes, stream, true, true, true);
+}
+
+namespace lowra {
+namespace {
+// epilogue: null, or what stands behind all tokens' products
+lowra_status run_adapter_groups(const lowra_layout* layout, const uint8_t* packed_dev, const float* absmax_dev, const float* maps_dev, int32_t n_adapters,
+                                const uint16_t* X_dev, int32_t M, const int32_t* group_start_host, const uint16_t* A_dev, const uint16_t* B_dev, int32_t r,
+                                float s, const Epilogue* epilogue, uint16_t* Y_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
     lowra_status st = check_layout(layout);
     if (st != LOWRA_OK) return st;
     if (!maps_dev || !X_dev || !A_dev || !B_dev || !Y_dev || !group_start_host) return LOWRA_ERR_NULL;
@@ -574,9 +611,16 @@ extern "C" lowra_status lowra_lora_forward_adapters(const lowra_layout* layout, 
     // rows lie in the T of a call for all M tokens.
     auto member = [&](int a) {
         const int m0 = group_start_host[a];
-        return MemberArgs{layout, packed_dev, absmax_dev, maps_dev + (size_t)a * N * kTableStride, X_dev + (size_t)m0 * K,
-                          A_dev + (size_t)a * K * (size_t)r, B_dev + (size_t)a * (size_t)r * N, Y_dev + (size_t)m0 * N,
-                          group_start_host[a + 1] - m0};
+        const size_t rows = (size_t)m0 * N;
+        MemberArgs m = {layout, packed_dev, absmax_dev, maps_dev + (size_t)a * N * kTableStride, X_dev + (size_t)m0 * K,
+                        A_dev + (size_t)a * K * (size_t)r, B_dev + (size_t)a * (size_t)r * N, Y_dev + rows, group_start_host[a + 1] - m0, {}};
+        if (epilogue != nullptr) {
+            m.epilogue = *epilogue;
+            if (m.epilogue.multiply) m.epilogue.multiply += rows;
+            if (m.epilogue.residual) m.epilogue.residual += rows;
+            if (m.epilogue.pre) m.epilogue.pre += rows;
+        }
+        return m;
     };
     const bool dropping = dropping_flags();   // (asked once: the launches below use the diagnostic's calls up)
     GroupPaths paths(layout, r, group_start_host, n_adapters, together);
@@ -592,7 +636,7 @@ extern "C" lowra_status lowra_lora_forward_adapters(const lowra_layout* layout, 
             few[n_few++] = member(a);
         }
         if (n_few > 0 && (a == n_adapters || n_few == kSmallMembers)) {
-            if ((st = run_small(few, few_T, n_few, r, s, true, workspace_dev, (cudaStream_t)stream)) != LOWRA_OK) return st;
+            if ((st = run_small(few, few_T, n_few, r, s, true, workspace_dev, (cudaStream_t)stream, epilogue != nullptr)) != LOWRA_OK) return st;
             n_few = 0;
         }
     }
@@ -602,12 +646,36 @@ extern "C" lowra_status lowra_lora_forward_adapters(const lowra_layout* layout, 
             mem[n++] = member(a);
         }
         if (n > 0 && (a == n_adapters || n == (together ? kMaxBatch : 1))) {
-            st = run_members(false, mem, n, r, s, workspace_dev, workspace_bytes, stream, true, false);
+            st = run_members(false, mem, n, r, s, workspace_dev, workspace_bytes, stream, true, false, epilogue != nullptr);
             if (st != LOWRA_OK) return st;
             n = 0;
         }
     }
     return LOWRA_OK;
+}
+}  // namespace
+}  // namespace lowra
+
+extern "C" lowra_status lowra_lora_forward_adapters(const lowra_layout* layout, const uint8_t* packed_dev,
+                                                    const float* absmax_dev, const float* maps_dev, int32_t n_adapters,
+                                                    const uint16_t* X_dev, int32_t M, const int32_t* group_start_host,
+                                                    const uint16_t* A_dev, const uint16_t* B_dev, int32_t r, float s,
+                                                    uint16_t* Y_dev, void* workspace_dev, size_t workspace_bytes,
+                                                    void* stream) {
+    return lowra::run_adapter_groups(layout, packed_dev, absmax_dev, maps_dev, n_adapters, X_dev, M, group_start_host, A_dev, B_dev, r, s, nullptr, Y_dev,
+                                     workspace_dev, workspace_bytes, stream);
+}
+
+extern "C" lowra_status lowra_lora_forward_adapters_epilogue(const lowra_layout* layout, const uint8_t* packed_dev, const float* absmax_dev,
+                                                             const float* maps_dev, int32_t n_adapters, const uint16_t* X_dev, int32_t M,
+                                                             const int32_t* group_start_host, const uint16_t* A_dev, const uint16_t* B_dev, int32_t r,
+                                                             float s, const lowra_epilogue* epilogue_host, uint16_t* Y_dev, void* workspace_dev,
+                                                             size_t workspace_bytes, void* stream) {
+    lowra::Epilogue epilogue;
+    const lowra_status st = lowra::take_epilogue(epilogue_host, Y_dev, &epilogue);
+    if (st != LOWRA_OK) return st;
+    return lowra::run_adapter_groups(layout, packed_dev, absmax_dev, maps_dev, n_adapters, X_dev, M, group_start_host, A_dev, B_dev, r, s, &epilogue, Y_dev,
+                                     workspace_dev, workspace_bytes, stream);
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -859,5 +927,5 @@ extern "C" lowra_status lowra_dense_nt(const uint16_t* P_dev, const uint16_t* Q_
     if (!make_map(&TM.m[0].tmFl, Q_dev, (uint64_t)N, (uint64_t)K, (uint64_t)K, kTileR)) return LOWRA_ERR_CUDA;
     TM.m[0].tmT = TM.m[0].tmB;
     TM.m[0].tmFt = TM.m[0].tmB;
-    return launch_fused(kModeDense, G, TM, stream);
+    return launch_fused(kModeDense, G, TM, nullptr, stream);
 }

@@ -3,6 +3,7 @@
 
 #include <cuda.h>
 
+#include "epilogue.cuh"
 #include "lowra_common.cuh"
 
 namespace lowra {
@@ -56,6 +57,7 @@ static_assert(kProducerGroups <= kSlotsW, "see stage_free in the kernel");
 constexpr int kTmemCols = 512;    // two 128 x 256 fp32 accumulators per CTA
 
 constexpr int kModeForward = 0, kModeBackward = 1, kModeDense = 2;
+constexpr int kModeEpilogue = 3;  // forward, with what stands behind the product (epilogue.cuh)
 
 constexpr int kMaxBatch = 4;      // weights of the same shape that one launch can walk (lowra_lora_*_batch)
 
@@ -142,7 +144,16 @@ constexpr uint32_t kSmemBarriers = 1024;
 constexpr uint32_t kGemmSmemBytes = kSmemRing + kSmemBarriers;
 static_assert(kGemmSmemBytes <= 232448, "227 KB of shared memory per CTA");
 
-lowra_status launch_fused(int mode, const GemmParams& G, const BatchMaps& TM, cudaStream_t stream);
+// What stands behind the members' products: parameters of their own, so that the other modes' launches do not carry them.
+template <int MODE, int NB>
+struct KEpilogues {};
+template <int NB>
+struct KEpilogues<kModeEpilogue, NB> {
+    Epilogue m[NB];
+};
+
+// epilogues: one for every member in mode kModeEpilogue, else null
+lowra_status launch_fused(int mode, const GemmParams& G, const BatchMaps& TM, const Epilogue* epilogues, cudaStream_t stream);
 float fused_estimate(int N, int K, int M, int r, int count);
 int fused_schedule(bool backward, int N, int K, const int32_t* Ms, int count, int r, int* tile_tokens, int* w_split, int* t_split);   // what a call would run (diagnostic)
 
@@ -168,7 +179,15 @@ struct SmallParams {
     int clear_status;         // the call brings no deal: its status word starts from zero
     int one_weight;           // all members have the same layout, codes and absmax (several adapters)
 };
-lowra_status launch_small(const SmallParams<kSmallMembers>& P, cudaStream_t stream);
+// With what stands behind the members' products (EPI), or without.
+template <int NB, bool EPI>
+struct SmallArgs : SmallParams<NB> {};
+template <int NB>
+struct SmallArgs<NB, true> : SmallParams<NB> {
+    Epilogue e[NB];
+};
+// epilogues: one for every member, or null
+lowra_status launch_small(const SmallParams<kSmallMembers>& P, const Epilogue* epilogues, cudaStream_t stream);
 bool small_takes_units(const SmallParams<kSmallMembers>& P);     // whether that launch is units_kernel
 
 // One skinny product D [R, rp] = P . Q (see gemm_grad.cu), written in bf16 as out [R, ld_out] or, transposed,

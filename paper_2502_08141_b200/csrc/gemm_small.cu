@@ -417,8 +417,16 @@ struct OwnT {
 //   MERGED: one CTA does all slices of a group, each half of its warps every other half of them.  For grids of several waves: a CTA costs
 //           about 4 us beside its steps (its launch in a cluster, the way from a row's number to its codes, a barrier of the cluster).
 // OWN: one slice, and every CTA forms T itself (OwnT); no launch goes before this one.
-template <int NT8, int NB, bool MERGED, int CTAS, bool OWN>
-__global__ void __launch_bounds__(kSmallThreads, CTAS) small_kernel(const __grid_constant__ SmallParams<NB> P, const int slices) {
+// The sum of token m and channel n of a member's product: with what stands behind it, rounded, stored.
+template <int NB, bool EPI>
+__device__ __forceinline__ void store(const SmallArgs<NB, EPI>& P, int member, int m, int n, float sum) {
+    const size_t at = (size_t)m * P.N + n;
+    if constexpr (EPI) P.m[member].Y[at] = finish1(P.e[member], n, at, sum);
+    else P.m[member].Y[at] = (uint16_t)pack_bf16x2(sum, 0.0f);
+}
+
+template <int NT8, int NB, bool MERGED, int CTAS, bool OWN, bool EPI>
+__global__ void __launch_bounds__(kSmallThreads, CTAS) small_kernel(const __grid_constant__ SmallArgs<NB, EPI> P, const int slices) {
     extern __shared__ __align__(128) unsigned char small_smem[];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (OWN) {
@@ -545,7 +553,7 @@ __global__ void __launch_bounds__(kSmallThreads, CTAS) small_kernel(const __grid
             const float* from = sums + m * kMergedPitch + row;
             float sum = from[0];
             for (int s = 0; s < slices / 2; ++s) sum += from[(2 + s) * (kTokens * kMergedPitch)];
-            W.Y[(size_t)(un.m0 + m) * P.N + __ldg(W.L.perm + p_first + row)] = (uint16_t)pack_bf16x2(sum, 0.0f);
+            store(P, un.member, un.m0 + m, __ldg(W.L.perm + p_first + row), sum);
         }
         return;
     }
@@ -555,7 +563,7 @@ __global__ void __launch_bounds__(kSmallThreads, CTAS) small_kernel(const __grid
         if (un.m0 + m >= W.M || p_first + row >= p_end) continue;
         float sum = 0.0f;
         for (int s = 0; s < slices; ++s) sum += sums[((2 * s * kTokens) << share_log) + i] + sums[(((2 * s + 1) * kTokens) << share_log) + i];
-        W.Y[(size_t)(un.m0 + m) * P.N + __ldg(W.L.perm + p_first + row)] = (uint16_t)pack_bf16x2(sum, 0.0f);
+        store(P, un.member, un.m0 + m, __ldg(W.L.perm + p_first + row), sum);
     }
 }
 
@@ -575,8 +583,9 @@ struct UnitOrder {                               // runs of CTAs: a unit's row g
 
 __device__ __forceinline__ void barrier_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
-template <int B, int NT8, int NB>
-__device__ __forceinline__ void unit_rows(const SmallParams<NB>& P, const SmallMember& W, int m0, int p0, int p_end, int slices, unsigned char* smem) {
+template <int B, int NT8, int NB, bool EPI>
+__device__ __forceinline__ void unit_rows(const SmallArgs<NB, EPI>& P, int member, int m0, int p0, int p_end, int slices, unsigned char* smem) {
+    const SmallMember& W = P.m[member];
     constexpr uint32_t kStep = 8u * NT8 * kSmallSpan * 2u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, half = warp >> 2;
     const int K = P.K, n_span = (K + kSmallSpan - 1) / kSmallSpan, nb = K / kBlock, slots = 2 * slices;
@@ -704,16 +713,16 @@ __device__ __forceinline__ void unit_rows(const SmallParams<NB>& P, const SmallM
                 for (int e = 0; e < 2; ++e) {
                     const int m = m0 + nt * 8 + 2 * t + e;
                     if (m >= W.M) continue;
-                    if (live0) W.Y[(size_t)m * P.N + r0] = (uint16_t)pack_bf16x2(acc[nt][e], 0.0f);
-                    if (live1) W.Y[(size_t)m * P.N + r1] = (uint16_t)pack_bf16x2(acc[nt][2 + e], 0.0f);
+                    if (live0) store(P, member, m, r0, acc[nt][e]);
+                    if (live1) store(P, member, m, r1, acc[nt][2 + e]);
                 }
             }
         }
     }
 }
 
-template <int NB>
-__global__ void __launch_bounds__(kSmallThreads, 2) units_kernel(const __grid_constant__ SmallParams<NB> P, const __grid_constant__ UnitOrder order, const int slices) {
+template <int NB, bool EPI>
+__global__ void __launch_bounds__(kSmallThreads, 2) units_kernel(const __grid_constant__ SmallArgs<NB, EPI> P, const __grid_constant__ UnitOrder order, const int slices) {
     extern __shared__ __align__(128) unsigned char small_smem[];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int run = 0, above = order.count - 1;
@@ -722,16 +731,17 @@ __global__ void __launch_bounds__(kSmallThreads, 2) units_kernel(const __grid_co
         if ((int)blockIdx.x < order.end[mid]) above = mid;
         else run = mid + 1;
     }
-    const SmallMember& W = P.m[order.member[run]];
+    const int member = order.member[run];
+    const SmallMember& W = P.m[member];
     const int m0 = order.first[run] * kUnitTokens, c = order.cls[run], grp = (int)blockIdx.x - (run > 0 ? order.end[run - 1] : 0);
     const int p0 = W.L.class_start[c] + grp * kSmallRows + (int)((threadIdx.x >> 5) & 3) * 16, p_end = W.L.class_start[c + 1];
     const int tokens = W.M - m0;
     auto work = [&](auto bits) {
         constexpr int B = decltype(bits)::value;
-        if (tokens <= 8) unit_rows<B, 1, NB>(P, W, m0, p0, p_end, slices, small_smem);
-        else if (tokens <= 16) unit_rows<B, 2, NB>(P, W, m0, p0, p_end, slices, small_smem);
-        else if (tokens <= 24) unit_rows<B, 3, NB>(P, W, m0, p0, p_end, slices, small_smem);
-        else unit_rows<B, 4, NB>(P, W, m0, p0, p_end, slices, small_smem);
+        if (tokens <= 8) unit_rows<B, 1, NB, EPI>(P, member, m0, p0, p_end, slices, small_smem);
+        else if (tokens <= 16) unit_rows<B, 2, NB, EPI>(P, member, m0, p0, p_end, slices, small_smem);
+        else if (tokens <= 24) unit_rows<B, 3, NB, EPI>(P, member, m0, p0, p_end, slices, small_smem);
+        else unit_rows<B, 4, NB, EPI>(P, member, m0, p0, p_end, slices, small_smem);
     };
     if (c == 0) work(std::integral_constant<int, 1>());
     else if (c == 1) work(std::integral_constant<int, 2>());
@@ -774,8 +784,8 @@ float unit_cost(int cls, int eights) {
     return kCost[cls][eights - 1];
 }
 
-template <int NB>
-lowra_status launch_units(const SmallParams<NB>& P, int slices, cudaStream_t stream) {
+template <int NB, bool EPI>
+lowra_status launch_units(const SmallArgs<NB, EPI>& P, int slices, cudaStream_t stream) {
     struct Run { float cost; int groups; uint8_t member, first, cls; } runs[kUnitRuns];
     int n = 0, widest = 1;
     for (int i = 0; i < P.count; ++i) {
@@ -804,7 +814,7 @@ lowra_status launch_units(const SmallParams<NB>& P, int slices, cudaStream_t str
     }
     const size_t smem = 4u * (8 * widest) * kSmallSpan * 2u + 3u * 4 * widest * 128 * 4u;
     static SmemLimit limit = {};
-    if (ensure_smem_limit(reinterpret_cast<const void*>(units_kernel<NB>), smem, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
+    if (ensure_smem_limit(reinterpret_cast<const void*>(units_kernel<NB, EPI>), smem, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -815,15 +825,15 @@ lowra_status launch_units(const SmallParams<NB>& P, int slices, cudaStream_t str
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, units_kernel<NB>, P, order, slices) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, units_kernel<NB, EPI>, P, order, slices) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
 }
 
-template <int NT8, int NB, bool MERGED, int CTAS, bool OWN = false>
-lowra_status launch_product(const SmallParams<NB>& P, int groups, int units, int slices, cudaStream_t stream) {
+template <int NT8, bool MERGED, int CTAS, bool OWN = false, int NB, bool EPI>
+lowra_status launch_product(const SmallArgs<NB, EPI>& P, int groups, int units, int slices, cudaStream_t stream) {
     const size_t smem = 4u * (8 * NT8) * kSmallSpan * 2u + (MERGED ? (2 + slices / 2) * (8 * NT8) * kMergedPitch * 4u : 2u * (8 * NT8) * kSmallRows * 4u) +
                         (OWN ? OwnT::bytes(P.K, P.r) : 0);
     static SmemLimit limit = {};
-    if (ensure_smem_limit(reinterpret_cast<const void*>(small_kernel<NT8, NB, MERGED, CTAS, OWN>), smem, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
+    if (ensure_smem_limit(reinterpret_cast<const void*>(small_kernel<NT8, NB, MERGED, CTAS, OWN, EPI>), smem, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -837,7 +847,7 @@ lowra_status launch_product(const SmallParams<NB>& P, int groups, int units, int
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = MERGED || slices == 1 ? 1 : 2;           // (a CTA is a cluster of its own without being told, and 0.4 us less host time)
-    return cudaLaunchKernelEx(&cfg, small_kernel<NT8, NB, MERGED, CTAS, OWN>, P, slices) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, small_kernel<NT8, NB, MERGED, CTAS, OWN, EPI>, P, slices) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
 }
 
 int product_slices(int N, int K) {
@@ -888,8 +898,8 @@ bool forms_own_t(int K, int r, int tokens, int groups, int four) {
     return groups <= (r > 16 ? 40 : K <= 256 || four == 0 ? kNumSMs : tokens > 8 ? 40 : 80);
 }
 
-template <int NB>
-lowra_status launch_members(const SmallParams<NB>& P, cudaStream_t stream) {
+template <int NB, bool EPI>
+lowra_status launch_members(const SmallArgs<NB, EPI>& P, cudaStream_t stream) {
     int m16 = 0, most = 0;
     const int groups = row_groups(P);
     for (int i = 0; i < P.count; ++i) {
@@ -901,7 +911,7 @@ lowra_status launch_members(const SmallParams<NB>& P, cudaStream_t stream) {
     if constexpr (NB == 1) {
         const int* start = P.m[0].L.class_start;
         if (slices == 1 && forms_own_t(P.K, P.r, most, groups, start[3] - start[2]))
-            return most <= 8 ? launch_product<1, NB, false, 2, true>(P, groups, 1, 1, stream) : launch_product<2, NB, false, 2, true>(P, groups, 1, 1, stream);
+            return most <= 8 ? launch_product<1, false, 2, true>(P, groups, 1, 1, stream) : launch_product<2, false, 2, true>(P, groups, 1, 1, stream);
     }
     // ---- T: the contraction over up to eight CTAs, 128 indices or more each
     {
@@ -922,12 +932,12 @@ lowra_status launch_members(const SmallParams<NB>& P, cudaStream_t stream) {
         cfg.stream = stream;
         cfg.attrs = attr;
         cfg.numAttrs = 2;
-        if (cudaLaunchKernelEx(&cfg, project_kernel<NB>, P) != cudaSuccess) return LOWRA_ERR_CUDA;
+        if (cudaLaunchKernelEx(&cfg, project_kernel<NB>, static_cast<const SmallParams<NB>&>(P)) != cudaSuccess) return LOWRA_ERR_CUDA;
     }
     // ---- the product: slices of the contraction until the grid is about three CTAs per two places, as long as every warp keeps
     // a step of 256.  The choice depends on the weight's shape alone, so that a member's result does not depend on its company.
     const int nt8 = most <= 8 ? 1 : most <= 16 ? 2 : most <= 24 ? 3 : 4;
-    if (P.one_weight && units_pay(P, slices)) return launch_units<NB>(P, slices, stream);
+    if (P.one_weight && units_pay(P, slices)) return launch_units(P, slices, stream);
     int units = 0;
     for (int i = 0; i < P.count; ++i) units += (P.m[i].M + 8 * nt8 - 1) / (8 * nt8);
     // Merged where a CTA's own cost outweighs its steps: slots of one or two steps, few tokens, more CTAs than run at a time.  (Groups of
@@ -935,14 +945,14 @@ lowra_status launch_members(const SmallParams<NB>& P, cudaStream_t stream) {
     // tokens a group 64 in 2 38.5 against 34.8; on 4096 x 11008 - slots of five steps - 6 in 3 54.5 against 46.1; one group 18.8 against 10.6.)
     if constexpr (NB > 1) {
         if (slices > 1 && nt8 <= 2 && n_span <= 2 * (2 * slices) && groups * slices * units > 2 * kNumSMs)
-            return nt8 == 1 ? launch_product<1, NB, true, 2>(P, groups, units, slices, stream) : launch_product<2, NB, true, 2>(P, groups, units, slices, stream);
+            return nt8 == 1 ? launch_product<1, true, 2>(P, groups, units, slices, stream) : launch_product<2, true, 2>(P, groups, units, slices, stream);
     }
     const int* start = P.m[0].L.class_start;
     const bool three = three_pay(start[3] - start[2], P.N, P.r, n_span, slices, groups * slices * units, 8 * m16, nt8);
-    if (nt8 == 1) return three ? launch_product<1, NB, false, 3>(P, groups, units, slices, stream) : launch_product<1, NB, false, 2>(P, groups, units, slices, stream);
-    if (nt8 == 2) return three ? launch_product<2, NB, false, 3>(P, groups, units, slices, stream) : launch_product<2, NB, false, 2>(P, groups, units, slices, stream);
-    if (nt8 == 3) return three ? launch_product<3, NB, false, 3>(P, groups, units, slices, stream) : launch_product<3, NB, false, 2>(P, groups, units, slices, stream);
-    return launch_product<4, NB, false, 2>(P, groups, units, slices, stream);
+    if (nt8 == 1) return three ? launch_product<1, false, 3>(P, groups, units, slices, stream) : launch_product<1, false, 2>(P, groups, units, slices, stream);
+    if (nt8 == 2) return three ? launch_product<2, false, 3>(P, groups, units, slices, stream) : launch_product<2, false, 2>(P, groups, units, slices, stream);
+    if (nt8 == 3) return three ? launch_product<3, false, 3>(P, groups, units, slices, stream) : launch_product<3, false, 2>(P, groups, units, slices, stream);
+    return launch_product<4, false, 2>(P, groups, units, slices, stream);
 }
 
 }  // namespace
@@ -972,12 +982,19 @@ float small_estimate(const int32_t* n, int K, int r, int units, int most) {
 bool small_takes_units(const SmallParams<kSmallMembers>& P) { return P.one_weight && units_pay(P, product_slices(P.N, P.K)); }
 
 // (A call with one member carries 0.3 KB of kernel parameters instead of 1.5 KB, which its launches show.)
-lowra_status launch_small(const SmallParams<kSmallMembers>& P, cudaStream_t stream) {
-    if (P.count > 1) return launch_members<kSmallMembers>(P, stream);
-    SmallParams<1> Q;
-    Q.m[0] = P.m[0];
-    Q.count = 1; Q.N = P.N; Q.K = P.K; Q.r = P.r; Q.rp = P.rp; Q.s = P.s; Q.status = P.status; Q.clear_status = P.clear_status; Q.one_weight = P.one_weight;
-    return launch_members<1>(Q, stream);
+template <int NB, bool EPI>
+static lowra_status launch_few(const SmallParams<kSmallMembers>& P, const Epilogue* epilogues, cudaStream_t stream) {
+    SmallArgs<NB, EPI> Q;
+    for (int i = 0; i < NB; ++i) Q.m[i] = P.m[i < P.count ? i : 0];
+    if constexpr (EPI) {
+        for (int i = 0; i < NB; ++i) Q.e[i] = epilogues[i < P.count ? i : 0];
+    }
+    Q.count = P.count; Q.N = P.N; Q.K = P.K; Q.r = P.r; Q.rp = P.rp; Q.s = P.s; Q.status = P.status; Q.clear_status = P.clear_status; Q.one_weight = P.one_weight;
+    return launch_members(Q, stream);
+}
+lowra_status launch_small(const SmallParams<kSmallMembers>& P, const Epilogue* epilogues, cudaStream_t stream) {
+    if (epilogues != nullptr) return P.count > 1 ? launch_few<kSmallMembers, true>(P, epilogues, stream) : launch_few<1, true>(P, epilogues, stream);
+    return P.count > 1 ? launch_few<kSmallMembers, false>(P, nullptr, stream) : launch_few<1, false>(P, nullptr, stream);
 }
 
 }  // namespace lowra

@@ -8,6 +8,7 @@
 // a status that is not LOWRA_OK, or None for everything that is not the ordinary case - other types, memory of other devices than the
 // current one, other layouts in memory, shapes that do not fit, arrays that are too short, subclasses, errors: the caller then takes the
 // interpreted way, which says what is wrong.  Likewise
+//   forward_epilogue(as forward, then bias or None, the activation's number, multiply, residual and pre or None each)
 //   batch(backward, members, s, workspace)                                          the list of outputs
 //   gradients(X, dY, A, B, s, dA or None, dB or None, workspace or None)            the pair of gradients
 //   gradients_reuse(X, dY, T, U, r, dA or None, dB or None, workspace or None)      likewise
@@ -23,6 +24,8 @@ namespace {
 
 using Product = lowra_status (*)(const lowra_layout*, const uint8_t*, const float*, const float*, const uint16_t*, int32_t, const uint16_t*,
                                  const uint16_t*, int32_t, float, uint16_t*, void*, size_t, void*);
+using ProductEpilogue = lowra_status (*)(const lowra_layout*, const uint8_t*, const float*, const float*, const uint16_t*, int32_t, const uint16_t*, const uint16_t*,
+                                         int32_t, float, const lowra_epilogue*, uint16_t*, void*, size_t, void*);
 using WorkspaceBytes = size_t (*)(const lowra_layout*, int32_t, int32_t);
 using WorkspaceInit = lowra_status (*)(void*, size_t, void*);
 using Batch = lowra_status (*)(const lowra_member*, int32_t, int32_t, int32_t, float, void*, size_t, void*);
@@ -41,6 +44,7 @@ struct Library {
     GradientsReuse gradients_reuse;
     GradientsBytes gradients_bytes;
     Projection projection;
+    ProductEpilogue forward_epilogue;
 } library;
 
 bool plain(PyObject* o) { return THPVariable_CheckExact(o); }
@@ -64,8 +68,11 @@ struct Held {
     ~Held() { Py_XDECREF(o); }
 };
 
-PyObject* product(PyObject* const* args, Py_ssize_t n, bool backward) {
-    if (n != 11 || library.forward == nullptr) Py_RETURN_NONE;
+// epilogue: with the arguments of one behind the others
+PyObject* product(PyObject* const* args, Py_ssize_t n, bool backward, bool epilogue = false) {
+    if (n != (epilogue ? 16 : 11) || library.forward == nullptr) Py_RETURN_NONE;
+    for (int i = 11; i < n; ++i)
+        if (i == 12 ? !PyLong_CheckExact(args[i]) : args[i] != Py_None && !plain(args[i])) Py_RETURN_NONE;
     for (int i = 2; i <= 7; ++i)
         if (!plain(args[i])) Py_RETURN_NONE;
     const bool out_given = args[9] != Py_None, workspace_given = args[10] != Py_None;
@@ -86,6 +93,26 @@ PyObject* product(PyObject* const* args, Py_ssize_t n, bool backward) {
         if (!on(packed, dev) || packed.nbytes() < layout->packed_bytes || !array(absmax, at::kFloat, N * (K / 64), dev) || !array(maps, at::kFloat, N * 16, dev)) Py_RETURN_NONE;
         if (out_given && !array(THPVariable_Unpack(args[9]), at::kBFloat16, M * cols, dev)) Py_RETURN_NONE;
         if (workspace_given && !on(THPVariable_Unpack(args[10]), dev)) Py_RETURN_NONE;
+        lowra_epilogue behind = {};
+        if (epilogue) {
+            if (args[11] != Py_None) {
+                const at::Tensor& bias = THPVariable_Unpack(args[11]);
+                behind.bias_bf16 = bias.scalar_type() == at::kBFloat16;
+                if (!array(bias, behind.bias_bf16 ? at::kBFloat16 : at::kFloat, N, dev) || bias.numel() != N) Py_RETURN_NONE;
+                behind.bias_dev = bias.data_ptr();
+            }
+            behind.activation = (int32_t)PyLong_AsLong(args[12]);
+            const uint16_t* rows[3] = {};
+            for (int i = 0; i < 3; ++i) {
+                if (args[13 + i] == Py_None) continue;
+                const at::Tensor& t = THPVariable_Unpack(args[13 + i]);
+                if (!matrix(t, M, N, dev)) Py_RETURN_NONE;
+                rows[i] = static_cast<const uint16_t*>(t.data_ptr());
+            }
+            behind.multiply_dev = rows[0];
+            behind.residual_dev = rows[1];
+            behind.pre_dev = const_cast<uint16_t*>(rows[2]);
+        }
         const Product call = backward ? library.backward_input : library.forward;
         const auto* packed_p = static_cast<const uint8_t*>(packed.data_ptr());
         const auto *absmax_p = static_cast<const float*>(absmax.data_ptr()), *maps_p = static_cast<const float*>(maps.data_ptr());
@@ -108,8 +135,11 @@ PyObject* product(PyObject* const* args, Py_ssize_t n, bool backward) {
                 if (ready && layout->deal_dev != nullptr) ready = library.workspace_init(workspace.data_ptr(), bytes, stream) == LOWRA_OK;   // no prologue launch will clear it
             }
             if (ready) {
-                st = call(layout, packed_p, absmax_p, maps_p, act_p, (int32_t)M, A_p, B_p, (int32_t)r, (float)s, static_cast<uint16_t*>(out.data_ptr()),
-                          workspace.data_ptr(), (size_t)workspace.numel(), stream);
+                auto* out_p = static_cast<uint16_t*>(out.data_ptr());
+                st = epilogue ? library.forward_epilogue(layout, packed_p, absmax_p, maps_p, act_p, (int32_t)M, A_p, B_p, (int32_t)r, (float)s, &behind, out_p,
+                                                         workspace.data_ptr(), (size_t)workspace.numel(), stream)
+                              : call(layout, packed_p, absmax_p, maps_p, act_p, (int32_t)M, A_p, B_p, (int32_t)r, (float)s, out_p, workspace.data_ptr(),
+                                     (size_t)workspace.numel(), stream);
                 called = true;
             }
         }
@@ -128,6 +158,8 @@ PyObject* product(PyObject* const* args, Py_ssize_t n, bool backward) {
 
 PyObject* forward(PyObject*, PyObject* const* args, Py_ssize_t n) { return product(args, n, false); }
 PyObject* backward_input(PyObject*, PyObject* const* args, Py_ssize_t n) { return product(args, n, true); }
+
+PyObject* forward_epilogue(PyObject*, PyObject* const* args, Py_ssize_t n) { return product(args, n, false, true); }
 
 // A number, or not: an exact int within an int32, an exact float or int.
 bool number(PyObject* o, int32_t* v) {
@@ -322,24 +354,25 @@ PyObject* fits(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 // bind(addresses of lowra_lora_forward, lowra_lora_backward_input, lowra_workspace_bytes, lowra_workspace_init, lowra_lora_forward_batch, lowra_lora_backward_input_batch,
-// lowra_lora_backward_adapters, lowra_lora_backward_adapters_reuse, lowra_adapter_workspace_bytes, lowra_workspace_projection)
+// lowra_lora_backward_adapters, lowra_lora_backward_adapters_reuse, lowra_adapter_workspace_bytes, lowra_workspace_projection, lowra_lora_forward_epilogue)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    void* p[10] = {};
-    for (int i = 0; i < 10; ++i) {
+    void* p[11] = {};
+    for (int i = 0; i < 11; ++i) {
         p[i] = i < n ? PyLong_AsVoidPtr(args[i]) : nullptr;
         if (p[i] == nullptr) {
-            if (PyErr_Occurred() == nullptr) PyErr_SetString(PyExc_ValueError, "bind takes ten addresses");
+            if (PyErr_Occurred() == nullptr) PyErr_SetString(PyExc_ValueError, "bind takes eleven addresses");
             return nullptr;
         }
     }
     library = Library{reinterpret_cast<Product>(p[0]), reinterpret_cast<Product>(p[1]), reinterpret_cast<WorkspaceBytes>(p[2]), reinterpret_cast<WorkspaceInit>(p[3]),
                       reinterpret_cast<Batch>(p[4]), reinterpret_cast<Batch>(p[5]), reinterpret_cast<Gradients>(p[6]), reinterpret_cast<GradientsReuse>(p[7]),
-                      reinterpret_cast<GradientsBytes>(p[8]), reinterpret_cast<Projection>(p[9])};
+                      reinterpret_cast<GradientsBytes>(p[8]), reinterpret_cast<Projection>(p[9]), reinterpret_cast<ProductEpilogue>(p[10])};
     Py_RETURN_NONE;
 }
 
 PyMethodDef methods[] = {
     {"forward", (PyCFunction)(void (*)())forward, METH_FASTCALL, nullptr},
+    {"forward_epilogue", (PyCFunction)(void (*)())forward_epilogue, METH_FASTCALL, nullptr},
     {"backward_input", (PyCFunction)(void (*)())backward_input, METH_FASTCALL, nullptr},
     {"batch", (PyCFunction)(void (*)())batch, METH_FASTCALL, nullptr},
     {"gradients", (PyCFunction)(void (*)())gradients, METH_FASTCALL, nullptr},
