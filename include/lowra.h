@@ -363,6 +363,24 @@ lowra_status lowra_lora_forward_adapters_epilogue(const lowra_layout* layout, co
                                                   const uint16_t* A_dev, const uint16_t* B_dev, int32_t r, float s, const lowra_epilogue* epilogue_host,
                                                   uint16_t* Y_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
 
+/*
+ * The gradient through what stands behind a product (the calls above), in one pass; dZ then goes into lowra_lora_backward_input and
+ * lowra_lora_backward_adapters in the place of dY.  The residual's gradient is dY itself.
+ *     dZ = dY * multiply * act'(Z)          bf16 [M, N] (out), or NULL
+ *     dmultiply = dY * act(Z)               bf16 [M, N] (out), or NULL
+ *     dbias[n] = sum over m of dZ[m, n]     fp32 [N] (out), or NULL: sums of the unrounded values in a fixed order
+ *   dY_dev bf16 [M, N];  pre_dev bf16 [M, N]: the Z that the forward call left (may be NULL without an activation and without dmultiply);
+ *   multiply_dev as in the forward call, or NULL;  relu's slope at zero is 0.
+ *   Outputs may be inputs themselves (dZ in the place of dY or pre, dmultiply in that of multiply), else they overlap nothing.
+ *   workspace_dev: >= lowra_epilogue_workspace_bytes(M, N) bytes, 256-byte aligned, contents overwritten; used for dbias only.
+ * Errors: dY missing, no output, pre or multiply missing where it is needed -> LOWRA_ERR_NULL; M < 1, N % 8 != 0, an activation that is none, dZ and
+ * dmultiply in one place -> LOWRA_ERR_SHAPE; LOWRA_ERR_ALIGN, LOWRA_ERR_WORKSPACE as elsewhere.
+ */
+size_t lowra_epilogue_workspace_bytes(int32_t M, int32_t N);
+lowra_status lowra_epilogue_backward(const uint16_t* dY_dev, const uint16_t* pre_dev, const uint16_t* multiply_dev, int32_t M, int32_t N, int32_t activation,
+                                     uint16_t* dZ_dev, uint16_t* dmultiply_dev, float* dbias_dev, void* workspace_dev, size_t workspace_bytes,
+                                     void* stream);
+
 /* Bytes of device scratch that lowra_lora_backward_adapters needs for M tokens and rank r (0 if the
  * arguments are invalid).  The first 256 bytes hold the device status word. */
 size_t lowra_adapter_workspace_bytes(int32_t M, int32_t r);

@@ -40,7 +40,7 @@ EXPORTS = (
     "lowra_lora_forward_batch", "lowra_lora_backward_input_batch", "lowra_lora_backward_adapters_reuse",
     "lowra_workspace_projection", "lowra_set_wait_limit", "lowra_diag_wait_expiry", "lowra_diag_drop_t_flags",
     "lowra_encode_group", "lowra_decode_group", "lowra_diag_choose", "lowra_lora_forward_epilogue",
-    "lowra_lora_forward_batch_epilogue", "lowra_lora_forward_adapters_epilogue",
+    "lowra_lora_forward_batch_epilogue", "lowra_lora_forward_adapters_epilogue", "lowra_epilogue_workspace_bytes", "lowra_epilogue_backward",
 )
 
 
@@ -155,6 +155,10 @@ def lib() -> ctypes.CDLL:
         L.lowra_lora_forward_batch_epilogue.restype = ctypes.c_int
         L.lowra_lora_forward_adapters_epilogue.argtypes = [lp, vp, vp, vp, i32, vp, i32, vp, vp, vp, i32, ctypes.c_float, ep, vp, vp, ctypes.c_size_t, vp]
         L.lowra_lora_forward_adapters_epilogue.restype = ctypes.c_int
+        L.lowra_epilogue_workspace_bytes.argtypes = [i32, i32]
+        L.lowra_epilogue_workspace_bytes.restype = ctypes.c_size_t
+        L.lowra_epilogue_backward.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.lowra_epilogue_backward.restype = ctypes.c_int
         L.lowra_lora_forward_static.argtypes = [lp, vp, vp, vp, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp, vp]
         L.lowra_lora_forward_static.restype = ctypes.c_int
         L.lowra_learn_codebooks.argtypes = [lp, vp, vp, vp, i32, vp, vp, vp]
@@ -870,6 +874,46 @@ def lowra_channel_errors(W: torch.Tensor, maps3: torch.Tensor, thresholds3: torc
     code = lib().lowra_channel_errors(N, K, _ptr(W), _ptr(maps3), _ptr(thresholds3), _ptr(sse3), _stream(stream))
     _check(code, "lowra_channel_errors")
     return sse3
+
+
+def lowra_epilogue_workspace_bytes(M: int, N: int) -> int:
+    return int(lib().lowra_epilogue_workspace_bytes(int(M), int(N)))
+
+
+def lowra_epilogue_backward(dY: torch.Tensor, pre: Optional[torch.Tensor] = None, activation: str = "none", multiply: Optional[torch.Tensor] = None,
+                            dZ: Optional[torch.Tensor] = None, dmultiply: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                            want_bias: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
+    """The gradient through what stands behind a product (lowra_lora_forward_epilogue): dZ = dY * multiply * act'(pre) bf16 [M, N], which takes dY's place in
+    lowra_lora_backward_input and lowra_lora_backward_adapters, dmultiply = dY * act(pre) where there is a multiply, dbias fp32 [N] if it is given or wanted.
+    Returns (dZ, dmultiply or None, dbias or None)."""
+    number = _activation(activation)
+    if dY.dim() != 2:
+        raise ValueError(f"dY must be [M, N], got {tuple(dY.shape)}")
+    M, N = dY.shape
+    if not _fits(dY.get_device(), dY, "h", 0, pre, "h", 0, multiply, "h", 0, dZ, "h", 0, dmultiply, "h", 0, dbias, "f", 0, workspace, "B", 0):
+        for t, name in ((dY, "dY"), (pre, "pre"), (multiply, "multiply"), (dZ, "dZ"), (dmultiply, "dmultiply")):
+            if t is not None:
+                _dev(t, _BF16, name)
+        if dbias is not None:
+            _dev(dbias, torch.float32, "dbias")
+        _extent(workspace, 0, "workspace")
+    for t, name in ((pre, "pre"), (multiply, "multiply"), (dZ, "dZ"), (dmultiply, "dmultiply")):
+        if t is not None and t.shape != dY.shape:
+            raise ValueError(f"{name} must be [{M}, {N}], got {tuple(t.shape)}")
+    if dbias is not None and dbias.shape != (N,):
+        raise ValueError(f"dbias must be [{N}], got {tuple(dbias.shape)}")
+    if dZ is None:
+        dZ = torch.empty_like(dY)
+    if dmultiply is None and multiply is not None:
+        dmultiply = torch.empty_like(dY)
+    if dbias is None and want_bias:
+        dbias = torch.empty(N, dtype=torch.float32, device=dY.device)
+    if workspace is None and dbias is not None:
+        workspace = _scratch(max(lowra_epilogue_workspace_bytes(M, N), 256), dY.device, stream)
+    code = lib().lowra_epilogue_backward(dY.data_ptr(), _ptr(pre), _ptr(multiply), M, N, number, dZ.data_ptr(), _ptr(dmultiply), _ptr(dbias), _ptr(workspace),
+                                         0 if workspace is None else workspace.numel(), _stream(stream))
+    _check(code, "lowra_epilogue_backward")
+    return dZ, dmultiply, dbias
 
 
 def lowra_adapter_workspace_bytes(M: int, r: int) -> int:

@@ -1,0 +1,176 @@
+// lowra_epilogue_backward: the gradient through what stands behind a product,
+//     dZ = dY * multiply * act'(Z),   dmultiply = dY * act(Z),   dbias[n] = sum over the tokens of dZ[m, n]
+// Bound by memory: 2 bytes for every element of every array, each read or written once.  A thread takes eight neighbouring channels (16 bytes) of a row;
+// without a bias the elements are dealt out flat, with one a CTA takes 256 channels of a run of rows, sums them up in registers (fp32, before dZ is rounded),
+// its eight warps' sums through shared memory, and writes them down for a second kernel that adds up the runs in their order: no atomics, so repeated calls
+// agree bit for bit.  The second launch is left out where one run holds all rows.
+#include "epilogue.cuh"
+
+namespace lowra {
+
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32, kCols = 32 * 8;
+constexpr int kRowsAtOnce = 2;            // rows whose loads are under way together
+constexpr int kCtasPerSm = 6;             // what the runs are cut for
+constexpr int kLeastRows = 32;            // of a run
+
+struct BackwardParams {
+    const uint16_t *dY, *pre, *multiply;
+    uint16_t *dZ, *dmultiply;
+    float* sums;                          // [runs][N], or dbias itself
+    int M, N, activation, rows;           // rows of a run
+};
+
+struct Vec8 {
+    uint4 dY, z, m;
+};
+
+__device__ __forceinline__ void load(const BackwardParams& P, size_t at, Vec8& v) {
+    v.dY = ld_stream_v4(P.dY + at);
+    if (P.pre != nullptr) v.z = ld_stream_v4(P.pre + at);
+    if (P.multiply != nullptr) v.m = ld_stream_v4(P.multiply + at);
+}
+
+// Eight elements: dZ, returned in fp32 too, and dmultiply.
+__device__ __forceinline__ void differentiate(const BackwardParams& P, size_t at, const Vec8& v, float (&dz)[8]) {
+    float dh[8], z[8], h[8];
+    unpack8(v.dY, dz);
+    if (P.pre != nullptr) unpack8(v.z, z);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dh[i] = dz[i];
+    if (P.multiply != nullptr) {
+        float m[8];
+        unpack8(v.m, m);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dz[i] *= m[i];
+    }
+    auto all = [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 a = activate_and_slope<decltype(act)::value>(z[i]);
+            dz[i] *= a.y;
+            h[i] = a.x;
+        }
+    };
+    if (P.activation == LOWRA_ACT_RELU) all(std::integral_constant<int, LOWRA_ACT_RELU>());
+    else if (P.activation == LOWRA_ACT_GELU) all(std::integral_constant<int, LOWRA_ACT_GELU>());
+    else if (P.activation == LOWRA_ACT_GELU_TANH) all(std::integral_constant<int, LOWRA_ACT_GELU_TANH>());
+    else if (P.activation == LOWRA_ACT_SILU) all(std::integral_constant<int, LOWRA_ACT_SILU>());
+    else if (P.pre != nullptr) all(std::integral_constant<int, LOWRA_ACT_NONE>());
+    if (P.dZ != nullptr) *reinterpret_cast<uint4*>(P.dZ + at) = pack8(dz);
+    if (P.dmultiply != nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] *= dh[i];
+        *reinterpret_cast<uint4*>(P.dmultiply + at) = pack8(h);
+    }
+}
+
+__global__ void __launch_bounds__(kThreads, 4) flat_kernel(const __grid_constant__ BackwardParams P) {
+    pdl_enter();
+    const size_t vectors = (size_t)P.M * (size_t)(P.N / 8), step = (size_t)gridDim.x * kThreads;
+    for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < vectors; i += kRowsAtOnce * step) {
+        Vec8 v[kRowsAtOnce];
+#pragma unroll
+        for (int u = 0; u < kRowsAtOnce; ++u)
+            if (i + u * step < vectors) load(P, (i + u * step) * 8, v[u]);
+#pragma unroll
+        for (int u = 0; u < kRowsAtOnce; ++u) {
+            float dz[8];
+            if (i + u * step < vectors) differentiate(P, (i + u * step) * 8, v[u], dz);
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kThreads, 3) rows_kernel(const __grid_constant__ BackwardParams P) {
+    __shared__ float shared[kWarps][kCols];
+    pdl_enter();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = (int)blockIdx.x * kCols + lane * 8;
+    const int m_first = (int)blockIdx.y * P.rows, m_end = min(P.M, m_first + P.rows);
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    for (int m = m_first + warp; n < P.N && m < m_end; m += kRowsAtOnce * kWarps) {
+        Vec8 v[kRowsAtOnce];
+#pragma unroll
+        for (int u = 0; u < kRowsAtOnce; ++u)
+            if (m + u * kWarps < m_end) load(P, (size_t)(m + u * kWarps) * P.N + n, v[u]);
+#pragma unroll
+        for (int u = 0; u < kRowsAtOnce; ++u) {
+            if (m + u * kWarps >= m_end) break;
+            float dz[8];
+            differentiate(P, (size_t)(m + u * kWarps) * P.N + n, v[u], dz);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += dz[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) shared[warp][lane * 8 + i] = sum[i];
+    __syncthreads();
+    const int col = (int)blockIdx.x * kCols + (int)threadIdx.x;
+    if (col >= P.N) return;
+    float total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) total += shared[w][threadIdx.x];
+    P.sums[(size_t)blockIdx.y * P.N + col] = total;
+}
+
+__global__ void __launch_bounds__(128) sum_runs_kernel(const float* sums, int runs, int N, float* out) {
+    pdl_enter();
+    const int n = (int)blockIdx.x * 128 + (int)threadIdx.x;
+    if (n >= N) return;
+    float total = 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < runs; ++i) total += sums[(size_t)i * N + n];
+    out[n] = total;
+}
+
+int runs_of(int M, int N) {
+    const int tiles = (N + kCols - 1) / kCols, wanted = (kNumSMs * kCtasPerSm + tiles - 1) / tiles, most = (M + kLeastRows - 1) / kLeastRows;
+    return wanted < most ? wanted : most;
+}
+
+}  // namespace
+}  // namespace lowra
+
+extern "C" size_t lowra_epilogue_workspace_bytes(int32_t M, int32_t N) {
+    if (M < 1 || N < 8 || N % 8 != 0) return 0;
+    return ((size_t)lowra::runs_of(M, N) * (size_t)N * 4 + 255) / 256 * 256;
+}
+
+extern "C" lowra_status lowra_epilogue_backward(const uint16_t* dY_dev, const uint16_t* pre_dev, const uint16_t* multiply_dev, int32_t M, int32_t N,
+                                                int32_t activation, uint16_t* dZ_dev, uint16_t* dmultiply_dev, float* dbias_dev, void* workspace_dev,
+                                                size_t workspace_bytes, void* stream_v) {
+    using namespace lowra;
+    if (!dY_dev || (!dZ_dev && !dmultiply_dev && !dbias_dev) || (!pre_dev && (activation != LOWRA_ACT_NONE || dmultiply_dev)) || (dmultiply_dev && !multiply_dev))
+        return LOWRA_ERR_NULL;
+    if (M < 1 || N < 8 || N % 8 != 0 || activation < LOWRA_ACT_NONE || activation > LOWRA_ACT_SILU || (dZ_dev && dZ_dev == dmultiply_dev)) return LOWRA_ERR_SHAPE;
+    if (!aligned16(dY_dev) || !aligned16(pre_dev) || !aligned16(multiply_dev) || !aligned16(dZ_dev) || !aligned16(dmultiply_dev) || !aligned16(dbias_dev))
+        return LOWRA_ERR_ALIGN;
+    int runs = dbias_dev ? runs_of(M, N) : 0;
+    if (runs > 1 && (!workspace_dev || workspace_bytes < lowra_epilogue_workspace_bytes(M, N) || (reinterpret_cast<uintptr_t>(workspace_dev) & 255u) != 0))
+        return LOWRA_ERR_WORKSPACE;
+    lowra_status st = check_device();
+    if (st != LOWRA_OK) return st;
+    cudaStream_t stream = (cudaStream_t)stream_v;
+    BackwardParams P = {dY_dev, pre_dev, multiply_dev, dZ_dev, dmultiply_dev, nullptr, M, N, activation, M};
+    if (!dbias_dev) {
+        const size_t ctas = ((size_t)M * (size_t)(N / 8) + kThreads - 1) / kThreads, most = (size_t)kNumSMs * kCtasPerSm;
+        return launch_pdl(flat_kernel, (unsigned)(ctas < most ? ctas : most), kThreads, stream, P) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
+    }
+    P.rows = (M + runs - 1) / runs;
+    runs = (M + P.rows - 1) / P.rows;
+    P.sums = runs > 1 ? static_cast<float*>(workspace_dev) : dbias_dev;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)((N + kCols - 1) / kCols), (unsigned)runs, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, rows_kernel, P) != cudaSuccess) return LOWRA_ERR_CUDA;
+    if (runs > 1 && launch_pdl(sum_runs_kernel, (unsigned)((N + 127) / 128), 128, stream, (const float*)P.sums, runs, N, dbias_dev) != cudaSuccess) return LOWRA_ERR_CUDA;
+    return LOWRA_OK;
+}
