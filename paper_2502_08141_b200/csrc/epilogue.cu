@@ -3,7 +3,8 @@
 // Bound by memory: 2 bytes for every element of every array, each read or written once.  A thread takes eight neighbouring channels (16 bytes) of a row;
 // without a bias the elements are dealt out flat, with one a CTA takes 256 channels of a run of rows, sums them up in registers (fp32, before dZ is rounded),
 // its eight warps' sums through shared memory, and writes them down for a second kernel that adds up the runs in their order: no atomics, so repeated calls
-// agree bit for bit.  The second launch is left out where one run holds all rows.
+// agree bit for bit.  The second launch is left out where one run holds all rows.  (Up to eight runs as a cluster that adds up through distributed shared memory:
+// no second launch, but 333 x 4096 with GELU 6.7 -> 7.1 us, 1001 x 13824 20.2 -> 27.2, whose clusters do not all find room at once.)
 #include "epilogue.cuh"
 
 namespace lowra {
@@ -11,9 +12,8 @@ namespace lowra {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kCols = 32 * 8;
-constexpr int kRowsAtOnce = 2;            // rows whose loads are under way together
-constexpr int kCtasPerSm = 6;             // what the runs are cut for
-constexpr int kLeastRows = 32;            // of a run
+constexpr int kResident = 3;              // CTAs to an SM
+constexpr int kLeastRows = 16;            // of a run
 
 struct BackwardParams {
     const uint16_t *dY, *pre, *multiply;
@@ -26,20 +26,22 @@ struct Vec8 {
     uint4 dY, z, m;
 };
 
+template <bool MULTIPLY>
 __device__ __forceinline__ void load(const BackwardParams& P, size_t at, Vec8& v) {
     v.dY = ld_stream_v4(P.dY + at);
     if (P.pre != nullptr) v.z = ld_stream_v4(P.pre + at);
-    if (P.multiply != nullptr) v.m = ld_stream_v4(P.multiply + at);
+    if (MULTIPLY) v.m = ld_stream_v4(P.multiply + at);
 }
 
 // Eight elements: dZ, returned in fp32 too, and dmultiply.
+template <bool MULTIPLY>
 __device__ __forceinline__ void differentiate(const BackwardParams& P, size_t at, const Vec8& v, float (&dz)[8]) {
     float dh[8], z[8], h[8];
     unpack8(v.dY, dz);
     if (P.pre != nullptr) unpack8(v.z, z);
 #pragma unroll
     for (int i = 0; i < 8; ++i) dh[i] = dz[i];
-    if (P.multiply != nullptr) {
+    if (MULTIPLY) {
         float m[8];
         unpack8(v.m, m);
 #pragma unroll
@@ -59,30 +61,34 @@ __device__ __forceinline__ void differentiate(const BackwardParams& P, size_t at
     else if (P.activation == LOWRA_ACT_SILU) all(std::integral_constant<int, LOWRA_ACT_SILU>());
     else if (P.pre != nullptr) all(std::integral_constant<int, LOWRA_ACT_NONE>());
     if (P.dZ != nullptr) *reinterpret_cast<uint4*>(P.dZ + at) = pack8(dz);
-    if (P.dmultiply != nullptr) {
+    if (MULTIPLY && P.dmultiply != nullptr) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[i] *= dh[i];
         *reinterpret_cast<uint4*>(P.dmultiply + at) = pack8(h);
     }
 }
 
-__global__ void __launch_bounds__(kThreads, 4) flat_kernel(const __grid_constant__ BackwardParams P) {
+template <bool MULTIPLY>
+__global__ void __launch_bounds__(kThreads, kResident) flat_kernel(const __grid_constant__ BackwardParams P) {
+    constexpr int kRowsAtOnce = MULTIPLY ? 2 : 4;         // whose loads are under way together
     pdl_enter();
     const size_t vectors = (size_t)P.M * (size_t)(P.N / 8), step = (size_t)gridDim.x * kThreads;
     for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < vectors; i += kRowsAtOnce * step) {
         Vec8 v[kRowsAtOnce];
 #pragma unroll
         for (int u = 0; u < kRowsAtOnce; ++u)
-            if (i + u * step < vectors) load(P, (i + u * step) * 8, v[u]);
+            if (i + u * step < vectors) load<MULTIPLY>(P, (i + u * step) * 8, v[u]);
 #pragma unroll
         for (int u = 0; u < kRowsAtOnce; ++u) {
             float dz[8];
-            if (i + u * step < vectors) differentiate(P, (i + u * step) * 8, v[u], dz);
+            if (i + u * step < vectors) differentiate<MULTIPLY>(P, (i + u * step) * 8, v[u], dz);
         }
     }
 }
 
-__global__ void __launch_bounds__(kThreads, 3) rows_kernel(const __grid_constant__ BackwardParams P) {
+template <bool MULTIPLY>
+__global__ void __launch_bounds__(kThreads, kResident) rows_kernel(const __grid_constant__ BackwardParams P) {
+    constexpr int kRowsAtOnce = MULTIPLY ? 2 : 4;         // whose loads are under way together
     __shared__ float shared[kWarps][kCols];
     pdl_enter();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = (int)blockIdx.x * kCols + lane * 8;
@@ -94,12 +100,12 @@ __global__ void __launch_bounds__(kThreads, 3) rows_kernel(const __grid_constant
         Vec8 v[kRowsAtOnce];
 #pragma unroll
         for (int u = 0; u < kRowsAtOnce; ++u)
-            if (m + u * kWarps < m_end) load(P, (size_t)(m + u * kWarps) * P.N + n, v[u]);
+            if (m + u * kWarps < m_end) load<MULTIPLY>(P, (size_t)(m + u * kWarps) * P.N + n, v[u]);
 #pragma unroll
         for (int u = 0; u < kRowsAtOnce; ++u) {
             if (m + u * kWarps >= m_end) break;
             float dz[8];
-            differentiate(P, (size_t)(m + u * kWarps) * P.N + n, v[u], dz);
+            differentiate<MULTIPLY>(P, (size_t)(m + u * kWarps) * P.N + n, v[u], dz);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += dz[i];
         }
@@ -108,26 +114,34 @@ __global__ void __launch_bounds__(kThreads, 3) rows_kernel(const __grid_constant
     for (int i = 0; i < 8; ++i) shared[warp][lane * 8 + i] = sum[i];
     __syncthreads();
     const int col = (int)blockIdx.x * kCols + (int)threadIdx.x;
-    if (col >= P.N) return;
     float total = 0.0f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) total += shared[w][threadIdx.x];
-    P.sums[(size_t)blockIdx.y * P.N + col] = total;
+    if (col < P.N) P.sums[(size_t)blockIdx.y * P.N + col] = total;
 }
 
-__global__ void __launch_bounds__(128) sum_runs_kernel(const float* sums, int runs, int N, float* out) {
+// A CTA takes 32 channels, each of its eight warps an eighth of the runs.
+__global__ void __launch_bounds__(kThreads) sum_runs_kernel(const float* sums, int runs, int N, float* out) {
+    __shared__ float shared[kWarps][32];
     pdl_enter();
-    const int n = (int)blockIdx.x * 128 + (int)threadIdx.x;
-    if (n >= N) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = (int)blockIdx.x * 32 + lane;
+    const int first = runs * warp / kWarps, end = runs * (warp + 1) / kWarps;
     float total = 0.0f;
-#pragma unroll 8
-    for (int i = 0; i < runs; ++i) total += sums[(size_t)i * N + n];
+    if (n < N) {
+#pragma unroll 4
+        for (int i = first; i < end; ++i) total += sums[(size_t)i * N + n];
+    }
+    shared[warp][lane] = total;
+    __syncthreads();
+    if (warp != 0 || n >= N) return;
+    for (int w = 1; w < kWarps; ++w) total += shared[w][lane];
     out[n] = total;
 }
 
+// So many that their CTAs are all resident at once (one more wave of a few cost a third of the time: 4096 x 11008 gated 72 -> 100 us).
 int runs_of(int M, int N) {
-    const int tiles = (N + kCols - 1) / kCols, wanted = (kNumSMs * kCtasPerSm + tiles - 1) / tiles, most = (M + kLeastRows - 1) / kLeastRows;
-    return wanted < most ? wanted : most;
+    const int tiles = (N + kCols - 1) / kCols, wanted = kNumSMs * kResident / tiles, most = (M + kLeastRows - 1) / kLeastRows;
+    return wanted < 1 ? 1 : wanted < most ? wanted : most;
 }
 
 }  // namespace
@@ -155,8 +169,8 @@ extern "C" lowra_status lowra_epilogue_backward(const uint16_t* dY_dev, const ui
     cudaStream_t stream = (cudaStream_t)stream_v;
     BackwardParams P = {dY_dev, pre_dev, multiply_dev, dZ_dev, dmultiply_dev, nullptr, M, N, activation, M};
     if (!dbias_dev) {
-        const size_t ctas = ((size_t)M * (size_t)(N / 8) + kThreads - 1) / kThreads, most = (size_t)kNumSMs * kCtasPerSm;
-        return launch_pdl(flat_kernel, (unsigned)(ctas < most ? ctas : most), kThreads, stream, P) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
+        const size_t ctas = ((size_t)M * (size_t)(N / 8) + kThreads - 1) / kThreads, most = (size_t)kNumSMs * kResident;
+        return launch_pdl(multiply_dev ? flat_kernel<true> : flat_kernel<false>, (unsigned)(ctas < most ? ctas : most), kThreads, stream, P) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
     }
     P.rows = (M + runs - 1) / runs;
     runs = (M + P.rows - 1) / P.rows;
@@ -170,7 +184,7 @@ extern "C" lowra_status lowra_epilogue_backward(const uint16_t* dY_dev, const ui
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, rows_kernel, P) != cudaSuccess) return LOWRA_ERR_CUDA;
-    if (runs > 1 && launch_pdl(sum_runs_kernel, (unsigned)((N + 127) / 128), 128, stream, (const float*)P.sums, runs, N, dbias_dev) != cudaSuccess) return LOWRA_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, multiply_dev ? rows_kernel<true> : rows_kernel<false>, P) != cudaSuccess) return LOWRA_ERR_CUDA;
+    if (runs > 1 && launch_pdl(sum_runs_kernel, (unsigned)((N + 31) / 32), kThreads, stream, (const float*)P.sums, runs, N, dbias_dev) != cudaSuccess) return LOWRA_ERR_CUDA;
     return LOWRA_OK;
 }
