@@ -426,6 +426,49 @@ lowra_status lowra_lora_backward_adapters_reuse(const uint16_t* X_dev, const uin
                                                 size_t workspace_bytes, void* stream);
 
 /*
+ * (No counterpart in the paper.)  A training step's last part: momentum and an update of the low-rank factors that Newton-Schulz products make orthogonal,
+ * for the factors of a layer, or of several, in one call of three launches.  For every factor (A [K, r] or B [r, N]), all in fp32 or more:
+ *     m' = momentum * m + g;     u = g + momentum * m' (nesterov) or m' (else);  without a momentum buffer u = g
+ *     X_0 = u / (|u| + eps), |u| the Frobenius norm;     X <- a X + X (b G + c G^2), G = X^T X (of the side r), `steps` times
+ *     w' = (1 - lr weight_decay) w - lr scale X;         weight = bf16(w')
+ * The matrices G are formed and iterated in fp64 (their condition is the square of u's).
+ *   lowra_factor: rows x cols, one of them r, the other a multiple of 8; row-major, without gaps, device, 16-byte aligned
+ *     grad_dev           bf16 (as lowra_lora_backward_adapters writes it) or, with grad_fp32 != 0, fp32                    (in)
+ *     momentum_dev       fp32, or NULL: no momentum                      (in);   momentum_out_dev  m', may be momentum_dev itself     (out)
+ *     master_dev         fp32 w, or NULL                                 (in);   master_out_dev    w', may be master_dev itself       (out)
+ *     weight_dev         bf16, or NULL: the factor as the products above take it; only with a master                          (out)
+ *     update_dev         fp32 X, or NULL; at least one of master and update                                                   (out)
+ *     scale              factor of lr for this member (for instance sqrt(max(1, rows / cols)))
+ *   members_host: HOST array of 1 .. LOWRA_MAX_FACTORS members, read before the call returns; their arrays overlap nothing else
+ *   lowra_update_step: steps 1 .. 32; coefficients a, b, c (usually 3.4445, -4.775, 2.0315); eps > 0 keeps a factor of zeros at zero
+ *   workspace_dev: >= lowra_update_workspace_bytes(members_host, count, r) bytes (rows and cols are read), 256-byte aligned, contents overwritten
+ * A factor whose u holds a NaN or an infinity gets NaN; the others are not touched by it.  Results do not depend on the run (no atomics), but on which
+ * factors share a call, by roundings of fp64.
+ * Errors: r not in {16, 32, ..., 128}, shapes, count or steps out of range -> LOWRA_ERR_SHAPE; LOWRA_ERR_NULL (an array without its partner too),
+ * LOWRA_ERR_ALIGN, LOWRA_ERR_WORKSPACE as elsewhere.
+ */
+#define LOWRA_MAX_FACTORS 64
+typedef struct {
+    int32_t rows, cols;
+    const void* grad_dev;
+    const float* momentum_dev;
+    float* momentum_out_dev;
+    const float* master_dev;
+    float* master_out_dev;
+    uint16_t* weight_dev;
+    float* update_dev;
+    double scale;
+    int32_t grad_fp32;
+} lowra_factor;
+typedef struct {
+    double lr, momentum, weight_decay, eps, coefficients[3];
+    int32_t nesterov, steps;
+} lowra_update_step;
+size_t lowra_update_workspace_bytes(const lowra_factor* members_host, int32_t count, int32_t r);
+lowra_status lowra_update_factors(const lowra_factor* members_host, int32_t count, int32_t r, const lowra_update_step* step_host, void* workspace_dev,
+                                  size_t workspace_bytes, void* stream);
+
+/*
  * Synchronises `stream` and returns the status word that the last forward / backward call wrote
  * into its workspace: LOWRA_OK, or LOWRA_ERR_TIMEOUT if a bounded wait inside a kernel ran out
  * (the kernel then released its resources and returned; the output is not valid).

@@ -41,6 +41,7 @@ EXPORTS = (
     "lowra_workspace_projection", "lowra_set_wait_limit", "lowra_diag_wait_expiry", "lowra_diag_drop_t_flags",
     "lowra_encode_group", "lowra_decode_group", "lowra_diag_choose", "lowra_lora_forward_epilogue",
     "lowra_lora_forward_batch_epilogue", "lowra_lora_forward_adapters_epilogue", "lowra_epilogue_workspace_bytes", "lowra_epilogue_backward",
+    "lowra_update_workspace_bytes", "lowra_update_factors",
 )
 
 
@@ -79,6 +80,17 @@ class _CMember(ctypes.Structure):
 class _CEpilogue(ctypes.Structure):
     _fields_ = [("bias_dev", ctypes.c_void_p), ("multiply_dev", ctypes.c_void_p), ("residual_dev", ctypes.c_void_p), ("pre_dev", ctypes.c_void_p),
                 ("activation", ctypes.c_int32), ("bias_bf16", ctypes.c_int32)]
+
+
+class _CFactor(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("grad_dev", ctypes.c_void_p), ("momentum_dev", ctypes.c_void_p),
+                ("momentum_out_dev", ctypes.c_void_p), ("master_dev", ctypes.c_void_p), ("master_out_dev", ctypes.c_void_p), ("weight_dev", ctypes.c_void_p),
+                ("update_dev", ctypes.c_void_p), ("scale", ctypes.c_double), ("grad_fp32", ctypes.c_int32)]
+
+
+class _CUpdateStep(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("weight_decay", ctypes.c_double), ("eps", ctypes.c_double),
+                ("coefficients", ctypes.c_double * 3), ("nesterov", ctypes.c_int32), ("steps", ctypes.c_int32)]
 
 
 _lib = None
@@ -159,6 +171,11 @@ def lib() -> ctypes.CDLL:
         L.lowra_epilogue_workspace_bytes.restype = ctypes.c_size_t
         L.lowra_epilogue_backward.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.lowra_epilogue_backward.restype = ctypes.c_int
+        fp = ctypes.POINTER(_CFactor)
+        L.lowra_update_workspace_bytes.argtypes = [fp, i32, i32]
+        L.lowra_update_workspace_bytes.restype = ctypes.c_size_t
+        L.lowra_update_factors.argtypes = [fp, i32, i32, ctypes.POINTER(_CUpdateStep), vp, ctypes.c_size_t, vp]
+        L.lowra_update_factors.restype = ctypes.c_int
         L.lowra_lora_forward_static.argtypes = [lp, vp, vp, vp, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp, vp]
         L.lowra_lora_forward_static.restype = ctypes.c_int
         L.lowra_learn_codebooks.argtypes = [lp, vp, vp, vp, i32, vp, vp, vp]
@@ -1003,6 +1020,73 @@ def lowra_lora_backward_adapters_reuse(X, dY, T, U, r: int, dA: Optional[torch.T
                                                     _ptr(workspace), workspace.numel(), _stream(stream))
     _check(code, "lowra_lora_backward_adapters_reuse")
     return dA, dB
+
+
+LOWRA_MAX_FACTORS = 64
+
+
+def lowra_update_workspace_bytes(shapes, r: int) -> int:
+    """Scratch of lowra_update_factors for factors of these shapes (rows, cols)."""
+    arr = (_CFactor * max(len(shapes), 1))()
+    for c, (rows, cols) in zip(arr, shapes):
+        c.rows, c.cols = int(rows), int(cols)
+    return int(lib().lowra_update_workspace_bytes(arr, len(shapes), int(r)))
+
+
+def lowra_update_factors(members, lr: float, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, steps: int = 5,
+                         coefficients=(3.4445, -4.775, 2.0315), eps: float = 1e-7, rank: Optional[int] = None, workspace: Optional[torch.Tensor] = None,
+                         stream=None):
+    """Momentum and an orthogonalised (Newton-Schulz) update of up to LOWRA_MAX_FACTORS low-rank factors of one rank.  `members`: dicts with
+    grad (bf16 or fp32 [rows, cols]: dA [K, r] or dB [r, N]) and, optionally, momentum (fp32; updated in place unless momentum_out is given), master (fp32
+    weights; updated in place unless master_out is given), weight (bf16, receives the rounded weights), update (fp32, receives the orthogonal matrix) and
+    scale (a factor of lr, 1 if not given).  A member without a master needs an update.  `rank`: the side that all have in common (which one is taken where there are two
+    makes no difference but of roundings).  Returns the members."""
+    n = len(members)
+    if n == 0:
+        raise ValueError("no members")
+    arr = (_CFactor * n)()
+    common = None
+    for i, m in enumerate(members):
+        grad = m["grad"]
+        if grad.dim() != 2:
+            raise ValueError(f"grad of member {i} must be a matrix, got {tuple(grad.shape)}")
+        if grad.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"grad of member {i} must be {torch.bfloat16} or {torch.float32}, got {grad.dtype}")
+        shape, fp32 = grad.shape, grad.dtype == torch.float32
+        old, new, w, w_new = m.get("momentum"), m.get("momentum_out"), m.get("master"), m.get("master_out")
+        new = old if new is None else new
+        w_new = w if w_new is None else w_new
+        weight, update = m.get("weight"), m.get("update")
+        if not _fits(grad.get_device(), grad, "f" if fp32 else "h", 0, old, "f", 0, new, "f", 0, w, "f", 0, w_new, "f", 0, weight, "h", 0, update, "f", 0):
+            _dev(grad, grad.dtype, "grad")
+            for t, name in ((old, "momentum"), (new, "momentum_out"), (w, "master"), (w_new, "master_out"), (update, "update")):
+                if t is not None:
+                    _dev(t, torch.float32, name)
+            if weight is not None:
+                _dev(weight, _BF16, "weight")
+        for t, name in ((old, "momentum"), (new, "momentum_out"), (w, "master"), (w_new, "master_out"), (weight, "weight"), (update, "update")):
+            if t is not None and t.shape != shape:
+                raise ValueError(f"{name} of member {i} must be {list(shape)}, got {list(t.shape)}")
+        common = set(shape) if common is None else common & set(shape)
+        c = arr[i]
+        c.rows, c.cols = shape
+        c.grad_dev, c.momentum_dev, c.momentum_out_dev = grad.data_ptr(), _ptr(old), _ptr(new)
+        c.master_dev, c.master_out_dev, c.weight_dev, c.update_dev = _ptr(w), _ptr(w_new), _ptr(weight), _ptr(update)
+        c.scale, c.grad_fp32 = float(m.get("scale", 1.0)), int(fp32)
+    if rank is None:
+        if not common:
+            raise ValueError("the members have no side in common that could be the rank")
+        rank = min(common, key=lambda d: (d % 16 != 0 or d > 128, d))
+    step = _CUpdateStep(float(lr), float(momentum), float(weight_decay), float(eps), (ctypes.c_double * 3)(*coefficients), int(bool(nesterov)), int(steps))
+    _extent(workspace, 0, "workspace")
+    if workspace is None:
+        size = int(lib().lowra_update_workspace_bytes(arr, n, rank))
+        if size == 0:
+            raise LowraError(LOWRA_ERR_SHAPE, "lowra_update_workspace_bytes")
+        workspace = _scratch(size, members[0]["grad"].device, stream)
+    code = lib().lowra_update_factors(arr, n, rank, ctypes.byref(step), _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(code, "lowra_update_factors")
+    return members
 
 
 def lowra_device_status(workspace: torch.Tensor, stream=None) -> int:
