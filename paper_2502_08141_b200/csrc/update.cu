@@ -20,7 +20,8 @@ namespace {
 constexpr int kThreads = 128, kWarps = kThreads / 32;     // of the two kernels that walk over u
 constexpr int kTileElements = 4096;                       // of u at a time: 32 to a thread
 constexpr int kQuads = kTileElements / 4 / kThreads;      // four neighbouring elements each, to a thread
-constexpr int kWalkers = 2 * kNumSMs;                     // CTAs that share the tiles of all factors out
+constexpr int kWalkers = 2 * kNumSMs;                     // CTAs that share the tiles of all factors out, in gram_kernel
+constexpr int kApplyResident = 2;                         // CTAs of apply_kernel to an SM
 constexpr int kMaxFactors = LOWRA_MAX_FACTORS;
 
 struct Factor {
@@ -51,7 +52,6 @@ template <int NB>
 struct Shape {
     static constexpr int r = 16 * NB, blocks = 2 * NB, tri = blocks * (blocks + 1) / 2;
     static constexpr int TL = kTileElements / r / 16 * 16 < 48 ? kTileElements / r / 8 * 8 : kTileElements / r / 16 * 16;    // u at a time: so many of the long side
-    static constexpr int quads = TL * r / 4;
     // shared memory of a tile of u, element (l, c) at l * sl + c * sc: without bank conflicts for the stores of four neighbours in memory and for the
     // fragments (eight c, four l)
     static constexpr int tall_pitch = r + 8, wide_pitch = (TL + 31) / 32 * 32 + 4;
@@ -63,39 +63,67 @@ __device__ __forceinline__ void dmma(double (&c)[2], double a, double b) {
     asm("mma.sync.aligned.m8n8k4.row.col.f64.f64.f64.f64 {%0, %1}, {%2}, {%3}, {%0, %1};" : "+d"(c[0]), "+d"(c[1]) : "d"(a), "d"(b));
 }
 
-// What a thread holds of a tile: its quads of the gradient and of the momentum.
-template <int NB>
+// How a tile's quads (four neighbours in memory) go to the threads: rows of them in passes, the threads of a pass side by side in memory.  A row is one of the
+// long side (tall: its r values) or of the rank (wide: TL values).
+template <int NB, bool TALL>
+struct Deal {
+    using S = Shape<NB>;
+    static constexpr int per_row = (TALL ? S::r : S::TL) / 4, rows = TALL ? S::TL : S::r, at_once = kThreads / per_row, passes = rows / at_once;
+    static_assert(at_once * passes == rows && passes <= kQuads, "whole passes");
+    bool in;                      // this thread has quads (wide: that lie inside; the length is a multiple of 8, so a quad is in or out as a whole)
+    int row, col;                 // of its first one
+    size_t at;                    // in the factor's arrays
+    size_t step;
+    int left;                     // tall: rows of the tile inside the factor
+    __device__ __forceinline__ Deal(const Factor& F, int l0) {
+        row = (int)threadIdx.x / per_row;
+        col = (int)threadIdx.x % per_row * 4;
+        in = row < at_once && (TALL || l0 + col < F.L);
+        at = TALL ? (size_t)(l0 + row) * S::r + col : (size_t)row * F.L + (l0 + col);
+        step = TALL ? (size_t)(at_once * S::r) : (size_t)at_once * F.L;
+        left = F.L - l0;
+    }
+    template <typename Body>      // body(pass, place in memory, inside)
+    __device__ __forceinline__ void each(Body body) const {
+        size_t p = at;
+#pragma unroll
+        for (int i = 0; i < passes; ++i, p += step) body(i, p, in && (!TALL || row + i * at_once < left));
+    }
+};
+
+// What a thread holds of a tile: its quads of the gradient (bf16 or fp32) and of the momentum.
 struct Held {
     uint4 g[kQuads];
     float4 m[kQuads];
 };
 
-template <int NB, typename Body>
-__device__ __forceinline__ void for_quads(const Factor& F, int l0, Body body) {
-    using S = Shape<NB>;
-#pragma unroll
-    for (int i = 0; i < kQuads; ++i) {
-        const int q = (int)threadIdx.x + i * kThreads;
-        int l, c;
-        if (F.tall) { l = q / (S::r / 4); c = q % (S::r / 4) * 4; }
-        else { c = q / (S::TL / 4); l = q % (S::TL / 4) * 4; }
-        if (S::quads % kThreads != 0 && q >= S::quads) continue;
-        const bool in = l0 + l < F.L;                  // (wide: the length is a multiple of 8, so a quad is in or out as a whole)
-        const size_t at = F.tall ? (size_t)(l0 + l) * S::r + c : (size_t)c * F.L + (l0 + l);
-        body(i, l, c, at, in);
-    }
-}
-
 __device__ __forceinline__ float4 grad_quad(const Factor& F, uint4 g) {
     if (F.grad_fp32) return make_float4(__uint_as_float(g.x), __uint_as_float(g.y), __uint_as_float(g.z), __uint_as_float(g.w));
     return make_float4(__uint_as_float(g.x << 16), __uint_as_float(g.x & 0xffff0000u), __uint_as_float(g.y << 16), __uint_as_float(g.y & 0xffff0000u));
 }
-__device__ __forceinline__ uint4 load_grad(const Factor& F, size_t at) {
-    if (F.grad_fp32) return *reinterpret_cast<const uint4*>(static_cast<const float*>(F.grad) + at);
-    const uint2 p = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(F.grad) + at);
-    return make_uint4(p.x, p.y, 0u, 0u);
-}
 __device__ __forceinline__ float4 axpy(float a, float4 x, float4 y) { return make_float4(fmaf(a, x.x, y.x), fmaf(a, x.y, y.y), fmaf(a, x.z, y.z), fmaf(a, x.w, y.w)); }
+
+__device__ __forceinline__ float4 axpy2(float a, float4 x, float4 y) {       // two products to an instruction
+    const float2 aa = make_float2(a, a), lo = fma2(aa, make_float2(x.x, x.y), make_float2(y.x, y.y)), hi = fma2(aa, make_float2(x.z, x.w), make_float2(y.z, y.w));
+    return make_float4(lo.x, lo.y, hi.x, hi.y);
+}
+__device__ __forceinline__ float4 zero4() { return make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+
+// The tile's gradient, and its old momentum (OLD) or the new one where u needs it.
+template <int NB, bool TALL, bool OLD>
+__device__ __forceinline__ void fetch(const UpdateParams& P, const Factor& F, int l0, Held& held) {
+    const Deal<NB, TALL> deal(F, l0);
+    const float* m = OLD ? F.momentum : F.momentum_out;
+    if (OLD || m == nullptr || P.nesterov) {
+        if (F.grad_fp32) deal.each([&](int i, size_t at, bool in) { held.g[i] = in ? *reinterpret_cast<const uint4*>(static_cast<const float*>(F.grad) + at) : make_uint4(0u, 0u, 0u, 0u); });
+        else deal.each([&](int i, size_t at, bool in) {
+            const uint2 p = in ? *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(F.grad) + at) : make_uint2(0u, 0u);
+            held.g[i].x = p.x;
+            held.g[i].y = p.y;
+        });
+    }
+    if (m != nullptr) deal.each([&](int i, size_t at, bool in) { held.m[i] = in ? __ldcg(reinterpret_cast<const float4*>(m + at)) : zero4(); });
+}
 
 // The walkers' shares of the tiles; the factor of a tile.
 __device__ __forceinline__ int share(const UpdateParams& P, int walker) { return (int)((long long)P.tiles * walker / gridDim.x); }
@@ -127,23 +155,26 @@ __global__ void __launch_bounds__(kThreads, 2) gram_kernel(const __grid_constant
     const int first = share(P, blockIdx.x), end = share(P, blockIdx.x + 1);
     if (first >= end) return;
     int f = factor_of(P, first);
-    Held<NB> held;
-    auto fetch = [&](int tile) {
-        const Factor& F = P.f[factor_of(P, tile)];
-        for_quads<NB>(F, (tile - F.tile0) * S::TL, [&](int i, int, int, size_t at, bool in) {
-            held.g[i] = in ? load_grad(F, at) : make_uint4(0u, 0u, 0u, 0u);
-            held.m[i] = in && F.momentum != nullptr ? *reinterpret_cast<const float4*>(F.momentum + at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        });
+    Held held;
+    auto fetch_tile = [&](int tile, int factor) {
+        const Factor& F = P.f[factor];
+        const int l0 = (tile - F.tile0) * S::TL;
+        if (F.tall) fetch<NB, true, true>(P, F, l0, held);
+        else fetch<NB, false, true>(P, F, l0, held);
     };
-    fetch(first);
+    fetch_tile(first, f);
     double acc[kAcc][2];
 #pragma unroll
     for (int i = 0; i < kAcc; ++i) acc[i][0] = acc[i][1] = 0.0;
-    for (int tile = first; tile < end; ++tile) {
-        const Factor& F = P.f[f];
-        float* u = tiles[(tile - first) & 1];
-        const int sl = F.tall ? S::tall_pitch : 1, sc = F.tall ? 1 : S::wide_pitch;
-        for_quads<NB>(F, (tile - F.tile0) * S::TL, [&](int i, int l, int c, size_t at, bool in) {
+    // u of the tile into shared memory, the new momentum into its own
+    auto put = [&](auto tall, const Factor& F, int l0, float* u) {
+        constexpr bool TALL = decltype(tall)::value;
+        using D = Deal<NB, TALL>;
+        constexpr int pitch = TALL ? S::tall_pitch : S::wide_pitch;
+        const D deal(F, l0);
+        float* to = u + deal.row * pitch + deal.col;
+        const bool has = deal.row < D::at_once;
+        deal.each([&](int i, size_t at, bool in) {
             const float4 grad = grad_quad(F, held.g[i]);
             float4 x = grad;
             if (F.momentum != nullptr) {
@@ -151,19 +182,29 @@ __global__ void __launch_bounds__(kThreads, 2) gram_kernel(const __grid_constant
                 if (in) *reinterpret_cast<float4*>(F.momentum_out + at) = m;
                 x = P.nesterov ? axpy(P.mu, m, grad) : m;
             }
-            *reinterpret_cast<float4*>(u + l * sl + c * sc) = x;
+            if (has) *reinterpret_cast<float4*>(to + i * D::at_once * pitch) = x;
         });
-        if (tile + 1 < end) fetch(tile + 1);
-        __syncthreads();                                                     // the tile is there (and the one before it has been read)
-        const int k0 = kSplit ? 0 : warp * (S::TL / kWarps), k1 = kSplit ? S::TL : k0 + S::TL / kWarps;
-        const float* at = u + g * sc + t4 * sl;
+    };
+    auto multiply = [&](auto tall, const float* u) {
+        constexpr bool TALL = decltype(tall)::value;
+        constexpr int sl = TALL ? S::tall_pitch : 1, sc = TALL ? 1 : S::wide_pitch;
+        constexpr int steps = (kSplit ? S::TL : S::TL / kWarps) / 4;
+        const float* at = u + g * sc + t4 * sl + (kSplit ? 0 : warp * (S::TL / kWarps) * sl);
         if (!kSplit || warp < 2) {
             at += kSplit ? warp * (8 * NB) * sc : 0;
+            float next[kSide];
+#pragma unroll
+            for (int i = 0; i < kSide; ++i) next[i] = at[i * 8 * sc];
 #pragma unroll 1
-            for (int k = k0; k < k1; k += 4) {
+            for (int k = 0; k < steps; ++k) {
                 double x[kSide];
 #pragma unroll
-                for (int i = 0; i < kSide; ++i) x[i] = (double)at[k * sl + i * 8 * sc];
+                for (int i = 0; i < kSide; ++i) x[i] = (double)next[i];
+                if (k + 1 < steps) {
+                    at += 4 * sl;
+#pragma unroll
+                    for (int i = 0; i < kSide; ++i) next[i] = at[i * 8 * sc];
+                }
                 int n = 0;
 #pragma unroll
                 for (int i = 0; i < kSide; ++i) {
@@ -173,13 +214,14 @@ __global__ void __launch_bounds__(kThreads, 2) gram_kernel(const __grid_constant
             }
         } else {
             const int j0 = (warp - 2) * kHalf;
+            const float* bt = at + (NB + j0) * 8 * sc;
 #pragma unroll 1
-            for (int k = k0; k < k1; k += 4) {
+            for (int k = 0; k < steps; ++k, at += 4 * sl, bt += 4 * sl) {
                 double x[NB], y[kHalf];
 #pragma unroll
-                for (int i = 0; i < NB; ++i) x[i] = (double)at[k * sl + i * 8 * sc];
+                for (int i = 0; i < NB; ++i) x[i] = (double)at[i * 8 * sc];
 #pragma unroll
-                for (int j = 0; j < kHalf; ++j) y[j] = j0 + j < NB ? (double)at[k * sl + (NB + j0 + j) * 8 * sc] : 0.0;
+                for (int j = 0; j < kHalf; ++j) y[j] = j0 + j < NB ? (double)bt[j * 8 * sc] : 0.0;
 #pragma unroll
                 for (int i = 0; i < NB; ++i) {
 #pragma unroll
@@ -187,8 +229,19 @@ __global__ void __launch_bounds__(kThreads, 2) gram_kernel(const __grid_constant
                 }
             }
         }
-        const bool last = tile + 1 == end || P.f[f].tile0 + (P.f[f].L + S::TL - 1) / S::TL == tile + 1;
-        if (!last) continue;
+    };
+    for (int tile = first; tile < end; ++tile) {
+        const Factor& F = P.f[f];
+        const int l0 = (tile - F.tile0) * S::TL;
+        const bool last_of_factor = l0 + S::TL >= F.L;
+        float* u = tiles[(tile - first) & 1];
+        if (F.tall) put(std::true_type(), F, l0, u);
+        else put(std::false_type(), F, l0, u);
+        if (tile + 1 < end) fetch_tile(tile + 1, last_of_factor ? f + 1 : f);
+        __syncthreads();                                                     // the tile is there (and the one before it has been read)
+        if (F.tall) multiply(std::true_type(), u);
+        else multiply(std::false_type(), u);
+        if (tile + 1 < end && !last_of_factor) continue;
         double2* out = reinterpret_cast<double2*>(P.sums) + (size_t)(blockIdx.x + f) * S::tri * 32;
         if (kSplit) {
             if (warp < 2) {
@@ -208,18 +261,20 @@ __global__ void __launch_bounds__(kThreads, 2) gram_kernel(const __grid_constant
                 }
             }
         } else {
-            // the warps' sums, one warp after the other, in the places of the tiles' shared memory
-            for (int w = 0; w < kWarps; ++w) {
-                __syncthreads();
-                if (warp == w) {
+            // the warps' sums, through shared memory, in the warps' order
+            __syncthreads();
 #pragma unroll
-                    for (int n = 0; n < S::tri; ++n) {
-                        double2 v = make_double2(acc[n][0], acc[n][1]);
-                        if (w > 0) { v.x += joined[n * 32 + lane].x; v.y += joined[n * 32 + lane].y; }
-                        if (w + 1 < kWarps) joined[n * 32 + lane] = v;
-                        else out[n * 32 + lane] = v;
-                    }
+            for (int n = 0; n < S::tri; ++n) joined[(n * kWarps + warp) * 32 + lane] = make_double2(acc[n][0], acc[n][1]);
+            __syncthreads();
+            for (int n = warp; n < S::tri; n += kWarps) {
+                double2 v = joined[n * kWarps * 32 + lane];
+#pragma unroll
+                for (int w = 1; w < kWarps; ++w) {
+                    const double2 x = joined[(n * kWarps + w) * 32 + lane];
+                    v.x += x.x;
+                    v.y += x.y;
                 }
+                out[n * 32 + lane] = v;
             }
             __syncthreads();
         }
@@ -250,7 +305,8 @@ __global__ void __launch_bounds__(1024) iterate_kernel(const __grid_constant__ U
     double* Q = Pk + S::tri * 64;
     double* M = kThree ? G : Q + S::tri * 64;
     double* trace = Q + (kThree ? 1 : 2) * S::tri * 64;          // [B], of the diagonal blocks
-    pdl_enter();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (behind the wait: apply_kernel reads what gram_kernel wrote before its own)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     const int f = (int)blockIdx.x / ctas, rank = (int)blockIdx.x % ctas;
     const Factor& F = P.f[f];
@@ -264,24 +320,52 @@ __global__ void __launch_bounds__(1024) iterate_kernel(const __grid_constant__ U
         const uint32_t at = ptx::smem_u32(X + own);
         for (int i = 0; i < ctas; ++i) st_cluster_f64x2(ptx::map_to_cta(at, (uint32_t)i), v[0], v[1]);
     };
-    // fragments of block (i, k) as the first operand and of block (k, j) as the second, of its four contraction indices 4 h ..
-    auto first = [&](const double* X, int k, int h) {
-        return k >= bi ? X[tri_index(B, bi, k) * 64 + in_block(g, 4 * h + t4)] : X[tri_index(B, k, bi) * 64 + in_block(4 * h + t4, g)];
-    };
-    auto second = [&](const double* X, int k, int h) {
-        return k <= bj ? X[tri_index(B, k, bj) * 64 + in_block(4 * h + t4, g)] : X[tri_index(B, bj, k) * 64 + in_block(g, 4 * h + t4)];
-    };
-    auto product = [&](const double* X, const double* Y, double (&v)[2]) {
-        double odd[2] = {0.0, 0.0};
+    // Blocks (bi, k) of X times blocks (k, bj) of Y, for one or two X.  Those left of the diagonal in X's row and below it in Y's column are read as transposes:
+    // three ranges of k, in each of which the places of the blocks follow by simple steps.
+    const int straight = in_block(g, t4), across = in_block(t4, g), straight4 = in_block(g, 4 + t4) - straight;      // (across: 32 further)
+    auto products = [&](auto two, const double* X, const double* X2, const double* Y, double (&v)[2], double (&v2)[2]) {
+        constexpr bool TWO = decltype(two)::value;
+        double odd[2] = {0.0, 0.0}, odd2[2] = {0.0, 0.0};
         v[0] = v[1] = 0.0;
+        if (TWO) v2[0] = v2[1] = 0.0;
+        int xo = bi * 64, yo = bj * 64;                          // block (0, bi), block (0, bj)
+        auto step = [&](int xl, int x4, int yl, int y4) {
+            const double y0 = Y[yo + yl], y1 = Y[yo + yl + y4];
+            dmma(v, X[xo + xl], y0);
+            dmma(odd, X[xo + xl + x4], y1);
+            if (TWO) {
+                dmma(v2, X2[xo + xl], y0);
+                dmma(odd2, X2[xo + xl + x4], y1);
+            }
+        };
+        int k = 0;
 #pragma unroll 2
-        for (int k = 0; k < B; ++k) {
-            dmma(v, first(X, k, 0), second(Y, k, 0));
-            dmma(odd, first(X, k, 1), second(Y, k, 1));
+        for (; k < bi; ++k) {
+            step(across, 32, across, 32);
+            xo += (B - 1 - k) * 64;
+            yo += (B - 1 - k) * 64;
+        }
+#pragma unroll 2
+        for (; k <= bj; ++k) {
+            step(straight, straight4, across, 32);
+            xo += 64;
+            yo += (k < bj ? B - 1 - k : 1) * 64;                 // (the block behind (bj, bj) is (bj, bj + 1))
+        }
+#pragma unroll 2
+        for (; k < B; ++k) {
+            step(straight, straight4, straight, straight4);
+            xo += 64;
+            yo += 64;
         }
         v[0] += odd[0];
         v[1] += odd[1];
+        if (TWO) {
+            v2[0] += odd2[0];
+            v2[1] += odd2[1];
+        }
     };
+    double unused[2];
+    auto product = [&](const double* X, const double* Y, double (&v)[2]) { products(std::false_type(), X, X, Y, v, unused); };
     ptx::cluster_sync();                                          // (every CTA of the cluster runs: its shared memory may be written)
     // ---- S, from its parts in the walkers' order
     if (mine) {
@@ -326,13 +410,17 @@ __global__ void __launch_bounds__(1024) iterate_kernel(const __grid_constant__ U
         ptx::cluster_sync();
         const bool more = step + 1 < P.steps;
         if (mine) {
-            if (step > 0) product(Q, Pk, q);
-            else { q[0] = p[0]; q[1] = p[1]; }
-            if (more) {
-                product(G, Pk, v);
-                v[0] *= alpha;
-                v[1] *= alpha;
+            if (step == 0) {
+                q[0] = p[0];
+                q[1] = p[1];
+                if (more) product(G, Pk, v);
+            } else if (more) {
+                products(std::true_type(), G, Q, Pk, v, q);
+            } else {
+                product(Q, Pk, q);
             }
+            v[0] *= alpha;
+            v[1] *= alpha;
         }
         if (!more) break;
         if (kThree) ptx::cluster_sync();                          // everybody has read G
@@ -360,102 +448,127 @@ __global__ void __launch_bounds__(1024) iterate_kernel(const __grid_constant__ U
 }
 
 // ------------------------------------------------------------------------------------------------ u Q, and the weights
-// A thread forms eight of the long side times four ranks, from the tile of u and Q in shared memory, fp32.
+// A thread forms eight of the long side times four ranks, from the tile of u and Q in shared memory, fp32.  What the tile after this one needs of the gradient
+// and the momentum, and this one's master weights, are under way meanwhile.
 template <int NB>
-__global__ void __launch_bounds__(kThreads, 2) apply_kernel(const __grid_constant__ UpdateParams P) {
+__global__ void __launch_bounds__(kThreads, kApplyResident) apply_kernel(const __grid_constant__ UpdateParams P) {
     using S = Shape<NB>;
     constexpr int kPitch = S::r + 4;                              // u, tall: [l][c]
     extern __shared__ __align__(16) unsigned char update_smem[];
     float* Q = reinterpret_cast<float*>(update_smem);             // [r][r]
     float* u = Q + S::r * S::r;                                   // tall: [TL][kPitch]; wide: [r][TL]
-    pdl_enter();
     const int first = share(P, blockIdx.x), end = share(P, blockIdx.x + 1);
-    int f = first < end ? factor_of(P, first) : 0, loaded = -1;
+    if (first >= end) return;
+    int f = factor_of(P, first), loaded = -1;
+    Held held;
+    auto fetch_tile = [&](int tile, int factor) {
+        const Factor& F = P.f[factor];
+        const int l0 = (tile - F.tile0) * S::TL;
+        if (F.tall) fetch<NB, true, false>(P, F, l0, held);
+        else fetch<NB, false, false>(P, F, l0, held);
+    };
+    auto put = [&](auto tall, const Factor& F, int l0) {
+        constexpr bool TALL = decltype(tall)::value;
+        using D = Deal<NB, TALL>;
+        constexpr int pitch = TALL ? kPitch : S::TL;
+        const D deal(F, l0);
+        float* to = u + deal.row * pitch + deal.col;
+        if (deal.row >= D::at_once) return;
+        deal.each([&](int i, size_t, bool) {
+            float4 x = F.momentum != nullptr ? held.m[i] : grad_quad(F, held.g[i]);
+            if (F.momentum != nullptr && P.nesterov) x = axpy(P.mu, x, grad_quad(F, held.g[i]));
+            *reinterpret_cast<float4*>(to + i * D::at_once * pitch) = x;
+        });
+    };
+    // thread's outputs, quads of four neighbours in memory: number i of eight at place + (i / 4) * far + (i % 4) * near
+    auto work = [&](auto tall, const Factor& F, int l0, auto next) {
+        constexpr bool TALL = decltype(tall)::value;
+        constexpr int groups = S::TL / 8;
+        // tall: ranks c .. c + 3, rows lg, lg + TL / 8, ...: a warp's lanes lie side by side along the rank
+        // wide: ranks c .. c + 3, and two runs of four of the long side: the lanes lie side by side along it
+        const int cg = TALL ? (int)threadIdx.x % (S::r / 4) : (int)threadIdx.x / groups, lg = TALL ? (int)threadIdx.x / (S::r / 4) : (int)threadIdx.x % groups;
+        const bool has = TALL ? lg < groups : cg < S::r / 4;
+        const size_t place = TALL ? (size_t)(l0 + lg) * S::r + cg * 4 : (size_t)(cg * 4) * F.L + (l0 + lg * 4);
+        const size_t near_by = TALL ? (size_t)(groups * S::r) : (size_t)F.L, far = TALL ? 4 * near_by : (size_t)(S::TL / 2);
+        auto inside = [&](int i) { return has && (TALL ? l0 + lg + i * groups < F.L : l0 + lg * 4 + (i / 4) * (S::TL / 2) < F.L); };
+        float4 w[8];
+        if (F.master != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = inside(i) ? *reinterpret_cast<const float4*>(F.master + place + (i / 4) * far + (i % 4) * near_by) : zero4();
+        }
+        next();
+        float4 acc[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] = zero4();
+        if (has) {
+            if (TALL) {
+                const float *x_at = u + lg * kPitch, *q_at = Q + cg * 4;
+#pragma unroll 1
+                for (int j = 0; j < S::r; j += 4, x_at += 4, q_at += 4 * S::r) {
+                    float4 q[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) q[k] = *reinterpret_cast<const float4*>(q_at + k * S::r);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float4 x = *reinterpret_cast<const float4*>(x_at + i * groups * kPitch);
+                        acc[i] = axpy2(x.x, q[0], acc[i]);
+                        acc[i] = axpy2(x.y, q[1], acc[i]);
+                        acc[i] = axpy2(x.z, q[2], acc[i]);
+                        acc[i] = axpy2(x.w, q[3], acc[i]);
+                    }
+                }
+            } else {
+                const float *x_at = u + lg * 4, *q_at = Q + cg * 4;
+#pragma unroll 4
+                for (int j = 0; j < S::r; ++j, x_at += S::TL, q_at += S::r) {
+                    const float4 q = *reinterpret_cast<const float4*>(q_at);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float4 x = *reinterpret_cast<const float4*>(x_at + h * (S::TL / 2));
+                        acc[4 * h] = axpy2(q.x, x, acc[4 * h]);
+                        acc[4 * h + 1] = axpy2(q.y, x, acc[4 * h + 1]);
+                        acc[4 * h + 2] = axpy2(q.z, x, acc[4 * h + 2]);
+                        acc[4 * h + 3] = axpy2(q.w, x, acc[4 * h + 3]);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (!inside(i)) continue;
+            const size_t at = place + (i / 4) * far + (i % 4) * near_by;
+            if (F.update != nullptr) *reinterpret_cast<float4*>(F.update + at) = acc[i];
+            if (F.master != nullptr) {
+                const float4 n = make_float4(fmaf(-F.rate, acc[i].x, P.decay * w[i].x), fmaf(-F.rate, acc[i].y, P.decay * w[i].y),
+                                             fmaf(-F.rate, acc[i].z, P.decay * w[i].z), fmaf(-F.rate, acc[i].w, P.decay * w[i].w));
+                *reinterpret_cast<float4*>(F.master_out + at) = n;
+                if (F.weight != nullptr) *reinterpret_cast<uint2*>(F.weight + at) = make_uint2(pack_bf16x2(n.x, n.y), pack_bf16x2(n.z, n.w));
+            }
+        }
+    };
+    // (iterate_kernel lets this kernel start when gram_kernel is through: u may be read before the wait for Q)
+    fetch_tile(first, f);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     for (int tile = first; tile < end; ++tile) {
-        while (f + 1 < P.count && P.f[f + 1].tile0 <= tile) ++f;
         const Factor& F = P.f[f];
         const int l0 = (tile - F.tile0) * S::TL;
+        const bool last_of_factor = l0 + S::TL >= F.L;
+        if (F.tall) put(std::true_type(), F, l0);
+        else put(std::false_type(), F, l0);
         if (loaded != f) {
+            if (loaded < 0) asm volatile("griddepcontrol.wait;" ::: "memory");
             for (int i = threadIdx.x; i < S::r * S::r / 4; i += kThreads)
                 reinterpret_cast<float4*>(Q)[i] = __ldcg(reinterpret_cast<const float4*>(P.Q + (size_t)f * S::r * S::r) + i);
             loaded = f;
         }
-        for_quads<NB>(F, l0, [&](int, int l, int c, size_t at, bool in) {
-            float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (in) {
-                if (F.momentum == nullptr) x = grad_quad(F, load_grad(F, at));
-                else {
-                    x = *reinterpret_cast<const float4*>(F.momentum_out + at);
-                    if (P.nesterov) x = axpy(P.mu, x, grad_quad(F, load_grad(F, at)));
-                }
-            }
-            *reinterpret_cast<float4*>(F.tall ? u + l * kPitch + c : u + c * S::TL + l) = x;
-        });
         __syncthreads();
-        auto finish = [&](size_t at, float4 x) {
-            if (F.update != nullptr) *reinterpret_cast<float4*>(F.update + at) = x;
-            if (F.master != nullptr) {
-                const float4 w = *reinterpret_cast<const float4*>(F.master + at);
-                const float4 n = make_float4(fmaf(-F.rate, x.x, P.decay * w.x), fmaf(-F.rate, x.y, P.decay * w.y), fmaf(-F.rate, x.z, P.decay * w.z),
-                                             fmaf(-F.rate, x.w, P.decay * w.w));
-                *reinterpret_cast<float4*>(F.master_out + at) = n;
-                if (F.weight != nullptr) *reinterpret_cast<uint2*>(F.weight + at) = make_uint2(pack_bf16x2(n.x, n.y), pack_bf16x2(n.z, n.w));
-            }
+        auto next = [&]() {
+            if (tile + 1 < end) fetch_tile(tile + 1, last_of_factor ? f + 1 : f);
         };
-        if (F.tall) {
-            // thread: ranks c0 .. c0 + 3, rows lg, lg + TL / 8, ...: a warp's lanes lie side by side along the rank
-            const int cg = (int)threadIdx.x % (S::r / 4), lg = (int)threadIdx.x / (S::r / 4);
-            if (lg < S::TL / 8) {
-                float4 acc[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 1
-                for (int j = 0; j < S::r; j += 4) {
-                    float4 x[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const float4*>(u + (lg + i * (S::TL / 8)) * kPitch + j);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float4 q = *reinterpret_cast<const float4*>(Q + (j + k) * S::r + cg * 4);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) acc[i] = axpy(k == 0 ? x[i].x : k == 1 ? x[i].y : k == 2 ? x[i].z : x[i].w, q, acc[i]);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int l = l0 + lg + i * (S::TL / 8);
-                    if (l < F.L) finish((size_t)l * S::r + cg * 4, acc[i]);
-                }
-            }
-        } else {
-            // thread: ranks c0 .. c0 + 3, and two runs of four of the long side: a warp's lanes lie side by side along it
-            const int lg = (int)threadIdx.x % (S::TL / 8), cg = (int)threadIdx.x / (S::TL / 8);
-            if (cg < S::r / 4) {
-                float4 acc[2][4];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i / 4][i % 4] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-                for (int j = 0; j < S::r; ++j) {
-                    const float4 q = *reinterpret_cast<const float4*>(Q + j * S::r + cg * 4);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float4 x = *reinterpret_cast<const float4*>(u + j * S::TL + h * (S::TL / 2) + lg * 4);
-                        acc[h][0] = axpy(q.x, x, acc[h][0]);
-                        acc[h][1] = axpy(q.y, x, acc[h][1]);
-                        acc[h][2] = axpy(q.z, x, acc[h][2]);
-                        acc[h][3] = axpy(q.w, x, acc[h][3]);
-                    }
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int l = l0 + h * (S::TL / 2) + lg * 4;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        if (l < F.L) finish((size_t)(cg * 4 + c) * F.L + l, acc[h][c]);
-                }
-            }
-        }
-        __syncthreads();
+        if (F.tall) work(std::true_type(), F, l0, next);
+        else work(std::false_type(), F, l0, next);
+        __syncthreads();                                          // u and Q have been read
+        if (last_of_factor) ++f;
     }
 }
 
@@ -491,7 +604,7 @@ lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream
     cfg.blockDim = dim3(kThreads, 1, 1);
     {
         static SmemLimit limit = {};
-        const size_t tiles = 2 * S::floats * 4, joined = NB > 4 ? 0 : (size_t)S::tri * 512;
+        const size_t tiles = 2 * S::floats * 4, joined = NB > 4 ? 0 : (size_t)S::tri * 512 * kWarps;
         cfg.dynamicSmemBytes = tiles > joined ? tiles : joined;
         if (ensure_smem_limit(reinterpret_cast<const void*>(gram_kernel<NB>), cfg.dynamicSmemBytes, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
         if (cudaLaunchKernelEx(&cfg, gram_kernel<NB>, P) != cudaSuccess) return LOWRA_ERR_CUDA;
@@ -514,7 +627,7 @@ lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream
     static SmemLimit limit = {};
     const size_t tall = (size_t)S::TL * (S::r + 4), wide = (size_t)S::TL * S::r;
     cfg.dynamicSmemBytes = ((size_t)S::r * S::r + (tall > wide ? tall : wide)) * 4;
-    cfg.gridDim = dim3(walkers, 1, 1);
+    cfg.gridDim = dim3((unsigned)(P.tiles < kApplyResident * kNumSMs ? P.tiles : kApplyResident * kNumSMs), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
     if (ensure_smem_limit(reinterpret_cast<const void*>(apply_kernel<NB>), cfg.dynamicSmemBytes, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
     return cudaLaunchKernelEx(&cfg, apply_kernel<NB>, P) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
