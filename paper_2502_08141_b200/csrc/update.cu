@@ -17,11 +17,12 @@ namespace lowra {
 
 namespace {
 
-constexpr int kThreads = 128, kWarps = kThreads / 32;     // of the two kernels that walk over u
+constexpr int kThreads = 128, kWarps = kThreads / 32;     // that share a tile of u
 constexpr int kTileElements = 4096;                       // of u at a time: 32 to a thread
 constexpr int kQuads = kTileElements / 4 / kThreads;      // four neighbouring elements each, to a thread
-constexpr int kWalkers = 2 * kNumSMs;                     // CTAs that share the tiles of all factors out, in gram_kernel
-constexpr int kApplyResident = 2;                         // CTAs of apply_kernel to an SM
+constexpr int kWalkers = kNumSMs;                         // CTAs that share the tiles of all factors out, in gram_kernel
+constexpr int kStages = 4, kFillers = 2;                  // tiles in its shared memory; groups of kThreads that fill them
+constexpr int kGramThreads = (1 + kFillers) * kThreads;
 constexpr int kMaxFactors = LOWRA_MAX_FACTORS;
 
 struct Factor {
@@ -34,13 +35,13 @@ struct Factor {
     float* update;
     int L;
     float rate;                    // lr * scale
-    int tile0;                     // tiles of the factors before this one
+    int tile0, item0;              // tiles of the factors before this one; tiles of apply_kernel
     uint8_t tall, grad_fp32;
 };
 struct UpdateParams {
     double* sums;                  // [walker + factor][tiles of S][64]: the part of S that a walker has formed
     float* Q;                      // [factor][r][r]
-    int count, tiles;
+    int count, tiles, items;
     float mu, decay;               // decay: 1 - lr wd
     int nesterov, steps;
     double a, b, c, eps;
@@ -63,31 +64,34 @@ __device__ __forceinline__ void dmma(double (&c)[2], double a, double b) {
     asm("mma.sync.aligned.m8n8k4.row.col.f64.f64.f64.f64 {%0, %1}, {%2}, {%3}, {%0, %1};" : "+d"(c[0]), "+d"(c[1]) : "d"(a), "d"(b));
 }
 
+// The most rows up to `most` that `rows` is a multiple of.
+__host__ __device__ constexpr int whole_rows(int rows, int most) { return rows % most == 0 ? most : whole_rows(rows, most - 1); }
+
 // How a tile's quads (four neighbours in memory) go to the threads: rows of them in passes, the threads of a pass side by side in memory.  A row is one of the
 // long side (tall: its r values) or of the rank (wide: TL values).
-template <int NB, bool TALL>
+template <int NB, bool TALL, int T = kThreads, int TL = Shape<NB>::TL>
 struct Deal {
     using S = Shape<NB>;
-    static constexpr int per_row = (TALL ? S::r : S::TL) / 4, rows = TALL ? S::TL : S::r, at_once = kThreads / per_row, passes = rows / at_once;
+    static constexpr int per_row = (TALL ? S::r : TL) / 4, rows = TALL ? TL : S::r, at_once = whole_rows(rows, T / per_row), passes = rows / at_once;
     static_assert(at_once * passes == rows && passes <= kQuads, "whole passes");
     bool in;                      // this thread has quads (wide: that lie inside; the length is a multiple of 8, so a quad is in or out as a whole)
     int row, col;                 // of its first one
     size_t at;                    // in the factor's arrays
     size_t step;
     int left;                     // tall: rows of the tile inside the factor
-    __device__ __forceinline__ Deal(const Factor& F, int l0) {
-        row = (int)threadIdx.x / per_row;
-        col = (int)threadIdx.x % per_row * 4;
+    __device__ __forceinline__ Deal(const Factor& F, int l0, int thread) {      // (several groups of T threads may take a tile each)
+        row = thread / per_row;
+        col = thread % per_row * 4;
         in = row < at_once && (TALL || l0 + col < F.L);
         at = TALL ? (size_t)(l0 + row) * S::r + col : (size_t)row * F.L + (l0 + col);
         step = TALL ? (size_t)(at_once * S::r) : (size_t)at_once * F.L;
         left = F.L - l0;
     }
-    template <typename Body>      // body(pass, place in memory, inside)
+    template <int FROM = 0, int N = kQuads, typename Body>      // body(pass, place in memory, inside), for passes FROM .. FROM + N - 1
     __device__ __forceinline__ void each(Body body) const {
-        size_t p = at;
+        size_t p = at + FROM * step;
 #pragma unroll
-        for (int i = 0; i < passes; ++i, p += step) body(i, p, in && (!TALL || row + i * at_once < left));
+        for (int i = FROM; i < FROM + N && i < passes; ++i, p += step) body(i, p, in && (!TALL || row + i * at_once < left));
     }
 };
 
@@ -110,81 +114,111 @@ __device__ __forceinline__ float4 axpy2(float a, float4 x, float4 y) {       // 
 __device__ __forceinline__ float4 zero4() { return make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
 
 // The tile's gradient, and its old momentum (OLD) or the new one where u needs it.
-template <int NB, bool TALL, bool OLD>
-__device__ __forceinline__ void fetch(const UpdateParams& P, const Factor& F, int l0, Held& held) {
-    const Deal<NB, TALL> deal(F, l0);
+template <bool OLD, int FROM = 0, int N = kQuads, typename D>
+__device__ __forceinline__ void fetch(const UpdateParams& P, const Factor& F, const D& deal, Held& held) {
     const float* m = OLD ? F.momentum : F.momentum_out;
     if (OLD || m == nullptr || P.nesterov) {
-        if (F.grad_fp32) deal.each([&](int i, size_t at, bool in) { held.g[i] = in ? *reinterpret_cast<const uint4*>(static_cast<const float*>(F.grad) + at) : make_uint4(0u, 0u, 0u, 0u); });
-        else deal.each([&](int i, size_t at, bool in) {
+        if (F.grad_fp32) deal.template each<FROM, N>([&](int i, size_t at, bool in) { held.g[i] = in ? *reinterpret_cast<const uint4*>(static_cast<const float*>(F.grad) + at) : make_uint4(0u, 0u, 0u, 0u); });
+        else deal.template each<FROM, N>([&](int i, size_t at, bool in) {
             const uint2 p = in ? *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(F.grad) + at) : make_uint2(0u, 0u);
             held.g[i].x = p.x;
             held.g[i].y = p.y;
         });
     }
-    if (m != nullptr) deal.each([&](int i, size_t at, bool in) { held.m[i] = in ? __ldcg(reinterpret_cast<const float4*>(m + at)) : zero4(); });
+    if (m != nullptr) deal.template each<FROM, N>([&](int i, size_t at, bool in) { held.m[i] = in ? __ldcg(reinterpret_cast<const float4*>(m + at)) : zero4(); });
+}
+
+// The thread's number, as if it were another one every time: what follows from it is then worked out where it is needed.  (Kept from tile to tile, the places of
+// both orientations' quads and outputs took 400 bytes of local memory a thread, more traffic than u.)
+__device__ __forceinline__ int thread_here() {
+    int t;
+    asm volatile("mov.u32 %0, %%tid.x;" : "=r"(t));
+    return t;
 }
 
 // The walkers' shares of the tiles; the factor of a tile.
-__device__ __forceinline__ int share(const UpdateParams& P, int walker) { return (int)((long long)P.tiles * walker / gridDim.x); }
+__device__ __forceinline__ int share_of(int tiles, int walker) { return (int)((long long)tiles * walker / gridDim.x); }
+__device__ __forceinline__ int share(const UpdateParams& P, int walker) { return share_of(P.tiles, walker); }
+template <int Factor::*FIRST = &Factor::tile0>
 __device__ __forceinline__ int factor_of(const UpdateParams& P, int tile) {
     int lo = 0, hi = P.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (P.f[mid].tile0 <= tile) lo = mid;
+        if (P.f[mid].*FIRST <= tile) lo = mid;
         else hi = mid - 1;
     }
     return lo;
 }
 
 // ------------------------------------------------------------------------------------------------ parts of S
-// A walker takes neighbouring tiles; what it forms of a factor's S goes to slot walker + factor (both only ever go up, so a slot is one walker's and one
-// factor's).  Up to r = 64 every warp takes a quarter of the tile's long side and all blocks of S (36 at r = 64: 144 registers); above that each warp takes
+// A walker (one CTA to an SM) takes neighbouring tiles; what it forms of a factor's S goes to slot walker + factor (both only ever go up, so a slot is one
+// walker's and one factor's).  Two groups of four warps take the tiles in turn: gradient and momentum into registers, the new momentum to memory, u to shared
+// memory.  The four warps of a third group feed the tensor instructions, one warp to a scheduler, which is enough to keep them busy.  (All warps doing both in turn, two CTAs
+// to an SM: the tensor pipe 52 % busy while an SM was, with the filling's instructions in between.)
+// Up to r = 64 every warp takes a quarter of the tile's long side and all blocks of S (36 at r = 64: 144 registers); above that each warp takes
 // all of it and a quarter of the blocks: the triangles of the two halves of the rank, and two halves of the square between them.
+__device__ __forceinline__ void barrier_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+constexpr int kFull = 1, kEmpty = kFull + kStages, kJoin = kEmpty + kStages;       // named barriers
+
 template <int NB>
-__global__ void __launch_bounds__(kThreads, 2) gram_kernel(const __grid_constant__ UpdateParams P) {
+struct GramMemory {
+    static constexpr size_t tiles = (size_t)kStages * Shape<NB>::floats * 4, joined = NB > 4 ? 0 : (size_t)Shape<NB>::tri * 512 * kWarps, bytes = tiles + joined;
+};
+
+template <int NB>
+__global__ void __launch_bounds__(kGramThreads, 1) gram_kernel(const __grid_constant__ UpdateParams P) {
     using S = Shape<NB>;
     constexpr bool kSplit = NB > 4;
     constexpr int kSide = kSplit ? NB : 2 * NB, kHalf = (NB + 1) / 2;       // blocks of a triangle's side; columns of a part of the square
     constexpr int kAcc = kSplit && NB * kHalf > kSide * (kSide + 1) / 2 ? NB * kHalf : kSide * (kSide + 1) / 2;
     extern __shared__ __align__(16) unsigned char update_smem[];
-    float* tiles[2] = {reinterpret_cast<float*>(update_smem), reinterpret_cast<float*>(update_smem) + S::floats};
-    double2* joined = reinterpret_cast<double2*>(update_smem);              // (after the last tile)
+    float* tiles = reinterpret_cast<float*>(update_smem);
     pdl_enter();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
-    const int first = share(P, blockIdx.x), end = share(P, blockIdx.x + 1);
-    if (first >= end) return;
+    const int group = (int)threadIdx.x / kThreads;
+    const int first = share(P, blockIdx.x), count = share(P, blockIdx.x + 1) - first;
     int f = factor_of(P, first);
-    Held held;
-    auto fetch_tile = [&](int tile, int factor) {
-        const Factor& F = P.f[factor];
-        const int l0 = (tile - F.tile0) * S::TL;
-        if (F.tall) fetch<NB, true, true>(P, F, l0, held);
-        else fetch<NB, false, true>(P, F, l0, held);
-    };
-    fetch_tile(first, f);
+    if (group > 0) {
+        // ================================================================== fillers: tiles group - 1, group - 1 + kFillers, ...
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 136;");
+        Held held;
+        for (int n = group - 1; n < count; n += kFillers) {
+            while (f + 1 < P.count && P.f[f + 1].tile0 <= first + n) ++f;
+            const Factor& F = P.f[f];
+            const int l0 = (first + n - F.tile0) * S::TL, stage = n % kStages;
+            float* u = tiles + stage * S::floats;
+            auto fill = [&](auto tall) {
+                constexpr bool TALL = decltype(tall)::value;
+                using D = Deal<NB, TALL>;
+                constexpr int pitch = TALL ? S::tall_pitch : S::wide_pitch;
+                const D deal(F, l0, thread_here() % kThreads);
+                fetch<true>(P, F, deal, held);
+                float* to = u + deal.row * pitch + deal.col;
+                const bool has = deal.row < D::at_once;
+                if (n >= kStages) ptx::named_barrier_sync(kEmpty + stage, 2 * kThreads);      // the tile there before has been read
+                deal.each([&](int i, size_t at, bool in) {
+                    const float4 grad = grad_quad(F, held.g[i]);
+                    float4 x = grad;
+                    if (F.momentum != nullptr) {
+                        const float4 m = axpy2(P.mu, held.m[i], grad);
+                        if (in) *reinterpret_cast<float4*>(F.momentum_out + at) = m;
+                        x = P.nesterov ? axpy2(P.mu, m, grad) : m;
+                    }
+                    if (has) *reinterpret_cast<float4*>(to + i * D::at_once * pitch) = x;
+                });
+            };
+            if (F.tall) fill(std::true_type());
+            else fill(std::false_type());
+            barrier_arrive(kFull + stage, 2 * kThreads);
+        }
+        return;
+    }
+    // ====================================================================== the products
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    double2* joined = reinterpret_cast<double2*>(update_smem + GramMemory<NB>::tiles);
     double acc[kAcc][2];
 #pragma unroll
     for (int i = 0; i < kAcc; ++i) acc[i][0] = acc[i][1] = 0.0;
-    // u of the tile into shared memory, the new momentum into its own
-    auto put = [&](auto tall, const Factor& F, int l0, float* u) {
-        constexpr bool TALL = decltype(tall)::value;
-        using D = Deal<NB, TALL>;
-        constexpr int pitch = TALL ? S::tall_pitch : S::wide_pitch;
-        const D deal(F, l0);
-        float* to = u + deal.row * pitch + deal.col;
-        const bool has = deal.row < D::at_once;
-        deal.each([&](int i, size_t at, bool in) {
-            const float4 grad = grad_quad(F, held.g[i]);
-            float4 x = grad;
-            if (F.momentum != nullptr) {
-                const float4 m = axpy(P.mu, held.m[i], grad);
-                if (in) *reinterpret_cast<float4*>(F.momentum_out + at) = m;
-                x = P.nesterov ? axpy(P.mu, m, grad) : m;
-            }
-            if (has) *reinterpret_cast<float4*>(to + i * D::at_once * pitch) = x;
-        });
-    };
     auto multiply = [&](auto tall, const float* u) {
         constexpr bool TALL = decltype(tall)::value;
         constexpr int sl = TALL ? S::tall_pitch : 1, sc = TALL ? 1 : S::wide_pitch;
@@ -215,13 +249,24 @@ __global__ void __launch_bounds__(kThreads, 2) gram_kernel(const __grid_constant
         } else {
             const int j0 = (warp - 2) * kHalf;
             const float* bt = at + (NB + j0) * 8 * sc;
+            float nx[NB], ny[kHalf];
+            auto ask = [&]() {
+#pragma unroll
+                for (int i = 0; i < NB; ++i) nx[i] = at[i * 8 * sc];
+#pragma unroll
+                for (int j = 0; j < kHalf; ++j) ny[j] = j0 + j < NB ? bt[j * 8 * sc] : 0.0f;
+            };
+            ask();
 #pragma unroll 1
-            for (int k = 0; k < steps; ++k, at += 4 * sl, bt += 4 * sl) {
+            for (int k = 0; k < steps; ++k) {
                 double x[NB], y[kHalf];
 #pragma unroll
-                for (int i = 0; i < NB; ++i) x[i] = (double)at[i * 8 * sc];
+                for (int i = 0; i < NB; ++i) x[i] = (double)nx[i];
 #pragma unroll
-                for (int j = 0; j < kHalf; ++j) y[j] = j0 + j < NB ? (double)bt[j * 8 * sc] : 0.0;
+                for (int j = 0; j < kHalf; ++j) y[j] = (double)ny[j];
+                at += 4 * sl;
+                bt += 4 * sl;
+                if (k + 1 < steps) ask();
 #pragma unroll
                 for (int i = 0; i < NB; ++i) {
 #pragma unroll
@@ -230,26 +275,24 @@ __global__ void __launch_bounds__(kThreads, 2) gram_kernel(const __grid_constant
             }
         }
     };
-    for (int tile = first; tile < end; ++tile) {
+    for (int n = 0; n < count; ++n) {
         const Factor& F = P.f[f];
-        const int l0 = (tile - F.tile0) * S::TL;
-        const bool last_of_factor = l0 + S::TL >= F.L;
-        float* u = tiles[(tile - first) & 1];
-        if (F.tall) put(std::true_type(), F, l0, u);
-        else put(std::false_type(), F, l0, u);
-        if (tile + 1 < end) fetch_tile(tile + 1, last_of_factor ? f + 1 : f);
-        __syncthreads();                                                     // the tile is there (and the one before it has been read)
+        const int stage = n % kStages;
+        ptx::named_barrier_sync(kFull + stage, 2 * kThreads);
+        const float* u = tiles + stage * S::floats;
         if (F.tall) multiply(std::true_type(), u);
         else multiply(std::false_type(), u);
-        if (tile + 1 < end && !last_of_factor) continue;
+        if (n + kStages < count) barrier_arrive(kEmpty + stage, 2 * kThreads);
+        const bool last_of_factor = (first + n - F.tile0 + 1) * S::TL >= F.L;
+        if (n + 1 < count && !last_of_factor) continue;
         double2* out = reinterpret_cast<double2*>(P.sums) + (size_t)(blockIdx.x + f) * S::tri * 32;
         if (kSplit) {
             if (warp < 2) {
-                int n = 0;
+                int b = 0;
 #pragma unroll
                 for (int i = 0; i < kSide; ++i) {
 #pragma unroll
-                    for (int j = i; j < kSide; ++j, ++n) out[tri_index(S::blocks, warp * NB + i, warp * NB + j) * 32 + lane] = make_double2(acc[n][0], acc[n][1]);
+                    for (int j = i; j < kSide; ++j, ++b) out[tri_index(S::blocks, warp * NB + i, warp * NB + j) * 32 + lane] = make_double2(acc[b][0], acc[b][1]);
                 }
             } else {
                 const int j0 = (warp - 2) * kHalf;
@@ -262,21 +305,20 @@ __global__ void __launch_bounds__(kThreads, 2) gram_kernel(const __grid_constant
             }
         } else {
             // the warps' sums, through shared memory, in the warps' order
-            __syncthreads();
 #pragma unroll
-            for (int n = 0; n < S::tri; ++n) joined[(n * kWarps + warp) * 32 + lane] = make_double2(acc[n][0], acc[n][1]);
-            __syncthreads();
-            for (int n = warp; n < S::tri; n += kWarps) {
-                double2 v = joined[n * kWarps * 32 + lane];
+            for (int b = 0; b < S::tri; ++b) joined[(b * kWarps + warp) * 32 + lane] = make_double2(acc[b][0], acc[b][1]);
+            ptx::named_barrier_sync(kJoin, kThreads);
+            for (int b = warp; b < S::tri; b += kWarps) {
+                double2 v = joined[b * kWarps * 32 + lane];
 #pragma unroll
                 for (int w = 1; w < kWarps; ++w) {
-                    const double2 x = joined[(n * kWarps + w) * 32 + lane];
+                    const double2 x = joined[(b * kWarps + w) * 32 + lane];
                     v.x += x.x;
                     v.y += x.y;
                 }
-                out[n * 32 + lane] = v;
+                out[b * 32 + lane] = v;
             }
-            __syncthreads();
+            ptx::named_barrier_sync(kJoin, kThreads);
         }
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) acc[i][0] = acc[i][1] = 0.0;
@@ -448,127 +490,147 @@ __global__ void __launch_bounds__(1024) iterate_kernel(const __grid_constant__ U
 }
 
 // ------------------------------------------------------------------------------------------------ u Q, and the weights
-// A thread forms eight of the long side times four ranks, from the tile of u and Q in shared memory, fp32.  What the tile after this one needs of the gradient
-// and the momentum, and this one's master weights, are under way meanwhile.
+// On the fp32 pipe: a thread forms eight of the long side times four ranks, from a tile of u and Q in shared memory.  (In two or three tf32 parts on the tensor
+// instructions it was no faster, and its errors, 2e-5 of the update, were ten times those of fp32.)  Three CTAs to an SM up to rank 64, above that one of three times the
+// threads and tile, which share Q: the warps cover one another's loads.
+// u, four neighbours in memory, from the gradient and the new momentum.
+struct Raw {
+    uint4 g;
+    float4 m;
+};
+__device__ __forceinline__ Raw load_raw(const UpdateParams& P, const Factor& F, size_t at, bool in) {
+    Raw r;
+    r.g = make_uint4(0u, 0u, 0u, 0u);
+    r.m = zero4();
+    if (in && F.momentum_out != nullptr) r.m = __ldcg(reinterpret_cast<const float4*>(F.momentum_out + at));
+    if (in && (F.momentum_out == nullptr || P.nesterov)) {
+        if (F.grad_fp32) r.g = __ldg(reinterpret_cast<const uint4*>(static_cast<const float*>(F.grad) + at));
+        else {
+            const uint2 p = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(F.grad) + at));
+            r.g.x = p.x;
+            r.g.y = p.y;
+        }
+    }
+    return r;
+}
+__device__ __forceinline__ float4 u_of(const UpdateParams& P, const Factor& F, const Raw& r) {
+    if (F.momentum_out == nullptr) return grad_quad(F, r.g);
+    return P.nesterov ? axpy(P.mu, r.m, grad_quad(F, r.g)) : r.m;
+}
+
 template <int NB>
-__global__ void __launch_bounds__(kThreads, kApplyResident) apply_kernel(const __grid_constant__ UpdateParams P) {
+struct ApplyShape {
     using S = Shape<NB>;
-    constexpr int kPitch = S::r + 4;                              // u, tall: [l][c]
+    static constexpr int groups_of_threads = NB > 4 ? 3 : 1, threads = kThreads * groups_of_threads, TL = S::TL * groups_of_threads, resident = NB > 4 ? 1 : 3;
+    static constexpr int pitch = S::r + 4;                        // u, tall: [l][c]
+    static constexpr size_t tall = (size_t)TL * pitch, wide = (size_t)TL * S::r, bytes = ((size_t)S::r * S::r + (tall > wide ? tall : wide)) * 4;
+};
+template <int NB>
+__global__ void __launch_bounds__(ApplyShape<NB>::threads, ApplyShape<NB>::resident) apply_kernel(const __grid_constant__ UpdateParams P) {
+    using S = Shape<NB>;
+    using A = ApplyShape<NB>;
+    constexpr int TL = A::TL, groups = TL / 8;
     extern __shared__ __align__(16) unsigned char update_smem[];
     float* Q = reinterpret_cast<float*>(update_smem);             // [r][r]
-    float* u = Q + S::r * S::r;                                   // tall: [TL][kPitch]; wide: [r][TL]
-    const int first = share(P, blockIdx.x), end = share(P, blockIdx.x + 1);
-    if (first >= end) return;
-    int f = factor_of(P, first), loaded = -1;
-    Held held;
-    auto fetch_tile = [&](int tile, int factor) {
-        const Factor& F = P.f[factor];
-        const int l0 = (tile - F.tile0) * S::TL;
-        if (F.tall) fetch<NB, true, false>(P, F, l0, held);
-        else fetch<NB, false, false>(P, F, l0, held);
-    };
+    float* u = Q + S::r * S::r;                                   // tall: [TL][pitch]; wide: [r][TL]
+    const int first = share_of(P.items, blockIdx.x), end = share_of(P.items, blockIdx.x + 1);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    int f = factor_of<&Factor::item0>(P, first), loaded = -1;
     auto put = [&](auto tall, const Factor& F, int l0) {
         constexpr bool TALL = decltype(tall)::value;
-        using D = Deal<NB, TALL>;
-        constexpr int pitch = TALL ? kPitch : S::TL;
-        const D deal(F, l0);
+        using D = Deal<NB, TALL, A::threads, TL>;
+        constexpr int pitch = TALL ? A::pitch : TL;
+        const D deal(F, l0, thread_here());
         float* to = u + deal.row * pitch + deal.col;
-        if (deal.row >= D::at_once) return;
+        const bool has = deal.row < D::at_once;
+        Raw raw[D::passes];
+        deal.each([&](int i, size_t at, bool in) { raw[i] = load_raw(P, F, at, in); });
         deal.each([&](int i, size_t, bool) {
-            float4 x = F.momentum != nullptr ? held.m[i] : grad_quad(F, held.g[i]);
-            if (F.momentum != nullptr && P.nesterov) x = axpy(P.mu, x, grad_quad(F, held.g[i]));
-            *reinterpret_cast<float4*>(to + i * D::at_once * pitch) = x;
+            if (has) *reinterpret_cast<float4*>(to + i * D::at_once * pitch) = u_of(P, F, raw[i]);
         });
     };
-    // thread's outputs, quads of four neighbours in memory: number i of eight at place + (i / 4) * far + (i % 4) * near
-    auto work = [&](auto tall, const Factor& F, int l0, auto next) {
+    // thread's outputs, quads of four neighbours in memory: number i of eight at place + (i / 4) * far + (i % 4) * near_by
+    auto work = [&](auto tall, const Factor& F, int l0) {
         constexpr bool TALL = decltype(tall)::value;
-        constexpr int groups = S::TL / 8;
         // tall: ranks c .. c + 3, rows lg, lg + TL / 8, ...: a warp's lanes lie side by side along the rank
         // wide: ranks c .. c + 3, and two runs of four of the long side: the lanes lie side by side along it
-        const int cg = TALL ? (int)threadIdx.x % (S::r / 4) : (int)threadIdx.x / groups, lg = TALL ? (int)threadIdx.x / (S::r / 4) : (int)threadIdx.x % groups;
+        const int thread = thread_here(), cg = TALL ? thread % (S::r / 4) : thread / groups, lg = TALL ? thread / (S::r / 4) : thread % groups;
         const bool has = TALL ? lg < groups : cg < S::r / 4;
         const size_t place = TALL ? (size_t)(l0 + lg) * S::r + cg * 4 : (size_t)(cg * 4) * F.L + (l0 + lg * 4);
-        const size_t near_by = TALL ? (size_t)(groups * S::r) : (size_t)F.L, far = TALL ? 4 * near_by : (size_t)(S::TL / 2);
-        auto inside = [&](int i) { return has && (TALL ? l0 + lg + i * groups < F.L : l0 + lg * 4 + (i / 4) * (S::TL / 2) < F.L); };
+        const size_t near_by = TALL ? (size_t)(groups * S::r) : (size_t)F.L, far = TALL ? 4 * near_by : (size_t)(TL / 2);
+        auto inside = [&](int i) { return has && (TALL ? l0 + lg + i * groups < F.L : l0 + lg * 4 + (i / 4) * (TL / 2) < F.L); };
+        float4 acc[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] = zero4();
+        if (TALL) {
+            const float *x_at = u + (has ? lg : 0) * A::pitch, *q_at = Q + cg * 4;
+#pragma unroll 1
+            for (int j = 0; j < S::r; j += 4, x_at += 4, q_at += 4 * S::r) {
+                float4 q[4], x[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) q[k] = *reinterpret_cast<const float4*>(q_at + k * S::r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const float4*>(x_at + i * groups * A::pitch);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[i] = axpy2(k == 0 ? x[i].x : k == 1 ? x[i].y : k == 2 ? x[i].z : x[i].w, q[k], acc[i]);
+                }
+            }
+        } else {
+            const float *x_at = u + lg * 4, *q_at = Q + (has ? cg : 0) * 4;
+#pragma unroll 4
+            for (int j = 0; j < S::r; ++j, x_at += TL, q_at += S::r) {
+                const float4 q = *reinterpret_cast<const float4*>(q_at);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float4 x = *reinterpret_cast<const float4*>(x_at + h * (TL / 2));
+                    acc[4 * h] = axpy2(q.x, x, acc[4 * h]);
+                    acc[4 * h + 1] = axpy2(q.y, x, acc[4 * h + 1]);
+                    acc[4 * h + 2] = axpy2(q.z, x, acc[4 * h + 2]);
+                    acc[4 * h + 3] = axpy2(q.w, x, acc[4 * h + 3]);
+                }
+            }
+        }
         float4 w[8];
         if (F.master != nullptr) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = inside(i) ? *reinterpret_cast<const float4*>(F.master + place + (i / 4) * far + (i % 4) * near_by) : zero4();
         }
-        next();
-        float4 acc[8];
+        if (F.update != nullptr) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] = zero4();
-        if (has) {
-            if (TALL) {
-                const float *x_at = u + lg * kPitch, *q_at = Q + cg * 4;
-#pragma unroll 1
-                for (int j = 0; j < S::r; j += 4, x_at += 4, q_at += 4 * S::r) {
-                    float4 q[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) q[k] = *reinterpret_cast<const float4*>(q_at + k * S::r);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float4 x = *reinterpret_cast<const float4*>(x_at + i * groups * kPitch);
-                        acc[i] = axpy2(x.x, q[0], acc[i]);
-                        acc[i] = axpy2(x.y, q[1], acc[i]);
-                        acc[i] = axpy2(x.z, q[2], acc[i]);
-                        acc[i] = axpy2(x.w, q[3], acc[i]);
-                    }
-                }
-            } else {
-                const float *x_at = u + lg * 4, *q_at = Q + cg * 4;
-#pragma unroll 4
-                for (int j = 0; j < S::r; ++j, x_at += S::TL, q_at += S::r) {
-                    const float4 q = *reinterpret_cast<const float4*>(q_at);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float4 x = *reinterpret_cast<const float4*>(x_at + h * (S::TL / 2));
-                        acc[4 * h] = axpy2(q.x, x, acc[4 * h]);
-                        acc[4 * h + 1] = axpy2(q.y, x, acc[4 * h + 1]);
-                        acc[4 * h + 2] = axpy2(q.z, x, acc[4 * h + 2]);
-                        acc[4 * h + 3] = axpy2(q.w, x, acc[4 * h + 3]);
-                    }
-                }
-            }
+            for (int i = 0; i < 8; ++i)
+                if (inside(i)) *reinterpret_cast<float4*>(F.update + place + (i / 4) * far + (i % 4) * near_by) = acc[i];
         }
+        if (F.master == nullptr) return;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (!inside(i)) continue;
             const size_t at = place + (i / 4) * far + (i % 4) * near_by;
-            if (F.update != nullptr) *reinterpret_cast<float4*>(F.update + at) = acc[i];
-            if (F.master != nullptr) {
-                const float4 n = make_float4(fmaf(-F.rate, acc[i].x, P.decay * w[i].x), fmaf(-F.rate, acc[i].y, P.decay * w[i].y),
-                                             fmaf(-F.rate, acc[i].z, P.decay * w[i].z), fmaf(-F.rate, acc[i].w, P.decay * w[i].w));
-                *reinterpret_cast<float4*>(F.master_out + at) = n;
-                if (F.weight != nullptr) *reinterpret_cast<uint2*>(F.weight + at) = make_uint2(pack_bf16x2(n.x, n.y), pack_bf16x2(n.z, n.w));
-            }
+            const float4 x = acc[i];
+            const float4 n = make_float4(fmaf(-F.rate, x.x, P.decay * w[i].x), fmaf(-F.rate, x.y, P.decay * w[i].y), fmaf(-F.rate, x.z, P.decay * w[i].z),
+                                         fmaf(-F.rate, x.w, P.decay * w[i].w));
+            *reinterpret_cast<float4*>(F.master_out + at) = n;
+            if (F.weight != nullptr) *reinterpret_cast<uint2*>(F.weight + at) = make_uint2(pack_bf16x2(n.x, n.y), pack_bf16x2(n.z, n.w));
         }
     };
-    // (iterate_kernel lets this kernel start when gram_kernel is through: u may be read before the wait for Q)
-    fetch_tile(first, f);
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     for (int tile = first; tile < end; ++tile) {
         const Factor& F = P.f[f];
-        const int l0 = (tile - F.tile0) * S::TL;
-        const bool last_of_factor = l0 + S::TL >= F.L;
+        const int l0 = (tile - F.item0) * TL;
+        // (iterate_kernel lets this kernel start when gram_kernel is through: u may be read before the wait for Q)
         if (F.tall) put(std::true_type(), F, l0);
         else put(std::false_type(), F, l0);
         if (loaded != f) {
             if (loaded < 0) asm volatile("griddepcontrol.wait;" ::: "memory");
-            for (int i = threadIdx.x; i < S::r * S::r / 4; i += kThreads)
+            for (int i = threadIdx.x; i < S::r * S::r / 4; i += A::threads)
                 reinterpret_cast<float4*>(Q)[i] = __ldcg(reinterpret_cast<const float4*>(P.Q + (size_t)f * S::r * S::r) + i);
             loaded = f;
         }
         __syncthreads();
-        auto next = [&]() {
-            if (tile + 1 < end) fetch_tile(tile + 1, last_of_factor ? f + 1 : f);
-        };
-        if (F.tall) work(std::true_type(), F, l0, next);
-        else work(std::false_type(), F, l0, next);
+        if (F.tall) work(std::true_type(), F, l0);
+        else work(std::false_type(), F, l0);
         __syncthreads();                                          // u and Q have been read
-        if (last_of_factor) ++f;
+        if (l0 + TL >= F.L) ++f;
     }
 }
 
@@ -585,10 +647,13 @@ int iterate_ctas(int tri) { return tri <= 10 ? 1 : tri <= 21 ? 2 : tri <= 55 ? 4
 template <int NB>
 lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream) {
     using S = Shape<NB>;
-    P.tiles = 0;
+    using A = ApplyShape<NB>;
+    P.tiles = P.items = 0;
     for (int i = 0; i < P.count; ++i) {
         P.f[i].tile0 = P.tiles;
+        P.f[i].item0 = P.items;
         P.tiles += tiles_of<NB>(P.f[i].L);
+        P.items += (P.f[i].L + A::TL - 1) / A::TL;
     }
     P.sums = static_cast<double*>(workspace);
     P.Q = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + sums_bytes<NB>(P.tiles, P.count));
@@ -601,11 +666,10 @@ lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cfg.gridDim = dim3(walkers, 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.blockDim = dim3(kGramThreads, 1, 1);
     {
         static SmemLimit limit = {};
-        const size_t tiles = 2 * S::floats * 4, joined = NB > 4 ? 0 : (size_t)S::tri * 512 * kWarps;
-        cfg.dynamicSmemBytes = tiles > joined ? tiles : joined;
+        cfg.dynamicSmemBytes = GramMemory<NB>::bytes;
         if (ensure_smem_limit(reinterpret_cast<const void*>(gram_kernel<NB>), cfg.dynamicSmemBytes, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
         if (cudaLaunchKernelEx(&cfg, gram_kernel<NB>, P) != cudaSuccess) return LOWRA_ERR_CUDA;
     }
@@ -614,6 +678,8 @@ lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream
         const int ctas = iterate_ctas(S::tri);
         constexpr bool three = 4 * S::tri * 512 > 220 * 1024;
         cfg.dynamicSmemBytes = (size_t)(three ? 3 : 4) * S::tri * 512 + S::blocks * 8;
+        // one to an SM where there are SMs enough (several clusters on the same ones, as they come in one after the other: 8.8 us a step instead of 4.5)
+        if (P.count * ctas <= kNumSMs && cfg.dynamicSmemBytes < 120 * 1024) cfg.dynamicSmemBytes = 120 * 1024;
         cfg.gridDim = dim3((unsigned)(P.count * ctas), 1, 1);
         cfg.blockDim = dim3(32u * (unsigned)((S::tri + ctas - 1) / ctas), 1, 1);
         attr[1].id = cudaLaunchAttributeClusterDimension;
@@ -625,10 +691,9 @@ lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream
         cfg.numAttrs = 1;
     }
     static SmemLimit limit = {};
-    const size_t tall = (size_t)S::TL * (S::r + 4), wide = (size_t)S::TL * S::r;
-    cfg.dynamicSmemBytes = ((size_t)S::r * S::r + (tall > wide ? tall : wide)) * 4;
-    cfg.gridDim = dim3((unsigned)(P.tiles < kApplyResident * kNumSMs ? P.tiles : kApplyResident * kNumSMs), 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = A::bytes;
+    cfg.gridDim = dim3((unsigned)(P.items < A::resident * kNumSMs ? P.items : A::resident * kNumSMs), 1, 1);
+    cfg.blockDim = dim3(A::threads, 1, 1);
     if (ensure_smem_limit(reinterpret_cast<const void*>(apply_kernel<NB>), cfg.dynamicSmemBytes, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
     return cudaLaunchKernelEx(&cfg, apply_kernel<NB>, P) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
 }
@@ -701,7 +766,7 @@ extern "C" lowra_status lowra_update_factors(const lowra_factor* members_host, i
             return LOWRA_ERR_ALIGN;
         const bool tall = m.rows != r;
         P.f[i] = Factor{m.grad_dev, m.momentum_dev, m.momentum_out_dev, m.master_dev, m.master_out_dev, m.weight_dev, m.update_dev, tall ? m.rows : m.cols,
-                        (float)(step_host->lr * m.scale), 0, (uint8_t)tall, (uint8_t)(m.grad_fp32 != 0)};
+                        (float)(step_host->lr * m.scale), 0, 0, (uint8_t)tall, (uint8_t)(m.grad_fp32 != 0)};
     }
     if (workspace_bytes < lowra_update_workspace_bytes(members_host, count, r) || (reinterpret_cast<uintptr_t>(workspace_dev) & 255u) != 0) return LOWRA_ERR_WORKSPACE;
     if ((st = check_device()) != LOWRA_OK) return st;
