@@ -327,77 +327,109 @@ __global__ void __launch_bounds__(kGramThreads, 1) gram_kernel(const __grid_cons
 }
 
 // ------------------------------------------------------------------------------------------------ the iteration on r x r matrices
-// A cluster takes a factor, a warp one block of the upper triangle of every product, which it writes into the shared memory of all CTAs.  Blocks below the
-// diagonal are read as the transposes of those above it: the products of commuting symmetric matrices are symmetric.
-// A block is 8 x 8 doubles, row by row, the halves of rows 2, 3, 6 and 7 changed over (both ways of reading fragments are then without bank conflicts).
-__device__ __forceinline__ int in_block(int row, int col) { return row * 8 + (col ^ ((row & 2) << 1)); }
+// A cluster takes a factor, a warp one block of 8 x 8 of the upper triangle of every product.  The products of commuting symmetric matrices are symmetric, so
+// a block below the diagonal is the transpose of one above it, and the second operand's block (k, j) is the first operand's block (j, k): both are read along
+// rows.  In the result of m8n8k4 a lane holds two neighbours of a row, and as the contraction may run in any order these two are just what it needs of that
+// block as an operand (contraction indices 2 t and 2 t + 1, one for each of two instructions): blocks are stored as 32 pairs in the lanes' order, written and read
+// without conflicts, 16 bytes at a time.  The whole matrix, both triangles, up to rank 48, where one CTA does a factor; above that, where every block is written
+// into the shared memory of all CTAs of the cluster, the upper triangle, whose transposes are read as two single values.
 __device__ __forceinline__ void st_cluster_f64x2(uint32_t at, double x, double y) {
     asm volatile("st.shared::cluster.v2.f64 [%0], {%1, %2};" ::"r"(at), "d"(x), "d"(y) : "memory");
 }
 __device__ __forceinline__ void st_cluster_f64(uint32_t at, double x) { asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(at), "d"(x) : "memory"); }
 
-template <int NB>
-__global__ void __launch_bounds__(1024) iterate_kernel(const __grid_constant__ UpdateParams P, const int ctas) {
+// `few` factors, whose clusters all find room at once: more CTAs to each (64 factors of rank 64 at 4 / 2 CTAs: 8.9 / 5.1 us a step, 14 of them 4.1 / 4.9).
+template <int NB, bool FEW>
+struct IterateShape {
+    static constexpr int B = 2 * NB, tri = B * (B + 1) / 2;
+    static constexpr bool whole = NB <= 3;                        // (in clusters the transposes' single stores cost more than they save)
+    static constexpr int blocks = whole ? B * B : tri, bytes = blocks * 512;         // of a matrix
+    static constexpr bool three = 4 * bytes > 220 * 1024;        // three matrices: the product that follows G takes G's place (two barriers more a step)
+    // CTAs of a cluster: one warp to a block
+    static constexpr int ctas = tri <= 21 ? 1 : tri <= 55 ? (FEW ? 4 : 2) : tri <= 105 ? (FEW ? 8 : 4) : 8, warps = (tri + ctas - 1) / ctas;
+    static constexpr size_t smem = (size_t)(three ? 3 : 4) * bytes + B * 8;
+};
+
+template <int NB, bool FEW>
+__global__ void __launch_bounds__(32 * IterateShape<NB, FEW>::warps) iterate_kernel(const __grid_constant__ UpdateParams P) {
     using S = Shape<NB>;
-    constexpr int B = S::blocks;
-    constexpr bool kThree = 4 * S::tri * 512 > 220 * 1024;       // the product that follows G takes G's place (one barrier more a step)
+    using I = IterateShape<NB, FEW>;
+    constexpr int B = I::B, ctas = I::ctas;
     extern __shared__ __align__(16) unsigned char update_smem[];
-    double* G = reinterpret_cast<double*>(update_smem);
-    double* Pk = G + S::tri * 64;
-    double* Q = Pk + S::tri * 64;
-    double* M = kThree ? G : Q + S::tri * 64;
-    double* trace = Q + (kThree ? 1 : 2) * S::tri * 64;          // [B], of the diagonal blocks
+    unsigned char* const G = update_smem;
+    unsigned char* const Pk = G + I::bytes;
+    unsigned char* const Q = Pk + I::bytes;
+    unsigned char* const M = I::three ? G : Q + I::bytes;
+    double* trace = reinterpret_cast<double*>(Q + (I::three ? 1 : 2) * I::bytes);      // [B], of the diagonal blocks
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (behind the wait: apply_kernel reads what gram_kernel wrote before its own)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     const int f = (int)blockIdx.x / ctas, rank = (int)blockIdx.x % ctas;
     const Factor& F = P.f[f];
-    const int block = rank * (int)(blockDim.x >> 5) + warp;
-    const bool mine = block < S::tri;
+    const int block = rank * I::warps + warp;
+    const bool mine = block < I::tri;
     int bi = 0;
     while (mine && tri_index(B, bi + 1, bi + 1) <= block) ++bi;
     const int bj = mine ? bi + block - tri_index(B, bi, bi) : 0;
-    const int own = block * 64 + in_block(g, 2 * t4);            // this lane's two values of its block
-    auto store = [&](double* X, const double (&v)[2]) {
-        const uint32_t at = ptx::smem_u32(X + own);
-        for (int i = 0; i < ctas; ++i) st_cluster_f64x2(ptx::map_to_cta(at, (uint32_t)i), v[0], v[1]);
+    auto meet = [&]() {
+        if (ctas > 1) ptx::cluster_sync();
+        else __syncthreads();
     };
-    // Blocks (bi, k) of X times blocks (k, bj) of Y, for one or two X.  Those left of the diagonal in X's row and below it in Y's column are read as transposes:
-    // three ranges of k, in each of which the places of the blocks follow by simple steps.
-    const int straight = in_block(g, t4), across = in_block(t4, g), straight4 = in_block(g, 4 + t4) - straight;      // (across: 32 further)
-    auto products = [&](auto two, const double* X, const double* X2, const double* Y, double (&v)[2], double (&v2)[2]) {
+    // Place of a lane's pair in its block (triangle: changed over so that the transposes are read without conflicts), and of its transposes' two values.
+    const auto place_of = [](int l) { return I::whole ? l * 16 : (l ^ (l >> 3) ^ ((l >> 3 & 1) << 2)) * 16; };
+    const int straight = place_of(lane), across0 = place_of(8 * t4 + (g >> 1)) + 8 * (g & 1), across1 = place_of(8 * t4 + 4 + (g >> 1)) + 8 * (g & 1);
+    const int own = (I::whole ? bi * B + bj : block) * 512 + straight, other = (bj * B + bi) * 512;
+    auto store = [&](unsigned char* X, const double (&v)[2]) {
+        if (ctas == 1) {
+            *reinterpret_cast<double2*>(X + own) = make_double2(v[0], v[1]);
+            if (I::whole && bi != bj) {
+                *reinterpret_cast<double*>(X + other + across0) = v[0];
+                *reinterpret_cast<double*>(X + other + across1) = v[1];
+            }
+            return;
+        }
+        const uint32_t at = ptx::smem_u32(X);
+#pragma unroll
+        for (int i = 0; i < ctas; ++i) {
+            const uint32_t there = ptx::map_to_cta(at, (uint32_t)i);
+            st_cluster_f64x2(there + own, v[0], v[1]);
+            if (I::whole && bi != bj) {
+                st_cluster_f64(there + other + across0, v[0]);
+                st_cluster_f64(there + other + across1, v[1]);
+            }
+        }
+    };
+    // Block (bi, bj) of X Y, and of X2 Y.
+    auto products = [&](auto two, const unsigned char* X, const unsigned char* X2, const unsigned char* Y, double (&v)[2], double (&v2)[2]) {
         constexpr bool TWO = decltype(two)::value;
         double odd[2] = {0.0, 0.0}, odd2[2] = {0.0, 0.0};
         v[0] = v[1] = 0.0;
         if (TWO) v2[0] = v2[1] = 0.0;
-        int xo = bi * 64, yo = bj * 64;                          // block (0, bi), block (0, bj)
-        auto step = [&](int xl, int x4, int yl, int y4) {
-            const double y0 = Y[yo + yl], y1 = Y[yo + yl + y4];
-            dmma(v, X[xo + xl], y0);
-            dmma(odd, X[xo + xl + x4], y1);
+        auto step = [&](double2 x, double2 x2, double2 y) {
+            dmma(v, x.x, y.x);
+            dmma(odd, x.y, y.y);
             if (TWO) {
-                dmma(v2, X2[xo + xl], y0);
-                dmma(odd2, X2[xo + xl + x4], y1);
+                dmma(v2, x2.x, y.x);
+                dmma(odd2, x2.y, y.y);
             }
         };
-        int k = 0;
+        auto along = [&](const unsigned char* Z, int at) { return *reinterpret_cast<const double2*>(Z + at + straight); };
+        if (I::whole) {
+            const int x_at = bi * B * 512, y_at = bj * B * 512;
+#pragma unroll
+            for (int k = 0; k < B; ++k) step(along(X, x_at + k * 512), along(X2, x_at + k * 512), along(Y, y_at + k * 512));
+        } else {
+            // Blocks (i, k) left of the diagonal are read as transposes of (k, i): three ranges of k, in each of which the blocks follow by simple steps.
+            auto across = [&](const unsigned char* Z, int at) {
+                return make_double2(*reinterpret_cast<const double*>(Z + at + across0), *reinterpret_cast<const double*>(Z + at + across1));
+            };
+            int x_at = bi * 512, y_at = bj * 512, k = 0;         // blocks (0, bi), (0, bj)
 #pragma unroll 2
-        for (; k < bi; ++k) {
-            step(across, 32, across, 32);
-            xo += (B - 1 - k) * 64;
-            yo += (B - 1 - k) * 64;
-        }
+            for (; k < bi; ++k, x_at += (B - k) * 512, y_at += (B - k) * 512) step(across(X, x_at), across(X2, x_at), across(Y, y_at));
 #pragma unroll 2
-        for (; k <= bj; ++k) {
-            step(straight, straight4, across, 32);
-            xo += 64;
-            yo += (k < bj ? B - 1 - k : 1) * 64;                 // (the block behind (bj, bj) is (bj, bj + 1))
-        }
+            for (; k < bj; ++k, x_at += 512, y_at += (B - k) * 512) step(along(X, x_at), along(X2, x_at), across(Y, y_at));
 #pragma unroll 2
-        for (; k < B; ++k) {
-            step(straight, straight4, straight, straight4);
-            xo += 64;
-            yo += 64;
+            for (; k < B; ++k, x_at += 512, y_at += 512) step(along(X, x_at), along(X2, x_at), along(Y, y_at));
         }
         v[0] += odd[0];
         v[1] += odd[1];
@@ -407,9 +439,10 @@ __global__ void __launch_bounds__(1024) iterate_kernel(const __grid_constant__ U
         }
     };
     double unused[2];
-    auto product = [&](const double* X, const double* Y, double (&v)[2]) { products(std::false_type(), X, X, Y, v, unused); };
-    ptx::cluster_sync();                                          // (every CTA of the cluster runs: its shared memory may be written)
+    auto product = [&](const unsigned char* X, const unsigned char* Y, double (&v)[2]) { products(std::false_type(), X, X, Y, v, unused); };
+    if (ctas > 1) ptx::cluster_sync();                            // (every CTA of the cluster runs: its shared memory may be written)
     // ---- S, from its parts in the walkers' order
+    double s[2] = {0.0, 0.0};                                     // this lane's values of G
     if (mine) {
         const int walkers = (int)min(kWalkers, P.tiles), tiles = (F.L + S::TL - 1) / S::TL;
         auto walker_of = [&](int tile) {                          // the one whose share holds the tile
@@ -420,22 +453,22 @@ __global__ void __launch_bounds__(1024) iterate_kernel(const __grid_constant__ U
         };
         const int w0 = walker_of(F.tile0), w1 = walker_of(F.tile0 + tiles - 1);
         const double2* from = reinterpret_cast<const double2*>(P.sums) + (size_t)block * 32 + lane;
-        double v[2] = {0.0, 0.0};
 #pragma unroll 8
         for (int w = w0; w <= w1; ++w) {
             const double2 x = __ldcg(from + (size_t)(w + f) * S::tri * 32);
-            v[0] += x.x;
-            v[1] += x.y;
+            s[0] += x.x;
+            s[1] += x.y;
         }
         if (bi == bj) {
-            double d = g == 2 * t4 ? v[0] : g == 2 * t4 + 1 ? v[1] : 0.0;
+            double d = g == 2 * t4 ? s[0] : g == 2 * t4 + 1 ? s[1] : 0.0;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-            if (lane < ctas) st_cluster_f64(ptx::map_to_cta(ptx::smem_u32(trace + bi), (uint32_t)lane), d);
+            if (ctas == 1 && lane == 0) trace[bi] = d;
+            if (ctas > 1 && lane < ctas) st_cluster_f64(ptx::map_to_cta(ptx::smem_u32(trace + bi), (uint32_t)lane), d);
         }
-        store(G, v);
+        store(G, s);
     }
-    ptx::cluster_sync();
+    meet();
     double norm = 0.0;
     for (int i = 0; i < B; ++i) norm += trace[i];
     norm = sqrt(norm) + P.eps;
@@ -446,10 +479,10 @@ __global__ void __launch_bounds__(1024) iterate_kernel(const __grid_constant__ U
         if (mine) {
             product(G, G, v);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) p[i] = (bi == bj && g == 2 * t4 + i ? P.a : 0.0) + P.b * (alpha * G[own + i]) + P.c * (alpha * alpha * v[i]);
+            for (int i = 0; i < 2; ++i) p[i] = (bi == bj && g == 2 * t4 + i ? P.a : 0.0) + P.b * (alpha * s[i]) + P.c * (alpha * alpha * v[i]);
             store(Pk, p);
         }
-        ptx::cluster_sync();
+        meet();
         const bool more = step + 1 < P.steps;
         if (mine) {
             if (step == 0) {
@@ -465,16 +498,16 @@ __global__ void __launch_bounds__(1024) iterate_kernel(const __grid_constant__ U
             v[1] *= alpha;
         }
         if (!more) break;
-        if (kThree) ptx::cluster_sync();                          // everybody has read G
+        if (I::three) meet();                                     // everybody has read G
         if (mine) store(M, v);
-        ptx::cluster_sync();
+        meet();
         if (mine) {
-            product(M, Pk, v);
+            product(M, Pk, s);
             store(Q, q);                                          // (read by all before the barrier)
         }
-        if (kThree) ptx::cluster_sync();                          // everybody has read M
-        if (mine) store(G, v);
-        ptx::cluster_sync();
+        if (I::three) meet();                                     // everybody has read M
+        if (mine) store(G, s);
+        meet();
         alpha = 1.0;
     }
     if (mine) {
@@ -641,9 +674,6 @@ int tiles_of(int L) { return (L + Shape<NB>::TL - 1) / Shape<NB>::TL; }
 template <int NB>
 size_t sums_bytes(int tiles, int count) { return (size_t)((tiles < kWalkers ? tiles : kWalkers) + count) * Shape<NB>::tri * 512; }
 
-// CTAs of a factor's cluster in iterate_kernel
-int iterate_ctas(int tri) { return tri <= 10 ? 1 : tri <= 21 ? 2 : tri <= 55 ? 4 : 8; }
-
 template <int NB>
 lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream) {
     using S = Shape<NB>;
@@ -673,23 +703,24 @@ lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream
         if (ensure_smem_limit(reinterpret_cast<const void*>(gram_kernel<NB>), cfg.dynamicSmemBytes, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
         if (cudaLaunchKernelEx(&cfg, gram_kernel<NB>, P) != cudaSuccess) return LOWRA_ERR_CUDA;
     }
-    {
+    auto iterate = [&](auto few) -> bool {
+        constexpr bool FEW = decltype(few)::value;
+        using I = IterateShape<NB, FEW>;
         static SmemLimit limit = {};
-        const int ctas = iterate_ctas(S::tri);
-        constexpr bool three = 4 * S::tri * 512 > 220 * 1024;
-        cfg.dynamicSmemBytes = (size_t)(three ? 3 : 4) * S::tri * 512 + S::blocks * 8;
+        cfg.dynamicSmemBytes = I::smem;
         // one to an SM where there are SMs enough (several clusters on the same ones, as they come in one after the other: 8.8 us a step instead of 4.5)
-        if (P.count * ctas <= kNumSMs && cfg.dynamicSmemBytes < 120 * 1024) cfg.dynamicSmemBytes = 120 * 1024;
-        cfg.gridDim = dim3((unsigned)(P.count * ctas), 1, 1);
-        cfg.blockDim = dim3(32u * (unsigned)((S::tri + ctas - 1) / ctas), 1, 1);
+        if (P.count * I::ctas <= kNumSMs && cfg.dynamicSmemBytes < 120 * 1024) cfg.dynamicSmemBytes = 120 * 1024;
+        cfg.gridDim = dim3((unsigned)(P.count * I::ctas), 1, 1);
+        cfg.blockDim = dim3(32u * I::warps, 1, 1);
         attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = (unsigned)ctas;
+        attr[1].val.clusterDim.x = (unsigned)I::ctas;
         attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-        cfg.numAttrs = 2;
-        if (ensure_smem_limit(reinterpret_cast<const void*>(iterate_kernel<NB>), cfg.dynamicSmemBytes, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
-        if (cudaLaunchKernelEx(&cfg, iterate_kernel<NB>, P, ctas) != cudaSuccess) return LOWRA_ERR_CUDA;
-        cfg.numAttrs = 1;
-    }
+        cfg.numAttrs = I::ctas > 1 ? 2 : 1;
+        if (ensure_smem_limit(reinterpret_cast<const void*>(iterate_kernel<NB, FEW>), cfg.dynamicSmemBytes, &limit) != LOWRA_OK) return false;
+        return cudaLaunchKernelEx(&cfg, iterate_kernel<NB, FEW>, P) == cudaSuccess;
+    };
+    if (!(P.count * IterateShape<NB, true>::ctas <= kNumSMs ? iterate(std::true_type()) : iterate(std::false_type()))) return LOWRA_ERR_CUDA;
+    cfg.numAttrs = 1;
     static SmemLimit limit = {};
     cfg.dynamicSmemBytes = A::bytes;
     cfg.gridDim = dim3((unsigned)(P.items < A::resident * kNumSMs ? P.items : A::resident * kNumSMs), 1, 1);
