@@ -110,36 +110,80 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
     return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
 
-// Eight neighbouring channels from n on of one token, whose element there is number `at` of the [M, N] arrays (a multiple of 8, as n is): the sums z -> packed
-// outputs; the copy of Z is written.
-__device__ __forceinline__ uint4 finish8(const Epilogue& E, int n, size_t at, float (&z)[8]) {
-    if (E.bias != nullptr) {
-        float b[8];
-        if (E.bias_bf16) {
-            unpack8(__ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(E.bias) + n)), b);
-        } else {
-            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(E.bias) + n);
-            const float4 lo = __ldg(p), hi = __ldg(p + 1);
-            b[0] = lo.x; b[1] = lo.y; b[2] = lo.z; b[3] = lo.w; b[4] = hi.x; b[5] = hi.y; b[6] = hi.z; b[7] = hi.w;
-        }
+// gelu of two values for an output that is rounded to bf16 next: max(z, 0) - |z| Phi(-|z|), Phi(-|z|) = exp(-z^2 / 2) R(|z|), R a polynomial on 0 .. 6.5 whose largest relative
+// error is least (4e-4, a fifth of half a rounding step of bf16; beyond 6.5, where |gelu| is below 3e-10, R stands still).  Ten instructions a value and one 2^x: with normal_cdf's division, and a
+// value at a time, the epilogue of a half tile was longer than the stages that hide it.
+__device__ __forceinline__ float2 gelu_rounded(float2 z) {
+    const float2 u = make_float2(fminf(fabsf(z.x), 6.5f), fminf(fabsf(z.y), 6.5f));
+    auto both = [](float c) { return make_float2(c, c); };
+    float2 p = fma2(both(-3.78604283e-07f), u, both(1.33567946e-05f));
+    p = fma2(p, u, both(-0.000205609975f));
+    p = fma2(p, u, both(0.00182332586f));
+    p = fma2(p, u, both(-0.0103983064f));
+    p = fma2(p, u, both(0.0405910417f));
+    p = fma2(p, u, both(-0.113886519f));
+    p = fma2(p, u, both(0.240768845f));
+    p = fma2(p, u, both(-0.397065467f));
+    p = fma2(p, u, both(0.499930565f));
+    const float2 e = mul2(mul2(z, z), both(-0.5f * kLog2E)), q = mul2(p, make_float2(exp2_fast(e.x), exp2_fast(e.y)));
+    return make_float2(fmaf(-fabsf(z.x), q.x, fmaxf(z.x, 0.0f)), fmaf(-fabsf(z.y), q.y, fmaxf(z.y, 0.0f)));      // (a NaN passes through the product)
+}
+
+// Sixteen neighbouring channels of one token, or the first eight of them (`groups` of eight), whose element there is number `at` of the [M, N] arrays (a
+// multiple of 8).  What is read of those arrays is asked for ahead of time.
+struct Behind {
+    uint4 m[2], d[2];
+};
+__device__ __forceinline__ void load_behind(const Epilogue& E, size_t at, int groups, Behind& x) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] += b[i];
+    for (int g = 0; g < 2; ++g) {
+        if (E.multiply != nullptr && g < groups) x.m[g] = *reinterpret_cast<const uint4*>(E.multiply + at + 8 * g);
+        if (E.residual != nullptr && g < groups) x.d[g] = *reinterpret_cast<const uint4*>(E.residual + at + 8 * g);
     }
-    if (E.pre != nullptr) *reinterpret_cast<uint4*>(E.pre + at) = pack8(z);
-    activate(z, E.activation);
-    if (E.multiply != nullptr) {
-        float m[8];
-        unpack8(*reinterpret_cast<const uint4*>(E.multiply + at), m);
+}
+__device__ __forceinline__ void pack16(const float (&v)[16], uint32_t (&o)[8]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] *= m[i];
+    for (int i = 0; i < 8; ++i) o[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+}
+// The sums z become outputs; before() is called with Z itself.
+template <typename Before>
+__device__ __forceinline__ void finish16(const Epilogue& E, const float* bias /* shared memory, 16 */, const Behind& x, float (&z)[16], Before before) {
+    if (E.bias != nullptr) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 b = reinterpret_cast<const float4*>(bias)[i];
+            z[4 * i] += b.x; z[4 * i + 1] += b.y; z[4 * i + 2] += b.z; z[4 * i + 3] += b.w;
+        }
+    }
+    if (E.pre != nullptr) before();
+    if (E.activation == LOWRA_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 h = gelu_rounded(make_float2(z[2 * i], z[2 * i + 1]));
+            z[2 * i] = h.x;
+            z[2 * i + 1] = h.y;
+        }
+    } else {
+        activate(z, E.activation);
+    }
+    if (E.multiply != nullptr) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            float m[8];
+            unpack8(x.m[g], m);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[8 * g + i] *= m[i];
+        }
     }
     if (E.residual != nullptr) {
-        float d[8];
-        unpack8(*reinterpret_cast<const uint4*>(E.residual + at), d);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] += d[i];
+        for (int g = 0; g < 2; ++g) {
+            float d[8];
+            unpack8(x.d[g], d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[8 * g + i] += d[i];
+        }
     }
-    return pack8(z);
 }
 
 // One channel of one token.

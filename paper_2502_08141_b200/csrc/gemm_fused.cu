@@ -514,6 +514,7 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
             }
         };
         uint32_t hc = 0;
+        [[maybe_unused]] float* const biases = reinterpret_cast<float*>(smem_raw + kGemmSmemBytes);
         for (int i = 0; i < n_segs && !failed; ++i) {
             const Seg t = seg_at(i);
             const int r0 = t.rt * kPairR, M = P.mem[t.prob].M;
@@ -542,31 +543,42 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                         if (j < left) dst[j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
                 }
             };
-            // 16 rows of one token from the tile's row c0 on, with what stands behind the product.  (16, not 32: the sums, a row of the residual and the
-            // activation's intermediate values have 72 registers between them.)
-            auto put16 = [&](int tok, int c0, uint32_t (&v)[16]) {
+            // 16 rows of one token from the tile's row c0 on, with what stands behind the product: x as asked for by ask(), the sums in z.  (16, not 32: the sums, two
+            // rows of the residual and the activation's intermediate values have 72 registers between them.)
+            auto groups_of = [&](int c0) { return min((cols - c0) >> 3, 2); };       // (the channels are a multiple of 8)
+            auto ask = [&](int tok, int c0, Behind& x) {
                 if constexpr (MODE == kModeEpilogue) {
-                    const size_t at = (size_t)tok * P.ld_out + r0 + c0;
-                    uint32_t o[8];
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        if (8 * g >= cols - c0) break;
-                        float z[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(v[8 * g + j]);
-                        const uint4 y = finish8(EP.m[t.prob], r0 + c0 + 8 * g, at + 8 * g, z);
-                        o[4 * g] = y.x; o[4 * g + 1] = y.y; o[4 * g + 2] = y.z; o[4 * g + 3] = y.w;
-                    }
-                    uint16_t* dst = P.mem[t.prob].out + at;
-                    if (P.out_align == 32 && cols - c0 >= 16) {
-                        ptx::st_global_v8(dst, o);
-                    } else {
-#pragma unroll
-                        for (int g = 0; g < 2; ++g)
-                            if (8 * g < cols - c0) *reinterpret_cast<uint4*>(dst + 8 * g) = make_uint4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
-                    }
+                    if (tok < M && c0 < cols) load_behind(EP.m[t.prob], (size_t)tok * P.ld_out + r0 + c0, groups_of(c0), x);
                 }
             };
+            auto put16 = [&](int tok, int c0, const Behind& x, float (&z)[16]) {
+                if constexpr (MODE == kModeEpilogue) {
+                    const size_t at = (size_t)tok * P.ld_out + r0 + c0;
+                    const int groups = groups_of(c0);
+                    auto write = [&](uint16_t* to) {
+                        uint32_t o[8];
+                        pack16(z, o);
+                        if (P.out_align == 32 && groups == 2) {
+                            ptx::st_global_v8(to, o);
+                        } else {
+                            *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[2], o[3]);
+                            if (groups == 2) *reinterpret_cast<uint4*>(to + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+                        }
+                    };
+                    finish16(EP.m[t.prob], biases + (i & 1) * kPairR + c0, x, z, [&]() { write(EP.m[t.prob].pre + at); });
+                    write(P.mem[t.prob].out + at);
+                }
+            };
+            if constexpr (MODE == kModeEpilogue) {
+                // this piece's biases; two places in turn: the writers of the next but one meet at a barrier that all readers of this one reach first
+                if (!t.is_t && !t.part && EP.m[t.prob].bias != nullptr) {
+                    const Epilogue& E = EP.m[t.prob];
+                    const int n = r0 + et;
+                    float v = 0.0f;
+                    if (et < cols) v = E.bias_bf16 ? bf16_value(__ldg(static_cast<const uint16_t*>(E.bias) + n)) : __ldg(static_cast<const float*>(E.bias) + n);
+                    biases[(i & 1) * kPairR + et] = v;
+                }
+            }
             // publish this CTA's tokens of T, resp. its half of the cluster's partial tile: the writers meet, and one thread's
             // release covers what all of them have written
             auto raise = [&](uint32_t* flag, bool withheld) {
@@ -658,15 +670,20 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                             if (MODE == kModeEpilogue && !t.is_t) {
 #pragma unroll 1
                                 for (int e = 0; e < 32; e += 16) {
+                                    Behind x;
+                                    ask(tok, c0 + e, x);
                                     uint32_t v[16];
                                     ptx::tmem_ld_32x16(tmem_lane + ((hc + (uint32_t)h) & 1u) * (uint32_t)kPairR + (uint32_t)(c0 + e), v);
                                     ptx::tmem_ld_wait();
+                                    float z[16];
+#pragma unroll
+                                    for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(v[j]);
                                     const float* from = ring + e * 128;
                                     for (int c = 1; c < S; ++c, from += kSmemSlot / 4) {
 #pragma unroll
-                                        for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + from[j * 128]);
+                                        for (int j = 0; j < 16; ++j) z[j] += from[j * 128];
                                     }
-                                    if (tok < M && c0 + e < cols) put16(tok, c0 + e, v);
+                                    if (tok < M && c0 + e < cols) put16(tok, c0 + e, x, z);
                                 }
                             } else {
                                 uint32_t v[32];
@@ -736,14 +753,19 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                     if constexpr (MODE == kModeEpilogue) {
 #pragma unroll 1
                         for (int e = 0; e < 32; e += 16) {
+                            Behind x;
+                            ask(tok, c0 + e, x);
                             uint32_t v[16];
                             ptx::tmem_ld_32x16(from + (uint32_t)e, v);
                             ptx::tmem_ld_wait();
+                            float z[16];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(v[j]);
                             for (int c = 0; c < nc; ++c) {
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[(size_t)(2 * c) * (kSmemSlot / 4) + (e + j) * 128]);
+                                for (int j = 0; j < 16; ++j) z[j] += ring[(size_t)(2 * c) * (kSmemSlot / 4) + (e + j) * 128];
                             }
-                            if (tok < M && c0 + e < cols) put16(tok, c0 + e, v);
+                            if (tok < M && c0 + e < cols) put16(tok, c0 + e, x, z);
                         }
                     } else {
                         uint32_t v[32];
@@ -768,6 +790,8 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                 const uint32_t taddr = tmem_lane + acc * (uint32_t)kPairR;
                 const int tok = t.m0 + h * kHalfT + (int)crank * 128 + my_tok;
                 const bool any = tok - lane < M;        // somebody in this warp has a token
+                [[maybe_unused]] Behind ahead;          // what the next 16 columns are multiplied by and added to: asked for before the sums are there
+                if (MODE == kModeEpilogue && !t.is_t && !t.part && c_first < c_last) ask(tok, c_first, ahead);
                 if (!ptx::mbar_wait_warp(&bars->tmem_full[acc], (hc >> 1) & 1u, abort_flag, wait_ns)) bars->abort = 1u;
                 if (agree_abort()) { failed = true; break; }
                 ptx::tc_fence_after();
@@ -777,8 +801,13 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                         for (int c0 = c_first; c0 < c_last && any; c0 += 16) {
                             uint32_t v[16];
                             ptx::tmem_ld_32x16(taddr + (uint32_t)c0, v);
+                            const Behind x = ahead;
+                            if (c0 + 16 < c_last) ask(tok, c0 + 16, ahead);
                             ptx::tmem_ld_wait();
-                            if (tok < M) put16(tok, c0, v);
+                            float z[16];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(v[j]);
+                            if (tok < M) put16(tok, c0, x, z);
                         }
                         release(acc);
                         continue;
@@ -1127,7 +1156,7 @@ static lowra_status prepare_fused(cudaLaunchConfig_t& cfg, int* max_clusters) {
         const int sms = device_sm_count();
         if (sms < CL) return LOWRA_ERR_CUDA;
         if (cudaFuncSetAttribute(fused_kernel<MODE, NB, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 (int)kGemmSmemBytes) != cudaSuccess)
+                                 (int)gemm_smem_bytes(MODE)) != cudaSuccess)
             return LOWRA_ERR_CUDA;
         // the persistent schedule needs every cluster of the grid resident (a tile waits for T of another)
         cfg.gridDim = dim3(sms / CL * CL, 1, 1);
@@ -1154,7 +1183,7 @@ static lowra_status launch_mode(const GemmParams& G, const BatchMaps& TM, const 
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.blockDim = dim3(kGemmThreads, 1, 1);
-    cfg.dynamicSmemBytes = kGemmSmemBytes;
+    cfg.dynamicSmemBytes = gemm_smem_bytes(MODE);
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = (MODE == kModeDense) ? 1 : 2;

@@ -335,6 +335,8 @@ lowra_status run_members(bool backward, const MemberArgs* mem, int count, int32_
     G.C = backward ? N : K;
     G.ld_out = G.R;
     G.out_align = out_alignment(mem, count, G.R);
+    for (int i = 0; epilogue && i < count; ++i)
+        if ((reinterpret_cast<uintptr_t>(mem[i].epilogue.pre) & 31u) != 0) G.out_align = 16;
     G.main_blocks = (G.C + kTileC - 1) / kTileC;
     G.lora_blocks = w.rp / kTileC;
     G.tiles_r = (G.R + kPairR - 1) / kPairR;

@@ -142,7 +142,9 @@ constexpr uint32_t kSmemBarriers = 1024;
 // no alignment slack: the dynamic shared memory of a kernel without static shared memory starts 1024-byte
 // aligned (checked by the kernel, which the swizzled operand tiles need)
 constexpr uint32_t kGemmSmemBytes = kSmemRing + kSmemBarriers;
-static_assert(kGemmSmemBytes <= 232448, "227 KB of shared memory per CTA");
+constexpr uint32_t kSmemBias = 2 * kPairR * 4;     // mode kModeEpilogue: the biases of two tiles' channels, fp32
+constexpr uint32_t gemm_smem_bytes(int mode) { return kGemmSmemBytes + (mode == kModeEpilogue ? kSmemBias : 0); }
+static_assert(gemm_smem_bytes(kModeEpilogue) <= 232448, "227 KB of shared memory per CTA");
 
 // What stands behind the members' products: parameters of their own, so that the other modes' launches do not carry them.
 template <int MODE, int NB>
