@@ -129,25 +129,25 @@ __device__ __forceinline__ float2 gelu_rounded(float2 z) {
     return make_float2(fmaf(-fabsf(z.x), q.x, fmaxf(z.x, 0.0f)), fmaf(-fabsf(z.y), q.y, fmaxf(z.y, 0.0f)));      // (a NaN passes through the product)
 }
 
-// Sixteen neighbouring channels of one token, or the first eight of them (`groups` of eight), whose element there is number `at` of the [M, N] arrays (a
-// multiple of 8).  What is read of those arrays is asked for ahead of time.
+// Thirty-two neighbouring channels of one token, `groups` (1 .. 4) of eight of them, whose element there is number `at` of the [M, N] arrays (a multiple of 8).
+// What is read first of those arrays is asked for ahead of time.
 struct Behind {
-    uint4 m[2], d[2];
+    uint4 v[4];                   // of multiply, or of the residual where there is none
 };
 __device__ __forceinline__ void load_behind(const Epilogue& E, size_t at, int groups, Behind& x) {
+    const uint16_t* from = E.multiply != nullptr ? E.multiply : E.residual;
+    if (from == nullptr) return;
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-        if (E.multiply != nullptr && g < groups) x.m[g] = *reinterpret_cast<const uint4*>(E.multiply + at + 8 * g);
-        if (E.residual != nullptr && g < groups) x.d[g] = *reinterpret_cast<const uint4*>(E.residual + at + 8 * g);
-    }
+    for (int g = 0; g < 4; ++g)
+        if (g < groups) x.v[g] = *reinterpret_cast<const uint4*>(from + at + 8 * g);
 }
 __device__ __forceinline__ void pack16(const float (&v)[16], uint32_t (&o)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
 }
-// The sums z become outputs; before() is called with Z itself.
-template <typename Before>
-__device__ __forceinline__ void finish16(const Epilogue& E, const float* bias /* shared memory, 16 */, const Behind& x, float (&z)[16], Before before) {
+// Sixteen of them, numbers 16 H ..: the sums z become outputs; before() is called with Z itself.
+template <int H, typename Before>
+__device__ __forceinline__ void finish16(const Epilogue& E, const float* bias /* shared memory, 16 */, const Behind& x, size_t at, int groups, float (&z)[16], Before before) {
     if (E.bias != nullptr) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -170,7 +170,7 @@ __device__ __forceinline__ void finish16(const Epilogue& E, const float* bias /*
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             float m[8];
-            unpack8(x.m[g], m);
+            unpack8(x.v[2 * H + g], m);
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[8 * g + i] *= m[i];
         }
@@ -178,8 +178,10 @@ __device__ __forceinline__ void finish16(const Epilogue& E, const float* bias /*
     if (E.residual != nullptr) {
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
+            uint4 p = x.v[2 * H + g];
+            if (E.multiply != nullptr && 2 * H + g < groups) p = *reinterpret_cast<const uint4*>(E.residual + at + 16 * H + 8 * g);
             float d[8];
-            unpack8(x.d[g], d);
+            unpack8(p, d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[8 * g + i] += d[i];
         }

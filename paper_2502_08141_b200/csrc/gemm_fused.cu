@@ -543,30 +543,40 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                         if (j < left) dst[j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
                 }
             };
-            // 16 rows of one token from the tile's row c0 on, with what stands behind the product: x as asked for by ask(), the sums in z.  (16, not 32: the sums, two
-            // rows of the residual and the activation's intermediate values have 72 registers between them.)
-            auto groups_of = [&](int c0) { return min((cols - c0) >> 3, 2); };       // (the channels are a multiple of 8)
+            // 32 rows of one token from the tile's row c0 on, with what stands behind the product: x as asked for by ask(), the sums in v.  (The sums are read 32 columns at
+            // a time, as elsewhere: a trip to the tensor memory takes 0.7 us while the tensor core works, and two of 16 columns each cost the call a tenth.)
+            auto groups_of = [&](int c0) { return min((cols - c0) >> 3, 4); };       // (the channels are a multiple of 8)
             auto ask = [&](int tok, int c0, Behind& x) {
                 if constexpr (MODE == kModeEpilogue) {
                     if (tok < M && c0 < cols) load_behind(EP.m[t.prob], (size_t)tok * P.ld_out + r0 + c0, groups_of(c0), x);
                 }
             };
-            auto put16 = [&](int tok, int c0, const Behind& x, float (&z)[16]) {
+            auto put_behind = [&](int tok, int c0, const Behind& x, uint32_t (&v)[32]) {
                 if constexpr (MODE == kModeEpilogue) {
+                    const Epilogue& E = EP.m[t.prob];
                     const size_t at = (size_t)tok * P.ld_out + r0 + c0;
                     const int groups = groups_of(c0);
-                    auto write = [&](uint16_t* to) {
-                        uint32_t o[8];
-                        pack16(z, o);
-                        if (P.out_align == 32 && groups == 2) {
-                            ptx::st_global_v8(to, o);
-                        } else {
-                            *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[2], o[3]);
-                            if (groups == 2) *reinterpret_cast<uint4*>(to + 8) = make_uint4(o[4], o[5], o[6], o[7]);
-                        }
+                    auto half = [&](auto which) {
+                        constexpr int H = decltype(which)::value;
+                        if (2 * H >= groups) return;
+                        float z[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(v[16 * H + j]);
+                        auto write = [&](uint16_t* to) {
+                            uint32_t o[8];
+                            pack16(z, o);
+                            if (P.out_align == 32 && groups >= 2 * H + 2) {
+                                ptx::st_global_v8(to, o);
+                            } else {
+                                *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[2], o[3]);
+                                if (groups >= 2 * H + 2) *reinterpret_cast<uint4*>(to + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+                            }
+                        };
+                        finish16<H>(E, biases + (i & 1) * kPairR + c0 + 16 * H, x, at, groups, z, [&]() { write(E.pre + at + 16 * H); });
+                        write(P.mem[t.prob].out + at + 16 * H);
                     };
-                    finish16(EP.m[t.prob], biases + (i & 1) * kPairR + c0, x, z, [&]() { write(EP.m[t.prob].pre + at); });
-                    write(P.mem[t.prob].out + at);
+                    half(std::integral_constant<int, 0>());
+                    half(std::integral_constant<int, 1>());
                 }
             };
             if constexpr (MODE == kModeEpilogue) {
@@ -667,40 +677,23 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                             const int u = k + (2 * st + ch) * S, h = u / per_half, c0 = (u - h * per_half) * width;
                             const int tok = t.m0 + h * kHalfT + (int)crank * 128 + my_tok;
                             const float* ring = reinterpret_cast<const float*>(x_ring) + (size_t)(((st % ahead) * 2 + ch) * (S - 1)) * (kSmemSlot / 4) + my_tok;
-                            if (MODE == kModeEpilogue && !t.is_t) {
-#pragma unroll 1
-                                for (int e = 0; e < 32; e += 16) {
-                                    Behind x;
-                                    ask(tok, c0 + e, x);
-                                    uint32_t v[16];
-                                    ptx::tmem_ld_32x16(tmem_lane + ((hc + (uint32_t)h) & 1u) * (uint32_t)kPairR + (uint32_t)(c0 + e), v);
-                                    ptx::tmem_ld_wait();
-                                    float z[16];
+                            [[maybe_unused]] Behind x;
+                            if (MODE == kModeEpilogue && !t.is_t) ask(tok, c0, x);
+                            uint32_t v[32];
+                            ptx::tmem_ld_32x32(tmem_lane + ((hc + (uint32_t)h) & 1u) * (uint32_t)kPairR + (uint32_t)c0, v);
+                            ptx::tmem_ld_wait();
+                            for (int c = 1; c < S; ++c, ring += kSmemSlot / 4) {
 #pragma unroll
-                                    for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(v[j]);
-                                    const float* from = ring + e * 128;
-                                    for (int c = 1; c < S; ++c, from += kSmemSlot / 4) {
+                                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[j * 128]);
+                                if (width == 32) {
 #pragma unroll
-                                        for (int j = 0; j < 16; ++j) z[j] += from[j * 128];
-                                    }
-                                    if (tok < M && c0 + e < cols) put16(tok, c0 + e, x, z);
+                                    for (int j = 16; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[j * 128]);
                                 }
-                            } else {
-                                uint32_t v[32];
-                                ptx::tmem_ld_32x32(tmem_lane + ((hc + (uint32_t)h) & 1u) * (uint32_t)kPairR + (uint32_t)c0, v);
-                                ptx::tmem_ld_wait();
-                                for (int c = 1; c < S; ++c, ring += kSmemSlot / 4) {
-#pragma unroll
-                                    for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[j * 128]);
-                                    if (width == 32) {
-#pragma unroll
-                                        for (int j = 16; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[j * 128]);
-                                    }
-                                }
-                                if (tok < M) {
-                                    if (t.is_t) put_t(tok, c0, 16, v);
-                                    else put(P.mem[t.prob].out + (size_t)tok * P.ld_out + r0 + c0, cols - c0, v);
-                                }
+                            }
+                            if (tok < M) {
+                                if (t.is_t) put_t(tok, c0, 16, v);
+                                else if (MODE == kModeEpilogue) put_behind(tok, c0, x, v);
+                                else put(P.mem[t.prob].out + (size_t)tok * P.ld_out + r0 + c0, cols - c0, v);
                             }
                         }
                         if (st + ahead < steps) {
@@ -749,33 +742,18 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                     const int tok = t.m0 + h * kHalfT + (int)crank * 128 + my_tok;
                     if (!ptx::mbar_wait_warp(&bars->part_full[s % kPartSteps], (uint32_t)(s / kPartSteps) & 1u, abort_flag, wait_ns)) bars->abort = 1u;
                     const float* ring = reinterpret_cast<const float*>(x_ring) + (size_t)((s % ahead) * pieces + ch) * (kSmemSlot / 4) + my_tok;
-                    const uint32_t from = tmem_lane + ((hc + (uint32_t)h) & 1u) * (uint32_t)kPairR + (uint32_t)c0;
-                    if constexpr (MODE == kModeEpilogue) {
-#pragma unroll 1
-                        for (int e = 0; e < 32; e += 16) {
-                            Behind x;
-                            ask(tok, c0 + e, x);
-                            uint32_t v[16];
-                            ptx::tmem_ld_32x16(from + (uint32_t)e, v);
-                            ptx::tmem_ld_wait();
-                            float z[16];
+                    [[maybe_unused]] Behind x;
+                    if (MODE == kModeEpilogue) ask(tok, c0, x);
+                    uint32_t v[32];
+                    ptx::tmem_ld_32x32(tmem_lane + ((hc + (uint32_t)h) & 1u) * (uint32_t)kPairR + (uint32_t)c0, v);
+                    ptx::tmem_ld_wait();
+                    for (int c = 0; c < nc; ++c) {
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(v[j]);
-                            for (int c = 0; c < nc; ++c) {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) z[j] += ring[(size_t)(2 * c) * (kSmemSlot / 4) + (e + j) * 128];
-                            }
-                            if (tok < M && c0 + e < cols) put16(tok, c0 + e, x, z);
-                        }
-                    } else {
-                        uint32_t v[32];
-                        ptx::tmem_ld_32x32(from, v);
-                        ptx::tmem_ld_wait();
-                        for (int c = 0; c < nc; ++c) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[(size_t)(2 * c) * (kSmemSlot / 4) + j * 128]);
-                        }
-                        if (tok < M && c0 < cols) put(P.mem[t.prob].out + (size_t)tok * P.ld_out + r0 + c0, cols - c0, v);
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ring[(size_t)(2 * c) * (kSmemSlot / 4) + j * 128]);
+                    }
+                    if (tok < M && c0 < cols) {
+                        if (MODE == kModeEpilogue) put_behind(tok, c0, x, v);
+                        else put(P.mem[t.prob].out + (size_t)tok * P.ld_out + r0 + c0, cols - c0, v);
                     }
                     if (s + ahead < steps) {
                         if (agree_abort()) { failed = true; break; }     // everybody has read the step's pieces: their place is filled again
@@ -790,33 +768,15 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                 const uint32_t taddr = tmem_lane + acc * (uint32_t)kPairR;
                 const int tok = t.m0 + h * kHalfT + (int)crank * 128 + my_tok;
                 const bool any = tok - lane < M;        // somebody in this warp has a token
-                [[maybe_unused]] Behind ahead;          // what the next 16 columns are multiplied by and added to: asked for before the sums are there
-                if (MODE == kModeEpilogue && !t.is_t && !t.part && c_first < c_last) ask(tok, c_first, ahead);
                 if (!ptx::mbar_wait_warp(&bars->tmem_full[acc], (hc >> 1) & 1u, abort_flag, wait_ns)) bars->abort = 1u;
                 if (agree_abort()) { failed = true; break; }
                 ptx::tc_fence_after();
-                if constexpr (MODE == kModeEpilogue) {
-                    if (!t.is_t && !t.part) {
-#pragma unroll 1
-                        for (int c0 = c_first; c0 < c_last && any; c0 += 16) {
-                            uint32_t v[16];
-                            ptx::tmem_ld_32x16(taddr + (uint32_t)c0, v);
-                            const Behind x = ahead;
-                            if (c0 + 16 < c_last) ask(tok, c0 + 16, ahead);
-                            ptx::tmem_ld_wait();
-                            float z[16];
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(v[j]);
-                            if (tok < M) put16(tok, c0, x, z);
-                        }
-                        release(acc);
-                        continue;
-                    }
-                }
 #pragma unroll 1
                 for (int c0 = c_first; c0 < c_last && any; c0 += c_step) {
+                    [[maybe_unused]] Behind x;
                     uint32_t v[32];
                     ptx::tmem_ld_32x32(taddr + (uint32_t)c0, v);
+                    if (MODE == kModeEpilogue && !t.is_t && !t.part) ask(tok, c0, x);
                     ptx::tmem_ld_wait();
                     if (t.part) {
                         // fp32 sums of a slice: [row][token], so that a warp writes 128 consecutive bytes
@@ -824,6 +784,7 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                         for (int j = 0; j < 32; ++j) __stcg(part + (size_t)h * kSkAllFloats + (size_t)(c0 + j) * 128, __uint_as_float(v[j]));
                     } else if (tok < M) {
                         if (t.is_t) put_t(tok, c0, 32, v);
+                        else if (MODE == kModeEpilogue) put_behind(tok, c0, x, v);
                         else put(P.mem[t.prob].out + (size_t)tok * P.ld_out + r0 + c0, cols - c0, v);
                     }
                 }
