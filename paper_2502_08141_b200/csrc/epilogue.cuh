@@ -188,14 +188,27 @@ __device__ __forceinline__ void finish16(const Epilogue& E, const float* bias /*
     }
 }
 
-// One channel of one token.
-__device__ __forceinline__ uint16_t finish1(const Epilogue& E, int n, size_t at, float sum) {
+// One channel of one token: what is read for it, and the output.
+struct Behind1 {
+    float bias, multiply, residual;
+};
+__device__ __forceinline__ float load_bias(const Epilogue& E, int n) {
+    if (E.bias == nullptr) return 0.0f;
+    return E.bias_bf16 ? bf16_value(__ldg(static_cast<const uint16_t*>(E.bias) + n)) : __ldg(static_cast<const float*>(E.bias) + n);
+}
+__device__ __forceinline__ Behind1 load_behind1(const Epilogue& E, int n, size_t at) {
+    Behind1 x = {load_bias(E, n), 1.0f, 0.0f};
+    if (E.multiply != nullptr) x.multiply = bf16_value(E.multiply[at]);
+    if (E.residual != nullptr) x.residual = bf16_value(E.residual[at]);
+    return x;
+}
+__device__ __forceinline__ uint16_t finish1(const Epilogue& E, const Behind1& x, size_t at, float sum) {
     float z[1] = {sum};
-    if (E.bias != nullptr) z[0] += E.bias_bf16 ? bf16_value(__ldg(static_cast<const uint16_t*>(E.bias) + n)) : __ldg(static_cast<const float*>(E.bias) + n);
+    if (E.bias != nullptr) z[0] += x.bias;
     if (E.pre != nullptr) E.pre[at] = bf16_bits(z[0]);
     activate(z, E.activation);
-    if (E.multiply != nullptr) z[0] *= bf16_value(E.multiply[at]);
-    if (E.residual != nullptr) z[0] += bf16_value(E.residual[at]);
+    if (E.multiply != nullptr) z[0] *= x.multiply;
+    if (E.residual != nullptr) z[0] += x.residual;
     return bf16_bits(z[0]);
 }
 

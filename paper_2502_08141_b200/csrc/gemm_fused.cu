@@ -768,6 +768,20 @@ fused_kernel(const __grid_constant__ KParams<NB> P, const __grid_constant__ KMap
                 const uint32_t taddr = tmem_lane + acc * (uint32_t)kPairR;
                 const int tok = t.m0 + h * kHalfT + (int)crank * 128 + my_tok;
                 const bool any = tok - lane < M;        // somebody in this warp has a token
+                if constexpr (MODE == kModeEpilogue) {
+                    // (while the sums are being formed: this token's rows from memory into L2)
+                    if (!t.is_t && !t.part && tok < M && c_first < c_last) {
+                        const Epilogue& E = EP.m[t.prob];
+                        const size_t at = (size_t)tok * P.ld_out + r0 + c_first;
+                        auto prefetch = [&](const uint16_t* p) {
+                            asm volatile("prefetch.global.L2 [%0];" ::"l"(p + at));
+                            asm volatile("prefetch.global.L2 [%0];" ::"l"(p + at + min(c_last - c_first, 128) / 2));
+                            asm volatile("prefetch.global.L2 [%0];" ::"l"(p + at + min(c_last - c_first, 128) - 1));
+                        };
+                        if (E.multiply != nullptr) prefetch(E.multiply);
+                        if (E.residual != nullptr) prefetch(E.residual);
+                    }
+                }
                 if (!ptx::mbar_wait_warp(&bars->tmem_full[acc], (hc >> 1) & 1u, abort_flag, wait_ns)) bars->abort = 1u;
                 if (agree_abort()) { failed = true; break; }
                 ptx::tc_fence_after();
