@@ -75,13 +75,13 @@ __device__ __forceinline__ float2 activate_and_slope(float z) {
         const float cdf = normal_cdf(z, &bell);
         return make_float2(z * cdf, cdf + z * (kNormPeak * bell));
     }
-    if (ACT == LOWRA_ACT_GELU_TANH) {
-        const float p = sigmoid(tanh_argument(z));
-        return make_float2(z * p, p + z * p * (1.0f - p) * (2.0f * kTanhScale) * (1.0f + 3.0f * kTanhCubic * z * z));
-    }
-    if (ACT == LOWRA_ACT_SILU) {
-        const float p = sigmoid(z);
-        return make_float2(z * p, p * (1.0f + z * (1.0f - p)));
+    if (ACT == LOWRA_ACT_GELU_TANH || ACT == LOWRA_ACT_SILU) {
+        // p = sigmoid(t) and p (1 - p) from exp(-|t|), which neither overflows nor is a difference of near values
+        const float t = ACT == LOWRA_ACT_SILU ? z : tanh_argument(z);
+        const float e = exp2_fast(-kLog2E * fabsf(t)), r = reciprocal_fast(1.0f + e), p = t >= 0.0f ? r : e * r, w = e * r * r;
+        if (ACT == LOWRA_ACT_SILU) return make_float2(z * p, p + z * w);
+        const float c = fminf(fmaxf(z, -16.0f), 16.0f);           // (w is zero further out, and its factor may be infinite)
+        return make_float2(z * p, p + c * w * (2.0f * kTanhScale) * (1.0f + 3.0f * kTanhCubic * c * c));
     }
     return make_float2(z, 1.0f);
 }
