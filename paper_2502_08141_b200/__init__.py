@@ -111,7 +111,8 @@ def _load_py_calls(L: ctypes.CDLL):
     address = lambda fn: ctypes.cast(fn, ctypes.c_void_p).value  # noqa: E731
     module.bind(*(address(fn) for fn in (L.lowra_lora_forward, L.lowra_lora_backward_input, L.lowra_workspace_bytes, L.lowra_workspace_init, L.lowra_lora_forward_batch,
                                          L.lowra_lora_backward_input_batch, L.lowra_lora_backward_adapters, L.lowra_lora_backward_adapters_reuse,
-                                         L.lowra_adapter_workspace_bytes, L.lowra_workspace_projection, L.lowra_lora_forward_epilogue)))
+                                         L.lowra_adapter_workspace_bytes, L.lowra_workspace_projection, L.lowra_lora_forward_epilogue,
+                                         L.lowra_epilogue_workspace_bytes, L.lowra_epilogue_backward, L.lowra_update_workspace_bytes, L.lowra_update_factors)))
     return module
 
 
@@ -904,6 +905,12 @@ def lowra_epilogue_backward(dY: torch.Tensor, pre: Optional[torch.Tensor] = None
     lowra_lora_backward_input and lowra_lora_backward_adapters, dmultiply = dY * act(pre) where there is a multiply, dbias fp32 [N] if it is given or wanted.
     Returns (dZ, dmultiply or None, dbias or None)."""
     number = _activation(activation)
+    if stream is None and _py_calls is not None:
+        done = _py_calls.epilogue_backward(dY, pre, number, multiply, dZ, dmultiply, dbias, want_bias, workspace)
+        if done is not None:
+            if done.__class__ is int:
+                _check(done, "lowra_epilogue_backward")
+            return done
     if dY.dim() != 2:
         raise ValueError(f"dY must be [M, N], got {tuple(dY.shape)}")
     M, N = dY.shape
@@ -1041,6 +1048,12 @@ def lowra_update_factors(members, lr: float, momentum: float = 0.95, nesterov: b
     weights; updated in place unless master_out is given), weight (bf16, receives the rounded weights), update (fp32, receives the orthogonal matrix) and
     scale (a factor of lr, 1 if not given).  A member without a master needs an update.  `rank`: the side that all have in common (which one is taken where there are two
     makes no difference but of roundings).  Returns the members."""
+    if stream is None and _py_calls is not None:
+        done = _py_calls.update_factors(members, lr, momentum, nesterov, weight_decay, steps, coefficients, eps, rank, workspace)
+        if done is not None:
+            if done.__class__ is int:
+                _check(done, "lowra_update_factors")
+            return done
     n = len(members)
     if n == 0:
         raise ValueError("no members")

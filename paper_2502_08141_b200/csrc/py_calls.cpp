@@ -13,7 +13,12 @@
 //   gradients(X, dY, A, B, s, dA or None, dB or None, workspace or None)            the pair of gradients
 //   gradients_reuse(X, dY, T, U, r, dA or None, dB or None, workspace or None)      likewise
 //   projection(workspace, M, r, member)                                             its view of the workspace
+//   epilogue_backward(dY, pre, the activation's number, multiply, dZ, dmultiply, dbias, whether dbias is wanted, workspace: dY given, the others may be None)    the three outputs
+//   update_factors(members, lr, momentum, nesterov, weight_decay, steps, coefficients, eps, rank or None, workspace or None)                                     the members
 #include <torch/extension.h>
+
+#include <algorithm>
+#include <vector>
 
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -35,6 +40,10 @@ using GradientsReuse = lowra_status (*)(const uint16_t*, const uint16_t*, int32_
                                         size_t, void*);
 using GradientsBytes = size_t (*)(int32_t, int32_t);
 using Projection = const uint16_t* (*)(const void*, int32_t, int32_t, int32_t);
+using EpilogueBytes = size_t (*)(int32_t, int32_t);
+using EpilogueBackward = lowra_status (*)(const uint16_t*, const uint16_t*, const uint16_t*, int32_t, int32_t, int32_t, uint16_t*, uint16_t*, float*, void*, size_t, void*);
+using UpdateBytes = size_t (*)(const lowra_factor*, int32_t, int32_t);
+using Update = lowra_status (*)(const lowra_factor*, int32_t, int32_t, const lowra_update_step*, void*, size_t, void*);
 struct Library {
     Product forward, backward_input;
     WorkspaceBytes workspace_bytes;
@@ -45,6 +54,10 @@ struct Library {
     GradientsBytes gradients_bytes;
     Projection projection;
     ProductEpilogue forward_epilogue;
+    EpilogueBytes epilogue_bytes;
+    EpilogueBackward epilogue_backward;
+    UpdateBytes update_bytes;
+    Update update;
 } library;
 
 bool plain(PyObject* o) { return THPVariable_CheckExact(o); }
@@ -325,6 +338,170 @@ PyObject* batch(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
 }
 
+PyObject* epilogue_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    int32_t activation = 0;
+    if (n != 9 || library.forward == nullptr || !plain(args[0]) || !number(args[2], &activation) || !PyBool_Check(args[7])) Py_RETURN_NONE;
+    for (int i = 1; i < 9; ++i)
+        if (i != 2 && i != 7 && args[i] != Py_None && !plain(args[i])) Py_RETURN_NONE;
+    try {
+        const int64_t dev = c10::cuda::current_device();
+        const at::Tensor& dY = THPVariable_Unpack(args[0]);
+        if (dY.dim() != 2) Py_RETURN_NONE;
+        const int64_t M = dY.size(0), N = dY.size(1);
+        if (M > INT32_MAX || N > INT32_MAX || !matrix(dY, M, N, dev)) Py_RETURN_NONE;
+        at::Tensor rows[4], dbias, workspace;          // pre, multiply, dZ, dmultiply
+        constexpr int kAt[4] = {1, 3, 4, 5};
+        for (int i = 0; i < 4; ++i) {
+            if (args[kAt[i]] == Py_None) continue;
+            rows[i] = THPVariable_Unpack(args[kAt[i]]);
+            if (!matrix(rows[i], M, N, dev)) Py_RETURN_NONE;
+        }
+        if (args[6] != Py_None) {
+            dbias = THPVariable_Unpack(args[6]);
+            if (!array(dbias, at::kFloat, N, dev) || dbias.dim() != 1 || dbias.size(0) != N) Py_RETURN_NONE;
+        }
+        if (args[8] != Py_None) {
+            workspace = THPVariable_Unpack(args[8]);
+            if (!on(workspace, dev)) Py_RETURN_NONE;
+        }
+        const at::TensorOptions options = dY.options().requires_grad(false);
+        const bool with_bias = dbias.defined() || args[7] == Py_True;
+        lowra_status st;
+        {
+            Released released;
+            void* stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
+            if (!rows[2].defined()) rows[2] = at::empty({M, N}, options);
+            if (!rows[3].defined() && rows[1].defined()) rows[3] = at::empty({M, N}, options);
+            if (!dbias.defined() && with_bias) dbias = at::empty({N}, options.dtype(at::kFloat));
+            if (!workspace.defined() && with_bias) workspace = at::empty({(int64_t)std::max<size_t>(library.epilogue_bytes((int32_t)M, (int32_t)N), 256)}, options.dtype(at::kByte));
+            auto at_of = [](const at::Tensor& t) { return t.defined() ? bf16(t) : nullptr; };
+            st = library.epilogue_backward(bf16(dY), at_of(rows[0]), at_of(rows[1]), (int32_t)M, (int32_t)N, activation, bf16(rows[2]), at_of(rows[3]),
+                                           dbias.defined() ? static_cast<float*>(dbias.data_ptr()) : nullptr, workspace.defined() ? workspace.data_ptr() : nullptr,
+                                           workspace.defined() ? (size_t)workspace.nbytes() : 0, stream);
+        }
+        if (st != LOWRA_OK) return PyLong_FromLong(st);
+        PyObject* all = PyTuple_New(3);
+        at::Tensor* out[3] = {&rows[2], &rows[3], &dbias};
+        for (int i = 0; all != nullptr && i < 3; ++i) {
+            PyObject* o = args[4 + i];
+            if (o != Py_None) Py_INCREF(o);
+            else if (out[i]->defined()) o = THPVariable_Wrap(std::move(*out[i]));
+            else Py_INCREF(o);
+            PyTuple_SET_ITEM(all, i, o);
+        }
+        return all;
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+}
+
+PyObject* update_factors(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    lowra_update_step step = {};
+    int32_t rank = 0;
+    if (n != 10 || library.forward == nullptr || !PyList_CheckExact(args[0]) || !number(args[1], &step.lr) || !number(args[2], &step.momentum) || !PyBool_Check(args[3]) ||
+        !number(args[4], &step.weight_decay) || !number(args[5], &step.steps) || !PyTuple_CheckExact(args[6]) || PyTuple_GET_SIZE(args[6]) != 3 || !number(args[7], &step.eps) ||
+        (args[8] != Py_None && !number(args[8], &rank)) || (args[9] != Py_None && !plain(args[9])))
+        Py_RETURN_NONE;
+    for (int i = 0; i < 3; ++i)
+        if (!number(PyTuple_GET_ITEM(args[6], i), &step.coefficients[i])) Py_RETURN_NONE;
+    step.nesterov = args[3] == Py_True;
+    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
+    if (count < 1 || count > LOWRA_MAX_FACTORS) Py_RETURN_NONE;
+    enum { kGrad, kMomentum, kMomentumOut, kMaster, kMasterOut, kWeight, kUpdate, kScale, kNames };
+    static PyObject* names[kNames] = {};
+    if (names[kNames - 1] == nullptr) {
+        constexpr const char* kText[kNames] = {"grad", "momentum", "momentum_out", "master", "master_out", "weight", "update", "scale"};
+        for (int i = 0; i < kNames; ++i) names[i] = PyUnicode_InternFromString(kText[i]);
+    }
+    // the members' arrays: their dicts are the caller's, and other threads run during the call
+    std::vector<at::Tensor> held;
+    held.reserve((size_t)count * kScale + 1);
+    lowra_factor factors[LOWRA_MAX_FACTORS];
+    int64_t common[2] = {-1, -1};
+    try {
+        const int64_t dev = c10::cuda::current_device();
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            PyObject* m = PyList_GET_ITEM(args[0], i);
+            if (!PyDict_CheckExact(m)) Py_RETURN_NONE;
+            void* at[kScale] = {};
+            int64_t rows = 0, cols = 0;
+            lowra_factor& f = factors[i];
+            f.grad_fp32 = 0;
+            for (int k = 0; k < kScale; ++k) {
+                PyObject* o = PyDict_GetItemWithError(m, names[k]);
+                if (o == nullptr || o == Py_None) {
+                    if (k == kGrad || PyErr_Occurred() != nullptr) {
+                        PyErr_Clear();
+                        Py_RETURN_NONE;
+                    }
+                    continue;
+                }
+                if (!plain(o)) Py_RETURN_NONE;
+                held.push_back(THPVariable_Unpack(o));
+                const at::Tensor& t = held.back();
+                if (t.dim() != 2 || !on(t, dev)) Py_RETURN_NONE;
+                if (k == kGrad) {
+                    rows = t.size(0);
+                    cols = t.size(1);
+                    f.grad_fp32 = t.scalar_type() == at::kFloat;
+                }
+                const at::ScalarType type = k == kWeight || (k == kGrad && !f.grad_fp32) ? at::kBFloat16 : at::kFloat;
+                if (t.scalar_type() != type || t.size(0) != rows || t.size(1) != cols || rows > INT32_MAX || cols > INT32_MAX) Py_RETURN_NONE;
+                at[k] = t.data_ptr();
+            }
+            PyObject* scale = PyDict_GetItemWithError(m, names[kScale]);
+            f.scale = 1.0;
+            if (PyErr_Occurred() != nullptr || (scale != nullptr && !number(scale, &f.scale))) {
+                PyErr_Clear();
+                Py_RETURN_NONE;
+            }
+            f.rows = (int32_t)rows;
+            f.cols = (int32_t)cols;
+            f.grad_dev = at[kGrad];
+            f.momentum_dev = static_cast<const float*>(at[kMomentum]);
+            f.momentum_out_dev = static_cast<float*>(at[kMomentumOut] != nullptr ? at[kMomentumOut] : at[kMomentum]);
+            f.master_dev = static_cast<const float*>(at[kMaster]);
+            f.master_out_dev = static_cast<float*>(at[kMasterOut] != nullptr ? at[kMasterOut] : at[kMaster]);
+            f.weight_dev = static_cast<uint16_t*>(at[kWeight]);
+            f.update_dev = static_cast<float*>(at[kUpdate]);
+            // the sides that all have in common
+            if (i == 0) {
+                common[0] = rows;
+                common[1] = cols;
+            }
+            for (int64_t& c : common)
+                if (c != rows && c != cols) c = -1;
+        }
+        if (args[8] == Py_None) {         // the least of them that can be a rank
+            for (const int64_t c : common)
+                if (c >= 16 && c <= 128 && c % 16 == 0 && (rank == 0 || c < rank)) rank = (int32_t)c;
+            if (rank == 0) Py_RETURN_NONE;
+        }
+        at::Tensor workspace;
+        if (args[9] != Py_None) {
+            workspace = THPVariable_Unpack(args[9]);
+            if (!on(workspace, dev)) Py_RETURN_NONE;
+        }
+        lowra_status st;
+        {
+            Released released;
+            void* stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
+            if (!workspace.defined()) {
+                const size_t bytes = library.update_bytes(factors, (int32_t)count, rank);
+                if (bytes > 0) workspace = at::empty({(int64_t)bytes}, held[0].options().requires_grad(false).dtype(at::kByte));
+            }
+            st = workspace.defined() ? library.update(factors, (int32_t)count, rank, &step, workspace.data_ptr(), (size_t)workspace.nbytes(), stream) : LOWRA_ERR_SHAPE;
+        }
+        if (st != LOWRA_OK) return PyLong_FromLong(st);
+        Py_INCREF(args[0]);
+        return args[0];
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+}
+
 // fits(device, then for each array: tensor or None, element type, least number of elements) -> whether every one is a plain tensor on that
 // device, which is the current one, without gaps, of that type and long enough; None fits.  Types: 'B' bytes of any type, 'u' uint8, 'h' bf16,
 // 'f' fp32, 'd' fp64.  The other calls' checks, a tenth of a microsecond an array where the interpreter takes one; what does not fit is looked at
@@ -354,19 +531,21 @@ PyObject* fits(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 // bind(addresses of lowra_lora_forward, lowra_lora_backward_input, lowra_workspace_bytes, lowra_workspace_init, lowra_lora_forward_batch, lowra_lora_backward_input_batch,
-// lowra_lora_backward_adapters, lowra_lora_backward_adapters_reuse, lowra_adapter_workspace_bytes, lowra_workspace_projection, lowra_lora_forward_epilogue)
+// lowra_lora_backward_adapters, lowra_lora_backward_adapters_reuse, lowra_adapter_workspace_bytes, lowra_workspace_projection, lowra_lora_forward_epilogue,
+// lowra_epilogue_workspace_bytes, lowra_epilogue_backward, lowra_update_workspace_bytes, lowra_update_factors)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    void* p[11] = {};
-    for (int i = 0; i < 11; ++i) {
+    void* p[15] = {};
+    for (int i = 0; i < 15; ++i) {
         p[i] = i < n ? PyLong_AsVoidPtr(args[i]) : nullptr;
         if (p[i] == nullptr) {
-            if (PyErr_Occurred() == nullptr) PyErr_SetString(PyExc_ValueError, "bind takes eleven addresses");
+            if (PyErr_Occurred() == nullptr) PyErr_SetString(PyExc_ValueError, "bind takes fifteen addresses");
             return nullptr;
         }
     }
     library = Library{reinterpret_cast<Product>(p[0]), reinterpret_cast<Product>(p[1]), reinterpret_cast<WorkspaceBytes>(p[2]), reinterpret_cast<WorkspaceInit>(p[3]),
                       reinterpret_cast<Batch>(p[4]), reinterpret_cast<Batch>(p[5]), reinterpret_cast<Gradients>(p[6]), reinterpret_cast<GradientsReuse>(p[7]),
-                      reinterpret_cast<GradientsBytes>(p[8]), reinterpret_cast<Projection>(p[9]), reinterpret_cast<ProductEpilogue>(p[10])};
+                      reinterpret_cast<GradientsBytes>(p[8]), reinterpret_cast<Projection>(p[9]), reinterpret_cast<ProductEpilogue>(p[10]), reinterpret_cast<EpilogueBytes>(p[11]), reinterpret_cast<EpilogueBackward>(p[12]),
+                      reinterpret_cast<UpdateBytes>(p[13]), reinterpret_cast<Update>(p[14])};
     Py_RETURN_NONE;
 }
 
@@ -378,6 +557,8 @@ PyMethodDef methods[] = {
     {"gradients", (PyCFunction)(void (*)())gradients, METH_FASTCALL, nullptr},
     {"gradients_reuse", (PyCFunction)(void (*)())gradients_reuse, METH_FASTCALL, nullptr},
     {"projection", (PyCFunction)(void (*)())projection, METH_FASTCALL, nullptr},
+    {"epilogue_backward", (PyCFunction)(void (*)())epilogue_backward, METH_FASTCALL, nullptr},
+    {"update_factors", (PyCFunction)(void (*)())update_factors, METH_FASTCALL, nullptr},
     {"fits", (PyCFunction)(void (*)())fits, METH_FASTCALL, nullptr},
     {"bind", (PyCFunction)(void (*)())bind, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
