@@ -35,13 +35,13 @@ struct Factor {
     float* update;
     int L;
     float rate;                    // lr * scale
-    int tile0, item0;              // tiles of the factors before this one; tiles of apply_kernel
+    int tile0;                     // tiles of the factors before this one
     uint8_t tall, grad_fp32;
 };
 struct UpdateParams {
     double* sums;                  // [walker + factor][tiles of S][64]: the part of S that a walker has formed
     float* Q;                      // [factor][r][r]
-    int count, tiles, items;
+    int count, tiles;
     float mu, decay;               // decay: 1 - lr wd
     int nesterov, steps;
     double a, b, c, eps;
@@ -69,17 +69,17 @@ __host__ __device__ constexpr int whole_rows(int rows, int most) { return rows %
 
 // How a tile's quads (four neighbours in memory) go to the threads: rows of them in passes, the threads of a pass side by side in memory.  A row is one of the
 // long side (tall: its r values) or of the rank (wide: TL values).
-template <int NB, bool TALL, int T = kThreads, int TL = Shape<NB>::TL>
+template <int NB, bool TALL>
 struct Deal {
     using S = Shape<NB>;
-    static constexpr int per_row = (TALL ? S::r : TL) / 4, rows = TALL ? TL : S::r, at_once = whole_rows(rows, T / per_row), passes = rows / at_once;
+    static constexpr int per_row = (TALL ? S::r : S::TL) / 4, rows = TALL ? S::TL : S::r, at_once = whole_rows(rows, kThreads / per_row), passes = rows / at_once;
     static_assert(at_once * passes == rows && passes <= kQuads, "whole passes");
     bool in;                      // this thread has quads (wide: that lie inside; the length is a multiple of 8, so a quad is in or out as a whole)
     int row, col;                 // of its first one
     size_t at;                    // in the factor's arrays
     size_t step;
     int left;                     // tall: rows of the tile inside the factor
-    __device__ __forceinline__ Deal(const Factor& F, int l0, int thread) {      // (several groups of T threads may take a tile each)
+    __device__ __forceinline__ Deal(const Factor& F, int l0, int thread) {      // (of kThreads: several groups of them may take a tile each)
         row = thread / per_row;
         col = thread % per_row * 4;
         in = row < at_once && (TALL || l0 + col < F.L);
@@ -137,14 +137,12 @@ __device__ __forceinline__ int thread_here() {
 }
 
 // The walkers' shares of the tiles; the factor of a tile.
-__device__ __forceinline__ int share_of(int tiles, int walker) { return (int)((long long)tiles * walker / gridDim.x); }
-__device__ __forceinline__ int share(const UpdateParams& P, int walker) { return share_of(P.tiles, walker); }
-template <int Factor::*FIRST = &Factor::tile0>
+__device__ __forceinline__ int share(const UpdateParams& P, int walker) { return (int)((long long)P.tiles * walker / gridDim.x); }
 __device__ __forceinline__ int factor_of(const UpdateParams& P, int tile) {
     int lo = 0, hi = P.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (P.f[mid].*FIRST <= tile) lo = mid;
+        if (P.f[mid].tile0 <= tile) lo = mid;
         else hi = mid - 1;
     }
     return lo;
@@ -524,8 +522,8 @@ __global__ void __launch_bounds__(32 * IterateShape<NB, FEW>::warps) iterate_ker
 
 // ------------------------------------------------------------------------------------------------ u Q, and the weights
 // On the fp32 pipe: a thread forms eight of the long side times four ranks, from a tile of u and Q in shared memory.  (In two or three tf32 parts on the tensor
-// instructions it was no faster, and its errors, 2e-5 of the update, were ten times those of fp32.)  Three CTAs to an SM up to rank 64, above that one of three times the
-// threads and tile, which share Q: the warps cover one another's loads.
+// instructions it was no faster, and its errors, 2e-5 of the update, were ten times those of fp32.)  One CTA to an SM: two groups of four warps fill tiles of u in turn, two others
+// multiply them by Q, each with a copy of its own.  Loads, products and stores then go on side by side; a CTA that did one after the other, three to an SM, took APPLYTIMES.
 // u, four neighbours in memory, from the gradient and the new momentum.
 struct Raw {
     uint4 g;
@@ -551,47 +549,81 @@ __device__ __forceinline__ float4 u_of(const UpdateParams& P, const Factor& F, c
     return P.nesterov ? axpy(P.mu, r.m, grad_quad(F, r.g)) : r.m;
 }
 
+constexpr int kApplyThreads = 4 * kThreads;
+constexpr int kMultiply = kEmpty + kStages;                       // named barriers of the two groups that multiply (gram_kernel has one there)
 template <int NB>
 struct ApplyShape {
     using S = Shape<NB>;
-    static constexpr int groups_of_threads = NB > 4 ? 3 : 1, threads = kThreads * groups_of_threads, TL = S::TL * groups_of_threads, resident = NB > 4 ? 1 : 3;
-    static constexpr int pitch = S::r + 4;                        // u, tall: [l][c]
-    static constexpr size_t tall = (size_t)TL * pitch, wide = (size_t)TL * S::r, bytes = ((size_t)S::r * S::r + (tall > wide ? tall : wide)) * 4;
+    static constexpr int pitch = S::r + 4;                        // u, tall: [l][c]; wide: [c][l]
+    static constexpr int floats = S::TL * pitch > S::r * S::TL ? S::TL * pitch : S::r * S::TL;
+    static constexpr size_t bytes = (size_t)(2 * S::r * S::r + kStages * floats) * 4;
 };
 template <int NB>
-__global__ void __launch_bounds__(ApplyShape<NB>::threads, ApplyShape<NB>::resident) apply_kernel(const __grid_constant__ UpdateParams P) {
+__global__ void __launch_bounds__(kApplyThreads, 1) apply_kernel(const __grid_constant__ UpdateParams P) {
     using S = Shape<NB>;
     using A = ApplyShape<NB>;
-    constexpr int TL = A::TL, groups = TL / 8;
+    constexpr int TL = S::TL, groups = TL / 8;
     extern __shared__ __align__(16) unsigned char update_smem[];
-    float* Q = reinterpret_cast<float*>(update_smem);             // [r][r]
-    float* u = Q + S::r * S::r;                                   // tall: [TL][pitch]; wide: [r][TL]
-    const int first = share_of(P.items, blockIdx.x), end = share_of(P.items, blockIdx.x + 1);
+    float* const Qs = reinterpret_cast<float*>(update_smem);      // [2][r][r]
+    float* const tiles = Qs + 2 * S::r * S::r;
+    const int group = (int)threadIdx.x / kThreads, half = group & 1;
+    const int first = share(P, blockIdx.x), count = share(P, blockIdx.x + 1) - first;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    int f = factor_of<&Factor::item0>(P, first), loaded = -1;
-    auto put = [&](auto tall, const Factor& F, int l0) {
-        constexpr bool TALL = decltype(tall)::value;
-        using D = Deal<NB, TALL, A::threads, TL>;
-        constexpr int pitch = TALL ? A::pitch : TL;
-        const D deal(F, l0, thread_here());
-        float* to = u + deal.row * pitch + deal.col;
-        const bool has = deal.row < D::at_once;
-        Raw raw[D::passes];
-        deal.each([&](int i, size_t at, bool in) { raw[i] = load_raw(P, F, at, in); });
-        deal.each([&](int i, size_t, bool) {
-            if (has) *reinterpret_cast<float4*>(to + i * D::at_once * pitch) = u_of(P, F, raw[i]);
-        });
-    };
-    // thread's outputs, quads of four neighbours in memory: number i of eight at place + (i / 4) * far + (i % 4) * near_by
-    auto work = [&](auto tall, const Factor& F, int l0) {
+    int f = factor_of(P, first);
+    if (group >= 2) {
+        // ================================================================== fillers: tiles half, half + 2, ...
+        // (iterate_kernel lets this kernel start when gram_kernel is through: u may be read before the wait for Q)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        for (int n = half; n < count; n += 2) {
+            while (f + 1 < P.count && P.f[f + 1].tile0 <= first + n) ++f;
+            const Factor& F = P.f[f];
+            const int l0 = (first + n - F.tile0) * TL, stage = n % kStages;
+            float* u = tiles + stage * A::floats;
+            auto fill = [&](auto tall) {
+                constexpr bool TALL = decltype(tall)::value;
+                using D = Deal<NB, TALL>;
+                constexpr int pitch = TALL ? A::pitch : TL;
+                const D deal(F, l0, thread_here() % kThreads);
+                float* to = u + deal.row * pitch + deal.col;
+                const bool has = deal.row < D::at_once;
+                auto part = [&](auto from) {                      // (half of the quads at a time: registers)
+                    constexpr int FROM = decltype(from)::value, N = kQuads / 2;
+                    Raw raw[N];
+                    deal.template each<FROM, N>([&](int i, size_t at, bool in) { raw[i - FROM] = load_raw(P, F, at, in); });
+                    if (FROM == 0 && n >= kStages) ptx::named_barrier_sync(kEmpty + stage, 2 * kThreads);     // the tile there before has been read
+                    deal.template each<FROM, N>([&](int i, size_t, bool) {
+                        if (has) *reinterpret_cast<float4*>(to + i * D::at_once * pitch) = u_of(P, F, raw[i - FROM]);
+                    });
+                };
+                part(std::integral_constant<int, 0>());
+                part(std::integral_constant<int, kQuads / 2>());
+            };
+            if (F.tall) fill(std::true_type());
+            else fill(std::false_type());
+            barrier_arrive(kFull + stage, 2 * kThreads);
+        }
+        return;
+    }
+    // ====================================================================== u Q: tiles half, half + 2, ...
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    float* const Q = Qs + half * S::r * S::r;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    int loaded = -1;
+    // A thread's outputs, quads of four neighbours in memory: number i of eight at place + (i / 4) * far + (i % 4) * near_by
+    auto work = [&](auto tall, const Factor& F, int l0, const float* u, auto done) {
         constexpr bool TALL = decltype(tall)::value;
         // tall: ranks c .. c + 3, rows lg, lg + TL / 8, ...: a warp's lanes lie side by side along the rank
         // wide: ranks c .. c + 3, and two runs of four of the long side: the lanes lie side by side along it
-        const int thread = thread_here(), cg = TALL ? thread % (S::r / 4) : thread / groups, lg = TALL ? thread / (S::r / 4) : thread % groups;
+        const int thread = thread_here() % kThreads, cg = TALL ? thread % (S::r / 4) : thread / groups, lg = TALL ? thread / (S::r / 4) : thread % groups;
         const bool has = TALL ? lg < groups : cg < S::r / 4;
         const size_t place = TALL ? (size_t)(l0 + lg) * S::r + cg * 4 : (size_t)(cg * 4) * F.L + (l0 + lg * 4);
         const size_t near_by = TALL ? (size_t)(groups * S::r) : (size_t)F.L, far = TALL ? 4 * near_by : (size_t)(TL / 2);
         auto inside = [&](int i) { return has && (TALL ? l0 + lg + i * groups < F.L : l0 + lg * 4 + (i / 4) * (TL / 2) < F.L); };
+        float4 w[8];
+        if (F.master != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = inside(i) ? *reinterpret_cast<const float4*>(F.master + place + (i / 4) * far + (i % 4) * near_by) : zero4();
+        }
         float4 acc[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] = zero4();
@@ -625,11 +657,7 @@ __global__ void __launch_bounds__(ApplyShape<NB>::threads, ApplyShape<NB>::resid
                 }
             }
         }
-        float4 w[8];
-        if (F.master != nullptr) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = inside(i) ? *reinterpret_cast<const float4*>(F.master + place + (i / 4) * far + (i % 4) * near_by) : zero4();
-        }
+        done();
         if (F.update != nullptr) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -647,23 +675,24 @@ __global__ void __launch_bounds__(ApplyShape<NB>::threads, ApplyShape<NB>::resid
             if (F.weight != nullptr) *reinterpret_cast<uint2*>(F.weight + at) = make_uint2(pack_bf16x2(n.x, n.y), pack_bf16x2(n.z, n.w));
         }
     };
-    for (int tile = first; tile < end; ++tile) {
+    for (int n = half; n < count; n += 2) {
+        while (f + 1 < P.count && P.f[f + 1].tile0 <= first + n) ++f;
         const Factor& F = P.f[f];
-        const int l0 = (tile - F.item0) * TL;
-        // (iterate_kernel lets this kernel start when gram_kernel is through: u may be read before the wait for Q)
-        if (F.tall) put(std::true_type(), F, l0);
-        else put(std::false_type(), F, l0);
+        const int l0 = (first + n - F.tile0) * TL, stage = n % kStages;
         if (loaded != f) {
-            if (loaded < 0) asm volatile("griddepcontrol.wait;" ::: "memory");
-            for (int i = threadIdx.x; i < S::r * S::r / 4; i += A::threads)
+            ptx::named_barrier_sync(kMultiply + half, kThreads);  // the group has read the Q before
+            for (int i = (int)threadIdx.x % kThreads; i < S::r * S::r / 4; i += kThreads)
                 reinterpret_cast<float4*>(Q)[i] = __ldcg(reinterpret_cast<const float4*>(P.Q + (size_t)f * S::r * S::r) + i);
+            ptx::named_barrier_sync(kMultiply + half, kThreads);
             loaded = f;
         }
-        __syncthreads();
-        if (F.tall) work(std::true_type(), F, l0);
-        else work(std::false_type(), F, l0);
-        __syncthreads();                                          // u and Q have been read
-        if (l0 + TL >= F.L) ++f;
+        ptx::named_barrier_sync(kFull + stage, 2 * kThreads);
+        const float* u = tiles + stage * A::floats;
+        auto done = [&]() {
+            if (n + kStages < count) barrier_arrive(kEmpty + stage, 2 * kThreads);
+        };
+        if (F.tall) work(std::true_type(), F, l0, u, done);
+        else work(std::false_type(), F, l0, u, done);
     }
 }
 
@@ -678,12 +707,10 @@ template <int NB>
 lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream) {
     using S = Shape<NB>;
     using A = ApplyShape<NB>;
-    P.tiles = P.items = 0;
+    P.tiles = 0;
     for (int i = 0; i < P.count; ++i) {
         P.f[i].tile0 = P.tiles;
-        P.f[i].item0 = P.items;
         P.tiles += tiles_of<NB>(P.f[i].L);
-        P.items += (P.f[i].L + A::TL - 1) / A::TL;
     }
     P.sums = static_cast<double*>(workspace);
     P.Q = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + sums_bytes<NB>(P.tiles, P.count));
@@ -723,8 +750,8 @@ lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream
     cfg.numAttrs = 1;
     static SmemLimit limit = {};
     cfg.dynamicSmemBytes = A::bytes;
-    cfg.gridDim = dim3((unsigned)(P.items < A::resident * kNumSMs ? P.items : A::resident * kNumSMs), 1, 1);
-    cfg.blockDim = dim3(A::threads, 1, 1);
+    cfg.gridDim = dim3(walkers, 1, 1);
+    cfg.blockDim = dim3(kApplyThreads, 1, 1);
     if (ensure_smem_limit(reinterpret_cast<const void*>(apply_kernel<NB>), cfg.dynamicSmemBytes, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
     return cudaLaunchKernelEx(&cfg, apply_kernel<NB>, P) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
 }
@@ -797,7 +824,7 @@ extern "C" lowra_status lowra_update_factors(const lowra_factor* members_host, i
             return LOWRA_ERR_ALIGN;
         const bool tall = m.rows != r;
         P.f[i] = Factor{m.grad_dev, m.momentum_dev, m.momentum_out_dev, m.master_dev, m.master_out_dev, m.weight_dev, m.update_dev, tall ? m.rows : m.cols,
-                        (float)(step_host->lr * m.scale), 0, 0, (uint8_t)tall, (uint8_t)(m.grad_fp32 != 0)};
+                        (float)(step_host->lr * m.scale), 0, (uint8_t)tall, (uint8_t)(m.grad_fp32 != 0)};
     }
     if (workspace_bytes < lowra_update_workspace_bytes(members_host, count, r) || (reinterpret_cast<uintptr_t>(workspace_dev) & 255u) != 0) return LOWRA_ERR_WORKSPACE;
     if ((st = check_device()) != LOWRA_OK) return st;
