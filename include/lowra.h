@@ -373,8 +373,8 @@ lowra_status lowra_lora_forward_adapters_epilogue(const lowra_layout* layout, co
  *   multiply_dev as in the forward call, or NULL;  relu's slope at zero is 0.
  *   Outputs may be inputs themselves (dZ in the place of dY or pre, dmultiply in that of multiply), else they overlap nothing.
  *   workspace_dev: >= lowra_epilogue_workspace_bytes(M, N) bytes, 256-byte aligned, contents overwritten; used for dbias only.
- * Errors: dY missing, no output, pre or multiply missing where it is needed -> LOWRA_ERR_NULL; M < 1, N % 8 != 0, an activation that is none, dZ and
- * dmultiply in one place -> LOWRA_ERR_SHAPE; LOWRA_ERR_ALIGN, LOWRA_ERR_WORKSPACE as elsewhere.
+ * Errors: dY missing, no output, pre or multiply missing where it is needed -> LOWRA_ERR_NULL; M < 1 or > 2^30, N % 8 != 0 or > 2^24, an activation that
+ * is none, dZ and dmultiply in one place -> LOWRA_ERR_SHAPE; LOWRA_ERR_ALIGN, LOWRA_ERR_WORKSPACE as elsewhere.
  */
 size_t lowra_epilogue_workspace_bytes(int32_t M, int32_t N);
 lowra_status lowra_epilogue_backward(const uint16_t* dY_dev, const uint16_t* pre_dev, const uint16_t* multiply_dev, int32_t M, int32_t N, int32_t activation,
@@ -432,7 +432,7 @@ lowra_status lowra_lora_backward_adapters_reuse(const uint16_t* X_dev, const uin
  *     X_0 = u / (|u| + eps), |u| the Frobenius norm;     X <- a X + X (b G + c G^2), G = X^T X (of the side r), `steps` times
  *     w' = (1 - lr weight_decay) w - lr scale X;         weight = bf16(w')
  * The matrices G are formed and iterated in fp64 (their condition is the square of u's).
- *   lowra_factor: rows x cols, one of them r, the other a multiple of 8; row-major, without gaps, device, 16-byte aligned
+ *   lowra_factor: rows x cols, one of them r, the other a multiple of 8 up to 2^24; row-major, without gaps, device, 16-byte aligned
  *     grad_dev           bf16 (as lowra_lora_backward_adapters writes it) or, with grad_fp32 != 0, fp32                    (in)
  *     momentum_dev       fp32, or NULL: no momentum                      (in);   momentum_out_dev  m', may be momentum_dev itself     (out)
  *     master_dev         fp32 w, or NULL                                 (in);   master_out_dev    w', may be master_dev itself       (out)

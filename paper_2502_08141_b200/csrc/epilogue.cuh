@@ -85,6 +85,29 @@ __device__ __forceinline__ float2 activate_and_slope(float z) {
     }
     return make_float2(z, 1.0f);
 }
+// Two values; gelu with two products to an instruction (the backward pass is as much bound by its instructions as by memory there: 4096 x 11008 with a bias 53.3 -> 51.2 us).
+template <int ACT>
+__device__ __forceinline__ void activate_and_slope(float2 z, float2* act, float2* slope) {
+    if (ACT != LOWRA_ACT_GELU) {
+        const float2 a = activate_and_slope<ACT>(z.x), b = activate_and_slope<ACT>(z.y);
+        *act = make_float2(a.x, b.x);
+        *slope = make_float2(a.y, b.y);
+        return;
+    }
+    auto both = [](float c) { return make_float2(c, c); };
+    const float2 d = fma2(both(0.300520382f), make_float2(fabsf(z.x), fabsf(z.y)), both(1.0f)), t = make_float2(reciprocal_fast(d.x), reciprocal_fast(d.y));
+    const float2 x = mul2(mul2(z, z), both(-0.5f * kLog2E)), e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+    float2 p = fma2(both(0.0360919518f), t, both(-0.158048567f));
+    p = fma2(p, t, both(0.206342268f));
+    p = fma2(p, t, both(-0.0539579815f));
+    p = fma2(p, t, both(0.12877795f));
+    p = fma2(p, t, both(0.0999785458f));
+    p = fma2(p, t, both(0.120980384f));
+    p = fma2(p, t, both(0.11983539f));
+    const float2 q = mul2(mul2(p, t), e), cdf = make_float2(z.x < 0.0f ? q.x : 1.0f - q.x, z.y < 0.0f ? q.y : 1.0f - q.y);
+    *act = mul2(z, cdf);
+    *slope = fma2(z, mul2(both(kNormPeak), e), cdf);
+}
 // One activation for a few values: the choice is made once for all of them (it is the same in the whole launch).
 template <int N>
 __device__ __forceinline__ void activate(float (&z)[N], int activation) {

@@ -7,7 +7,7 @@
 // Three kernels: gram_kernel reads g and m, writes m', and forms parts of S; iterate_kernel adds them up and forms Q; apply_kernel forms u Q and writes
 // the weights.  u is read twice whatever the number of steps (the second time mostly from L2).
 // S holds the squares of u's singular values, so a value of 1e-3 |u|, which the iteration lifts to 0.5, is 1e-6 of S: in fp32 it would be off by a
-// percent.  S and everything of size r x r are therefore fp64, on the fp64 tensor instructions (m8n8k4, measured 36 TFLOP/s); u and u Q are fp32.
+// percent.  S and everything of size r x r are therefore fp64, on the fp64 tensor instructions (m8n8k4; 24 TFLOP/s in gram_kernel); u and u Q are fp32.
 #include <string.h>
 
 #include "epilogue.cuh"
@@ -23,7 +23,7 @@ constexpr int kQuads = kTileElements / 4 / kThreads;      // four neighbouring e
 constexpr int kWalkers = kNumSMs;                         // CTAs that share the tiles of all factors out, in gram_kernel
 constexpr int kStages = 4, kFillers = 2;                  // tiles in its shared memory; groups of kThreads that fill them
 constexpr int kGramThreads = (1 + kFillers) * kThreads;
-constexpr int kMaxFactors = LOWRA_MAX_FACTORS;
+constexpr int kMaxFactors = LOWRA_MAX_FACTORS, kLongest = 1 << 24;
 
 struct Factor {
     const void* grad;              // bf16 or fp32
@@ -113,19 +113,16 @@ __device__ __forceinline__ float4 axpy2(float a, float4 x, float4 y) {       // 
 }
 __device__ __forceinline__ float4 zero4() { return make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
 
-// The tile's gradient, and its old momentum (OLD) or the new one where u needs it.
-template <bool OLD, int FROM = 0, int N = kQuads, typename D>
-__device__ __forceinline__ void fetch(const UpdateParams& P, const Factor& F, const D& deal, Held& held) {
-    const float* m = OLD ? F.momentum : F.momentum_out;
-    if (OLD || m == nullptr || P.nesterov) {
-        if (F.grad_fp32) deal.template each<FROM, N>([&](int i, size_t at, bool in) { held.g[i] = in ? *reinterpret_cast<const uint4*>(static_cast<const float*>(F.grad) + at) : make_uint4(0u, 0u, 0u, 0u); });
-        else deal.template each<FROM, N>([&](int i, size_t at, bool in) {
-            const uint2 p = in ? *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(F.grad) + at) : make_uint2(0u, 0u);
-            held.g[i].x = p.x;
-            held.g[i].y = p.y;
-        });
-    }
-    if (m != nullptr) deal.template each<FROM, N>([&](int i, size_t at, bool in) { held.m[i] = in ? __ldcg(reinterpret_cast<const float4*>(m + at)) : zero4(); });
+// A tile's gradient and momentum.
+template <typename D>
+__device__ __forceinline__ void fetch(const Factor& F, const D& deal, Held& held) {
+    if (F.grad_fp32) deal.each([&](int i, size_t at, bool in) { held.g[i] = in ? *reinterpret_cast<const uint4*>(static_cast<const float*>(F.grad) + at) : make_uint4(0u, 0u, 0u, 0u); });
+    else deal.each([&](int i, size_t at, bool in) {
+        const uint2 p = in ? *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(F.grad) + at) : make_uint2(0u, 0u);
+        held.g[i].x = p.x;
+        held.g[i].y = p.y;
+    });
+    if (F.momentum != nullptr) deal.each([&](int i, size_t at, bool in) { held.m[i] = in ? *reinterpret_cast<const float4*>(F.momentum + at) : zero4(); });
 }
 
 // The thread's number, as if it were another one every time: what follows from it is then worked out where it is needed.  (Kept from tile to tile, the places of
@@ -151,8 +148,9 @@ __device__ __forceinline__ int factor_of(const UpdateParams& P, int tile) {
 // ------------------------------------------------------------------------------------------------ parts of S
 // A walker (one CTA to an SM) takes neighbouring tiles; what it forms of a factor's S goes to slot walker + factor (both only ever go up, so a slot is one
 // walker's and one factor's).  Two groups of four warps take the tiles in turn: gradient and momentum into registers, the new momentum to memory, u to shared
-// memory.  The four warps of a third group feed the tensor instructions, one warp to a scheduler, which is enough to keep them busy.  (All warps doing both in turn, two CTAs
-// to an SM: the tensor pipe 52 % busy while an SM was, with the filling's instructions in between.)
+// memory.  The four warps of a third group feed the tensor instructions, which is what bounds it: of the 22 us for a layer's fourteen factors of rank 64, 17 remain without the
+// filling, and 18 without the products.  (All warps doing both in turn, two CTAs to an SM: 26 us.  m16n8k4 on pairs of blocks, which runs at twice the rate in isolation but has
+// a tenth more to do: the same.  Three groups that fill: the same.)
 // Up to r = 64 every warp takes a quarter of the tile's long side and all blocks of S (36 at r = 64: 144 registers); above that each warp takes
 // all of it and a quarter of the blocks: the triangles of the two halves of the rank, and two halves of the square between them.
 __device__ __forceinline__ void barrier_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
@@ -189,7 +187,7 @@ __global__ void __launch_bounds__(kGramThreads, 1) gram_kernel(const __grid_cons
                 using D = Deal<NB, TALL>;
                 constexpr int pitch = TALL ? S::tall_pitch : S::wide_pitch;
                 const D deal(F, l0, thread_here() % kThreads);
-                fetch<true>(P, F, deal, held);
+                fetch(F, deal, held);
                 float* to = u + deal.row * pitch + deal.col;
                 const bool has = deal.row < D::at_once;
                 if (n >= kStages) ptx::named_barrier_sync(kEmpty + stage, 2 * kThreads);      // the tile there before has been read
@@ -523,7 +521,9 @@ __global__ void __launch_bounds__(32 * IterateShape<NB, FEW>::warps) iterate_ker
 // ------------------------------------------------------------------------------------------------ u Q, and the weights
 // On the fp32 pipe: a thread forms eight of the long side times four ranks, from a tile of u and Q in shared memory.  (In two or three tf32 parts on the tensor
 // instructions it was no faster, and its errors, 2e-5 of the update, were ten times those of fp32.)  One CTA to an SM: two groups of four warps fill tiles of u in turn, two others
-// multiply them by Q, each with a copy of its own.  Loads, products and stores then go on side by side; a CTA that did one after the other, three to an SM, took APPLYTIMES.
+// multiply them by Q, each with a copy of its own.  Loads, products and stores then go on side by side; CTAs that did one after the
+// other, three to an SM, took 50 us for fourteen factors of 11008 x 64 where these take 44 (and 150 where these take 131 at rank 128).  What bounds it is shared memory, three reads of 16 bytes for
+// 32 products (eight by eight values a thread: fewer reads, but tiles too large to be dealt out evenly).
 // u, four neighbours in memory, from the gradient and the new momentum.
 struct Raw {
     uint4 g;
@@ -768,14 +768,12 @@ size_t workspace_bytes_of(const lowra_factor* m, int count) {
 lowra_status check_shapes(const lowra_factor* m, int32_t count, int32_t r) {
     if (!m) return LOWRA_ERR_NULL;
     if (count < 1 || count > kMaxFactors || r < 16 || r > 128 || r % 16 != 0) return LOWRA_ERR_SHAPE;
-    long long elements = 0;
     for (int i = 0; i < count; ++i) {
         if (m[i].rows != r && m[i].cols != r) return LOWRA_ERR_SHAPE;
         const int32_t L = m[i].rows == r ? m[i].cols : m[i].rows;
-        if (L < 8 || L % 8 != 0) return LOWRA_ERR_SHAPE;
-        elements += (long long)L * r;
+        if (L < 8 || L > kLongest || L % 8 != 0) return LOWRA_ERR_SHAPE;      // (their tiles, and those of all, then are numbers of 32 bits)
     }
-    return elements < (1ll << 40) ? LOWRA_OK : LOWRA_ERR_SHAPE;
+    return LOWRA_OK;
 }
 
 }  // namespace

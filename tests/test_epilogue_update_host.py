@@ -46,6 +46,7 @@ def test_backward():
     assert call(dm=AT + 64) == lw.LOWRA_ERR_NULL and call(pre=None, act=0, mul=AT, dm=AT + 64) == lw.LOWRA_ERR_NULL
     assert call(M=0) == lw.LOWRA_ERR_SHAPE and call(N=4) == lw.LOWRA_ERR_SHAPE and call(N=60) == lw.LOWRA_ERR_SHAPE and call(act=7) == lw.LOWRA_ERR_SHAPE
     assert call(mul=AT, dm=AT) == lw.LOWRA_ERR_SHAPE and call(dZ=AT + 2) == lw.LOWRA_ERR_ALIGN and call(M=4096, db=AT) == lw.LOWRA_ERR_WORKSPACE
+    assert call(M=(1 << 30) + 1) == lw.LOWRA_ERR_SHAPE and call(N=(1 << 24) + 8) == lw.LOWRA_ERR_SHAPE
     assert lw.lowra_epilogue_workspace_bytes(0, 64) == 0 and lw.lowra_epilogue_workspace_bytes(4, 60) == 0
     for M, N in ((1, 8), (17, 264), (8192, 512), (100000, 13824)):
         size = lw.lowra_epilogue_workspace_bytes(M, N)
@@ -64,7 +65,7 @@ def test_update():
         return lw.lib().lowra_update_factors(arr, count, r, ctypes.byref(step) if with_step else None, workspace, 0, None)
 
     assert lw.lib().lowra_update_factors(None, 1, 16, ctypes.byref(step), AT, 0, None) == lw.LOWRA_ERR_NULL
-    for bad in (dict(r=8), dict(r=24), dict(r=144), dict(count=0), dict(count=65), dict(rows=60), dict(rows=0), dict(rows=64, cols=24), dict(steps=0), dict(steps=33)):
+    for bad in (dict(r=8), dict(r=24), dict(r=144), dict(count=0), dict(count=65), dict(rows=60), dict(rows=0), dict(rows=(1 << 24) + 8), dict(rows=64, cols=24), dict(steps=0), dict(steps=33)):
         assert call(**bad) == lw.LOWRA_ERR_SHAPE, bad
     for bad in (dict(with_step=False), dict(workspace=None), dict(grad_dev=None), dict(momentum_dev=None), dict(momentum_out_dev=None), dict(master_out_dev=None),
                 dict(master_dev=None, master_out_dev=None), dict(master_dev=None, master_out_dev=None, update_dev=AT, weight_dev=AT)):
