@@ -331,7 +331,8 @@ lowra_status lowra_lora_forward_adapters(const lowra_layout* layout, const uint8
  *   residual_dev  bf16 [M, N], or NULL
  *   pre_dev       bf16 [M, N] (out), or NULL: Z
  * Arrays 16-byte aligned, row-major, without gaps, rows as in Y.  Y may be the residual itself (the residual stream, added to in place) or the multiplied
- * array; else Y and pre overlap nothing that the call reads or writes (a pre that is Y, multiply or residual -> LOWRA_ERR_SHAPE).
+ * array; else Y and pre overlap nothing that the call reads or writes (a pre that is Y, multiply, residual or X,
+ * and a Y that is X -> LOWRA_ERR_SHAPE: X may be the residual too, but then Y is an array of its own).
  * One epilogue belongs to one member; the array of epilogues is host memory and is read before the call returns.
  *   lowra_lora_forward_epilogue           as lowra_lora_forward (few tokens included)
  *   lowra_lora_forward_batch_epilogue     as lowra_lora_forward_batch: epilogues_host[count], one for every member

@@ -1090,6 +1090,8 @@ def lowra_update_factors(members, lr: float, momentum: float = 0.95, nesterov: b
         if not common:
             raise ValueError("the members have no side in common that could be the rank")
         rank = min(common, key=lambda d: (d % 16 != 0 or d > 128, d))
+    if len(coefficients) != 3:
+        raise ValueError(f"coefficients are three numbers, got {len(coefficients)}")
     step = _CUpdateStep(float(lr), float(momentum), float(weight_decay), float(eps), (ctypes.c_double * 3)(*coefficients), int(bool(nesterov)), int(steps))
     _extent(workspace, 0, "workspace")
     if workspace is None:

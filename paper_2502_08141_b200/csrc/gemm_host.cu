@@ -142,9 +142,11 @@ struct MemberArgs {
 };
 
 // The caller's description of what stands behind a product, checked.
-lowra_status take_epilogue(const lowra_epilogue* e, const uint16_t* Y, Epilogue* out) {
+lowra_status take_epilogue(const lowra_epilogue* e, const uint16_t* X, const uint16_t* Y, Epilogue* out) {
     if (!e) return LOWRA_ERR_NULL;
     if (e->activation < LOWRA_ACT_NONE || e->activation > LOWRA_ACT_SILU) return LOWRA_ERR_SHAPE;
+    // (a block's input that is its residual as well: added to in place it would change under the product)
+    if (X && (X == Y || X == e->pre_dev)) return LOWRA_ERR_SHAPE;
     // (the copy of Z is written before the other arrays are read)
     if (e->pre_dev && (e->pre_dev == Y || e->pre_dev == e->multiply_dev || e->pre_dev == e->residual_dev)) return LOWRA_ERR_SHAPE;
     if (!aligned16(e->bias_dev) || !aligned16(e->multiply_dev) || !aligned16(e->residual_dev) || !aligned16(e->pre_dev)) return LOWRA_ERR_ALIGN;
@@ -551,7 +553,7 @@ lowra_status run_batch(bool backward, const lowra_member* members, const lowra_e
         const lowra_member& m = members[i];
         mem[i] = MemberArgs{m.layout, m.packed_dev, m.absmax_dev, m.maps_dev, m.act_dev, m.A_dev, m.B_dev, m.out_dev, M, {}};
         if (epilogues != nullptr) {
-            const lowra_status st = take_epilogue(&epilogues[i], m.out_dev, &mem[i].epilogue);
+            const lowra_status st = take_epilogue(&epilogues[i], m.act_dev, m.out_dev, &mem[i].epilogue);
             if (st != LOWRA_OK) return st;
         }
         if (m.layout != nullptr && m.layout->deal_dev == nullptr) return LOWRA_ERR_NULL;   // also for a batch of one
@@ -584,7 +586,7 @@ extern "C" lowra_status lowra_lora_forward_epilogue(const lowra_layout* layout, 
                                                     void* stream) {
     using namespace lowra;
     MemberArgs m = {layout, packed_dev, absmax_dev, maps_dev, X_dev, A_dev, B_dev, Y_dev, M, {}};
-    const lowra_status st = take_epilogue(epilogue_host, Y_dev, &m.epilogue);
+    const lowra_status st = take_epilogue(epilogue_host, X_dev, Y_dev, &m.epilogue);
     if (st != LOWRA_OK) return st;
     return run_members(false, &m, 1, r, s, workspace_dev, workspace_bytes, stream, true, true, true);
 }
@@ -674,7 +676,7 @@ extern "C" lowra_status lowra_lora_forward_adapters_epilogue(const lowra_layout*
                                                              float s, const lowra_epilogue* epilogue_host, uint16_t* Y_dev, void* workspace_dev,
                                                              size_t workspace_bytes, void* stream) {
     lowra::Epilogue epilogue;
-    const lowra_status st = lowra::take_epilogue(epilogue_host, Y_dev, &epilogue);
+    const lowra_status st = lowra::take_epilogue(epilogue_host, X_dev, Y_dev, &epilogue);
     if (st != LOWRA_OK) return st;
     return lowra::run_adapter_groups(layout, packed_dev, absmax_dev, maps_dev, n_adapters, X_dev, M, group_start_host, A_dev, B_dev, r, s, &epilogue, Y_dev,
                                      workspace_dev, workspace_bytes, stream);

@@ -23,9 +23,9 @@ def epilogue(**fields):
     return e
 
 
-def forward(e, Y=AT):
+def forward(e, Y=AT, X=2 * AT):
     layout = lw.Layout(si.precisions(64, {1: 0.5, 2: 0.5}), 128, device="cpu")
-    return lw.lib().lowra_lora_forward_epilogue(layout.ref, AT, AT, AT, AT, 4, AT, AT, 16, 2.0, None if e is None else ctypes.byref(e), Y, AT, 0, None)
+    return lw.lib().lowra_lora_forward_epilogue(layout.ref, AT, AT, AT, X, 4, AT, AT, 16, 2.0, None if e is None else ctypes.byref(e), Y, AT, 0, None)
 
 
 def test_forward():
@@ -36,6 +36,8 @@ def test_forward():
     for other in ("multiply_dev", "residual_dev"):
         assert forward(epilogue(**{other: AT + 64, "pre_dev": AT + 64})) == lw.LOWRA_ERR_SHAPE
     assert forward(epilogue(pre_dev=AT)) == lw.LOWRA_ERR_SHAPE
+    assert forward(epilogue(residual_dev=AT), X=AT) == lw.LOWRA_ERR_SHAPE and forward(epilogue(pre_dev=2 * AT)) == lw.LOWRA_ERR_SHAPE
+    assert forward(epilogue(residual_dev=2 * AT)) == lw.LOWRA_ERR_WORKSPACE and forward(epilogue(residual_dev=AT)) == lw.LOWRA_ERR_WORKSPACE
     assert forward(epilogue()) == lw.LOWRA_ERR_WORKSPACE           # everything else is in order
     assert lw.lib().lowra_lora_forward_batch_epilogue(None, None, 1, 4, 16, 2.0, AT, 0, None) == lw.LOWRA_ERR_NULL
 

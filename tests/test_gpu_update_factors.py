@@ -216,6 +216,9 @@ def test_refusals():
                          (dict(update=new(264, 64)[:, ::2]), "contiguous"), (dict(master_out=new(256, 32)), "master")):
         with pytest.raises(ValueError, match=says):
             run(**change)
+    for wrong in ((3.4, -4.7), [1.0, 2.0, 3.0, 4.0]):
+        with pytest.raises(ValueError, match="three"):
+            run(dict(coefficients=wrong))
     with pytest.raises(ValueError, match="no members"):
         lw.lowra_update_factors([], 0.02)
     with pytest.raises(ValueError, match="common"):
