@@ -4,7 +4,7 @@
 // bias's sums 51).  A thread takes eight neighbouring channels (16 bytes) of a row;
 // without a bias the elements are dealt out flat, with one a CTA takes 256 channels of a run of rows, sums them up in registers (fp32, before dZ is rounded),
 // its eight warps' sums through shared memory, and writes them down for a second kernel that adds up the runs in their order: no atomics, so repeated calls
-// agree bit for bit.  The second launch is left out where one run holds all rows.  (Up to eight runs as a cluster that adds up through distributed shared memory:
+// agree bit for bit.  The second launch is left out where one run holds all rows, as with up to 128 rows, which narrower CTAs take whole.  (Up to eight runs as a cluster that adds up through distributed shared memory:
 // no second launch, but 333 x 4096 with GELU 6.7 -> 7.1 us, 1001 x 13824 20.2 -> 27.2, whose clusters do not all find room at once.)
 #include "epilogue.cuh"
 
@@ -13,6 +13,7 @@ namespace lowra {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kCols = 32 * 8;
+constexpr int kNarrowThreads = 512, kNarrowCols = 8 * 8, kNarrowRows = 128;
 constexpr int kResident = 3;              // CTAs to an SM
 constexpr int kLeastRows = 16;            // of a run
 
@@ -90,38 +91,44 @@ __global__ void __launch_bounds__(kThreads, kResident) flat_kernel(const __grid_
     }
 }
 
-template <bool MULTIPLY>
-__global__ void __launch_bounds__(kThreads, kResident) rows_kernel(const __grid_constant__ BackwardParams P) {
+template <bool MULTIPLY, int THREADS, int COLS>
+__global__ void __launch_bounds__(THREADS, THREADS == kThreads ? kResident : 1) rows_kernel(const __grid_constant__ BackwardParams P) {
     constexpr int kRowsAtOnce = MULTIPLY ? 2 : 4;         // whose loads are under way together
-    __shared__ float shared[kWarps][kCols];
+    constexpr int kLanes = COLS / 8, kStep = THREADS / kLanes;      // lanes to a row, rows side by side
+    __shared__ float shared[THREADS / 32][COLS];
     pdl_enter();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = (int)blockIdx.x * kCols + lane * 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x % kLanes, n = (int)blockIdx.x * COLS + lane * 8;
     const int m_first = (int)blockIdx.y * P.rows, m_end = min(P.M, m_first + P.rows);
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-    for (int m = m_first + warp; n < P.N && m < m_end; m += kRowsAtOnce * kWarps) {
+    for (int m = m_first + (int)threadIdx.x / kLanes; n < P.N && m < m_end; m += kRowsAtOnce * kStep) {
         Vec8 v[kRowsAtOnce];
 #pragma unroll
         for (int u = 0; u < kRowsAtOnce; ++u)
-            if (m + u * kWarps < m_end) load<MULTIPLY>(P, (size_t)(m + u * kWarps) * P.N + n, v[u]);
+            if (m + u * kStep < m_end) load<MULTIPLY>(P, (size_t)(m + u * kStep) * P.N + n, v[u]);
 #pragma unroll
         for (int u = 0; u < kRowsAtOnce; ++u) {
-            if (m + u * kWarps >= m_end) break;
+            if (m + u * kStep >= m_end) break;
             float dz[8];
-            differentiate<MULTIPLY>(P, (size_t)(m + u * kWarps) * P.N + n, v[u], dz);
+            differentiate<MULTIPLY>(P, (size_t)(m + u * kStep) * P.N + n, v[u], dz);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += dz[i];
         }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) shared[warp][lane * 8 + i] = sum[i];
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int other = kLanes; other < 32; other *= 2) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], other);
+        if ((threadIdx.x & 31) < kLanes) shared[warp][lane * 8 + i] = sum[i];
+    }
     __syncthreads();
-    const int col = (int)blockIdx.x * kCols + (int)threadIdx.x;
+    const int col = (int)blockIdx.x * COLS + (int)threadIdx.x;
+    if (threadIdx.x >= COLS || col >= P.N) return;
     float total = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) total += shared[w][threadIdx.x];
-    if (col < P.N) P.sums[(size_t)blockIdx.y * P.N + col] = total;
+    for (int w = 0; w < THREADS / 32; ++w) total += shared[w][threadIdx.x];
+    P.sums[(size_t)blockIdx.y * P.N + col] = total;
 }
 
 // A CTA takes 32 channels, each of its eight warps an eighth of the runs.
@@ -142,9 +149,15 @@ __global__ void __launch_bounds__(kThreads) sum_runs_kernel(const float* sums, i
     out[n] = total;
 }
 
-// So many that their CTAs are all resident at once (one more wave of a few cost a third of the time: 4096 x 11008 gated 72 -> 100 us).
 constexpr int kMostRows = 1 << 30, kMostCols = 1 << 24;       // (rows and their steps are counted in 32 bits)
+// Few rows: CTAs of 64 channels (eight lanes to a row, 64 rows side by side) that hold all rows each, and one launch, as long as all of them fit at once.
+// 512, 4096 and 9472 channels with GELU: 24 rows 1.6, 1.6, 1.7 us against 2.9, 3.1, 3.6 in runs, 128 rows 2.5, 2.7, 3.2 against 3.1, 4.2, 4.7; past either bound
+// it loses sooner or later (10240 channels, 128 rows 5.2 against 4.8; 512 channels gated, 200 rows 3.9 against 3.6; 4096, 333 rows 7.1 against 6.1).
+bool takes_narrow(int M, int N) { return M <= kNarrowRows && N <= kNumSMs * kNarrowCols; }
+
+// So many that their CTAs are all resident at once (one more wave of a few cost a third of the time: 4096 x 11008 gated 72 -> 100 us).
 int runs_of(int M, int N) {
+    if (takes_narrow(M, N)) return 1;
     const int tiles = (N + kCols - 1) / kCols, wanted = kNumSMs * kResident / tiles, most = (M + kLeastRows - 1) / kLeastRows;
     return wanted < 1 ? 1 : wanted < most ? wanted : most;
 }
@@ -167,7 +180,7 @@ extern "C" lowra_status lowra_epilogue_backward(const uint16_t* dY_dev, const ui
     if (!aligned16(dY_dev) || !aligned16(pre_dev) || !aligned16(multiply_dev) || !aligned16(dZ_dev) || !aligned16(dmultiply_dev) || !aligned16(dbias_dev))
         return LOWRA_ERR_ALIGN;
     int runs = dbias_dev ? runs_of(M, N) : 0;
-    if (runs > 1 && (!workspace_dev || workspace_bytes < lowra_epilogue_workspace_bytes(M, N) || (reinterpret_cast<uintptr_t>(workspace_dev) & 255u) != 0))
+    if (runs > 0 && (!workspace_dev || workspace_bytes < lowra_epilogue_workspace_bytes(M, N) || (reinterpret_cast<uintptr_t>(workspace_dev) & 255u) != 0))
         return LOWRA_ERR_WORKSPACE;
     lowra_status st = check_device();
     if (st != LOWRA_OK) return st;
@@ -184,12 +197,16 @@ extern "C" lowra_status lowra_epilogue_backward(const uint16_t* dY_dev, const ui
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((unsigned)((N + kCols - 1) / kCols), (unsigned)runs, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
+    const bool narrow = takes_narrow(M, N);
+    const int cols = narrow ? kNarrowCols : kCols;
+    cfg.gridDim = dim3((unsigned)((N + cols - 1) / cols), (unsigned)runs, 1);
+    cfg.blockDim = dim3(narrow ? kNarrowThreads : kThreads, 1, 1);
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, multiply_dev ? rows_kernel<true> : rows_kernel<false>, P) != cudaSuccess) return LOWRA_ERR_CUDA;
+    const auto gated = narrow ? rows_kernel<true, kNarrowThreads, kNarrowCols> : rows_kernel<true, kThreads, kCols>;
+    const auto plain = narrow ? rows_kernel<false, kNarrowThreads, kNarrowCols> : rows_kernel<false, kThreads, kCols>;
+    if (cudaLaunchKernelEx(&cfg, multiply_dev ? gated : plain, P) != cudaSuccess) return LOWRA_ERR_CUDA;
     if (runs > 1 && launch_pdl(sum_runs_kernel, (unsigned)((N + 31) / 32), kThreads, stream, (const float*)P.sums, runs, N, dbias_dev) != cudaSuccess) return LOWRA_ERR_CUDA;
     return LOWRA_OK;
 }

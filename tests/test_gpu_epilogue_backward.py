@@ -46,6 +46,21 @@ def test_against_the_formula(M, N, activation):
             assert all(a is None or torch.equal(a, b) for a, b in zip(again, got))
 
 
+@pytest.mark.parametrize("M,N", [(2, 72), (63, 8), (65, 136), (127, 4104), (128, 9472), (129, 9472), (128, 9480)])
+def test_few_rows(M, N):
+    """On both sides of the bounds of the narrow CTAs, which hold all rows each."""
+    import paper_2502_08141_b200 as lw
+
+    test_against_the_formula(M, N, "silu")
+    dY, pre, mul = inputs(M, N)
+    whole = lw.lowra_epilogue_backward(dY, pre, "gelu", multiply=mul, want_bias=True)
+    if M <= 128 and N <= 9472:
+        assert lw.lowra_epilogue_workspace_bytes(M, N) == (4 * N + 255) // 256 * 256
+    place = dY.clone()
+    got = lw.lowra_epilogue_backward(place, pre, "gelu", multiply=mul, dZ=place, want_bias=True)
+    assert got[0].data_ptr() == place.data_ptr() and torch.equal(got[0], whole[0]) and torch.equal(got[2], whole[2])
+
+
 @pytest.mark.parametrize("activation", ACTIVATIONS)
 def test_against_differences(activation):
     import paper_2502_08141_b200 as lw
