@@ -428,7 +428,7 @@ lowra_status lowra_lora_backward_adapters_reuse(const uint16_t* X_dev, const uin
 
 /*
  * (No counterpart in the paper.)  A training step's last part: momentum and an update of the low-rank factors that Newton-Schulz products make orthogonal,
- * for the factors of a layer, or of several, in one call of three launches.  For every factor (A [K, r] or B [r, N]), all in fp32 or more:
+ * for the factors of a layer, or of several, in one call of one launch or three.  For every factor (A [K, r] or B [r, N]), all in fp32 or more:
  *     m' = momentum * m + g;     u = g + momentum * m' (nesterov) or m' (else);  without a momentum buffer u = g
  *     X_0 = u / (|u| + eps), |u| the Frobenius norm;     X <- a X + X (b G + c G^2), G = X^T X (of the side r), `steps` times
  *     w' = (1 - lr weight_decay) w - lr scale X;         weight = bf16(w')

@@ -4,7 +4,7 @@
 // A factor is L x r (A, "tall") or r x L (B): the short side is the rank, and every product above is one of r x r matrices with u.  All of them are
 // polynomials in S = u^T u (over the long side), which commute, so X_n = u Q with an r x r matrix Q: with alpha = 1 / (|u| + eps)^2, G_0 = alpha S,
 //     P_k = a + b G_k + c G_k^2,   G_{k+1} = G_k P_k^2,   Q = P_0 P_1 ... / (|u| + eps),   |u|^2 = trace S.
-// Three kernels: gram_kernel reads g and m, writes m', and forms parts of S; iterate_kernel adds them up and forms Q; apply_kernel forms u Q and writes
+// One kernel for a few short factors of small rank (one_kernel); else three: gram_kernel reads g and m, writes m', and forms parts of S; iterate_kernel adds them up and forms Q; apply_kernel forms u Q and writes
 // the weights.  u is read twice whatever the number of steps (the second time mostly from L2).
 // S holds the squares of u's singular values, so a value of 1e-3 |u|, which the iteration lifts to 0.5, is 1e-6 of S: in fp32 it would be off by a
 // percent.  S and everything of size r x r are therefore fp64, on the fp64 tensor instructions (m8n8k4; 24 TFLOP/s in gram_kernel); u and u Q are fp32.
@@ -329,6 +329,7 @@ __global__ void __launch_bounds__(kGramThreads, 1) gram_kernel(const __grid_cons
 // block as an operand (contraction indices 2 t and 2 t + 1, one for each of two instructions): blocks are stored as 32 pairs in the lanes' order, written and read
 // without conflicts, 16 bytes at a time.  The whole matrix, both triangles, up to rank 48, where one CTA does a factor; above that, where every block is written
 // into the shared memory of all CTAs of the cluster, the upper triangle, whose transposes are read as two single values.
+// (Stores counted on mbarriers, st.async, in place of the cluster's barriers: rank 64 4.1 -> 4.4 us a step, 128 15.0 -> 15.7; bulk copies 4.4 and 17.5.)
 __device__ __forceinline__ void st_cluster_f64x2(uint32_t at, double x, double y) {
     asm volatile("st.shared::cluster.v2.f64 [%0], {%1, %2};" ::"r"(at), "d"(x), "d"(y) : "memory");
 }
@@ -346,22 +347,16 @@ struct IterateShape {
     static constexpr size_t smem = (size_t)(three ? 3 : 4) * bytes + B * 8;
 };
 
-template <int NB, bool FEW>
-__global__ void __launch_bounds__(32 * IterateShape<NB, FEW>::warps) iterate_kernel(const __grid_constant__ UpdateParams P) {
-    using S = Shape<NB>;
-    using I = IterateShape<NB, FEW>;
+// For one factor: sums(block, s) gives this lane's two values of a block of S, out(row, column, value) takes Q.  memory: I::smem bytes; rank: of the CTA in its cluster.
+template <typename I, typename Sums, typename Out>
+__device__ __forceinline__ void iterate(const UpdateParams& P, unsigned char* memory, int rank, Sums sums, Out out) {
     constexpr int B = I::B, ctas = I::ctas;
-    extern __shared__ __align__(16) unsigned char update_smem[];
-    unsigned char* const G = update_smem;
+    unsigned char* const G = memory;
     unsigned char* const Pk = G + I::bytes;
     unsigned char* const Q = Pk + I::bytes;
     unsigned char* const M = I::three ? G : Q + I::bytes;
     double* trace = reinterpret_cast<double*>(Q + (I::three ? 1 : 2) * I::bytes);      // [B], of the diagonal blocks
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (behind the wait: apply_kernel reads what gram_kernel wrote before its own)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
-    const int f = (int)blockIdx.x / ctas, rank = (int)blockIdx.x % ctas;
-    const Factor& F = P.f[f];
     const int block = rank * I::warps + warp;
     const bool mine = block < I::tri;
     int bi = 0;
@@ -437,24 +432,9 @@ __global__ void __launch_bounds__(32 * IterateShape<NB, FEW>::warps) iterate_ker
     double unused[2];
     auto product = [&](const unsigned char* X, const unsigned char* Y, double (&v)[2]) { products(std::false_type(), X, X, Y, v, unused); };
     if (ctas > 1) ptx::cluster_sync();                            // (every CTA of the cluster runs: its shared memory may be written)
-    // ---- S, from its parts in the walkers' order
     double s[2] = {0.0, 0.0};                                     // this lane's values of G
     if (mine) {
-        const int walkers = (int)min(kWalkers, P.tiles), tiles = (F.L + S::TL - 1) / S::TL;
-        auto walker_of = [&](int tile) {                          // the one whose share holds the tile
-            int w = (int)((long long)tile * walkers / P.tiles);
-            while ((int)((long long)P.tiles * (w + 1) / walkers) <= tile) ++w;
-            while ((int)((long long)P.tiles * w / walkers) > tile) --w;
-            return w;
-        };
-        const int w0 = walker_of(F.tile0), w1 = walker_of(F.tile0 + tiles - 1);
-        const double2* from = reinterpret_cast<const double2*>(P.sums) + (size_t)block * 32 + lane;
-#pragma unroll 8
-        for (int w = w0; w <= w1; ++w) {
-            const double2 x = __ldcg(from + (size_t)(w + f) * S::tri * 32);
-            s[0] += x.x;
-            s[1] += x.y;
-        }
+        sums(block, s);
         if (bi == bj) {
             double d = g == 2 * t4 ? s[0] : g == 2 * t4 + 1 ? s[1] : 0.0;
 #pragma unroll
@@ -507,15 +487,45 @@ __global__ void __launch_bounds__(32 * IterateShape<NB, FEW>::warps) iterate_ker
         alpha = 1.0;
     }
     if (mine) {
-        float* out = P.Q + (size_t)f * S::r * S::r;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int row = bi * 8 + g, col = bj * 8 + 2 * t4 + i;
             const float v = (float)(q[i] / norm);
-            out[row * S::r + col] = v;
-            if (bi != bj) out[col * S::r + row] = v;
+            out(row, col, v);
+            if (bi != bj) out(col, row, v);
         }
     }
+}
+
+template <int NB, bool FEW>
+__global__ void __launch_bounds__(32 * IterateShape<NB, FEW>::warps) iterate_kernel(const __grid_constant__ UpdateParams P) {
+    using S = Shape<NB>;
+    using I = IterateShape<NB, FEW>;
+    extern __shared__ __align__(16) unsigned char update_smem[];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (behind the wait: apply_kernel reads what gram_kernel wrote before its own)
+    const int f = (int)blockIdx.x / I::ctas, lane = threadIdx.x & 31;
+    const Factor& F = P.f[f];
+    // S, from its parts in the walkers' order
+    auto sums = [&](int block, double (&s)[2]) {
+        const int walkers = (int)min(kWalkers, P.tiles), tiles = (F.L + S::TL - 1) / S::TL;
+        auto walker_of = [&](int tile) {                          // the one whose share holds the tile
+            int w = (int)((long long)tile * walkers / P.tiles);
+            while ((int)((long long)P.tiles * (w + 1) / walkers) <= tile) ++w;
+            while ((int)((long long)P.tiles * w / walkers) > tile) --w;
+            return w;
+        };
+        const int w0 = walker_of(F.tile0), w1 = walker_of(F.tile0 + tiles - 1);
+        const double2* from = reinterpret_cast<const double2*>(P.sums) + (size_t)block * 32 + lane;
+#pragma unroll 8
+        for (int w = w0; w <= w1; ++w) {
+            const double2 x = __ldcg(from + (size_t)(w + f) * S::tri * 32);
+            s[0] += x.x;
+            s[1] += x.y;
+        }
+    };
+    float* const Q = P.Q + (size_t)f * S::r * S::r;
+    iterate<I>(P, update_smem, (int)blockIdx.x % I::ctas, sums, [&](int row, int col, float v) { Q[row * S::r + col] = v; });
 }
 
 // ------------------------------------------------------------------------------------------------ u Q, and the weights
@@ -696,6 +706,191 @@ __global__ void __launch_bounds__(kApplyThreads, 1) apply_kernel(const __grid_co
     }
 }
 
+// ------------------------------------------------------------------------------------------------ all of it in one launch
+// For up to 14 short factors of rank 16 or 32: a cluster of eight CTAs takes a factor, a CTA an eighth of the long side, whose u stays in its shared memory.  Each forms its
+// part of S, sends it to all others, adds the eight up in their order, and goes through the iteration by itself (all get the same Q), then forms its part of u Q.
+// What bounds it is the chain of dependent steps.  Five steps, 1 / 2 / 6 / 14 factors, against the three kernels, us:
+//     512 x 16    6.4 /  6.4 /  6.5 /  6.5   against   9.2 / 10.0 / 10.7 / 10.6        512 x 32   11.9 / 12.0 / 12.3 / 12.3   against  14.6 / 15.7 / 15.9 / 15.8
+//     4096 x 16   9.2 /  9.3 /  9.4 /  9.7   against  10.4 / 10.9 / 11.6 / 16.7       2048 x 32   15.4 / 15.5 / 15.8 / 16.2   against  15.5 / 15.9 / 16.5 / 21.8
+//     8192 x 16  13.3 / 13.2 / 13.4 / 15.5   against  11.6 / 12.2 / 15.8 / 22.4
+// and a call costs the host 5.5 us instead of 11.5.  Longer ones lose.  More factors: 16 clusters do not find room at once (64 x 16: 10.6 against 9.8).
+constexpr int kOneCtas = 8, kOneFactors = 14, kMostOne = 2;             // CTAs to a factor; factors; rank / 16
+constexpr int kOneRows = 1024;                                          // of the long side to a CTA, times (rank / 16)^2
+template <int NB>
+struct OneShape {
+    using I = IterateShape<NB, true>;
+    static constexpr int r = 16 * NB, tri = I::tri, warps = 16, threads = 32 * warps;
+    static constexpr int tall_pitch = r + 8;                      // u as in gram_kernel: tall [l][c], wide [c][l]
+    static constexpr size_t part = (size_t)tri * 512, joined = warps * part, first = joined > (I::smem + 15) / 16 * 16 ? joined : (I::smem + 15) / 16 * 16;
+    static constexpr size_t fixed = first + kOneCtas * part + r * r * 4;       // the warps' sums, then the iteration's matrices; parts of S; Q; u follows
+    static int wide_pitch(int rows) { return (rows + 31) / 32 * 32 + 4; }
+    static size_t bytes(int rows) { return fixed + (size_t)(rows * tall_pitch > r * wide_pitch(rows) ? rows * tall_pitch : r * wide_pitch(rows)) * 4; }
+    static_assert(I::ctas == 1, "a CTA goes through the iteration by itself");
+};
+__host__ __device__ inline int one_rows(int L) { return (L / 8 + kOneCtas - 1) / kOneCtas * 8; }      // of a CTA
+
+template <int NB>
+__global__ void __launch_bounds__(OneShape<NB>::threads, 1) one_kernel(const __grid_constant__ UpdateParams P) {
+    using O = OneShape<NB>;
+    constexpr int r = O::r, blocks = 2 * NB, kAtOnce = 4;
+    extern __shared__ __align__(16) unsigned char update_smem[];
+    double2* const joined = reinterpret_cast<double2*>(update_smem);
+    double2* const parts = reinterpret_cast<double2*>(update_smem + O::first);
+    float* const Q = reinterpret_cast<float*>(update_smem + O::first + kOneCtas * O::part);
+    float* const u = Q + r * r;
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    pdl_enter();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    const int f = (int)blockIdx.x / kOneCtas, rank = (int)blockIdx.x % kOneCtas;
+    const Factor& F = P.f[f];
+    const int most = one_rows(F.L), l0 = rank * most, rows = max(0, min(most, F.L - l0)), wide_pitch = (most + 31) / 32 * 32 + 4;
+    const int quads = rows * r / 4, wide_quads = max(rows / 4, 1);         // quads of four neighbours in memory; of a rank's row
+    // ---- u, into shared memory
+    for (int first = (int)threadIdx.x; first < quads; first += kAtOnce * O::threads) {
+        Raw raw[kAtOnce];
+        size_t at[kAtOnce];
+        int to[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int q = first + i * O::threads;
+            if (F.tall) {
+                at[i] = (size_t)l0 * r + (size_t)q * 4;
+                to[i] = q / (r / 4) * O::tall_pitch + q % (r / 4) * 4;
+            } else {
+                const int c = q / wide_quads, l = (q - c * wide_quads) * 4;
+                at[i] = (size_t)c * F.L + (l0 + l);
+                to[i] = c * wide_pitch + l;
+            }
+            raw[i].g = make_uint4(0u, 0u, 0u, 0u);
+            raw[i].m = zero4();
+            if (q >= quads) continue;
+            if (F.grad_fp32) raw[i].g = *reinterpret_cast<const uint4*>(static_cast<const float*>(F.grad) + at[i]);
+            else {
+                const uint2 two = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(F.grad) + at[i]);
+                raw[i].g.x = two.x;
+                raw[i].g.y = two.y;
+            }
+            if (F.momentum != nullptr) raw[i].m = *reinterpret_cast<const float4*>(F.momentum + at[i]);
+            if (F.master != nullptr) asm volatile("prefetch.global.L2 [%0];" ::"l"(F.master + at[i]));
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (first + i * O::threads >= quads) break;
+            const float4 grad = grad_quad(F, raw[i].g);
+            float4 x = grad;
+            if (F.momentum != nullptr) {
+                const float4 m = axpy2(P.mu, raw[i].m, grad);
+                *reinterpret_cast<float4*>(F.momentum_out + at[i]) = m;
+                x = P.nesterov ? axpy2(P.mu, m, grad) : m;
+            }
+            *reinterpret_cast<float4*>(u + to[i]) = x;
+        }
+    }
+    __syncthreads();
+    // ---- a warp's part of S, the CTA's, and everybody's
+    {
+        double acc[O::tri][2];
+#pragma unroll
+        for (int b = 0; b < O::tri; ++b) acc[b][0] = acc[b][1] = 0.0;
+        const int sl = F.tall ? O::tall_pitch : 1, sc = F.tall ? 1 : wide_pitch;
+        const float* at = u + t4 * sl + g * sc;
+#pragma unroll 2
+        for (int l = warp * 4; l < rows; l += 4 * O::warps) {
+            double x[blocks];
+#pragma unroll
+            for (int i = 0; i < blocks; ++i) x[i] = (double)at[l * sl + i * 8 * sc];
+            int b = 0;
+#pragma unroll
+            for (int i = 0; i < blocks; ++i) {
+#pragma unroll
+                for (int j = i; j < blocks; ++j) dmma(acc[b++], x[i], x[j]);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < O::tri; ++b) joined[(b * O::warps + warp) * 32 + lane] = make_double2(acc[b][0], acc[b][1]);
+    }
+    __syncthreads();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");           // (every CTA of the cluster runs: its shared memory may be written)
+    for (int b = warp; b < O::tri; b += O::warps) {
+        double2 v = joined[b * O::warps * 32 + lane];
+#pragma unroll
+        for (int w = 1; w < O::warps; ++w) {
+            const double2 x = joined[(b * O::warps + w) * 32 + lane];
+            v.x += x.x;
+            v.y += x.y;
+        }
+        const uint32_t to = ptx::smem_u32(parts + (rank * O::tri + b) * 32 + lane);
+#pragma unroll
+        for (int i = 0; i < kOneCtas; ++i) st_cluster_f64x2(ptx::map_to_cta(to, (uint32_t)i), v.x, v.y);
+    }
+    ptx::cluster_sync();
+    auto sums = [&](int block, double (&s)[2]) {
+#pragma unroll
+        for (int i = 0; i < kOneCtas; ++i) {
+            const double2 x = parts[(i * O::tri + block) * 32 + lane];
+            s[0] += x.x;
+            s[1] += x.y;
+        }
+    };
+    // ---- u Q: a thread forms four ranks of four of the long side (tall: a quarter of the rows apart, wide: neighbours); its first weights are asked for before the iteration
+    const int runs = rows / 4, items = runs * (r / 4);
+    const size_t step = F.tall ? (size_t)runs * r : (size_t)F.L;
+    int cg = 0, lg = 0;
+    size_t place = 0;
+    float4 w[4];
+    auto ask = [&](int item) {
+        cg = F.tall ? item % (r / 4) : item / wide_quads;
+        lg = F.tall ? item / (r / 4) : item - cg * wide_quads;
+        place = F.tall ? (size_t)(l0 + lg) * r + cg * 4 : (size_t)(cg * 4) * F.L + (l0 + lg * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = F.master != nullptr && item < items ? *reinterpret_cast<const float4*>(F.master + place + i * step) : zero4();
+    };
+    ask((int)threadIdx.x);
+    iterate<typename O::I>(P, update_smem, 0, sums, [&](int row, int col, float v) { Q[row * r + col] = v; });
+    __syncthreads();
+    for (int item = (int)threadIdx.x; item < items; item += O::threads) {
+        if (item >= O::threads) ask(item);
+        float4 acc[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = zero4();
+        if (F.tall) {
+#pragma unroll 2
+            for (int j = 0; j < r; j += 4) {
+                float4 q[4], x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) q[k] = *reinterpret_cast<const float4*>(Q + (j + k) * r + cg * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(u + (lg + i * runs) * O::tall_pitch + j);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[i] = axpy2(k == 0 ? x[i].x : k == 1 ? x[i].y : k == 2 ? x[i].z : x[i].w, q[k], acc[i]);
+                }
+            }
+        } else {
+#pragma unroll 4
+            for (int j = 0; j < r; ++j) {
+                const float4 q = *reinterpret_cast<const float4*>(Q + j * r + cg * 4), x = *reinterpret_cast<const float4*>(u + j * wide_pitch + lg * 4);
+                acc[0] = axpy2(q.x, x, acc[0]);
+                acc[1] = axpy2(q.y, x, acc[1]);
+                acc[2] = axpy2(q.z, x, acc[2]);
+                acc[3] = axpy2(q.w, x, acc[3]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const size_t at = place + i * step;
+            const float4 x = acc[i];
+            if (F.update != nullptr) *reinterpret_cast<float4*>(F.update + at) = x;
+            if (F.master == nullptr) continue;
+            const float4 n = make_float4(fmaf(-F.rate, x.x, P.decay * w[i].x), fmaf(-F.rate, x.y, P.decay * w[i].y), fmaf(-F.rate, x.z, P.decay * w[i].z),
+                                         fmaf(-F.rate, x.w, P.decay * w[i].w));
+            *reinterpret_cast<float4*>(F.master_out + at) = n;
+            if (F.weight != nullptr) *reinterpret_cast<uint2*>(F.weight + at) = make_uint2(pack_bf16x2(n.x, n.y), pack_bf16x2(n.z, n.w));
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ host
 template <int NB>
 int tiles_of(int L) { return (L + Shape<NB>::TL - 1) / Shape<NB>::TL; }
@@ -704,7 +899,39 @@ template <int NB>
 size_t sums_bytes(int tiles, int count) { return (size_t)((tiles < kWalkers ? tiles : kWalkers) + count) * Shape<NB>::tri * 512; }
 
 template <int NB>
+bool takes_one(const UpdateParams& P, int* rows) {
+    if (P.count > kOneFactors) return false;
+    *rows = 0;
+    for (int i = 0; i < P.count; ++i) *rows = max(*rows, one_rows(P.f[i].L));
+    return *rows * NB * NB <= kOneRows;
+}
+
+template <int NB>
+lowra_status launch_one(const UpdateParams& P, int rows, cudaStream_t stream) {
+    static SmemLimit limit = {};
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kOneCtas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    cfg.gridDim = dim3((unsigned)(P.count * kOneCtas), 1, 1);
+    cfg.blockDim = dim3(OneShape<NB>::threads, 1, 1);
+    cfg.dynamicSmemBytes = OneShape<NB>::bytes(rows);
+    if (ensure_smem_limit(reinterpret_cast<const void*>(one_kernel<NB>), OneShape<NB>::bytes(kOneRows / NB / NB), &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, one_kernel<NB>, P) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
+}
+
+template <int NB>
 lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream) {
+    if constexpr (NB <= kMostOne) {
+        int rows = 0;
+        if (takes_one<NB>(P, &rows)) return launch_one<NB>(P, rows, stream);
+    }
     using S = Shape<NB>;
     using A = ApplyShape<NB>;
     P.tiles = 0;

@@ -101,6 +101,46 @@ def test_long_factors(r, length):
     check(make([(length, r), (r, length)], r), r)
 
 
+@pytest.mark.parametrize("grad", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("r,longest", [(16, 8192), (32, 2048)])
+def test_both_sides_of_one_launch(r, longest, grad):
+    """Short factors of small rank go through one kernel: its longest, the next length, its most factors, one more, and lengths that leave CTAs of a cluster without rows."""
+    check(make([(longest, r), (r, longest)], r, grad), r)
+    check(make([(longest + 8, r), (r, longest + 8)], r, grad), r)
+    shapes = [(8 * (1 + 5 * i), r) if i % 2 else (r, 8 * (1 + 9 * i)) for i in range(15)]
+    check(make(shapes[:14], r, grad), r)
+    check(make(shapes, r, grad), r)
+    members = make([(264, r), (r, 520), (r, 72)], r, grad)
+    members[0]["momentum"] = members[2]["momentum"] = None
+    check(members, r, dict(nesterov=False, steps=3))
+
+
+@pytest.mark.parametrize("r", [16, 32])
+def test_one_launch_in_a_graph_and_in_place(r):
+    import paper_2502_08141_b200 as lw
+
+    start = make([(520, r), (r, 1032), (8, r)], r)
+    copy = lambda: [{k: v.clone() if torch.is_tensor(v) else v for k, v in m.items()} for m in start]
+    eager, replayed = copy(), copy()
+    lw.lowra_update_factors(replayed, 0.02, rank=r)          # loads the kernel
+    for m, s in zip(replayed, start):
+        for k, v in s.items():
+            if torch.is_tensor(v):
+                m[k].copy_(v)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lw.lowra_update_factors(replayed, 0.02, rank=r)
+    for _ in range(3):
+        graph.replay()
+        lw.lowra_update_factors(eager, 0.02, rank=r)
+    torch.cuda.synchronize()
+    for a, b in zip(eager, replayed):
+        for k, v in a.items():
+            if torch.is_tensor(v):
+                assert torch.equal(v, b[k]), k
+
+
 @pytest.mark.parametrize("steps,coefficients", [(1, COEFFICIENTS), (2, COEFFICIENTS), (3, (1.5, -0.5, 0.0)), (9, (1.875, -1.25, 0.375))])
 def test_steps_and_coefficients(steps, coefficients):
     check(make([(520, 48), (48, 264)], 48, fall=2.0), 48, dict(steps=steps, coefficients=coefficients))
