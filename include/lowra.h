@@ -445,7 +445,7 @@ lowra_status lowra_lora_backward_adapters_reuse(const uint16_t* X_dev, const uin
  *   workspace_dev: >= lowra_update_workspace_bytes(members_host, count, r) bytes (rows and cols are read), 256-byte aligned, contents overwritten
  * A factor whose u holds a NaN or an infinity gets NaN; the others are not touched by it.  Results do not depend on the run (no atomics), but on which
  * factors share a call, by roundings of fp64.
- * Errors: r not in {16, 32, ..., 128}, shapes, count or steps out of range -> LOWRA_ERR_SHAPE; LOWRA_ERR_NULL (an array without its partner too),
+ * Errors: r not in {16, 32, ..., 128}, shapes, count or steps out of range, two members with one output -> LOWRA_ERR_SHAPE; LOWRA_ERR_NULL (an array without its partner too),
  * LOWRA_ERR_ALIGN, LOWRA_ERR_WORKSPACE as elsewhere.
  */
 #define LOWRA_MAX_FACTORS 64

@@ -1051,6 +1051,14 @@ extern "C" lowra_status lowra_update_factors(const lowra_factor* members_host, i
         P.f[i] = Factor{m.grad_dev, m.momentum_dev, m.momentum_out_dev, m.master_dev, m.master_out_dev, m.weight_dev, m.update_dev, tall ? m.rows : m.cols,
                         (float)(step_host->lr * m.scale), 0, (uint8_t)tall, (uint8_t)(m.grad_fp32 != 0)};
     }
+    // (a factor named twice would be written by two at once)
+    const auto same = [](const void* p, const void* q) { return p != nullptr && p == q; };
+    for (int i = 1; i < count; ++i) {
+        const Factor& F = P.f[i];
+        for (int j = 0; j < i; ++j)
+            if (same(F.momentum_out, P.f[j].momentum_out) || same(F.master_out, P.f[j].master_out) || same(F.weight, P.f[j].weight) || same(F.update, P.f[j].update))
+                return LOWRA_ERR_SHAPE;
+    }
     if (workspace_bytes < lowra_update_workspace_bytes(members_host, count, r) || (reinterpret_cast<uintptr_t>(workspace_dev) & 255u) != 0) return LOWRA_ERR_WORKSPACE;
     if ((st = check_device()) != LOWRA_OK) return st;
     cudaStream_t stream = (cudaStream_t)stream_v;

@@ -72,6 +72,7 @@ def test_update():
     for bad in (dict(with_step=False), dict(workspace=None), dict(grad_dev=None), dict(momentum_dev=None), dict(momentum_out_dev=None), dict(master_out_dev=None),
                 dict(master_dev=None, master_out_dev=None), dict(master_dev=None, master_out_dev=None, update_dev=AT, weight_dev=AT)):
         assert call(**bad) == lw.LOWRA_ERR_NULL, bad
+    assert call(count=2) == lw.LOWRA_ERR_SHAPE                     # a factor named twice
     for name in ("grad_dev", "momentum_dev", "momentum_out_dev", "master_dev", "master_out_dev", "weight_dev", "update_dev"):
         assert call(**{name: AT + 8}) == lw.LOWRA_ERR_ALIGN, name
     assert call() == lw.LOWRA_ERR_WORKSPACE
