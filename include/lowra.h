@@ -325,6 +325,7 @@ lowra_status lowra_lora_forward_adapters(const lowra_layout* layout, const uint8
  * (No counterpart in the paper.)  The layer as it stands in a model: what follows the product is applied to its fp32 sums, in the kernel that forms them.
  *     Z = X . deq(Wq)^T + s * (X . A) . B + bias;    H = act(Z);    Y = H * multiply + residual
  * Everything in fp32; Y is rounded to bf16 once, and so is the copy of Z that lowra_epilogue_backward reads.
+ * (A Z of +infinity stays what it is through every activation; -infinity gives 0 through relu and NaN, the product of an infinity and a zero, through the others.)
  *   bias_dev      [N], bf16 (bias_bf16 != 0) or fp32, or NULL
  *   activation    lowra_activation
  *   multiply_dev  bf16 [M, N], or NULL: the other factor of a gated layer (the up projection's output, for a gate with SiLU)
