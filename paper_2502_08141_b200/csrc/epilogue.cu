@@ -28,11 +28,19 @@ struct Vec8 {
     uint4 dY, z, m;
 };
 
+// Read once, and not as read-only memory (ld_stream_v4): an output may be one of the inputs, and while a thread writes only what it has read itself, its
+// neighbours' values lie in the same sectors.  (Nothing comes before a load: what a thread reads it has not written.)
+__device__ __forceinline__ uint4 ld_once_v4(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
 template <bool MULTIPLY>
 __device__ __forceinline__ void load(const BackwardParams& P, size_t at, Vec8& v) {
-    v.dY = ld_stream_v4(P.dY + at);
-    if (P.pre != nullptr) v.z = ld_stream_v4(P.pre + at);
-    if (MULTIPLY) v.m = ld_stream_v4(P.multiply + at);
+    v.dY = ld_once_v4(P.dY + at);
+    if (P.pre != nullptr) v.z = ld_once_v4(P.pre + at);
+    if (MULTIPLY) v.m = ld_once_v4(P.multiply + at);
 }
 
 // Eight elements: dZ, returned in fp32 too, and dmultiply.
