@@ -141,15 +141,47 @@ struct MemberArgs {
     Epilogue epilogue;     // in the calls that have one
 };
 
+// An array as a call touches it.  Two of them are in each other's way where they share a byte.
+struct Span {
+    const void* at;
+    size_t bytes;
+};
+bool overlap(Span a, Span b) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a.at), q = reinterpret_cast<uintptr_t>(b.at);
+    return p != 0 && q != 0 && (p < q ? q - p < a.bytes : p - q < b.bytes);
+}
+
+// What a member with an epilogue reads and writes of its tokens.  (No extent without a layout or tokens: such a call is refused elsewhere.)
+struct MemberSpans {
+    Span X, Y, pre, multiply, residual;
+    MemberSpans(const lowra_layout* layout, int32_t M, const uint16_t* X_, const uint16_t* Y_, const lowra_epilogue& e) {
+        const size_t rows = layout != nullptr && M > 0 ? (size_t)M * 2 : 0, out = layout != nullptr ? rows * (size_t)layout->N : 0;
+        X = Span{X_, layout != nullptr ? rows * (size_t)layout->K : 0};
+        Y = Span{Y_, out};
+        pre = Span{e.pre_dev, out};
+        multiply = Span{e.multiply_dev, out};
+        residual = Span{e.residual_dev, out};
+    }
+    // Y may be the second factor or the residual, element for element; X may not change under the product, nor the others behind the copy of Z.
+    bool clash() const {
+        return overlap(Y, X) || overlap(pre, X) || overlap(pre, Y) || overlap(pre, multiply) || overlap(pre, residual) || (Y.at != multiply.at && overlap(Y, multiply)) ||
+               (Y.at != residual.at && overlap(Y, residual));
+    }
+    // Members of one launch run side by side: what this one writes is nothing that the other reads or writes.
+    bool writes_into(const MemberSpans& o) const {
+        for (const Span& w : {Y, pre})
+            for (const Span& x : {o.X, o.Y, o.pre, o.multiply, o.residual})
+                if (overlap(w, x)) return true;
+        return false;
+    }
+};
+
 // The caller's description of what stands behind a product, checked.
-lowra_status take_epilogue(const lowra_epilogue* e, const uint16_t* X, const uint16_t* Y, Epilogue* out) {
+lowra_status take_epilogue(const lowra_epilogue* e, const lowra_layout* layout, int32_t M, const uint16_t* X, const uint16_t* Y, Epilogue* out) {
     if (!e) return LOWRA_ERR_NULL;
     if (e->activation < LOWRA_ACT_NONE || e->activation > LOWRA_ACT_SILU) return LOWRA_ERR_SHAPE;
-    // (a block's input that is its residual as well: added to in place it would change under the product)
-    if (X && (X == Y || X == e->pre_dev)) return LOWRA_ERR_SHAPE;
-    // (the copy of Z is written before the other arrays are read)
-    if (e->pre_dev && (e->pre_dev == Y || e->pre_dev == e->multiply_dev || e->pre_dev == e->residual_dev)) return LOWRA_ERR_SHAPE;
     if (!aligned16(e->bias_dev) || !aligned16(e->multiply_dev) || !aligned16(e->residual_dev) || !aligned16(e->pre_dev)) return LOWRA_ERR_ALIGN;
+    if (MemberSpans(layout, M, X, Y, *e).clash()) return LOWRA_ERR_SHAPE;
     *out = Epilogue{e->bias_dev, e->multiply_dev, e->residual_dev, e->pre_dev, e->activation, e->bias_bf16 != 0 ? 1 : 0};
     return LOWRA_OK;
 }
@@ -553,8 +585,13 @@ lowra_status run_batch(bool backward, const lowra_member* members, const lowra_e
         const lowra_member& m = members[i];
         mem[i] = MemberArgs{m.layout, m.packed_dev, m.absmax_dev, m.maps_dev, m.act_dev, m.A_dev, m.B_dev, m.out_dev, M, {}};
         if (epilogues != nullptr) {
-            const lowra_status st = take_epilogue(&epilogues[i], m.act_dev, m.out_dev, &mem[i].epilogue);
+            const lowra_status st = take_epilogue(&epilogues[i], m.layout, M, m.act_dev, m.out_dev, &mem[i].epilogue);
             if (st != LOWRA_OK) return st;
+            const MemberSpans own(m.layout, M, m.act_dev, m.out_dev, epilogues[i]);
+            for (int j = 0; j < i; ++j) {
+                const MemberSpans before(members[j].layout, M, members[j].act_dev, members[j].out_dev, epilogues[j]);
+                if (own.writes_into(before) || before.writes_into(own)) return LOWRA_ERR_SHAPE;
+            }
         }
         if (m.layout != nullptr && m.layout->deal_dev == nullptr) return LOWRA_ERR_NULL;   // also for a batch of one
     }
@@ -586,7 +623,7 @@ extern "C" lowra_status lowra_lora_forward_epilogue(const lowra_layout* layout, 
                                                     void* stream) {
     using namespace lowra;
     MemberArgs m = {layout, packed_dev, absmax_dev, maps_dev, X_dev, A_dev, B_dev, Y_dev, M, {}};
-    const lowra_status st = take_epilogue(epilogue_host, X_dev, Y_dev, &m.epilogue);
+    const lowra_status st = take_epilogue(epilogue_host, layout, M, X_dev, Y_dev, &m.epilogue);
     if (st != LOWRA_OK) return st;
     return run_members(false, &m, 1, r, s, workspace_dev, workspace_bytes, stream, true, true, true);
 }
@@ -676,7 +713,7 @@ extern "C" lowra_status lowra_lora_forward_adapters_epilogue(const lowra_layout*
                                                              float s, const lowra_epilogue* epilogue_host, uint16_t* Y_dev, void* workspace_dev,
                                                              size_t workspace_bytes, void* stream) {
     lowra::Epilogue epilogue;
-    const lowra_status st = lowra::take_epilogue(epilogue_host, X_dev, Y_dev, &epilogue);
+    const lowra_status st = lowra::take_epilogue(epilogue_host, layout, M, X_dev, Y_dev, &epilogue);
     if (st != LOWRA_OK) return st;
     return lowra::run_adapter_groups(layout, packed_dev, absmax_dev, maps_dev, n_adapters, X_dev, M, group_start_host, A_dev, B_dev, r, s, &epilogue, Y_dev,
                                      workspace_dev, workspace_bytes, stream);
