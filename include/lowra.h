@@ -377,7 +377,7 @@ lowra_status lowra_lora_forward_adapters_epilogue(const lowra_layout* layout, co
  *   Outputs may be inputs themselves (dZ in the place of dY or pre, dmultiply in that of multiply), else they overlap nothing.
  *   workspace_dev: >= lowra_epilogue_workspace_bytes(M, N) bytes, 256-byte aligned, contents overwritten; used for dbias only.
  * Errors: dY missing, no output, pre or multiply missing where it is needed -> LOWRA_ERR_NULL; M < 1 or > 2^30, N % 8 != 0 or > 2^24, an activation that
- * is none, dZ and dmultiply in one place -> LOWRA_ERR_SHAPE; LOWRA_ERR_ALIGN, LOWRA_ERR_WORKSPACE as elsewhere.
+ * is none, an output that shares memory with another or with a part of an input -> LOWRA_ERR_SHAPE; LOWRA_ERR_ALIGN, LOWRA_ERR_WORKSPACE as elsewhere.
  */
 size_t lowra_epilogue_workspace_bytes(int32_t M, int32_t N);
 lowra_status lowra_epilogue_backward(const uint16_t* dY_dev, const uint16_t* pre_dev, const uint16_t* multiply_dev, int32_t M, int32_t N, int32_t activation,

@@ -190,6 +190,17 @@ extern "C" lowra_status lowra_epilogue_backward(const uint16_t* dY_dev, const ui
     int runs = dbias_dev ? runs_of(M, N) : 0;
     if (runs > 0 && (!workspace_dev || workspace_bytes < lowra_epilogue_workspace_bytes(M, N) || (reinterpret_cast<uintptr_t>(workspace_dev) & 255u) != 0))
         return LOWRA_ERR_WORKSPACE;
+    // An output may be an input, element for element; else it shares memory with nothing.
+    const size_t rows = (size_t)M * (size_t)N * 2;
+    const Span read[3] = {{dY_dev, rows}, {pre_dev, rows}, {multiply_dev, rows}}, written[2] = {{dZ_dev, rows}, {dmultiply_dev, rows}}, dbias = {dbias_dev, (size_t)N * 4};
+    for (const Span& w : written) {
+        for (const Span& x : read)
+            if (w.at != x.at && overlap(w, x)) return LOWRA_ERR_SHAPE;
+        if (overlap(w, dbias)) return LOWRA_ERR_SHAPE;
+    }
+    for (const Span& x : read)
+        if (overlap(x, dbias)) return LOWRA_ERR_SHAPE;
+    if (overlap(written[0], written[1])) return LOWRA_ERR_SHAPE;
     lowra_status st = check_device();
     if (st != LOWRA_OK) return st;
     cudaStream_t stream = (cudaStream_t)stream_v;

@@ -141,16 +141,6 @@ struct MemberArgs {
     Epilogue epilogue;     // in the calls that have one
 };
 
-// An array as a call touches it.  Two of them are in each other's way where they share a byte.
-struct Span {
-    const void* at;
-    size_t bytes;
-};
-bool overlap(Span a, Span b) {
-    const uintptr_t p = reinterpret_cast<uintptr_t>(a.at), q = reinterpret_cast<uintptr_t>(b.at);
-    return p != 0 && q != 0 && (p < q ? q - p < a.bytes : p - q < b.bytes);
-}
-
 // What a member with an epilogue reads and writes of its tokens.  (No extent without a layout or tokens: such a call is refused elsewhere.)
 struct MemberSpans {
     Span X, Y, pre, multiply, residual;

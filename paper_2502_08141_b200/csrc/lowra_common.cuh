@@ -37,6 +37,16 @@ RowLayout make_row_layout(const lowra_layout* L);
 
 static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// An array as a call touches it.  Two of them are in each other's way where they share a byte.
+struct Span {
+    const void* at;
+    size_t bytes;
+};
+static inline bool overlap(Span a, Span b) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a.at), q = reinterpret_cast<uintptr_t>(b.at);
+    return p != 0 && q != 0 && (p < q ? q - p < a.bytes : p - q < b.bytes);
+}
+
 // -------------------------------------------------------------------------------------------
 // programmatic dependent launch: every kernel of the library lets its successor in the stream start launching
 // right away (so the successor's launch latency and set-up overlap this kernel) and itself waits, before it

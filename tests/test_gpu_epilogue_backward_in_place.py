@@ -45,3 +45,19 @@ def test_captured():
         dbias.zero_()
         graph.replay()
         assert all(torch.equal(x, y) for x, y in zip((place, other, dbias), want))
+
+
+def test_side_by_side():
+    """All arrays in one piece of memory, one directly behind the other, are in nobody's way."""
+    import paper_2502_08141_b200 as lw
+
+    M, N = 37, 264
+    dY, pre, multiply = inputs(M, N, seed=2)
+    want = lw.lowra_epilogue_backward(dY, pre, "silu", multiply=multiply, want_bias=True)
+    block = torch.zeros(5 * M * N + 2 * N, dtype=torch.bfloat16, device="cuda")
+    rows = [block[i * M * N:(i + 1) * M * N].view(M, N) for i in range(5)]
+    dbias = block[5 * M * N:].view(torch.float32)
+    for to, t in zip(rows[1::2] + rows[4:], (dY, pre, multiply)):
+        to.copy_(t)
+    got = lw.lowra_epilogue_backward(rows[1], rows[3], "silu", multiply=rows[4], dZ=rows[0], dmultiply=rows[2], dbias=dbias)
+    assert all(torch.equal(x, y) for x, y in zip(got, want)) and torch.equal(rows[1], dY) and torch.equal(rows[3], pre) and torch.equal(rows[4], multiply)
