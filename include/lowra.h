@@ -442,12 +442,12 @@ lowra_status lowra_lora_backward_adapters_reuse(const uint16_t* X_dev, const uin
  *     weight_dev         bf16, or NULL: the factor as the products above take it; only with a master                          (out)
  *     update_dev         fp32 X, or NULL; at least one of master and update                                                   (out)
  *     scale              factor of lr for this member (for instance sqrt(max(1, rows / cols)))
- *   members_host: HOST array of 1 .. LOWRA_MAX_FACTORS members, read before the call returns; their arrays overlap nothing else
+ *   members_host: HOST array of 1 .. LOWRA_MAX_FACTORS members, read before the call returns; what is written overlaps nothing else in the call (members may read one gradient)
  *   lowra_update_step: steps 1 .. 32; coefficients a, b, c (usually 3.4445, -4.775, 2.0315); eps > 0 keeps a factor of zeros at zero
  *   workspace_dev: >= lowra_update_workspace_bytes(members_host, count, r) bytes (rows and cols are read), 256-byte aligned, contents overwritten
  * A factor whose u holds a NaN or an infinity gets NaN; the others are not touched by it.  Results do not depend on the run (no atomics), but on which
  * factors share a call, by roundings of fp64.
- * Errors: r not in {16, 32, ..., 128}, shapes, count or steps out of range, two members with one output -> LOWRA_ERR_SHAPE; LOWRA_ERR_NULL (an array without its partner too),
+ * Errors: r not in {16, 32, ..., 128}, shapes, count or steps out of range, an output that shares memory with another array of the call -> LOWRA_ERR_SHAPE; LOWRA_ERR_NULL (an array without its partner too),
  * LOWRA_ERR_ALIGN, LOWRA_ERR_WORKSPACE as elsewhere.
  */
 #define LOWRA_MAX_FACTORS 64

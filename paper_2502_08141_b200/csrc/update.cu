@@ -10,6 +10,8 @@
 // percent.  S and everything of size r x r are therefore fp64, on the fp64 tensor instructions (m8n8k4; 24 TFLOP/s in gram_kernel); u and u Q are fp32.
 #include <string.h>
 
+#include <algorithm>
+
 #include "epilogue.cuh"
 #include "ptx.cuh"
 
@@ -1003,6 +1005,47 @@ lowra_status check_shapes(const lowra_factor* m, int32_t count, int32_t r) {
     return LOWRA_OK;
 }
 
+// Arrays in each other's way: something written that shares memory with anything else that the call reads or writes, of another member or of the same one.  (Momentum
+// and master may be updated in place, element for element.)  In the order of their places, an array is in the way of one before it if it is in that of the one that
+// reaches furthest, among all if it is written, among the written if it is read.
+enum Clash { kNone, kWithin, kBetween };
+Clash find_clash(const UpdateParams& P, size_t r) {
+    struct Array {
+        uintptr_t at, end;
+        int member;
+        bool written;
+    } arrays[7 * kMaxFactors];
+    int n = 0;
+    for (int i = 0; i < P.count; ++i) {
+        const Factor& F = P.f[i];
+        const size_t elements = (size_t)F.L * r;
+        auto add = [&](const void* p, size_t bytes, bool written) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+            if (p != nullptr) arrays[n++] = Array{at, at + elements * bytes, i, written};
+        };
+        add(F.grad, F.grad_fp32 ? 4 : 2, false);
+        if (F.momentum != F.momentum_out) add(F.momentum, 4, false);
+        if (F.master != F.master_out) add(F.master, 4, false);
+        add(F.momentum_out, 4, true);
+        add(F.master_out, 4, true);
+        add(F.weight, 2, true);
+        add(F.update, 4, true);
+    }
+    std::sort(arrays, arrays + n, [](const Array& a, const Array& b) { return a.at < b.at; });
+    Clash found = kNone;
+    const Array *any = nullptr, *written = nullptr;             // of those before, the one that reaches furthest
+    for (int i = 0; i < n; ++i) {
+        const Array &a = arrays[i], *before = a.written ? any : written;
+        if (before != nullptr && a.at < before->end) {
+            if (a.member != before->member) return kBetween;
+            found = kWithin;
+        }
+        if (any == nullptr || a.end > any->end) any = &a;
+        if (a.written && (written == nullptr || a.end > written->end)) written = &a;
+    }
+    return found;
+}
+
 }  // namespace
 }  // namespace lowra
 
@@ -1051,15 +1094,10 @@ extern "C" lowra_status lowra_update_factors(const lowra_factor* members_host, i
         P.f[i] = Factor{m.grad_dev, m.momentum_dev, m.momentum_out_dev, m.master_dev, m.master_out_dev, m.weight_dev, m.update_dev, tall ? m.rows : m.cols,
                         (float)(step_host->lr * m.scale), 0, (uint8_t)tall, (uint8_t)(m.grad_fp32 != 0)};
     }
-    // (a factor named twice would be written by two at once)
-    const auto same = [](const void* p, const void* q) { return p != nullptr && p == q; };
-    for (int i = 1; i < count; ++i) {
-        const Factor& F = P.f[i];
-        for (int j = 0; j < i; ++j)
-            if (same(F.momentum_out, P.f[j].momentum_out) || same(F.master_out, P.f[j].master_out) || same(F.weight, P.f[j].weight) || same(F.update, P.f[j].update))
-                return LOWRA_ERR_SHAPE;
-    }
+    const Clash clash = find_clash(P, (size_t)r);
+    if (clash == kBetween) return LOWRA_ERR_SHAPE;
     if (workspace_bytes < lowra_update_workspace_bytes(members_host, count, r) || (reinterpret_cast<uintptr_t>(workspace_dev) & 255u) != 0) return LOWRA_ERR_WORKSPACE;
+    if (clash != kNone) return LOWRA_ERR_SHAPE;
     if ((st = check_device()) != LOWRA_OK) return st;
     cudaStream_t stream = (cudaStream_t)stream_v;
     switch (r / 16) {
