@@ -111,7 +111,7 @@ PyObject* product(PyObject* const* args, Py_ssize_t n, bool backward, bool epilo
             if (args[11] != Py_None) {
                 const at::Tensor& bias = THPVariable_Unpack(args[11]);
                 behind.bias_bf16 = bias.scalar_type() == at::kBFloat16;
-                if (!array(bias, behind.bias_bf16 ? at::kBFloat16 : at::kFloat, N, dev) || bias.numel() != N) Py_RETURN_NONE;
+                if (!array(bias, behind.bias_bf16 ? at::kBFloat16 : at::kFloat, N, dev) || bias.dim() != 1 || bias.size(0) != N) Py_RETURN_NONE;
                 behind.bias_dev = bias.data_ptr();
             }
             behind.activation = (int32_t)PyLong_AsLong(args[12]);
