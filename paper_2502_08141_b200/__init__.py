@@ -935,7 +935,7 @@ def lowra_epilogue_backward(dY: torch.Tensor, pre: Optional[torch.Tensor] = None
     if workspace is None and dbias is not None:
         workspace = _scratch(max(lowra_epilogue_workspace_bytes(M, N), 256), dY.device, stream)
     code = lib().lowra_epilogue_backward(dY.data_ptr(), _ptr(pre), _ptr(multiply), M, N, number, dZ.data_ptr(), _ptr(dmultiply), _ptr(dbias), _ptr(workspace),
-                                         0 if workspace is None else workspace.numel(), _stream(stream))
+                                         0 if workspace is None else workspace.nbytes, _stream(stream))
     _check(code, "lowra_epilogue_backward")
     return dZ, dmultiply, dbias
 
@@ -1099,7 +1099,7 @@ def lowra_update_factors(members, lr: float, momentum: float = 0.95, nesterov: b
         if size == 0:
             raise LowraError(LOWRA_ERR_SHAPE, "lowra_update_workspace_bytes")
         workspace = _scratch(size, members[0]["grad"].device, stream)
-    code = lib().lowra_update_factors(arr, n, rank, ctypes.byref(step), _ptr(workspace), workspace.numel(), _stream(stream))
+    code = lib().lowra_update_factors(arr, n, rank, ctypes.byref(step), _ptr(workspace), workspace.nbytes, _stream(stream))
     _check(code, "lowra_update_factors")
     return members
 
