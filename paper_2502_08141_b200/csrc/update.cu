@@ -711,13 +711,20 @@ __global__ void __launch_bounds__(kApplyThreads, 1) apply_kernel(const __grid_co
 // ------------------------------------------------------------------------------------------------ all of it in one launch
 // For up to 14 short factors of rank 16 or 32: a cluster of eight CTAs takes a factor, a CTA an eighth of the long side, whose u stays in its shared memory.  Each forms its
 // part of S, sends it to all others, adds the eight up in their order, and goes through the iteration by itself (all get the same Q), then forms its part of u Q.
-// What bounds it is the chain of dependent steps.  Five steps, 1 / 2 / 6 / 14 factors, against the three kernels, us:
-//     512 x 16    6.4 /  6.4 /  6.5 /  6.5   against   9.2 / 10.0 / 10.7 / 10.6        512 x 32   11.9 / 12.0 / 12.3 / 12.3   against  14.6 / 15.7 / 15.9 / 15.8
-//     4096 x 16   9.2 /  9.3 /  9.4 /  9.7   against  10.4 / 10.9 / 11.6 / 16.7       2048 x 32   15.4 / 15.5 / 15.8 / 16.2   against  15.5 / 15.9 / 16.5 / 21.8
-//     8192 x 16  13.3 / 13.2 / 13.4 / 15.5   against  11.6 / 12.2 / 15.8 / 22.4
+// What bounds it is the chain of dependent steps.  Five steps, 1 / 2 / 3 / 4 / 6 / 14 factors in a captured graph, against the three kernels, us:
+//     2048 x 16   7.4 /  7.5 /  7.4 /  7.4 /  7.6 /  7.5   against   9.8 / 10.8 / 10.9 / 10.6 / 10.9 / 11.4
+//     4096 x 16   9.1 /  9.2 /  9.2 /  9.3 /  9.5 /  9.4   against  10.6 / 11.5 / 11.3 / 11.5 / 11.9 / 15.5
+//     5632 x 16  11.4 / 11.4 / 11.5 / 11.4 / 11.4 / 11.6   against  12.3 / 13.0 / 12.9 / 13.2 / 13.6 / 18.3
+//     6144 x 16  11.6 / 11.6 / 11.7 / 11.6 / 11.7 / 11.8   against  10.9 / 11.9 / 12.1 / 12.2 / 13.5 / 18.6
+//     7680 x 16  12.9 / 12.9 / 13.0 / 13.0 / 13.0 / 13.1   against  12.5 / 13.3 / 14.0 / 14.0 / 15.7 / 18.8
+//     8192 x 16  13.2 / 13.3 / 13.4 / 13.3 / 13.4 / 13.4   against  11.8 / 12.7 / 12.9 / 13.4 / 15.5 / 19.7
+//     1024 x 32  13.0 / 13.1 / 13.1 / 13.1 / 13.3 / 13.4   against  14.7 / 15.5 / 15.6 / 15.7 / 15.7 / 16.1
+//     2048 x 32  15.4 / 15.5 / 15.5 / 15.6 / 15.7 / 15.9   against  15.4 / 15.9 / 16.1 / 16.2 / 16.4 / 20.6
 // and a call costs the host 5.5 us instead of 11.5.  Longer ones lose.  More factors: 16 clusters do not find room at once (64 x 16: 10.6 against 9.8).
 constexpr int kOneCtas = 8, kOneFactors = 14, kMostOne = 2;             // CTAs to a factor; factors; rank / 16
-constexpr int kOneRows = 1024;                                          // of the long side to a CTA, times (rank / 16)^2
+constexpr int kOneRows = 1024;                                          // of the long side to a CTA, times (rank / 16)^2: what its shared memory is sized for
+template <int NB>
+constexpr int rows_that_pay(int count) { return NB > 1 || count > 3 ? kOneRows : count > 1 ? 960 : 704; }      // up to which it is the faster way
 template <int NB>
 struct OneShape {
     using I = IterateShape<NB, true>;
@@ -905,7 +912,7 @@ bool takes_one(const UpdateParams& P, int* rows) {
     if (P.count > kOneFactors) return false;
     *rows = 0;
     for (int i = 0; i < P.count; ++i) *rows = max(*rows, one_rows(P.f[i].L));
-    return *rows * NB * NB <= kOneRows;
+    return *rows * NB * NB <= rows_that_pay<NB>(P.count);
 }
 
 template <int NB>
