@@ -347,6 +347,7 @@ struct IterateShape {
     // CTAs of a cluster: one warp to a block
     static constexpr int ctas = tri <= 21 ? 1 : tri <= 55 ? (FEW ? 4 : 2) : tri <= 105 ? (FEW ? 8 : 4) : 8, warps = (tri + ctas - 1) / ctas;
     static constexpr size_t smem = (size_t)(three ? 3 : 4) * bytes + B * 8;
+    static_assert(!whole || ctas == 1, "in a cluster a block goes to the other CTAs without its transpose");
 };
 
 // For one factor: sums(block, s) gives this lane's two values of a block of S, out(row, column, value) takes Q.  memory: I::smem bytes; rank: of the CTA in its cluster.
@@ -381,16 +382,9 @@ __device__ __forceinline__ void iterate(const UpdateParams& P, unsigned char* me
             }
             return;
         }
-        const uint32_t at = ptx::smem_u32(X);
+        const uint32_t at = ptx::smem_u32(X) + own;
 #pragma unroll
-        for (int i = 0; i < ctas; ++i) {
-            const uint32_t there = ptx::map_to_cta(at, (uint32_t)i);
-            st_cluster_f64x2(there + own, v[0], v[1]);
-            if (I::whole && bi != bj) {
-                st_cluster_f64(there + other + across0, v[0]);
-                st_cluster_f64(there + other + across1, v[1]);
-            }
-        }
+        for (int i = 0; i < ctas; ++i) st_cluster_f64x2(ptx::map_to_cta(at, (uint32_t)i), v[0], v[1]);
     };
     // Block (bi, bj) of X Y, and of X2 Y.
     auto products = [&](auto two, const unsigned char* X, const unsigned char* X2, const unsigned char* Y, double (&v)[2], double (&v2)[2]) {
@@ -982,7 +976,10 @@ lowra_status launch_update(UpdateParams& P, void* workspace, cudaStream_t stream
         if (ensure_smem_limit(reinterpret_cast<const void*>(iterate_kernel<NB, FEW>), cfg.dynamicSmemBytes, &limit) != LOWRA_OK) return false;
         return cudaLaunchKernelEx(&cfg, iterate_kernel<NB, FEW>, P) == cudaSuccess;
     };
-    if (!(P.count * IterateShape<NB, true>::ctas <= kNumSMs ? iterate(std::true_type()) : iterate(std::false_type()))) return LOWRA_ERR_CUDA;
+    bool launched = false;
+    if constexpr (IterateShape<NB, true>::ctas == IterateShape<NB, false>::ctas) launched = iterate(std::true_type());      // (the two forms are one)
+    else launched = P.count * IterateShape<NB, true>::ctas <= kNumSMs ? iterate(std::true_type()) : iterate(std::false_type());
+    if (!launched) return LOWRA_ERR_CUDA;
     cfg.numAttrs = 1;
     static SmemLimit limit = {};
     cfg.dynamicSmemBytes = A::bytes;
