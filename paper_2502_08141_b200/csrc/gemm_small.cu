@@ -581,8 +581,6 @@ struct UnitOrder {                               // runs of CTAs: a unit's row g
     uint8_t member[kUnitRuns], first[kUnitRuns], cls[kUnitRuns];     // the unit's member, and its first token in units
 };
 
-__device__ __forceinline__ void barrier_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-
 template <int B, int NT8, int NB, bool EPI>
 __device__ __forceinline__ void unit_rows(const SmallArgs<NB, EPI>& P, int member, int m0, int p0, int p_end, int slices, unsigned char* smem) {
     const SmallMember& W = P.m[member];
@@ -696,7 +694,7 @@ __device__ __forceinline__ void unit_rows(const SmallArgs<NB, EPI>& P, int membe
             if (slice >= 2) ptx::named_barrier_sync(5 + (slice & 1), 256);
 #pragma unroll
             for (int i = 0; i < 4 * NT8; ++i) at[i * 128] = acc[i >> 2][i & 3];
-            barrier_arrive(3 + (slice & 1), 256);
+            ptx::named_barrier_arrive(3 + (slice & 1), 256);
         } else {
             // what stands behind the product, all of it asked for before the other half's sums are waited for (one after the other, between the stores, it
             // took six groups of 101 tokens on 4096 x 4096 from 39 to 47 us)
@@ -721,7 +719,7 @@ __device__ __forceinline__ void unit_rows(const SmallArgs<NB, EPI>& P, int membe
             ptx::named_barrier_sync(3 + (slice & 1), 256);
 #pragma unroll
             for (int i = 0; i < 4 * NT8; ++i) acc[i >> 2][i & 3] = (slice > 0 ? total[i * 128] : 0.0f) + (acc[i >> 2][i & 3] + at[i * 128]);
-            if (slice + 2 < slices) barrier_arrive(5 + (slice & 1), 256);
+            if (slice + 2 < slices) ptx::named_barrier_arrive(5 + (slice & 1), 256);
             if (slice + 1 < slices) {
 #pragma unroll
                 for (int i = 0; i < 4 * NT8; ++i) total[i * 128] = acc[i >> 2][i & 3];

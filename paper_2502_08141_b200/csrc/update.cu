@@ -107,13 +107,17 @@ __device__ __forceinline__ float4 grad_quad(const Factor& F, uint4 g) {
     if (F.grad_fp32) return make_float4(__uint_as_float(g.x), __uint_as_float(g.y), __uint_as_float(g.z), __uint_as_float(g.w));
     return make_float4(__uint_as_float(g.x << 16), __uint_as_float(g.x & 0xffff0000u), __uint_as_float(g.y << 16), __uint_as_float(g.y & 0xffff0000u));
 }
-__device__ __forceinline__ float4 axpy(float a, float4 x, float4 y) { return make_float4(fmaf(a, x.x, y.x), fmaf(a, x.y, y.y), fmaf(a, x.z, y.z), fmaf(a, x.w, y.w)); }
-
 __device__ __forceinline__ float4 axpy2(float a, float4 x, float4 y) {       // two products to an instruction
     const float2 aa = make_float2(a, a), lo = fma2(aa, make_float2(x.x, x.y), make_float2(y.x, y.y)), hi = fma2(aa, make_float2(x.z, x.w), make_float2(y.z, y.w));
     return make_float4(lo.x, lo.y, hi.x, hi.y);
 }
 __device__ __forceinline__ float4 zero4() { return make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+// Four neighbours' weights: x of the update, w before it.
+__device__ __forceinline__ void step_weights(const UpdateParams& P, const Factor& F, size_t at, float4 x, float4 w) {
+    const float4 n = make_float4(fmaf(-F.rate, x.x, P.decay * w.x), fmaf(-F.rate, x.y, P.decay * w.y), fmaf(-F.rate, x.z, P.decay * w.z), fmaf(-F.rate, x.w, P.decay * w.w));
+    *reinterpret_cast<float4*>(F.master_out + at) = n;
+    if (F.weight != nullptr) *reinterpret_cast<uint2*>(F.weight + at) = make_uint2(pack_bf16x2(n.x, n.y), pack_bf16x2(n.z, n.w));
+}
 
 // A tile's gradient and momentum.
 template <typename D>
@@ -155,7 +159,6 @@ __device__ __forceinline__ int factor_of(const UpdateParams& P, int tile) {
 // a tenth more to do: the same.  Three groups that fill: the same.)
 // Up to r = 64 every warp takes a quarter of the tile's long side and all blocks of S (36 at r = 64: 144 registers); above that each warp takes
 // all of it and a quarter of the blocks: the triangles of the two halves of the rank, and two halves of the square between them.
-__device__ __forceinline__ void barrier_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 constexpr int kFull = 1, kEmpty = kFull + kStages, kJoin = kEmpty + kStages;       // named barriers
 
 template <int NB>
@@ -206,7 +209,7 @@ __global__ void __launch_bounds__(kGramThreads, 1) gram_kernel(const __grid_cons
             };
             if (F.tall) fill(std::true_type());
             else fill(std::false_type());
-            barrier_arrive(kFull + stage, 2 * kThreads);
+            ptx::named_barrier_arrive(kFull + stage, 2 * kThreads);
         }
         return;
     }
@@ -280,7 +283,7 @@ __global__ void __launch_bounds__(kGramThreads, 1) gram_kernel(const __grid_cons
         const float* u = tiles + stage * S::floats;
         if (F.tall) multiply(std::true_type(), u);
         else multiply(std::false_type(), u);
-        if (n + kStages < count) barrier_arrive(kEmpty + stage, 2 * kThreads);
+        if (n + kStages < count) ptx::named_barrier_arrive(kEmpty + stage, 2 * kThreads);
         const bool last_of_factor = (first + n - F.tile0 + 1) * S::TL >= F.L;
         if (n + 1 < count && !last_of_factor) continue;
         double2* out = reinterpret_cast<double2*>(P.sums) + (size_t)(blockIdx.x + f) * S::tri * 32;
@@ -552,7 +555,7 @@ __device__ __forceinline__ Raw load_raw(const UpdateParams& P, const Factor& F, 
 }
 __device__ __forceinline__ float4 u_of(const UpdateParams& P, const Factor& F, const Raw& r) {
     if (F.momentum_out == nullptr) return grad_quad(F, r.g);
-    return P.nesterov ? axpy(P.mu, r.m, grad_quad(F, r.g)) : r.m;
+    return P.nesterov ? axpy2(P.mu, r.m, grad_quad(F, r.g)) : r.m;
 }
 
 constexpr int kApplyThreads = 4 * kThreads;
@@ -606,7 +609,7 @@ __global__ void __launch_bounds__(kApplyThreads, 1) apply_kernel(const __grid_co
             };
             if (F.tall) fill(std::true_type());
             else fill(std::false_type());
-            barrier_arrive(kFull + stage, 2 * kThreads);
+            ptx::named_barrier_arrive(kFull + stage, 2 * kThreads);
         }
         return;
     }
@@ -672,13 +675,7 @@ __global__ void __launch_bounds__(kApplyThreads, 1) apply_kernel(const __grid_co
         if (F.master == nullptr) return;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (!inside(i)) continue;
-            const size_t at = place + (i / 4) * far + (i % 4) * near_by;
-            const float4 x = acc[i];
-            const float4 n = make_float4(fmaf(-F.rate, x.x, P.decay * w[i].x), fmaf(-F.rate, x.y, P.decay * w[i].y), fmaf(-F.rate, x.z, P.decay * w[i].z),
-                                         fmaf(-F.rate, x.w, P.decay * w[i].w));
-            *reinterpret_cast<float4*>(F.master_out + at) = n;
-            if (F.weight != nullptr) *reinterpret_cast<uint2*>(F.weight + at) = make_uint2(pack_bf16x2(n.x, n.y), pack_bf16x2(n.z, n.w));
+            if (inside(i)) step_weights(P, F, place + (i / 4) * far + (i % 4) * near_by, acc[i], w[i]);
         }
     };
     for (int n = half; n < count; n += 2) {
@@ -695,7 +692,7 @@ __global__ void __launch_bounds__(kApplyThreads, 1) apply_kernel(const __grid_co
         ptx::named_barrier_sync(kFull + stage, 2 * kThreads);
         const float* u = tiles + stage * A::floats;
         auto done = [&]() {
-            if (n + kStages < count) barrier_arrive(kEmpty + stage, 2 * kThreads);
+            if (n + kStages < count) ptx::named_barrier_arrive(kEmpty + stage, 2 * kThreads);
         };
         if (F.tall) work(std::true_type(), F, l0, u, done);
         else work(std::false_type(), F, l0, u, done);
@@ -883,13 +880,8 @@ __global__ void __launch_bounds__(OneShape<NB>::threads, 1) one_kernel(const __g
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const size_t at = place + i * step;
-            const float4 x = acc[i];
-            if (F.update != nullptr) *reinterpret_cast<float4*>(F.update + at) = x;
-            if (F.master == nullptr) continue;
-            const float4 n = make_float4(fmaf(-F.rate, x.x, P.decay * w[i].x), fmaf(-F.rate, x.y, P.decay * w[i].y), fmaf(-F.rate, x.z, P.decay * w[i].z),
-                                         fmaf(-F.rate, x.w, P.decay * w[i].w));
-            *reinterpret_cast<float4*>(F.master_out + at) = n;
-            if (F.weight != nullptr) *reinterpret_cast<uint2*>(F.weight + at) = make_uint2(pack_bf16x2(n.x, n.y), pack_bf16x2(n.z, n.w));
+            if (F.update != nullptr) *reinterpret_cast<float4*>(F.update + at) = acc[i];
+            if (F.master != nullptr) step_weights(P, F, at, acc[i], w[i]);
         }
     }
 }
