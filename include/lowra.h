@@ -334,6 +334,7 @@ lowra_status lowra_lora_forward_adapters(const lowra_layout* layout, const uint8
  * Arrays 16-byte aligned, row-major, without gaps, rows as in Y.  Y may be the residual itself (the residual stream, added to in place) or the multiplied
  * array; else Y and pre overlap nothing that the call reads or writes (a Y or pre that shares memory with X, pre with Y, multiply or residual, or Y with a part of
  * multiply or residual -> LOWRA_ERR_SHAPE: X may be the residual too, but then Y is an array of its own).
+ * A call that ends in LOWRA_ERR_TIMEOUT has written a part of Y: where Y is the residual or the multiplied array, that array is lost and the call cannot be repeated.
  * One epilogue belongs to one member; the array of epilogues is host memory and is read before the call returns.  The members of a batch run side by side: a Y or pre
  * of one that shares memory with another's X, Y, pre, multiply or residual (a gate and the up projection that it multiplies, in one batch) -> LOWRA_ERR_SHAPE.
  *   lowra_lora_forward_epilogue           as lowra_lora_forward (few tokens included)
