@@ -473,6 +473,107 @@ lowra_status lowra_update_factors(const lowra_factor* members_host, int32_t coun
                                   size_t workspace_bytes, void* stream);
 
 /*
+ * (No counterpart in the paper.)  The norm before a layer's projections, with the residual stream's addition on the way:
+ *     h = bf16(X + residual) (h = X without one);    Y = (h - mu) rstd weight + bias,    rstd = 1 / sqrt(mean (h - mu)^2 + eps)
+ * over the N channels of each row; LOWRA_NORM_LAYER as it stands, LOWRA_NORM_RMS with mu = 0 and without bias.  Statistics in fp32, Y rounded to bf16 once.
+ *   X_dev, residual_dev bf16 [M, N] (residual or NULL);  weight_dev, bias_dev [N], bf16 or, with params_fp32 != 0, fp32 (bias: LOWRA_NORM_LAYER only)
+ *   sum_dev   bf16 [M, N]: h (out; with a residual, and only then)        Y_dev bf16 [M, N] (out)
+ *   mean_dev, rstd_dev   fp32 [M] (out), or NULL: what the backward call reads (mean: LOWRA_NORM_LAYER only)
+ *   sum and Y may each be X or residual (in place); else outputs overlap nothing.
+ * The gradient, in one pass, with g = dY weight and xh = (h - mu) rstd:
+ *     dX = rstd (g - mean g - xh mean(g xh)) + dsum             bf16 [M, N] (out): the gradient of X and of the residual alike
+ *     dweight[n] = sum over the rows of dY xh,   dbias[n] = sum over the rows of dY      fp32 [N] (out), or NULL: sums in a fixed order
+ *   X_dev: h;   mean_dev, rstd_dev: as the forward call left them (mean NULL: the root mean square's gradient);   dsum_dev bf16 [M, N], or NULL: the gradient that reaches h
+ *   beside the norm.   dX may be dY, X or dsum (in place); else outputs overlap nothing.
+ *   workspace_dev: >= lowra_norm_workspace_bytes(M, N) bytes, 256-byte aligned, contents overwritten; used for dweight and dbias only.
+ * Errors: arrays missing -> LOWRA_ERR_NULL; M < 1 or > 2^30, N % 8 != 0 or > 16384, a kind that is none, eps < 0, a bias, mean or dbias for LOWRA_NORM_RMS, arrays that
+ * share memory -> LOWRA_ERR_SHAPE; LOWRA_ERR_ALIGN, LOWRA_ERR_WORKSPACE as elsewhere.
+ */
+typedef enum { LOWRA_NORM_LAYER = 0, LOWRA_NORM_RMS = 1 } lowra_norm_kind;
+size_t lowra_norm_workspace_bytes(int32_t M, int32_t N);
+lowra_status lowra_norm_forward(const uint16_t* X_dev, const uint16_t* residual_dev, const void* weight_dev, const void* bias_dev, int32_t params_fp32, int32_t M,
+                                int32_t N, int32_t kind, float eps, uint16_t* sum_dev, uint16_t* Y_dev, float* mean_dev, float* rstd_dev, void* stream);
+lowra_status lowra_norm_backward(const uint16_t* dY_dev, const uint16_t* X_dev, const void* weight_dev, int32_t params_fp32, const float* mean_dev,
+                                 const float* rstd_dev, const uint16_t* dsum_dev, int32_t M, int32_t N, uint16_t* dX_dev, float* dweight_dev, float* dbias_dev,
+                                 void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/*
+ * (No counterpart in the paper.)  Positions turned into the heads of queries and keys, behind the projections that lowra_lora_forward_batch forms: the pairs (a, b) among the
+ * first `dim` values of every head of token m become
+ *     scale * (a cos t - b sin t, b cos t + a sin t),     t = positions[m] * frequency of the pair          (inverse != 0: -t, the gradient's turn)
+ * in fp32, rounded to bf16 once; the values behind them stay as they are.  Pair i of a head is (value i, value dim/2 + i), or, interleaved, (2i, 2i + 1).
+ *   lowra_rotary_turns (host only) writes the pairs' frequencies, in turns a position as fractions of 2^64 (angles at every 32-bit position are then right to 2^-33 of a
+ *   turn), and the factor that the turned values get.  frequency_i = base^(-2i/dim), and by kind, for contexts longer than those trained on:
+ *     LOWRA_ROTARY_NONE    as it is;      LOWRA_ROTARY_LINEAR  divided by `factor`;      LOWRA_ROTARY_NTK   base * factor^(dim / (dim - 2)) in the place of base
+ *     LOWRA_ROTARY_YARN    pairs that turn more than `high` times in `original` positions as they are, those under `low` divided by `factor`, a ramp over the pairs between;
+ *                          turned values times 0.1 ln(factor) + 1
+ *     LOWRA_ROTARY_BANDS   the same with a ramp over the turns between, and no factor for the values
+ *   lowra_rotary_part: queries, or keys: x_dev, out_dev bf16, [M][heads][D] with strides in elements (slices of a fused projection), values of a head side by side;
+ *     out_dev may be x_dev with the same strides (in place); else outputs overlap nothing
+ *   parts_host: HOST array of 1 or 2 parts, read before the call returns;   positions_dev int32 [M];   turns_dev uint64 [dim / 2]: a device copy of the table
+ * Errors: arrays missing -> LOWRA_ERR_NULL; M < 1 or > 2^30, D % 8 != 0 or > 4096, dim % 16 != 0, > D or > 1024, heads < 1 or > 65536, strides that are no multiples of 8 or by which an
+ * output's values share memory, arrays that do -> LOWRA_ERR_SHAPE; x, out, turns not 16-byte aligned -> LOWRA_ERR_ALIGN.  lowra_rotary_turns: dim odd, < 2 or > 1024,
+ * base <= 1, factor < 1, original < 1, not 0 < low < high, a kind that is none -> LOWRA_ERR_SHAPE.
+ */
+#define LOWRA_MAX_ROTARY_PARTS 2
+typedef enum { LOWRA_ROTARY_NONE = 0, LOWRA_ROTARY_LINEAR = 1, LOWRA_ROTARY_NTK = 2, LOWRA_ROTARY_YARN = 3, LOWRA_ROTARY_BANDS = 4 } lowra_rotary_kind;
+typedef struct {
+    int32_t kind;
+    double factor, original, low, high;
+} lowra_rotary_scaling;
+typedef struct {
+    const uint16_t* x_dev;
+    uint16_t* out_dev;
+    int64_t x_token_stride, x_head_stride, out_token_stride, out_head_stride;
+    int32_t heads;
+} lowra_rotary_part;
+lowra_status lowra_rotary_turns(int32_t dim, double base, const lowra_rotary_scaling* scaling_host, uint64_t* turns_host, float* scale_host);
+lowra_status lowra_rotary(const lowra_rotary_part* parts_host, int32_t count, int32_t M, int32_t D, int32_t dim, const int32_t* positions_dev,
+                          const uint64_t* turns_dev, float scale, int32_t interleaved, int32_t inverse, void* stream);
+
+/*
+ * (No counterpart in the paper.)  The other optimiser's step (lowra_update_factors is the one that orthogonalises): adaptive moments with decoupled weight decay, over all factors of
+ * a model in one call, whatever their shapes; elements are counted flat.
+ *     m' = beta1 m + (1 - beta1) g;    v' = beta2 v + (1 - beta2) g^2;    w' = w (1 - lr weight_decay) - lr (m' / (1 - beta1^t)) / (sqrt(v' / (1 - beta2^t)) + eps)
+ * with g the gradient times *grad_scale_dev (a clipping factor, say), weight = bf16(w').  States of bits = 32: m and v fp32 [n].  Of bits = 8: of every LOWRA_ADAMW_BLOCK values
+ * one behind the other (the last block may be short) s = (largest magnitude) / 448, fp32, in m_scale, v_scale [ceil(n / LOWRA_ADAMW_BLOCK)], and in m and v, one byte each, m' / s and
+ * sqrt(v') / s as e4m3 (to nearest, ties to even; a root that is not zero becomes at least 2^-9; a block with s < 2^-126 is zero).  A block that meets a NaN or an infinity
+ * stays NaN.  w' is formed before m' and v' are rounded.
+ *   lowra_adamw_member: arrays on the device, 16-byte aligned (scales 4), of n elements without gaps: grad bf16 or, with grad_fp32 != 0, fp32 (all members alike); master fp32 w;
+ *     each *_out may be its input itself (in place); weight bf16, or NULL; what is written overlaps nothing else in the call (members may read one gradient)
+ *   members_host: HOST array of 1 .. LOWRA_MAX_ADAMW members, read before the call returns
+ *   lowra_adamw_step: t = step, counted from 1;  step_dev int32, lr_dev and grad_scale_dev fp32: one number each on the device that takes the place of step or lr, or multiplies the
+ *     gradient, or NULL.  (A captured call keeps its step and lr: where it is replayed, hand them over on the device.)
+ * Errors: count, n (1 .. 2^36), bits, step < 1 or betas outside [0, 1), arrays that share memory -> LOWRA_ERR_SHAPE; LOWRA_ERR_NULL, LOWRA_ERR_ALIGN as elsewhere.
+ */
+#define LOWRA_MAX_ADAMW 4096
+#define LOWRA_ADAMW_BLOCK 256
+typedef struct {
+    const void* grad_dev;
+    const float* master_dev;
+    float* master_out_dev;
+    uint16_t* weight_dev;
+    const void* m_dev;
+    void* m_out_dev;
+    const void* v_dev;
+    void* v_out_dev;
+    const float* m_scale_dev;
+    float* m_scale_out_dev;
+    const float* v_scale_dev;
+    float* v_scale_out_dev;
+    int64_t n;
+} lowra_adamw_member;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;
+    const float* grad_scale_dev;
+    const float* lr_dev;
+    const int32_t* step_dev;
+    int32_t bits, grad_fp32;
+} lowra_adamw_step;
+lowra_status lowra_adamw(const lowra_adamw_member* members_host, int32_t count, const lowra_adamw_step* step_host, void* stream);
+
+/*
  * Synchronises `stream` and returns the status word that the last forward / backward call wrote
  * into its workspace: LOWRA_OK, or LOWRA_ERR_TIMEOUT if a bounded wait inside a kernel ran out
  * (the kernel then released its resources and returned; the output is not valid).

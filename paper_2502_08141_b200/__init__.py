@@ -41,7 +41,8 @@ EXPORTS = (
     "lowra_workspace_projection", "lowra_set_wait_limit", "lowra_diag_wait_expiry", "lowra_diag_drop_t_flags",
     "lowra_encode_group", "lowra_decode_group", "lowra_diag_choose", "lowra_lora_forward_epilogue",
     "lowra_lora_forward_batch_epilogue", "lowra_lora_forward_adapters_epilogue", "lowra_epilogue_workspace_bytes", "lowra_epilogue_backward",
-    "lowra_update_workspace_bytes", "lowra_update_factors",
+    "lowra_update_workspace_bytes", "lowra_update_factors", "lowra_norm_workspace_bytes", "lowra_norm_forward", "lowra_norm_backward", "lowra_rotary_turns", "lowra_rotary",
+    "lowra_adamw",
 )
 
 
@@ -91,6 +92,26 @@ class _CFactor(ctypes.Structure):
 class _CUpdateStep(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("weight_decay", ctypes.c_double), ("eps", ctypes.c_double),
                 ("coefficients", ctypes.c_double * 3), ("nesterov", ctypes.c_int32), ("steps", ctypes.c_int32)]
+
+
+class _CRotaryScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_double), ("original", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class _CRotaryPart(ctypes.Structure):
+    _fields_ = [("x_dev", ctypes.c_void_p), ("out_dev", ctypes.c_void_p), ("x_token_stride", ctypes.c_int64), ("x_head_stride", ctypes.c_int64),
+                ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64), ("heads", ctypes.c_int32)]
+
+
+class _CAdamwMember(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("grad_dev", "master_dev", "master_out_dev", "weight_dev", "m_dev", "m_out_dev", "v_dev", "v_out_dev", "m_scale_dev",
+                                                     "m_scale_out_dev", "v_scale_dev", "v_scale_out_dev")] + [("n", ctypes.c_int64)]
+
+
+class _CAdamwStep(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [
+        ("step", ctypes.c_int64), ("grad_scale_dev", ctypes.c_void_p), ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p), ("bits", ctypes.c_int32),
+        ("grad_fp32", ctypes.c_int32)]
 
 
 _lib = None
@@ -177,6 +198,18 @@ def lib() -> ctypes.CDLL:
         L.lowra_update_workspace_bytes.restype = ctypes.c_size_t
         L.lowra_update_factors.argtypes = [fp, i32, i32, ctypes.POINTER(_CUpdateStep), vp, ctypes.c_size_t, vp]
         L.lowra_update_factors.restype = ctypes.c_int
+        L.lowra_norm_workspace_bytes.argtypes = [i32, i32]
+        L.lowra_norm_workspace_bytes.restype = ctypes.c_size_t
+        L.lowra_norm_forward.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp]
+        L.lowra_norm_forward.restype = ctypes.c_int
+        L.lowra_norm_backward.argtypes = [vp, vp, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.lowra_norm_backward.restype = ctypes.c_int
+        L.lowra_rotary_turns.argtypes = [i32, ctypes.c_double, ctypes.POINTER(_CRotaryScaling), vp, ctypes.POINTER(ctypes.c_float)]
+        L.lowra_rotary_turns.restype = ctypes.c_int
+        L.lowra_rotary.argtypes = [ctypes.POINTER(_CRotaryPart), i32, i32, i32, i32, vp, vp, ctypes.c_float, i32, i32, vp]
+        L.lowra_rotary.restype = ctypes.c_int
+        L.lowra_adamw.argtypes = [ctypes.POINTER(_CAdamwMember), i32, ctypes.POINTER(_CAdamwStep), vp]
+        L.lowra_adamw.restype = ctypes.c_int
         L.lowra_lora_forward_static.argtypes = [lp, vp, vp, vp, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp, vp]
         L.lowra_lora_forward_static.restype = ctypes.c_int
         L.lowra_learn_codebooks.argtypes = [lp, vp, vp, vp, i32, vp, vp, vp]
@@ -1101,6 +1134,231 @@ def lowra_update_factors(members, lr: float, momentum: float = 0.95, nesterov: b
         workspace = _scratch(size, members[0]["grad"].device, stream)
     code = lib().lowra_update_factors(arr, n, rank, ctypes.byref(step), _ptr(workspace), workspace.nbytes, _stream(stream))
     _check(code, "lowra_update_factors")
+    return members
+
+
+_NORMS = {"layer": 0, "rms": 1}
+
+
+def lowra_norm_workspace_bytes(M: int, N: int) -> int:
+    return int(lib().lowra_norm_workspace_bytes(int(M), int(N)))
+
+
+def _norm_params(N: int, **params) -> int:
+    """Whether the parameters of a norm, [N] each and of one type, are fp32."""
+    types = {t.dtype for t in params.values() if t is not None}
+    if len(types) != 1 or not types <= {_BF16, torch.float32}:
+        raise ValueError(f"{' and '.join(params)} must be {_BF16} or {torch.float32}, alike; got {', '.join(str(t.dtype) for t in params.values() if t is not None)}")
+    for name, t in params.items():
+        if t is not None:
+            _dev(t, t.dtype, name)
+            if t.shape != (N,):
+                raise ValueError(f"{name} must be [{N}], got {tuple(t.shape)}")
+    return int(types == {torch.float32})
+
+
+def _rows_like(X: torch.Tensor, **others) -> None:
+    for name, t in others.items():
+        if t is not None:
+            _dev(t, _BF16, name)
+            if t.shape != X.shape:
+                raise ValueError(f"{name} must be {list(X.shape)}, got {list(t.shape)}")
+
+
+def _vectors(n: int, **vectors) -> None:
+    for name, t in vectors.items():
+        if t is not None:
+            _dev(t, torch.float32, name)
+            if t.shape != (n,):
+                raise ValueError(f"{name} must be [{n}], got {tuple(t.shape)}")
+
+
+def lowra_norm_forward(X: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, eps: float = 1e-5, kind: str = "layer",
+                       residual: Optional[torch.Tensor] = None, sum: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None,
+                       rstd: Optional[torch.Tensor] = None, stream=None):
+    """h = X + residual (bf16 [M, N], rounded; X without one), Y = (h - mean) * rstd * weight + bias over the channels of each row; kind "layer", or "rms" (no mean, no
+    bias).  weight and bias [N], bf16 or fp32; mean and rstd fp32 [M], which the gradient reads.  sum and Y may be X or residual themselves (in place).
+    Returns (Y, rstd, mean or None, h or None where there is no residual)."""
+    number = _NORMS.get(kind)
+    if number is None:
+        raise ValueError(f"kind must be one of {', '.join(_NORMS)}, got {kind!r}")
+    if X.dim() != 2:
+        raise ValueError(f"X must be [M, N], got {tuple(X.shape)}")
+    _dev(X, _BF16, "X")
+    M, N = X.shape
+    _rows_like(X, residual=residual, sum=sum, Y=Y)
+    fp32 = _norm_params(N, weight=weight, bias=bias)
+    _vectors(M, mean=mean, rstd=rstd)
+    if Y is None:
+        Y = torch.empty_like(X)
+    if sum is None and residual is not None:
+        sum = torch.empty_like(X)
+    if rstd is None:
+        rstd = torch.empty(M, dtype=torch.float32, device=X.device)
+    if mean is None and number == 0:
+        mean = torch.empty(M, dtype=torch.float32, device=X.device)
+    code = lib().lowra_norm_forward(X.data_ptr(), _ptr(residual), weight.data_ptr(), _ptr(bias), fp32, M, N, number, eps, _ptr(sum), Y.data_ptr(), _ptr(mean),
+                                    rstd.data_ptr(), _stream(stream))
+    _check(code, "lowra_norm_forward")
+    return Y, rstd, mean, sum
+
+
+def lowra_norm_backward(dY: torch.Tensor, X: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, mean: Optional[torch.Tensor] = None,
+                        dsum: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None,
+                        dbias: Optional[torch.Tensor] = None, want_params: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
+    """The gradient through lowra_norm_forward: X is what was normalised (h where there was a residual), rstd and mean as that call left them (no mean: "rms"), dsum the gradient that
+    reaches h beside the norm.  dX bf16 [M, N], that of X and of the residual alike, may be dY, X or dsum themselves; dweight and, with a mean, dbias fp32 [N], if they are
+    given or wanted.  Returns (dX, dweight or None, dbias or None)."""
+    if X.dim() != 2:
+        raise ValueError(f"X must be [M, N], got {tuple(X.shape)}")
+    _dev(X, _BF16, "X")
+    M, N = X.shape
+    if dY is None or rstd is None:
+        raise ValueError("dY and rstd are needed")
+    _rows_like(X, dY=dY, dsum=dsum, dX=dX)
+    fp32 = _norm_params(N, weight=weight)
+    _vectors(M, rstd=rstd, mean=mean)
+    _vectors(N, dweight=dweight, dbias=dbias)
+    _extent(workspace, 0, "workspace")
+    if dX is None:
+        dX = torch.empty_like(X)
+    if dweight is None and want_params:
+        dweight = torch.empty(N, dtype=torch.float32, device=X.device)
+    if dbias is None and want_params and mean is not None:
+        dbias = torch.empty(N, dtype=torch.float32, device=X.device)
+    if workspace is None and (dweight is not None or dbias is not None):
+        workspace = _scratch(max(lowra_norm_workspace_bytes(M, N), 256), X.device, stream)
+    code = lib().lowra_norm_backward(dY.data_ptr(), X.data_ptr(), weight.data_ptr(), fp32, _ptr(mean), rstd.data_ptr(), _ptr(dsum), M, N, dX.data_ptr(), _ptr(dweight),
+                                     _ptr(dbias), _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream(stream))
+    _check(code, "lowra_norm_backward")
+    return dX, dweight, dbias
+
+
+_ROTARY_KINDS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
+
+
+def lowra_rotary_turns(dim: int, base: float = 10000.0, kind: str = "none", factor: float = 1.0, original: float = 4096.0, beta_fast: float = 32.0, beta_slow: float = 1.0,
+                       low: float = 1.0, high: float = 4.0) -> Tuple[np.ndarray, float]:
+    """The frequencies of the dim / 2 pairs of a head as lowra_rotary takes them (numpy uint64: turns a position as fractions of 2^64; upload as int64), and its `scale`.
+    kind: "none"; "linear" (positions over factor); "ntk" (a larger base); "yarn" (pairs that turn under beta_slow times in `original` positions over factor, above beta_fast as they
+    are, a ramp over the pairs between); "bands" (the same with low and high, a ramp over the turns)."""
+    number = _ROTARY_KINDS.get(kind)
+    if number is None:
+        raise ValueError(f"kind must be one of {', '.join(_ROTARY_KINDS)}, got {kind!r}")
+    limits = (beta_slow, beta_fast) if kind == "yarn" else (low, high)
+    scaling = _CRotaryScaling(number, float(factor), float(original), float(limits[0]), float(limits[1]))
+    turns, scale = np.zeros(max(int(dim) // 2, 1), dtype=np.uint64), ctypes.c_float(1.0)
+    _check(lib().lowra_rotary_turns(int(dim), float(base), ctypes.byref(scaling), turns.ctypes.data, ctypes.byref(scale)), "lowra_rotary_turns")
+    return turns, float(scale.value)
+
+
+def _heads(t: torch.Tensor, name: str) -> None:
+    """[tokens, heads, D] bf16 on the current device, the values of a head side by side."""
+    if t.dtype != _BF16 or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be {_BF16} [tokens, heads, D] with a head's values side by side, got {t.dtype} {list(t.shape)} by {list(t.stride())}")
+    _here(t, name)
+
+
+def lowra_rotary(q: torch.Tensor, positions: torch.Tensor, turns: torch.Tensor, k: Optional[torch.Tensor] = None, interleaved: bool = False, inverse: bool = False,
+                 scale: float = 1.0, out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
+    """Positions (int32 [tokens]) turned into the heads of q and, in the same launch, k: bf16 [tokens, heads, D], any strides of tokens and heads.  The first 2 * len(turns) values of a
+    head are turned (turns, scale: lowra_rotary_turns; 64-bit, on the device), pairs half of them apart or side by side (interleaved), the others stay.  inverse: the gradient's
+    way.  out, k_out: q and k themselves (in place), arrays of one's own, or None for new ones.  Returns out, or (out, k_out) with a k."""
+    _heads(q, "q")
+    M, _, D = q.shape
+    parts = [(q, out, "q", "out")] if k is None else [(q, out, "q", "out"), (k, k_out, "k", "k_out")]
+    if k is None and k_out is not None:
+        raise ValueError("k_out without k")
+    if turns.dim() != 1 or turns.element_size() != 8 or turns.is_floating_point():
+        raise ValueError("turns must be a vector of 64-bit numbers")
+    _extent(turns, 0, "turns")
+    _dev(positions, torch.int32, "positions")
+    if positions.shape != (M,):
+        raise ValueError(f"positions must be [{M}], got {tuple(positions.shape)}")
+    arr, outs = (_CRotaryPart * len(parts))(), []
+    for c, (x, y, name, out_name) in zip(arr, parts):
+        _heads(x, name)
+        if x.shape[0] != M or x.shape[2] != D:
+            raise ValueError(f"{name} must be [{M}, heads, {D}], got {list(x.shape)}")
+        if y is None:
+            y = torch.empty(x.shape, dtype=_BF16, device=x.device)
+        else:
+            _heads(y, out_name)
+            if y.shape != x.shape:
+                raise ValueError(f"{out_name} must be {list(x.shape)}, got {list(y.shape)}")
+        outs.append(y)
+        c.x_dev, c.out_dev, c.heads = x.data_ptr(), y.data_ptr(), x.shape[1]
+        c.x_token_stride, c.x_head_stride, c.out_token_stride, c.out_head_stride = x.stride(0), x.stride(1), y.stride(0), y.stride(1)
+    code = lib().lowra_rotary(arr, len(parts), M, D, 2 * turns.numel(), positions.data_ptr(), turns.data_ptr(), scale, int(bool(interleaved)), int(bool(inverse)),
+                              _stream(stream))
+    _check(code, "lowra_rotary")
+    return outs[0] if k is None else tuple(outs)
+
+
+LOWRA_ADAMW_BLOCK = 256
+_E4M3 = torch.float8_e4m3fn
+
+
+def _scalar(t: torch.Tensor, dtype, name: str) -> int:
+    _dev(t, dtype, name)
+    if t.numel() != 1:
+        raise ValueError(f"{name} must be one number, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def lowra_adamw(members, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, step=1, grad_scale: Optional[torch.Tensor] = None, stream=None):
+    """A step of adaptive moments with decoupled weight decay over the factors of a model, in one call.  `members`: dicts with grad (bf16 or fp32, all alike), master (fp32), m and v (fp32,
+    or torch.float8_e4m3fn with m_scale and v_scale, fp32 [ceil(n / LOWRA_ADAMW_BLOCK)]: v then holds the second moment's root) and, optionally, weight (bf16, receives the
+    rounded weights); all of one shape.  States and master are updated in place unless master_out, m_out, v_out, m_scale_out, v_scale_out are given; a state begins as zeros.
+    `step`, counted from 1, and lr: numbers, or CUDA tensors of one int32 or fp32 (what a captured call that is replayed needs); grad_scale: a CUDA tensor of one fp32 that
+    multiplies the gradients.  Returns the members."""
+    n = len(members)
+    if n == 0:
+        raise ValueError("no members")
+    arr, eight, fp32 = (_CAdamwMember * n)(), None, None
+    for i, (c, w) in enumerate(zip(arr, members)):
+        grad, m = w["grad"], w["m"]
+        if fp32 is None:
+            if grad.dtype not in (_BF16, torch.float32):
+                raise ValueError(f"grad must be {_BF16} or {torch.float32}, got {grad.dtype}")
+            if m.dtype not in (_E4M3, torch.float32):
+                raise ValueError(f"m must be {_E4M3} or {torch.float32}, got {m.dtype}")
+            eight, fp32 = m.dtype == _E4M3, grad.dtype == torch.float32
+        state = _E4M3 if eight else torch.float32
+        shape, blocks = grad.shape, (grad.numel() + LOWRA_ADAMW_BLOCK - 1) // LOWRA_ADAMW_BLOCK
+        c.n = grad.numel()
+        for name, dtype in (("grad", torch.float32 if fp32 else _BF16), ("master", torch.float32), ("m", state), ("v", state), ("weight", _BF16), ("m_scale", torch.float32),
+                            ("v_scale", torch.float32)):
+            t, new = w.get(name), w.get(name + "_out") if name not in ("grad", "weight") else None
+            if "scale" in name and not eight:
+                if t is not None or new is not None:
+                    raise ValueError(f"{name} of member {i}: states in fp32 have no scales")
+                continue
+            if t is None and name == "weight":
+                continue
+            if t is None:
+                raise ValueError(f"{name} of member {i} is missing")
+            for u, label in ((t, name), (new, name + "_out")):
+                if u is None:
+                    continue
+                _dev(u, dtype, f"{label} of member {i}")
+                if u.shape != ((blocks,) if "scale" in name else shape):
+                    raise ValueError(f"{label} of member {i} must be {[blocks] if 'scale' in name else list(shape)}, got {list(u.shape)}")
+            setattr(c, name + "_dev", t.data_ptr())
+            if name not in ("grad", "weight"):
+                setattr(c, name + "_out_dev", (t if new is None else new).data_ptr())
+    s = _CAdamwStep(0.0, float(betas[0]), float(betas[1]), float(eps), float(weight_decay), 0, None, None, None, 8 if eight else 32, int(fp32))
+    if isinstance(lr, torch.Tensor):
+        s.lr_dev = _scalar(lr, torch.float32, "lr")
+    else:
+        s.lr = float(lr)
+    if isinstance(step, torch.Tensor):
+        s.step_dev = _scalar(step, torch.int32, "step")
+    else:
+        s.step = int(step)
+    if grad_scale is not None:
+        s.grad_scale_dev = _scalar(grad_scale, torch.float32, "grad_scale")
+    _check(lib().lowra_adamw(arr, n, ctypes.byref(s), _stream(stream)), "lowra_adamw")
     return members
 
 

@@ -1,0 +1,332 @@
+// lowra_adamw: the optimiser's step over the factors of a model together, decoupled weight decay, states in fp32 or in 8 bits:
+//     m' = b1 m + (1 - b1) g;   v' = b2 v + (1 - b2) g^2;   w' = w (1 - lr wd) - lr (m' / (1 - b1^t)) / (sqrt(v' / (1 - b2^t)) + eps)
+// In 8 bits, of every 256 values one behind the other in a factor, are kept s = (their largest magnitude) / 448 in fp32 and the values over s as e4m3 (three bits behind the leading one, down
+// to 2^-9 of 448); of the second moment its root is kept that way, whose range is half as many octaves, and a root that is not zero is kept off zero, so that no step is divided by
+// eps for it.  m' and v' go into w' before they are rounded.
+// The states' arithmetic is fp32 with every operation rounded by itself, in the order above ((1 - b2) g first, then times g): what is rounded to 8 bits does not depend on
+// how a compiler joins operations.
+// Bound by memory: gradient, weights and states each read once and written once, 28 bytes a weight (bf16 gradient, fp32 states) or 16 (8 bits).  A warp takes 256 values at a
+// time, eight to a lane, so that a scale is two warp reductions and all accesses are 16 bytes wide (8 for codes); the factors' descriptions are kernel parameters, found by
+// a binary search over their first blocks (some 10 steps, behind 48 warps' loads).
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <string.h>
+
+#include <algorithm>
+#include <cmath>
+#include <memory>
+#include <new>
+
+#include "lowra_common.cuh"
+
+namespace lowra {
+
+namespace {
+
+constexpr int kAdamThreads = 256, kAdamBlock = LOWRA_ADAMW_BLOCK;
+constexpr int kAdamMembers = 224;                   // of a launch: what kernel parameters have room for
+static_assert(kAdamBlock == 32 * 8, "a warp's values");
+
+struct AdamMember {
+    const void* grad;
+    const float* master;
+    float* master_out;
+    uint16_t* weight;
+    const void *m, *v;
+    void *m_out, *v_out;
+    const float *m_scale, *v_scale;
+    float *m_scale_out, *v_scale_out;
+    long long n;
+};
+struct AdamParams {
+    AdamMember f[kAdamMembers];
+    uint32_t first[kAdamMembers + 1];               // blocks before each factor's, and of all
+    int count, grad_fp32;
+    float b1, c1, b2, c2, decay, rate, root_scale, eps;
+    // on the device, or null: the gradient's factor, the step and the learning rate
+    const float *grad_scale, *lr;
+    const int32_t* step;
+    double log_b1, log_b2, wd;
+};
+
+template <typename T>
+__device__ __forceinline__ T load(const void* p) {  // (not as read-only memory: states and weights are written in place)
+    T v;
+    static_assert(sizeof(T) == 16 || sizeof(T) == 8, "");
+    if constexpr (sizeof(T) == 16)
+        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    else
+        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+    return v;
+}
+
+// Eight values of a lane: `left` of them exist (eight but at a factor's end).
+__device__ __forceinline__ void load_floats(const float* p, int left, float (&x)[8]) {
+    if (left >= 8) {
+        const uint4 a = load<uint4>(p), b = load<uint4>(p + 4);
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < left ? *reinterpret_cast<const volatile float*>(p + i) : 0.0f;
+    }
+}
+__device__ __forceinline__ void store_floats(float* p, int left, const float (&x)[8]) {
+    if (left >= 8) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) p[i] = x[i];
+    }
+}
+__device__ __forceinline__ void load_bf16(const uint16_t* p, int left, float (&x)[8]) {
+    if (left >= 8) {
+        const uint4 a = load<uint4>(p);
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < left ? __uint_as_float((uint32_t)p[i] << 16) : 0.0f;
+    }
+}
+// codes (e4m3) times their block's scale
+__device__ __forceinline__ void load_codes(const uint8_t* p, int left, float scale, float (&x)[8]) {
+    uint32_t w[2] = {0u, 0u};
+    if (left >= 8) {
+        const uint2 a = load<uint2>(p);
+        w[0] = a.x;
+        w[1] = a.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) w[i >> 2] |= (uint32_t)*reinterpret_cast<const volatile uint8_t*>(p + i) << (8 * (i & 3));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3)));
+        x[2 * i] = __fmul_rn(f.x, scale);
+        x[2 * i + 1] = __fmul_rn(f.y, scale);
+    }
+}
+// The block's scale and the lane's codes.  Magnitudes are compared as integers: a NaN is above all, and its scale is NaN.
+template <bool ROOT>
+__device__ __forceinline__ float store_codes(uint8_t* p, int left, const float (&x)[8]) {
+    uint32_t most = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+    float scale = __fmul_rn(__uint_as_float(__reduce_max_sync(0xffffffffu, most)), 1.0f / 448.0f);
+    if (scale < 0x1p-126f) scale = 0.0f;             // its reciprocal would be out of range: the block is zero
+    const float over = scale > 0.0f ? __frcp_rn(scale) : 0.0f;
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float2 f = make_float2(__fmul_rn(x[2 * i], over), __fmul_rn(x[2 * i + 1], over));
+        if (ROOT) {
+            if (f.x > 0.0f) f.x = fmaxf(f.x, 0x1p-9f);
+            if (f.y > 0.0f) f.y = fmaxf(f.y, 0x1p-9f);
+        }
+        w[i >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3) << (16 * (i & 1));
+    }
+    if (left >= 8) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    }
+    return scale;
+}
+
+template <bool EIGHT>
+__global__ void __launch_bounds__(kAdamThreads, 3) adamw_kernel(const __grid_constant__ AdamParams P) {
+    __shared__ float shared[3];
+    pdl_enter();
+    float decay = P.decay, rate = P.rate, root_scale = P.root_scale;
+    if (P.step != nullptr || P.lr != nullptr) {      // a captured step reads them when it runs
+        if (threadIdx.x == 0) {
+            float lr = P.lr != nullptr ? *P.lr : 0.0f;
+            if (P.lr != nullptr) decay = (float)(1.0 - (double)lr * P.wd);
+            double one = 1.0;                        // 1 - b1^t, which rate holds already where the step is the host's
+            if (P.step != nullptr) {
+                const double t = (double)*P.step;
+                one = -expm1(t * P.log_b1);
+                root_scale = (float)(1.0 / sqrt(-expm1(t * P.log_b2)));
+            }
+            // rate: lr / (1 - b1^t) as far as the host knows it, else lr, 1 / (1 - b1^t) or 1
+            rate = (float)((double)rate * (P.lr != nullptr ? (double)lr : 1.0) / one);
+            shared[0] = decay;
+            shared[1] = rate;
+            shared[2] = root_scale;
+        }
+        __syncthreads();
+        decay = shared[0];
+        rate = shared[1];
+        root_scale = shared[2];
+    }
+    const float grad_scale = P.grad_scale != nullptr ? *P.grad_scale : 1.0f;
+    const int lane = threadIdx.x & 31;
+    const uint32_t blocks = P.first[P.count], step = gridDim.x * (kAdamThreads / 32);
+    for (uint32_t block = blockIdx.x * (kAdamThreads / 32) + (threadIdx.x >> 5); block < blocks; block += step) {
+        int lo = 0, hi = P.count;                    // first[lo] <= block < first[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (P.first[mid] <= block) lo = mid;
+            else hi = mid;
+        }
+        const AdamMember& F = P.f[lo];
+        const uint32_t in = block - P.first[lo];
+        const long long at = (long long)in * kAdamBlock + lane * 8;
+        const int left = (int)min((long long)8, F.n - at);             // (none or fewer: lanes past the end)
+        float g[8], w[8], m[8], v[8];
+        if (P.grad_fp32) load_floats(static_cast<const float*>(F.grad) + at, left, g);
+        else load_bf16(static_cast<const uint16_t*>(F.grad) + at, left, g);
+        load_floats(F.master + at, left, w);
+        if (EIGHT) {
+            load_codes(static_cast<const uint8_t*>(F.m) + at, left, F.m_scale[in], m);
+            load_codes(static_cast<const uint8_t*>(F.v) + at, left, F.v_scale[in], v);
+        } else {
+            load_floats(static_cast<const float*>(F.m) + at, left, m);
+            load_floats(static_cast<const float*>(F.v) + at, left, v);
+        }
+        float root[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float gi = P.grad_scale != nullptr ? __fmul_rn(g[i], grad_scale) : g[i];
+            if (EIGHT) v[i] = __fmul_rn(v[i], v[i]);   // (what is kept is the root)
+            m[i] = __fadd_rn(__fmul_rn(P.b1, m[i]), __fmul_rn(P.c1, gi));
+            v[i] = __fadd_rn(__fmul_rn(P.b2, v[i]), __fmul_rn(__fmul_rn(P.c2, gi), gi));
+            root[i] = __fsqrt_rn(v[i]);
+            w[i] = w[i] * decay - rate * __fdividef(m[i], root[i] * root_scale + P.eps);
+        }
+        store_floats(F.master_out + at, left, w);
+        if (F.weight != nullptr) {
+            if (left >= 8) {
+                *reinterpret_cast<uint4*>(F.weight + at) = make_uint4(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7]));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < left) F.weight[at + i] = (uint16_t)pack_bf16x2(w[i], 0.0f);
+            }
+        }
+        if (EIGHT) {
+            const float a = store_codes<false>(static_cast<uint8_t*>(F.m_out) + at, left, m), b = store_codes<true>(static_cast<uint8_t*>(F.v_out) + at, left, root);
+            if (lane == 0) {
+                F.m_scale_out[in] = a;
+                F.v_scale_out[in] = b;
+            }
+        } else {
+            store_floats(static_cast<float*>(F.m_out) + at, left, m);
+            store_floats(static_cast<float*>(F.v_out) + at, left, v);
+        }
+    }
+}
+
+// Something written that shares memory with anything else of the call.  In the order of their places, an array is in the way of one before it if it is in that of the one that reaches
+// furthest, among all if it is written, among the written if it is read.
+struct Place {
+    uintptr_t at, end;
+    bool written;
+};
+bool any_clash(Place* p, size_t n) {
+    std::sort(p, p + n, [](const Place& a, const Place& b) { return a.at < b.at; });
+    uintptr_t any = 0, written = 0;
+    for (size_t i = 0; i < n; ++i) {
+        if (p[i].at < (p[i].written ? any : written)) return true;
+        any = std::max(any, p[i].end);
+        if (p[i].written) written = std::max(written, p[i].end);
+    }
+    return false;
+}
+
+}  // namespace
+}  // namespace lowra
+
+extern "C" lowra_status lowra_adamw(const lowra_adamw_member* members_host, int32_t count, const lowra_adamw_step* step_host, void* stream_v) {
+    using namespace lowra;
+    if (!members_host || !step_host) return LOWRA_ERR_NULL;
+    const lowra_adamw_step& S = *step_host;
+    if (count < 1 || count > LOWRA_MAX_ADAMW || (S.bits != 8 && S.bits != 32) || (!S.step_dev && S.step < 1) || !(S.beta1 >= 0.0 && S.beta1 < 1.0) ||
+        !(S.beta2 >= 0.0 && S.beta2 < 1.0) || !(S.eps >= 0.0))
+        return LOWRA_ERR_SHAPE;
+    const bool eight = S.bits == 8;
+    const size_t wide = eight ? 1 : 4;
+    std::unique_ptr<Place[]> places(new (std::nothrow) Place[(size_t)count * 12 + 3]);
+    if (!places) return LOWRA_ERR_CUDA;
+    size_t n_places = 0;
+    auto add = [&](const void* p, size_t bytes, bool written) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        if (p != nullptr) places[n_places++] = Place{at, at + bytes, written};
+    };
+    unsigned long long blocks = 0;
+    for (int i = 0; i < count; ++i) {
+        const lowra_adamw_member& m = members_host[i];
+        if (!m.grad_dev || !m.master_dev || !m.master_out_dev || !m.m_dev || !m.m_out_dev || !m.v_dev || !m.v_out_dev) return LOWRA_ERR_NULL;
+        if (eight && (!m.m_scale_dev || !m.m_scale_out_dev || !m.v_scale_dev || !m.v_scale_out_dev)) return LOWRA_ERR_NULL;
+        if (m.n < 1 || m.n > (1ll << 36)) return LOWRA_ERR_SHAPE;
+        const void* all[12] = {m.grad_dev, m.master_dev, m.master_out_dev, m.weight_dev, m.m_dev, m.m_out_dev, m.v_dev, m.v_out_dev,
+                               eight ? m.m_scale_dev : nullptr, eight ? m.m_scale_out_dev : nullptr, eight ? m.v_scale_dev : nullptr, eight ? m.v_scale_out_dev : nullptr};
+        for (int k = 0; k < 8; ++k)
+            if (!aligned16(all[k])) return LOWRA_ERR_ALIGN;
+        for (int k = 8; k < 12; ++k)
+            if ((reinterpret_cast<uintptr_t>(all[k]) & 3u) != 0) return LOWRA_ERR_ALIGN;
+        const size_t n = (size_t)m.n, s = (n + kAdamBlock - 1) / kAdamBlock;
+        blocks += s;
+        add(m.grad_dev, n * (S.grad_fp32 ? 4 : 2), false);
+        add(m.weight_dev, n * 2, true);
+        add(m.master_out_dev, n * 4, true);
+        add(m.m_out_dev, n * wide, true);
+        add(m.v_out_dev, n * wide, true);
+        if (m.master_dev != m.master_out_dev) add(m.master_dev, n * 4, false);
+        if (m.m_dev != m.m_out_dev) add(m.m_dev, n * wide, false);
+        if (m.v_dev != m.v_out_dev) add(m.v_dev, n * wide, false);
+        if (!eight) continue;
+        add(m.m_scale_out_dev, s * 4, true);
+        add(m.v_scale_out_dev, s * 4, true);
+        if (m.m_scale_dev != m.m_scale_out_dev) add(m.m_scale_dev, s * 4, false);
+        if (m.v_scale_dev != m.v_scale_out_dev) add(m.v_scale_dev, s * 4, false);
+    }
+    add(S.grad_scale_dev, 4, false);
+    add(S.lr_dev, 4, false);
+    add(S.step_dev, 4, false);
+    if (((reinterpret_cast<uintptr_t>(S.grad_scale_dev) | reinterpret_cast<uintptr_t>(S.lr_dev) | reinterpret_cast<uintptr_t>(S.step_dev)) & 3u) != 0) return LOWRA_ERR_ALIGN;
+    if (blocks > 0x7fffffffull || any_clash(places.get(), n_places)) return LOWRA_ERR_SHAPE;
+    const lowra_status st = check_device();
+    if (st != LOWRA_OK) return st;
+    AdamParams P;
+    P.grad_fp32 = S.grad_fp32 != 0;
+    P.b1 = (float)S.beta1;
+    P.c1 = (float)(1.0 - S.beta1);
+    P.b2 = (float)S.beta2;
+    P.c2 = (float)(1.0 - S.beta2);
+    P.eps = (float)S.eps;
+    P.wd = S.weight_decay;
+    P.decay = (float)(1.0 - S.lr * S.weight_decay);
+    P.log_b1 = std::log(S.beta1);
+    P.log_b2 = std::log(S.beta2);
+    const double one = S.step_dev ? 1.0 : 1.0 - std::pow(S.beta1, (double)S.step);
+    P.rate = (float)((S.lr_dev ? 1.0 : S.lr) / one);
+    P.root_scale = S.step_dev ? 1.0f : (float)(1.0 / std::sqrt(1.0 - std::pow(S.beta2, (double)S.step)));
+    P.grad_scale = S.grad_scale_dev;
+    P.lr = S.lr_dev;
+    P.step = S.step_dev;
+    for (int i0 = 0; i0 < count; i0 += kAdamMembers) {
+        P.count = std::min(count - i0, kAdamMembers);
+        P.first[0] = 0;
+        for (int i = 0; i < P.count; ++i) {
+            const lowra_adamw_member& m = members_host[i0 + i];
+            P.f[i] = AdamMember{m.grad_dev, m.master_dev, m.master_out_dev, m.weight_dev, m.m_dev, m.v_dev, m.m_out_dev, m.v_out_dev,
+                                m.m_scale_dev, m.v_scale_dev, m.m_scale_out_dev, m.v_scale_out_dev, m.n};
+            P.first[i + 1] = P.first[i] + (uint32_t)((m.n + kAdamBlock - 1) / kAdamBlock);
+        }
+        const uint32_t wanted = (P.first[P.count] + kAdamThreads / 32 - 1) / (kAdamThreads / 32), most = (uint32_t)kNumSMs * 6;
+        if (launch_pdl(eight ? adamw_kernel<true> : adamw_kernel<false>, std::min(wanted, most), kAdamThreads, (cudaStream_t)stream_v, P) != cudaSuccess) return LOWRA_ERR_CUDA;
+    }
+    return LOWRA_OK;
+}
