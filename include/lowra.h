@@ -574,6 +574,24 @@ typedef struct {
 lowra_status lowra_adamw(const lowra_adamw_member* members_host, int32_t count, const lowra_adamw_step* step_host, void* stream);
 
 /*
+ * (No counterpart in the paper.)  The end of a training step's forward pass and the beginning of its backward pass: cross entropy over a vocabulary of V words straight from the
+ * hidden states, and the gradient of these.  The head's weights are frozen, as the base weights are, and get none.
+ *     l = X W^T;    loss[m] = log sum_v exp(l[m, v]) - l[m, labels[m]];    dX[m] = scale * weights[m] * (softmax(l[m]) - onehot(labels[m])) W
+ * The logits [M, V] are not kept: with a gradient, exponentials of a piece of the vocabulary and of up to 4096 tokens at a time (128 MB of the workspace).  Logits and sums in fp32;
+ * the exponentials are rounded to bf16 before they are multiplied by W, without the label's own, so that neither a small loss nor a gradient near zero loses digits.
+ *   X_dev bf16 [M, K];  W_dev bf16 [V, K];  labels_dev int64 [M]: words, or ignore_index: such a token's loss and gradient are 0.  A label that is neither gives NaN.
+ *   weights_dev   fp32 [M], or NULL: a factor of each token's gradient (not of its loss)
+ *   loss_dev      fp32 [M] (out);     dX_dev bf16 [M, K] (out), or NULL: losses only, the logits formed once
+ *   workspace_dev: >= lowra_cross_entropy_workspace_bytes(M, V, K, dX_dev != NULL) bytes, 256-byte aligned, contents overwritten; lowra_device_status reads its status word
+ * A logit that is a NaN or +infinity makes its token's loss and gradient NaN, no other's.  Results do not depend on the run.
+ * Errors: arrays missing -> LOWRA_ERR_NULL; M < 1 or > 2^30, V < 1 or > 2^24, K < 64, > 65536 or no multiple of 8, arrays that share memory with an output or the workspace ->
+ * LOWRA_ERR_SHAPE; LOWRA_ERR_ALIGN, LOWRA_ERR_WORKSPACE as elsewhere.
+ */
+size_t lowra_cross_entropy_workspace_bytes(int32_t M, int32_t V, int32_t K, int32_t grad);
+lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_t* W_dev, const int64_t* labels_dev, const float* weights_dev, int32_t M, int32_t V, int32_t K,
+                                 int64_t ignore_index, float scale, float* loss_dev, uint16_t* dX_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/*
  * Synchronises `stream` and returns the status word that the last forward / backward call wrote
  * into its workspace: LOWRA_OK, or LOWRA_ERR_TIMEOUT if a bounded wait inside a kernel ran out
  * (the kernel then released its resources and returned; the output is not valid).

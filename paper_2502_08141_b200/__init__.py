@@ -42,7 +42,7 @@ EXPORTS = (
     "lowra_encode_group", "lowra_decode_group", "lowra_diag_choose", "lowra_lora_forward_epilogue",
     "lowra_lora_forward_batch_epilogue", "lowra_lora_forward_adapters_epilogue", "lowra_epilogue_workspace_bytes", "lowra_epilogue_backward",
     "lowra_update_workspace_bytes", "lowra_update_factors", "lowra_norm_workspace_bytes", "lowra_norm_forward", "lowra_norm_backward", "lowra_rotary_turns", "lowra_rotary",
-    "lowra_adamw",
+    "lowra_adamw", "lowra_cross_entropy_workspace_bytes", "lowra_cross_entropy",
 )
 
 
@@ -210,6 +210,10 @@ def lib() -> ctypes.CDLL:
         L.lowra_rotary.restype = ctypes.c_int
         L.lowra_adamw.argtypes = [ctypes.POINTER(_CAdamwMember), i32, ctypes.POINTER(_CAdamwStep), vp]
         L.lowra_adamw.restype = ctypes.c_int
+        L.lowra_cross_entropy_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.lowra_cross_entropy_workspace_bytes.restype = ctypes.c_size_t
+        L.lowra_cross_entropy.argtypes = [vp, vp, vp, vp, i32, i32, i32, ctypes.c_int64, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp]
+        L.lowra_cross_entropy.restype = ctypes.c_int
         L.lowra_lora_forward_static.argtypes = [lp, vp, vp, vp, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp, vp]
         L.lowra_lora_forward_static.restype = ctypes.c_int
         L.lowra_learn_codebooks.argtypes = [lp, vp, vp, vp, i32, vp, vp, vp]
@@ -1360,6 +1364,42 @@ def lowra_adamw(members, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay
         s.grad_scale_dev = _scalar(grad_scale, torch.float32, "grad_scale")
     _check(lib().lowra_adamw(arr, n, ctypes.byref(s), _stream(stream)), "lowra_adamw")
     return members
+
+
+def lowra_cross_entropy_workspace_bytes(M: int, V: int, K: int, grad: bool) -> int:
+    return int(lib().lowra_cross_entropy_workspace_bytes(int(M), int(V), int(K), int(bool(grad))))
+
+
+def lowra_cross_entropy(X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, scale: float = 1.0, weights: Optional[torch.Tensor] = None, ignore_index: int = -100,
+                        loss: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None, want_grad: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Cross entropy of the tokens X (bf16 [M, K], the last hidden states) over the words of the head W (bf16 [V, K], frozen) against labels (int64 [M]; ignore_index: the token does not
+    count), without keeping the logits, and, if dX is given or wanted, the gradient of X: dX[m] = scale * weights[m] * (softmax - onehot) W, weights fp32 [M] if given.
+    Returns (loss fp32 [M], of every token and unweighted; dX or None)."""
+    if X.dim() != 2 or W.dim() != 2 or W.shape[1] != X.shape[1]:
+        raise ValueError(f"X and W must be [M, K] and [V, K], got {tuple(X.shape)} and {tuple(W.shape)}")
+    _dev(X, _BF16, "X")
+    _dev(W, _BF16, "W")
+    M, K = X.shape
+    V = W.shape[0]
+    _dev(labels, torch.int64, "labels")
+    if labels.shape != (M,):
+        raise ValueError(f"labels must be [{M}], got {tuple(labels.shape)}")
+    _vectors(M, weights=weights, loss=loss)
+    _rows_like(X, dX=dX)
+    _extent(workspace, 0, "workspace")
+    if loss is None:
+        loss = torch.empty(M, dtype=torch.float32, device=X.device)
+    if dX is None and want_grad:
+        dX = torch.empty_like(X)
+    if workspace is None:
+        nbytes = lowra_cross_entropy_workspace_bytes(M, V, K, dX is not None)
+        if nbytes == 0:
+            raise LowraError(LOWRA_ERR_SHAPE, "lowra_cross_entropy_workspace_bytes")
+        workspace = _scratch(nbytes, X.device, stream)
+    code = lib().lowra_cross_entropy(X.data_ptr(), W.data_ptr(), labels.data_ptr(), _ptr(weights), M, V, K, int(ignore_index), scale, loss.data_ptr(), _ptr(dX),
+                                     workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    _check(code, "lowra_cross_entropy")
+    return loss, dX
 
 
 def lowra_device_status(workspace: torch.Tensor, stream=None) -> int:

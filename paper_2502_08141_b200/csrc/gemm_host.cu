@@ -112,6 +112,8 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
     return fn;
 }
 
+}  // namespace
+
 // bf16 matrix [rows, cols] row-major with pitch `ld` elements; box = 64 columns x box_rows rows,
 // 128-byte swizzle, out-of-range elements read as zero.
 bool make_map(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows) {
@@ -126,6 +128,8 @@ bool make_map(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t cols, u
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return rc == CUDA_SUCCESS;
 }
+
+namespace {
 
 // One weight of a fused call, as the entry points receive it.
 struct MemberArgs {

@@ -141,3 +141,24 @@ def test_adamw():
         assert call(step=bad) == lw.LOWRA_ERR_SHAPE, bad
     for name in ("lr_dev", "step_dev", "grad_scale_dev"):
         assert call(step={name: 9 * AT + 2}) == lw.LOWRA_ERR_ALIGN
+
+
+def test_cross_entropy():
+    def call(X=AT, W=2 * AT, labels=3 * AT, weights=None, M=4, V=100, K=64, loss=4 * AT, dX=5 * AT, ws=64 * AT, n=1 << 40):
+        return lw.lib().lowra_cross_entropy(X, W, labels, weights, M, V, K, -100, 1.0, loss, dX, ws, n, None)
+
+    for name in ("X", "W", "labels", "loss", "ws"):
+        assert call(**{name: None}) == lw.LOWRA_ERR_NULL, name
+    for name in ("X", "W", "labels", "weights", "loss", "dX"):
+        assert call(**{name: 9 * AT + 8}) == lw.LOWRA_ERR_ALIGN, name
+    for bad in (dict(M=0), dict(M=(1 << 30) + 1), dict(V=0), dict(V=(1 << 24) + 1), dict(K=56), dict(K=68), dict(K=65544), dict(dX=AT), dict(loss=AT + 16), dict(loss=5 * AT), dict(dX=2 * AT + 128),
+                dict(weights=4 * AT), dict(loss=3 * AT + 16), dict(dX=64 * AT), dict(W=64 * AT)):
+        assert call(**bad) == lw.LOWRA_ERR_SHAPE, bad
+    size = lw.lowra_cross_entropy_workspace_bytes(4, 100, 64, True)
+    assert call(n=size - 1) == lw.LOWRA_ERR_WORKSPACE and call(ws=64 * AT + 64) == lw.LOWRA_ERR_WORKSPACE
+    for M, V, K in ((0, 100, 64), (4, 0, 64), (4, 100, 60), (4, 100, 32)):
+        assert lw.lowra_cross_entropy_workspace_bytes(M, V, K, True) == 0
+    # the logits are never kept: however many tokens and words, a piece of exponentials of 128 MB and O
+    assert lw.lowra_cross_entropy_workspace_bytes(4096, 32000, 4096, False) < 20 << 20
+    for M, V in ((4096, 32000), (100000, 32000), (4096, 1 << 24), (64, 1 << 24)):
+        assert lw.lowra_cross_entropy_workspace_bytes(M, V, 1024, True) < (160 << 20) + 17 * 4096 * 1024 * 4
