@@ -133,7 +133,8 @@ def _load_py_calls(L: ctypes.CDLL):
     module.bind(*(address(fn) for fn in (L.lowra_lora_forward, L.lowra_lora_backward_input, L.lowra_workspace_bytes, L.lowra_workspace_init, L.lowra_lora_forward_batch,
                                          L.lowra_lora_backward_input_batch, L.lowra_lora_backward_adapters, L.lowra_lora_backward_adapters_reuse,
                                          L.lowra_adapter_workspace_bytes, L.lowra_workspace_projection, L.lowra_lora_forward_epilogue,
-                                         L.lowra_epilogue_workspace_bytes, L.lowra_epilogue_backward, L.lowra_update_workspace_bytes, L.lowra_update_factors)))
+                                         L.lowra_epilogue_workspace_bytes, L.lowra_epilogue_backward, L.lowra_update_workspace_bytes, L.lowra_update_factors, L.lowra_norm_workspace_bytes, L.lowra_norm_forward,
+                                         L.lowra_norm_backward, L.lowra_rotary, L.lowra_cross_entropy_workspace_bytes, L.lowra_cross_entropy, L.lowra_adamw)))
     return module
 
 
@@ -1186,6 +1187,12 @@ def lowra_norm_forward(X: torch.Tensor, weight: torch.Tensor, bias: Optional[tor
     number = _NORMS.get(kind)
     if number is None:
         raise ValueError(f"kind must be one of {', '.join(_NORMS)}, got {kind!r}")
+    if stream is None and _py_calls is not None:
+        done = _py_calls.norm_forward(X, weight, bias, eps, number, residual, sum, Y, mean, rstd)
+        if done is not None:
+            if done.__class__ is int:
+                _check(done, "lowra_norm_forward")
+            return done
     if X.dim() != 2:
         raise ValueError(f"X must be [M, N], got {tuple(X.shape)}")
     _dev(X, _BF16, "X")
@@ -1213,6 +1220,12 @@ def lowra_norm_backward(dY: torch.Tensor, X: torch.Tensor, weight: torch.Tensor,
     """The gradient through lowra_norm_forward: X is what was normalised (h where there was a residual), rstd and mean as that call left them (no mean: "rms"), dsum the gradient that
     reaches h beside the norm.  dX bf16 [M, N], that of X and of the residual alike, may be dY, X or dsum themselves; dweight and, with a mean, dbias fp32 [N], if they are
     given or wanted.  Returns (dX, dweight or None, dbias or None)."""
+    if stream is None and _py_calls is not None:
+        done = _py_calls.norm_backward(dY, X, weight, rstd, mean, dsum, dX, dweight, dbias, want_params, workspace)
+        if done is not None:
+            if done.__class__ is int:
+                _check(done, "lowra_norm_backward")
+            return done
     if X.dim() != 2:
         raise ValueError(f"X must be [M, N], got {tuple(X.shape)}")
     _dev(X, _BF16, "X")
@@ -1268,6 +1281,12 @@ def lowra_rotary(q: torch.Tensor, positions: torch.Tensor, turns: torch.Tensor, 
     """Positions (int32 [tokens]) turned into the heads of q and, in the same launch, k: bf16 [tokens, heads, D], any strides of tokens and heads.  The first 2 * len(turns) values of a
     head are turned (turns, scale: lowra_rotary_turns; 64-bit, on the device), pairs half of them apart or side by side (interleaved), the others stay.  inverse: the gradient's
     way.  out, k_out: q and k themselves (in place), arrays of one's own, or None for new ones.  Returns out, or (out, k_out) with a k."""
+    if stream is None and _py_calls is not None:
+        done = _py_calls.rotary(q, positions, turns, k, interleaved, inverse, scale, out, k_out)
+        if done is not None:
+            if done.__class__ is int:
+                _check(done, "lowra_rotary")
+            return done
     _heads(q, "q")
     M, _, D = q.shape
     parts = [(q, out, "q", "out")] if k is None else [(q, out, "q", "out"), (k, k_out, "k", "k_out")]
@@ -1316,6 +1335,12 @@ def lowra_adamw(members, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay
     rounded weights); all of one shape.  States and master are updated in place unless master_out, m_out, v_out, m_scale_out, v_scale_out are given; a state begins as zeros.
     `step`, counted from 1, and lr: numbers, or CUDA tensors of one int32 or fp32 (what a captured call that is replayed needs); grad_scale: a CUDA tensor of one fp32 that
     multiplies the gradients.  Returns the members."""
+    if stream is None and _py_calls is not None:
+        done = _py_calls.adamw(members, lr, betas, eps, weight_decay, step, grad_scale)
+        if done is not None:
+            if done.__class__ is int:
+                _check(done, "lowra_adamw")
+            return done
     n = len(members)
     if n == 0:
         raise ValueError("no members")
@@ -1375,6 +1400,12 @@ def lowra_cross_entropy(X: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, 
     """Cross entropy of the tokens X (bf16 [M, K], the last hidden states) over the words of the head W (bf16 [V, K], frozen) against labels (int64 [M]; ignore_index: the token does not
     count), without keeping the logits, and, if dX is given or wanted, the gradient of X: dX[m] = scale * weights[m] * (softmax - onehot) W, weights fp32 [M] if given.
     Returns (loss fp32 [M], of every token and unweighted; dX or None)."""
+    if stream is None and _py_calls is not None:
+        done = _py_calls.cross_entropy(X, W, labels, scale, weights, ignore_index, loss, dX, want_grad, workspace)
+        if done is not None:
+            if done.__class__ is int:
+                _check(done, "lowra_cross_entropy")
+            return done
     if X.dim() != 2 or W.dim() != 2 or W.shape[1] != X.shape[1]:
         raise ValueError(f"X and W must be [M, K] and [V, K], got {tuple(X.shape)} and {tuple(W.shape)}")
     _dev(X, _BF16, "X")

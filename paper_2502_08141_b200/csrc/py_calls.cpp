@@ -14,10 +14,17 @@
 //   gradients_reuse(X, dY, T, U, r, dA or None, dB or None, workspace or None)      likewise
 //   projection(workspace, M, r, member)                                             its view of the workspace
 //   epilogue_backward(dY, pre, the activation's number, multiply, dZ, dmultiply, dbias, whether dbias is wanted, workspace: dY given, the others may be None)    the three outputs
+//   norm_forward(X, weight, bias, eps, the kind's number, residual, sum, Y, mean, rstd: X and weight given, the others may be None)                 Y, rstd, mean, sum
+//   norm_backward(dY, X, weight, rstd, mean, dsum, dX, dweight, dbias, whether these are wanted, workspace: the first four given, the others may be None)   dX, dweight, dbias
+//   rotary(q, positions, turns, k or None, interleaved, inverse, scale, out or None, k_out or None)                                                out, or the pair
+//   cross_entropy(X, W, labels, scale, weights, ignore_index, loss, dX, whether dX is wanted, workspace: tensors but the first three may be None)   loss, dX
+//   adamw(members, lr, betas, eps, weight_decay, step, grad_scale or None)                                                                          the members
 //   update_factors(members, lr, momentum, nesterov, weight_decay, steps, coefficients, eps, rank or None, workspace or None)                                     the members
 #include <torch/extension.h>
 
 #include <algorithm>
+#include <initializer_list>
+#include <utility>
 #include <vector>
 
 #include <c10/cuda/CUDAFunctions.h>
@@ -44,6 +51,13 @@ using EpilogueBytes = size_t (*)(int32_t, int32_t);
 using EpilogueBackward = lowra_status (*)(const uint16_t*, const uint16_t*, const uint16_t*, int32_t, int32_t, int32_t, uint16_t*, uint16_t*, float*, void*, size_t, void*);
 using UpdateBytes = size_t (*)(const lowra_factor*, int32_t, int32_t);
 using Update = lowra_status (*)(const lowra_factor*, int32_t, int32_t, const lowra_update_step*, void*, size_t, void*);
+using NormBytes = size_t (*)(int32_t, int32_t);
+using NormForward = decltype(&lowra_norm_forward);
+using NormBackward = decltype(&lowra_norm_backward);
+using Rotary = decltype(&lowra_rotary);
+using LossBytes = decltype(&lowra_cross_entropy_workspace_bytes);
+using Loss = decltype(&lowra_cross_entropy);
+using Adamw = decltype(&lowra_adamw);
 struct Library {
     Product forward, backward_input;
     WorkspaceBytes workspace_bytes;
@@ -58,6 +72,13 @@ struct Library {
     EpilogueBackward epilogue_backward;
     UpdateBytes update_bytes;
     Update update;
+    NormBytes norm_bytes;
+    NormForward norm_forward;
+    NormBackward norm_backward;
+    Rotary rotary;
+    LossBytes loss_bytes;
+    Loss loss;
+    Adamw adamw;
 } library;
 
 bool plain(PyObject* o) { return THPVariable_CheckExact(o); }
@@ -502,6 +523,276 @@ PyObject* update_factors(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
 }
 
+// ---- the operators of a training step beside the products
+bool each_plain_or_none(PyObject* const* args, std::initializer_list<int> places) {
+    for (int i : places)
+        if (args[i] != Py_None && !plain(args[i])) return false;
+    return true;
+}
+at::Tensor given(PyObject* o) { return o == Py_None ? at::Tensor() : THPVariable_Unpack(o); }
+float* fp32(const at::Tensor& t) { return t.defined() ? static_cast<float*>(t.data_ptr()) : nullptr; }
+uint16_t* bf16_or_null(const at::Tensor& t) { return t.defined() ? bf16(t) : nullptr; }
+bool vector_of(const at::Tensor& t, int64_t n, int64_t dev) { return !t.defined() || (array(t, at::kFloat, n, dev) && t.dim() == 1 && t.size(0) == n); }
+bool rows_of(const at::Tensor& t, int64_t M, int64_t N, int64_t dev) { return !t.defined() || matrix(t, M, N, dev); }
+// The results in order: the caller's own objects where they gave some, else the new ones, else None.
+PyObject* results(std::initializer_list<std::pair<PyObject*, at::Tensor*>> all) {
+    PyObject* tuple = PyTuple_New((Py_ssize_t)all.size());
+    Py_ssize_t i = 0;
+    for (const auto& [o, t] : all) {
+        PyObject* r = o != Py_None || !t->defined() ? Py_NewRef(o) : THPVariable_Wrap(std::move(*t));
+        if (tuple != nullptr) PyTuple_SET_ITEM(tuple, i++, r);
+        else Py_XDECREF(r);
+    }
+    return tuple;
+}
+
+PyObject* norm_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    double eps = 0.0;
+    int32_t kind = 0;
+    if (n != 10 || library.forward == nullptr || !plain(args[0]) || !plain(args[1]) || !number(args[3], &eps) || !number(args[4], &kind) ||
+        !each_plain_or_none(args, {2, 5, 6, 7, 8, 9}))
+        Py_RETURN_NONE;
+    try {
+        const int64_t dev = c10::cuda::current_device();
+        const at::Tensor &X = THPVariable_Unpack(args[0]), &weight = THPVariable_Unpack(args[1]);
+        if (X.dim() != 2) Py_RETURN_NONE;
+        const int64_t M = X.size(0), N = X.size(1);
+        const at::ScalarType type = weight.scalar_type();
+        if (M > INT32_MAX || N > INT32_MAX || !matrix(X, M, N, dev) || (type != at::kFloat && type != at::kBFloat16)) Py_RETURN_NONE;
+        at::Tensor bias = given(args[2]), residual = given(args[5]), sum = given(args[6]), Y = given(args[7]), mean = given(args[8]), rstd = given(args[9]);
+        for (const at::Tensor* t : {&weight, static_cast<const at::Tensor*>(&bias)})
+            if (t->defined() && (!array(*t, type, N, dev) || t->dim() != 1 || t->size(0) != N)) Py_RETURN_NONE;
+        if (!rows_of(residual, M, N, dev) || !rows_of(sum, M, N, dev) || !rows_of(Y, M, N, dev) || !vector_of(mean, M, dev) || !vector_of(rstd, M, dev)) Py_RETURN_NONE;
+        const at::TensorOptions options = X.options().requires_grad(false);
+        lowra_status st;
+        {
+            Released released;
+            void* stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
+            if (!Y.defined()) Y = at::empty({M, N}, options);
+            if (!sum.defined() && residual.defined()) sum = at::empty({M, N}, options);
+            if (!rstd.defined()) rstd = at::empty({M}, options.dtype(at::kFloat));
+            if (!mean.defined() && kind == LOWRA_NORM_LAYER) mean = at::empty({M}, options.dtype(at::kFloat));
+            st = library.norm_forward(bf16(X), bf16_or_null(residual), weight.data_ptr(), bias.defined() ? bias.data_ptr() : nullptr, type == at::kFloat, (int32_t)M, (int32_t)N, kind,
+                                      (float)eps, bf16_or_null(sum), bf16(Y), fp32(mean), fp32(rstd), stream);
+        }
+        if (st != LOWRA_OK) return PyLong_FromLong(st);
+        return results({{args[7], &Y}, {args[9], &rstd}, {args[8], &mean}, {args[6], &sum}});
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+}
+
+PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 11 || library.forward == nullptr || !PyBool_Check(args[9]) || !each_plain_or_none(args, {4, 5, 6, 7, 8, 10})) Py_RETURN_NONE;
+    for (int i = 0; i < 4; ++i)
+        if (!plain(args[i])) Py_RETURN_NONE;
+    try {
+        const int64_t dev = c10::cuda::current_device();
+        const at::Tensor &dY = THPVariable_Unpack(args[0]), &X = THPVariable_Unpack(args[1]), &weight = THPVariable_Unpack(args[2]), &rstd = THPVariable_Unpack(args[3]);
+        if (X.dim() != 2) Py_RETURN_NONE;
+        const int64_t M = X.size(0), N = X.size(1);
+        const at::ScalarType type = weight.scalar_type();
+        if (M > INT32_MAX || N > INT32_MAX || !matrix(X, M, N, dev) || !matrix(dY, M, N, dev) || (type != at::kFloat && type != at::kBFloat16) || !array(weight, type, N, dev) ||
+            weight.dim() != 1 || weight.size(0) != N || !vector_of(rstd, M, dev))
+            Py_RETURN_NONE;
+        at::Tensor mean = given(args[4]), dsum = given(args[5]), dX = given(args[6]), dweight = given(args[7]), dbias = given(args[8]), workspace = given(args[10]);
+        if (!vector_of(mean, M, dev) || !rows_of(dsum, M, N, dev) || !rows_of(dX, M, N, dev) || !vector_of(dweight, N, dev) || !vector_of(dbias, N, dev) ||
+            (workspace.defined() && !on(workspace, dev)))
+            Py_RETURN_NONE;
+        const at::TensorOptions options = X.options().requires_grad(false);
+        const bool want = args[9] == Py_True;
+        lowra_status st;
+        {
+            Released released;
+            void* stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
+            if (!dX.defined()) dX = at::empty({M, N}, options);
+            if (!dweight.defined() && want) dweight = at::empty({N}, options.dtype(at::kFloat));
+            if (!dbias.defined() && want && mean.defined()) dbias = at::empty({N}, options.dtype(at::kFloat));
+            if (!workspace.defined() && (dweight.defined() || dbias.defined()))
+                workspace = at::empty({(int64_t)std::max<size_t>(library.norm_bytes((int32_t)M, (int32_t)N), 256)}, options.dtype(at::kByte));
+            st = library.norm_backward(bf16(dY), bf16(X), weight.data_ptr(), type == at::kFloat, fp32(mean), fp32(rstd), bf16_or_null(dsum), (int32_t)M, (int32_t)N, bf16(dX),
+                                       fp32(dweight), fp32(dbias), workspace.defined() ? workspace.data_ptr() : nullptr, workspace.defined() ? (size_t)workspace.nbytes() : 0, stream);
+        }
+        if (st != LOWRA_OK) return PyLong_FromLong(st);
+        return results({{args[6], &dX}, {args[7], &dweight}, {args[8], &dbias}});
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+}
+
+PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    double scale = 1.0;
+    if (n != 9 || library.forward == nullptr || !plain(args[0]) || !plain(args[1]) || !plain(args[2]) || !PyBool_Check(args[4]) || !PyBool_Check(args[5]) || !number(args[6], &scale) ||
+        !each_plain_or_none(args, {3, 7, 8}) || (args[3] == Py_None && args[8] != Py_None))
+        Py_RETURN_NONE;
+    try {
+        const int64_t dev = c10::cuda::current_device();
+        const at::Tensor &q = THPVariable_Unpack(args[0]), &positions = THPVariable_Unpack(args[1]), &turns = THPVariable_Unpack(args[2]);
+        if (q.dim() != 3 || positions.dim() != 1 || turns.dim() != 1) Py_RETURN_NONE;
+        const int64_t M = q.size(0), D = q.size(2), pairs = turns.size(0);
+        if (M > INT32_MAX || D > INT32_MAX || pairs > 65536 || !array(positions, at::kInt, M, dev) || positions.size(0) != M || !on(turns, dev) ||
+            (turns.scalar_type() != at::kLong && turns.scalar_type() != at::kUInt64))
+            Py_RETURN_NONE;
+        const int count = args[3] == Py_None ? 1 : 2;
+        at::Tensor x[2] = {q, given(args[3])}, out[2] = {given(args[7]), given(args[8])};
+        lowra_rotary_part parts[2] = {};
+        for (int i = 0; i < count; ++i)
+            for (const at::Tensor* t : {&x[i], &out[i]})
+                if (t->defined() && (t->device() != at::Device(at::kCUDA, (c10::DeviceIndex)dev) || t->scalar_type() != at::kBFloat16 || t->dim() != 3 || t->size(0) != M ||
+                                     t->size(1) != x[i].size(1) || t->size(1) > INT32_MAX || t->size(2) != D || (D > 1 && t->stride(2) != 1)))
+                    Py_RETURN_NONE;
+        lowra_status st;
+        {
+            Released released;
+            void* stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
+            for (int i = 0; i < count; ++i) {
+                if (!out[i].defined()) out[i] = at::empty({M, x[i].size(1), D}, q.options().requires_grad(false));
+                parts[i] = lowra_rotary_part{bf16(x[i]), bf16(out[i]), x[i].stride(0), x[i].stride(1), out[i].stride(0), out[i].stride(1), (int32_t)x[i].size(1)};
+            }
+            st = library.rotary(parts, count, (int32_t)M, (int32_t)D, (int32_t)(2 * pairs), static_cast<const int32_t*>(positions.data_ptr()),
+                                static_cast<const uint64_t*>(turns.data_ptr()), (float)scale, args[4] == Py_True, args[5] == Py_True, stream);
+        }
+        if (st != LOWRA_OK) return PyLong_FromLong(st);
+        if (count == 2) return results({{args[7], &out[0]}, {args[8], &out[1]}});
+        return args[7] != Py_None ? Py_NewRef(args[7]) : THPVariable_Wrap(std::move(out[0]));
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+}
+
+PyObject* cross_entropy(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    double scale = 1.0;
+    int overflow = 0;
+    if (n != 10 || library.forward == nullptr || !plain(args[0]) || !plain(args[1]) || !plain(args[2]) || !number(args[3], &scale) || !PyLong_CheckExact(args[5]) ||
+        !PyBool_Check(args[8]) || !each_plain_or_none(args, {4, 6, 7, 9}))
+        Py_RETURN_NONE;
+    const long long ignore = PyLong_AsLongLongAndOverflow(args[5], &overflow);
+    if (overflow != 0) Py_RETURN_NONE;
+    try {
+        const int64_t dev = c10::cuda::current_device();
+        const at::Tensor &X = THPVariable_Unpack(args[0]), &W = THPVariable_Unpack(args[1]), &labels = THPVariable_Unpack(args[2]);
+        if (X.dim() != 2 || W.dim() != 2 || labels.dim() != 1) Py_RETURN_NONE;
+        const int64_t M = X.size(0), K = X.size(1), V = W.size(0);
+        at::Tensor weights = given(args[4]), loss = given(args[6]), dX = given(args[7]), workspace = given(args[9]);
+        if (M > INT32_MAX || K > INT32_MAX || V > INT32_MAX || !matrix(X, M, K, dev) || !matrix(W, V, K, dev) || !array(labels, at::kLong, M, dev) || labels.size(0) != M ||
+            !vector_of(weights, M, dev) || !vector_of(loss, M, dev) || !rows_of(dX, M, K, dev) || (workspace.defined() && !on(workspace, dev)))
+            Py_RETURN_NONE;
+        const bool grad = dX.defined() || args[8] == Py_True;
+        const at::TensorOptions options = X.options().requires_grad(false);
+        lowra_status st;
+        {
+            Released released;
+            void* stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
+            if (!loss.defined()) loss = at::empty({M}, options.dtype(at::kFloat));
+            if (!dX.defined() && grad) dX = at::empty({M, K}, options);
+            if (!workspace.defined()) {
+                const size_t bytes = library.loss_bytes((int32_t)M, (int32_t)V, (int32_t)K, grad);
+                if (bytes > 0) workspace = at::empty({(int64_t)bytes}, options.dtype(at::kByte));
+            }
+            st = workspace.defined() ? library.loss(bf16(X), bf16(W), static_cast<const int64_t*>(labels.data_ptr()), fp32(weights), (int32_t)M, (int32_t)V, (int32_t)K, ignore,
+                                                    (float)scale, fp32(loss), bf16_or_null(dX), workspace.data_ptr(), (size_t)workspace.nbytes(), stream)
+                                     : LOWRA_ERR_SHAPE;
+        }
+        if (st != LOWRA_OK) return PyLong_FromLong(st);
+        return results({{args[6], &loss}, {args[7], &dX}});
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+}
+
+PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    lowra_adamw_step step = {};
+    if (n != 7 || library.forward == nullptr || !PyList_CheckExact(args[0]) || !PyTuple_CheckExact(args[2]) || PyTuple_GET_SIZE(args[2]) != 2 ||
+        !number(PyTuple_GET_ITEM(args[2], 0), &step.beta1) || !number(PyTuple_GET_ITEM(args[2], 1), &step.beta2) || !number(args[3], &step.eps) ||
+        !number(args[4], &step.weight_decay))
+        Py_RETURN_NONE;
+    int32_t t = 0;
+    const bool lr_here = number(args[1], &step.lr), step_here = number(args[5], &t);
+    if ((!lr_here && !plain(args[1])) || (!step_here && !plain(args[5])) || (args[6] != Py_None && !plain(args[6]))) Py_RETURN_NONE;
+    step.step = t;
+    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
+    if (count < 1 || count > LOWRA_MAX_ADAMW) Py_RETURN_NONE;
+    // (read in this order; from kMasterOut on each may be missing)
+    enum { kGrad, kMaster, kM, kV, kMScale, kVScale, kMasterOut, kMOut, kVOut, kMScaleOut, kVScaleOut, kWeight, kNames };
+    static PyObject* names[kNames] = {};
+    if (names[kNames - 1] == nullptr) {
+        constexpr const char* kText[kNames] = {"grad", "master", "m", "v", "m_scale", "v_scale", "master_out", "m_out", "v_out", "m_scale_out", "v_scale_out", "weight"};
+        for (int i = 0; i < kNames; ++i) names[i] = PyUnicode_InternFromString(kText[i]);
+    }
+    try {
+        // the members' arrays: their dicts are the caller's, and other threads run during the call
+        std::vector<at::Tensor> held;
+        held.reserve((size_t)count * kNames + 3);
+        std::vector<lowra_adamw_member> members((size_t)count);
+        const int64_t dev = c10::cuda::current_device();
+        auto scalar = [&](PyObject* o, at::ScalarType type, const void** p) {
+            held.push_back(THPVariable_Unpack(o));
+            *p = held.back().data_ptr();
+            return array(held.back(), type, 1, dev) && held.back().numel() == 1;
+        };
+        const void *lr = nullptr, *at_step = nullptr, *factor = nullptr;
+        if ((!lr_here && !scalar(args[1], at::kFloat, &lr)) || (!step_here && !scalar(args[5], at::kInt, &at_step)) || (args[6] != Py_None && !scalar(args[6], at::kFloat, &factor)))
+            Py_RETURN_NONE;
+        step.lr_dev = static_cast<const float*>(lr);
+        step.step_dev = static_cast<const int32_t*>(at_step);
+        step.grad_scale_dev = static_cast<const float*>(factor);
+        at::ScalarType grad_type = at::kFloat, state_type = at::kFloat;
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            PyObject* m = PyList_GET_ITEM(args[0], i);
+            if (!PyDict_CheckExact(m)) Py_RETURN_NONE;
+            void* at[kNames] = {};
+            const at::Tensor* grad = nullptr;
+            int64_t elements = 0, blocks = 0;
+            for (int k = 0; k < kNames; ++k) {
+                PyObject* o = PyDict_GetItemWithError(m, names[k]);
+                if (o == nullptr || o == Py_None) {
+                    if (PyErr_Occurred() != nullptr || k < kMScale || ((k == kMScale || k == kVScale) && state_type != at::kFloat)) {
+                        PyErr_Clear();
+                        Py_RETURN_NONE;
+                    }
+                    continue;
+                }
+                if (!plain(o)) Py_RETURN_NONE;
+                held.push_back(THPVariable_Unpack(o));
+                const at::Tensor& a = held.back();
+                const bool scales = k == kMScale || k == kVScale || k == kMScaleOut || k == kVScaleOut, states = k == kM || k == kV || k == kMOut || k == kVOut;
+                if (k == kGrad) {
+                    grad = &a;
+                    elements = a.numel();
+                    blocks = (elements + LOWRA_ADAMW_BLOCK - 1) / LOWRA_ADAMW_BLOCK;
+                    if (i == 0) grad_type = a.scalar_type();
+                }
+                if (k == kM && i == 0) state_type = a.scalar_type();
+                const at::ScalarType type = k == kGrad ? grad_type : k == kWeight ? at::kBFloat16 : states ? state_type : at::kFloat;
+                if (!on(a, dev) || a.scalar_type() != type || (scales && state_type == at::kFloat) || (scales ? a.dim() != 1 || a.size(0) != blocks : !a.sizes().equals(grad->sizes())))
+                    Py_RETURN_NONE;
+                at[k] = a.data_ptr();
+            }
+            auto in = [&](int k) { return static_cast<const float*>(at[k]); };
+            auto out = [&](int new_place, int old) { return static_cast<float*>(at[new_place] != nullptr ? at[new_place] : at[old]); };
+            members[(size_t)i] = lowra_adamw_member{at[kGrad], in(kMaster), out(kMasterOut, kMaster), static_cast<uint16_t*>(at[kWeight]), at[kM], out(kMOut, kM), at[kV], out(kVOut, kV),
+                                                    in(kMScale), out(kMScaleOut, kMScale), in(kVScale), out(kVScaleOut, kVScale), elements};
+        }
+        if ((grad_type != at::kFloat && grad_type != at::kBFloat16) || (state_type != at::kFloat && state_type != at::kFloat8_e4m3fn)) Py_RETURN_NONE;
+        step.bits = state_type == at::kFloat ? 32 : 8;
+        step.grad_fp32 = grad_type == at::kFloat;
+        lowra_status st;
+        {
+            Released released;
+            st = library.adamw(members.data(), (int32_t)count, &step, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream());
+        }
+        if (st != LOWRA_OK) return PyLong_FromLong(st);
+        return Py_NewRef(args[0]);
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+}
+
 // fits(device, then for each array: tensor or None, element type, least number of elements) -> whether every one is a plain tensor on that
 // device, which is the current one, without gaps, of that type and long enough; None fits.  Types: 'B' bytes of any type, 'u' uint8, 'h' bf16,
 // 'f' fp32, 'd' fp64.  The other calls' checks, a tenth of a microsecond an array where the interpreter takes one; what does not fit is looked at
@@ -532,20 +823,24 @@ PyObject* fits(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 // bind(addresses of lowra_lora_forward, lowra_lora_backward_input, lowra_workspace_bytes, lowra_workspace_init, lowra_lora_forward_batch, lowra_lora_backward_input_batch,
 // lowra_lora_backward_adapters, lowra_lora_backward_adapters_reuse, lowra_adapter_workspace_bytes, lowra_workspace_projection, lowra_lora_forward_epilogue,
-// lowra_epilogue_workspace_bytes, lowra_epilogue_backward, lowra_update_workspace_bytes, lowra_update_factors)
+// lowra_epilogue_workspace_bytes, lowra_epilogue_backward, lowra_update_workspace_bytes, lowra_update_factors, lowra_norm_workspace_bytes, lowra_norm_forward, lowra_norm_backward,
+// lowra_rotary, lowra_cross_entropy_workspace_bytes, lowra_cross_entropy, lowra_adamw)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    void* p[15] = {};
-    for (int i = 0; i < 15; ++i) {
+    constexpr int kAddresses = 22;
+    void* p[kAddresses] = {};
+    for (int i = 0; i < kAddresses; ++i) {
         p[i] = i < n ? PyLong_AsVoidPtr(args[i]) : nullptr;
         if (p[i] == nullptr) {
-            if (PyErr_Occurred() == nullptr) PyErr_SetString(PyExc_ValueError, "bind takes fifteen addresses");
+            if (PyErr_Occurred() == nullptr) PyErr_SetString(PyExc_ValueError, "bind takes twenty-two addresses");
             return nullptr;
         }
     }
     library = Library{reinterpret_cast<Product>(p[0]), reinterpret_cast<Product>(p[1]), reinterpret_cast<WorkspaceBytes>(p[2]), reinterpret_cast<WorkspaceInit>(p[3]),
                       reinterpret_cast<Batch>(p[4]), reinterpret_cast<Batch>(p[5]), reinterpret_cast<Gradients>(p[6]), reinterpret_cast<GradientsReuse>(p[7]),
                       reinterpret_cast<GradientsBytes>(p[8]), reinterpret_cast<Projection>(p[9]), reinterpret_cast<ProductEpilogue>(p[10]), reinterpret_cast<EpilogueBytes>(p[11]), reinterpret_cast<EpilogueBackward>(p[12]),
-                      reinterpret_cast<UpdateBytes>(p[13]), reinterpret_cast<Update>(p[14])};
+                      reinterpret_cast<UpdateBytes>(p[13]), reinterpret_cast<Update>(p[14]), reinterpret_cast<NormBytes>(p[15]), reinterpret_cast<NormForward>(p[16]),
+                      reinterpret_cast<NormBackward>(p[17]), reinterpret_cast<Rotary>(p[18]), reinterpret_cast<LossBytes>(p[19]), reinterpret_cast<Loss>(p[20]),
+                      reinterpret_cast<Adamw>(p[21])};
     Py_RETURN_NONE;
 }
 
@@ -559,6 +854,11 @@ PyMethodDef methods[] = {
     {"projection", (PyCFunction)(void (*)())projection, METH_FASTCALL, nullptr},
     {"epilogue_backward", (PyCFunction)(void (*)())epilogue_backward, METH_FASTCALL, nullptr},
     {"update_factors", (PyCFunction)(void (*)())update_factors, METH_FASTCALL, nullptr},
+    {"norm_forward", (PyCFunction)(void (*)())norm_forward, METH_FASTCALL, nullptr},
+    {"norm_backward", (PyCFunction)(void (*)())norm_backward, METH_FASTCALL, nullptr},
+    {"rotary", (PyCFunction)(void (*)())rotary, METH_FASTCALL, nullptr},
+    {"cross_entropy", (PyCFunction)(void (*)())cross_entropy, METH_FASTCALL, nullptr},
+    {"adamw", (PyCFunction)(void (*)())adamw, METH_FASTCALL, nullptr},
     {"fits", (PyCFunction)(void (*)())fits, METH_FASTCALL, nullptr},
     {"bind", (PyCFunction)(void (*)())bind, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
