@@ -1,17 +1,22 @@
 // lowra_cross_entropy: cross entropy over a vocabulary of V words from hidden states X [M, K] and the head's weights W [V, K], in pieces of the vocabulary, and the gradient of X:
 //     l = X W^T;   loss = log sum_v exp(l_v) - l_y;   dX = c (softmax(l) - onehot(y)) W,   c = scale * weights[m]
 // The logits are never kept.  Without the gradient a tile of them leaves, of every token, its largest and the sum of the exponentials under it.  With the gradient a piece of the
-// vocabulary at a time goes through two products: e = exp(l - R) of the piece, in bf16, into scratch; O += e W_piece in fp32.  Both work off one and the same R per token, so that the pieces
-// add up: R is the label's own logit, formed first (M dot products).  Where a tile's largest is more than 64 octaves above that, its exponentials are taken 2^lift lower, and what the
-// token has so far (its exponentials in the piece, sums and O) is brought to the largest lift between the two products: by a power of two, exactly, and hardly ever.
+// vocabulary at a time goes through two products: e = exp(l - lift) of the piece, in bf16, into scratch; O += e W_piece in fp32.  The lift of a token is a whole number of octaves,
+// zero as long as the largest logits of all its tiles are within 64 octaves of zero.  Where a tile's are not, its exponentials are taken under a lift of its own, and between the two products
+// what the token has so far (its exponentials in the piece, sums and O) is brought to the largest lift: by a power of two, exactly, and hardly ever.
 // The label's own word is left out of e and of the sum S, and comes back at the end:
-//     p_y = E / (S + E);   dX = c (O - S W_y) / (S + E);   loss = log(1 + S / E)          E = exp(l_y - R)
+//     p_y = E / (S + E);   dX = c (O - S W_y) / (S + E);   loss = log(1 + S / E)          E = exp(l_y - lift)
 // so that 1 - p_y = S / (S + E) and a small loss have no cancellation (with e_y among the others, a token known to 0.99 got its gradient to 2^-9 / 0.01).
 // That is two products of 2 M V K operations, where forming the sums first and the exponentials again would be three.
+// The tensor core adds up in fp32 without rounding to nearest, which over 256 additions takes some 2^-18 off a logit; so a logit's sum is formed in segments of 1024 features, which the epilogue
+// adds (losses over 4096 features: error against fp64 2.0e-6 -> 5e-7).
 //
 // The products: CTA pairs (clusters of two) walk over tiles of 256 tokens x up to 256 words (features), tcgen05.mma with cta_group::2, both operands by TMA, 64 contraction indices
 // (32 KB a CTA) to a stage, six stages; two accumulators in turn, so the epilogue's eight warps work on one tile while the next is formed.
-// warp 0 = TMA, 1 = MMA (of the CTA of rank 0) and TMEM, 2-9 = epilogue.  All waits are bounded (lowra_set_wait_limit); no CTA waits for another cluster.
+// warp 0 = TMA, 1 = MMA (of the CTA of rank 0) and TMEM, 4-11 = epilogue.  The 128 columns that an epilogue's thread holds, and 32 more on their way, do not fit into the 168 registers that
+// twelve warps get: the first four give some to the others.  All waits are bounded (lowra_set_wait_limit); no CTA waits for another cluster.
+#include <atomic>
+
 #include "gemm_params.cuh"
 #include "ptx.cuh"
 
@@ -22,11 +27,14 @@ namespace {
 constexpr int kTile = 256;                        // tokens, and at most so many words or features, of a pair's tile
 constexpr int kStages = 6, kDepth = 64;           // contraction indices of a stage
 constexpr uint32_t kHalfBytes = 128 * kDepth * 2, kStageBytes = 2 * kHalfBytes;
-constexpr int kThreads = 320, kEpilogue = 8;      // threads; epilogue warps
+constexpr int kThreads = 384, kEpilogue = 8, kFirstEpilogue = 4;      // threads; epilogue warps, behind four others
+constexpr int kLaunchRegisters = 168, kFewRegisters = 40, kManyRegisters = 232;   // a thread: at the launch, of the first four warps, of the others
+static_assert(128 * kFewRegisters + 256 * kManyRegisters <= kThreads * kLaunchRegisters, "what the others take, the first four have given (a larger share would be waited for without end)");
 constexpr uint32_t kSmem = kStages * kStageBytes + 1024;
 constexpr uint64_t kGrace = 50ull * 1000ull;      // after a failure: time for copies and MMAs still in flight to land
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kHeadroom = 64.0f;                // octaves above R that exponentials are let be
+constexpr float kHeadroom = 64.0f;                // octaves that the largest exponentials may be from one
+constexpr int kSegment = 16;                      // contraction blocks of a logit that are added up in the tensor memory
 constexpr int kSums = 0, kExponentials = 1, kGradient = 2;
 
 struct CeBarriers {
@@ -42,10 +50,10 @@ struct CeParams {
     int v0;                                       // the piece's first word
     int width, tiles_m, tiles_n, splits;          // columns of a tile; tiles; (gradient) parts of the contraction
     int blocks;                                   // contraction blocks in all
-    int first;                                    // (gradient) the first piece: O has no value yet
+    int first;                                    // the first piece: lift and O have no value yet
     const long long* labels;
-    const float *ref, *lift;                      // of a token: R in octaves (log2), the lift so far
-    float* label_logit;                           // (sums) l_y (out)
+    const float* lift;                            // (exponentials) a token's lift so far, in octaves
+    float* label_logit;                           // l_y (out)
     float2* stats;                                // [2 tiles_n][M]: of half a tile, (largest in octaves, or lift; sum)
     uint16_t* e;                                  // [M, ld_e]
     long long ld_e;
@@ -101,6 +109,9 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         *kb0 = (int)((long long)P.blocks * s / P.splits);
         return (int)((long long)P.blocks * (s + 1) / P.splits) - *kb0;
     };
+    auto segments_of = [&](int n) { return KIND == kGradient ? (n > 0 ? 1 : 0) : (n + kSegment - 1) / kSegment; };
+    if (warp < kFirstEpilogue) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
     if (warp == 0) {
         const bool leader = ptx::elect_one();
         ptx::fence_proxy_async_all();               // (the exponentials were written by ordinary stores)
@@ -140,49 +151,52 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             int s = 0, i = 0;
             uint32_t ph = 0;
             bool ready = false;
-            for (int u = pair; u < units && !failed; u += pairs, ++i) {
+            for (int u = pair; u < units && !failed; u += pairs) {
                 int kb0;
-                const int n = blocks_of(u, &kb0);
-                if (n == 0) { --i; continue; }      // (a short last piece: fewer blocks than parts)
-                const uint32_t acc = (uint32_t)i & 1u, d = tmem_base + acc * kTile;
-                if (!ptx::mbar_wait_lanes(&bars->tmem_empty[acc], (((uint32_t)i >> 1) & 1u) ^ 1u, abort_flag, P.wait_ns)) { failed = true; break; }
-                ptx::tc_fence_after();
-                for (int kb = 0; kb < n; ++kb) {
-                    if (!ready && !ptx::mbar_wait_lanes(&bars->full[s], ph, abort_flag, P.wait_ns)) { failed = true; break; }
+                const int n = blocks_of(u, &kb0), segments = segments_of(n);      // (none in a part without blocks: a short last piece)
+                for (int g = 0; g < segments && !failed; ++g, ++i) {
+                    const uint32_t acc = (uint32_t)i & 1u, d = tmem_base + acc * kTile;
+                    if (!ptx::mbar_wait_lanes(&bars->tmem_empty[acc], (((uint32_t)i >> 1) & 1u) ^ 1u, abort_flag, P.wait_ns)) { failed = true; break; }
                     ptx::tc_fence_after();
-                    const uint64_t a = a0 + (uint64_t)s * (kStageBytes >> 4), b = b0 + (uint64_t)s * (kStageBytes >> 4);
-                    const int here = s;
-                    if (++s == kStages) { s = 0; ph ^= 1u; }
-                    ready = __all_sync(0xffffffffu, ptx::mbar_test_wait(&bars->full[s], ph));      // (asked for ahead of its use)
-                    if (leader) {
+                    const int first = n * g / segments, last = n * (g + 1) / segments - 1;
+                    for (int kb = first; kb <= last; ++kb) {
+                        if (!ready && !ptx::mbar_wait_lanes(&bars->full[s], ph, abort_flag, P.wait_ns)) { failed = true; break; }
+                        ptx::tc_fence_after();
+                        const uint64_t a = a0 + (uint64_t)s * (kStageBytes >> 4), b = b0 + (uint64_t)s * (kStageBytes >> 4);
+                        const int here = s;
+                        if (++s == kStages) { s = 0; ph ^= 1u; }
+                        ready = __all_sync(0xffffffffu, ptx::mbar_test_wait(&bars->full[s], ph));      // (asked for ahead of its use)
+                        if (leader) {
 #pragma unroll
-                        for (uint32_t k = 0; k < kDepth / 16; ++k) ptx::umma_bf16_pair(d, a + 2u * k, b + b_step * k, idesc, (kb != 0 || k != 0) ? 1u : 0u);
-                        ptx::umma_commit_pair(&bars->empty[here]);
-                        if (kb + 1 == n) ptx::umma_commit_pair(&bars->tmem_full[acc]);
+                            for (uint32_t k = 0; k < kDepth / 16; ++k) ptx::umma_bf16_pair(d, a + 2u * k, b + b_step * k, idesc, (kb != first || k != 0) ? 1u : 0u);
+                            ptx::umma_commit_pair(&bars->empty[here]);
+                            if (kb == last) ptx::umma_commit_pair(&bars->tmem_full[acc]);
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
                 }
             }
             if (failed) bars->abort = 1u;
         }
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
         // ------------------------------------------------------------------ epilogue: a lane is a token, a warp takes half of the tile's columns, 32 at a time
-        const int q = warp & 3, ch = (warp - 2) >> 2;
+        const int q = warp & 3, ch = (warp - kFirstEpilogue) >> 2;
         const int chunks = P.width / 32, c_first = ch == 0 ? 0 : (chunks + 1) / 2, c_count = ch == 0 ? (chunks + 1) / 2 : chunks / 2;
         const uint32_t empty0 = ptx::map_to_cta(ptx::smem_u32(&bars->tmem_empty[0]), 0u);
         int i = 0;
-        for (int u = pair; u < units && !failed; u += pairs, ++i) {
+        for (int u = pair; u < units && !failed; u += pairs) {
             const int t = u % tiles, tn = t / P.tiles_m, row = t % P.tiles_m * kTile + (int)crank * 128 + q * 32 + lane;
-            const uint32_t acc = (uint32_t)i & 1u;
             const bool mine = row < P.M;
             int kb0;
-            const bool empty = KIND == kGradient && blocks_of(u, &kb0) == 0;
+            const int segments = segments_of(blocks_of(u, &kb0));
             __syncwarp();
             // what belongs to the token is asked for ahead of the tile
-            float ref = INFINITY, lift = 0.0f, scale = 1.0f;
+            float lift = -INFINITY, scale = 1.0f;
             int label = -1;
             if (mine) {
-                if (KIND == kExponentials) { ref = P.ref[row]; lift = P.lift[row]; }
+                if (KIND == kExponentials && !P.first) lift = P.lift[row];
                 if (KIND != kGradient) {
                     const long long y = P.labels[row];
                     label = y >= 0 && y < P.V ? (int)y : -1;
@@ -190,26 +204,45 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 if (KIND == kGradient && !P.first) scale = P.scale[row];
             }
             uint32_t v[4][32];
-            if (empty) {
-                --i;
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[c][j] = 0u;
-            } else {
-                if (!ptx::mbar_wait_warp(&bars->tmem_full[acc], ((uint32_t)i >> 1) & 1u, abort_flag, P.wait_ns)) { failed = true; break; }
+            // the next accumulator's columns: `take` reads them, then it is free
+            auto drain = [&](auto take) {
+                const uint32_t acc = (uint32_t)i & 1u;
+                if (!ptx::mbar_wait_warp(&bars->tmem_full[acc], ((uint32_t)i >> 1) & 1u, abort_flag, P.wait_ns)) { failed = true; return; }
                 ptx::tc_fence_after();
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (c < c_count) ptx::tmem_ld_32x32(tmem_base + acc * kTile + ((uint32_t)(q * 32) << 16) + (uint32_t)(c_first + c) * 32u, v[c]);
-                ptx::tmem_ld_wait();
+                take(tmem_base + acc * kTile + ((uint32_t)(q * 32) << 16) + (uint32_t)c_first * 32u);
                 ptx::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
                     if (crank == 0u) ptx::mbar_arrive(&bars->tmem_empty[acc]);
                     else ptx::mbar_arrive_cluster(empty0 + acc * 8u);
                 }
+                ++i;
+            };
+            if (KIND != kGradient || segments > 0) {
+                drain([&](uint32_t from) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(from + (uint32_t)c * 32u, v[c]);
+                    ptx::tmem_ld_wait();
+                });
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[c][j] = 0u;
             }
+            if constexpr (KIND != kGradient)
+                for (int g = 1; g < segments && !failed; ++g)
+                    drain([&](uint32_t from) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t w[32];
+                            ptx::tmem_ld_32x32(from + (uint32_t)c * 32u, w);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[c][j] = __float_as_uint(__uint_as_float(v[c][j]) + __uint_as_float(w[j]));
+                        }
+                    });
+            if (failed) break;
             const int n0 = tn * P.width + c_first * 32;      // the first column, in the piece
             if constexpr (KIND == kGradient) {
                 float* out = P.out + (size_t)(u / tiles) * P.M * P.N + (size_t)row * P.N + n0;
@@ -230,43 +263,44 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                     }
                 }
             } else {
-                // the label's word and those past the last do not take part
-                const int at = label - (P.v0 + n0), last = P.V - (P.v0 + n0);
-                if (__any_sync(0xffffffffu, (at >= 0 && at < c_count * 32) || last < c_count * 32)) {
+                // the label's word and those past the last do not take part, nor do columns that a narrower tile does not have
+                const int at = label - (P.v0 + n0), last = min(P.V - (P.v0 + n0), c_count * 32);
+                if (__any_sync(0xffffffffu, (at >= 0 && at < last) || last < 128)) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (c < c_count && (c * 32 + j == at || c * 32 + j >= last)) {
-                                if (KIND == kSums && c * 32 + j == at) P.label_logit[row] = __uint_as_float(v[c][j]);
-                                v[c][j] = 0xff800000u;
-                            }
+                        for (int j = 0; j < 32; ++j) {
+                            if (c * 32 + j == at && at < last) P.label_logit[row] = __uint_as_float(v[c][j]);
+                            if (c * 32 + j == at || c * 32 + j >= last) v[c][j] = 0xff800000u;
+                        }
                 }
                 float most = -INFINITY, sum = 0.0f;
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    if (c < c_count)
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) most = fmaxf(most, __uint_as_float(v[c][j]));
-                if (KIND == kSums) ref = most == -INFINITY ? 0.0f : most * kLog2e;
-                else if (most * kLog2e - ref - lift > kHeadroom) lift = ceilf(most * kLog2e - ref);
+                    for (int j = 0; j < 32; ++j) most = fmaxf(most, __uint_as_float(v[c][j]));
+                // under which the exponentials are taken, in octaves: the largest, or the token's lift
+                const float octaves = most * kLog2e;
+                float under = 0.0f;
+                if (KIND == kSums) {
+                    if (most != -INFINITY) under = octaves;
+                } else {
+                    if (lift != -INFINITY) under = lift;
+                    if (octaves - under > kHeadroom || (lift == -INFINITY && octaves - under < -kHeadroom)) under = most == -INFINITY ? under : ceilf(octaves);
+                }
                 float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                const bool lifted = KIND == kExponentials && __any_sync(0xffffffffu, lift != 0.0f);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    if (c >= c_count) continue;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
-                        float x = fmaf(__uint_as_float(v[c][j]), kLog2e, -ref);
-                        if (lifted) x -= lift;
-                        const float y = exp2_fast(x);
+                        const float y = exp2_fast(fmaf(__uint_as_float(v[c][j]), kLog2e, -under));
                         v[c][j] = __float_as_uint(y);
                         part[j & 3] += y;
                     }
                 }
                 sum = (part[0] + part[1]) + (part[2] + part[3]);
                 if (mine) {
-                    P.stats[(size_t)(tn * 2 + ch) * P.M + row] = make_float2(KIND == kSums ? (most == -INFINITY ? -INFINITY : ref) : lift, sum);
+                    P.stats[(size_t)(tn * 2 + ch) * P.M + row] = make_float2(most == -INFINITY ? -INFINITY : under, sum);
                     if constexpr (KIND == kExponentials) {
                         uint16_t* e = P.e + (size_t)row * P.ld_e + n0;
 #pragma unroll
@@ -309,45 +343,10 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 }
 
 // ------------------------------------------------------------------------------------------------ the tokens' own numbers
-// Of a token: the label's logit, R in octaves, lift and sum so far.
+// Of a token: the label's logit, lift and sum so far, 2^-(lift added by the last piece).
 struct CeRows {
-    float *logit, *ref, *lift, *sum, *scale;
+    float *logit, *lift, *sum, *scale;
 };
-
-__device__ __forceinline__ float dot8(uint4 a, uint4 b) {
-    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        s = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
-        s = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
-    }
-    return s;
-}
-
-// The labels' logits, a warp to a token.  A token that does not count gets an R above everything, so that its exponentials are zero; one with a label that is no word gets NaN.
-__global__ void __launch_bounds__(256) label_kernel(const uint16_t* X, const uint16_t* W, const long long* labels, int M, int V, int K, long long ignore, CeRows R, uint32_t* status) {
-    pdl_enter();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0u;
-    const int m = (int)blockIdx.x * 8 + (int)(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (m >= M) return;
-    const long long y = labels[m];
-    float l = 0.0f;
-    if (y >= 0 && y < V) {
-        const uint4 *x = reinterpret_cast<const uint4*>(X + (size_t)m * K), *w = reinterpret_cast<const uint4*>(W + (size_t)y * K);
-#pragma unroll 4
-        for (int k = lane; k < K / 8; k += 32) l += dot8(__ldg(x + k), __ldg(w + k));
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-    } else if (y != ignore) {
-        l = NAN;
-    }
-    if (lane == 0) {
-        R.logit[m] = l;
-        R.ref[m] = y == ignore ? INFINITY : l * kLog2e;
-        R.lift[m] = R.sum[m] = 0.0f;
-    }
-}
 
 // Loss without a gradient: from the halves of tiles, (largest in octaves, sum) each.  32 tokens to a CTA, an eighth of the halves to a warp.
 __global__ void __launch_bounds__(256) loss_kernel(const float2* stats, int count, const float* logit, const long long* labels, int M, int V, long long ignore, float* loss) {
@@ -377,48 +376,52 @@ __global__ void __launch_bounds__(256) loss_kernel(const float2* stats, int coun
     loss[m] = top == -INFINITY ? sum : over >= 0.0f ? log1pf(sum * exp2f(-over)) : logf(sum + exp2f(over)) - over * kLn2;
 }
 
-// Between a piece's two products: the largest lift of each token, its sum, the factor for O; exponentials that were formed at a smaller lift are brought to it.
-__global__ void __launch_bounds__(256) lift_kernel(const float2* stats, int count, int M, int width, uint16_t* e, long long ld_e, CeRows R) {
+// Between a piece's two products: the largest lift of each token, its sum, the factor for O; exponentials that were formed under a smaller lift are brought to it.
+__global__ void __launch_bounds__(256) lift_kernel(const float2* stats, int count, int M, int width, int first, uint16_t* e, long long ld_e, CeRows R) {
     __shared__ float2 shared[8][32];
-    __shared__ float common[32];
+    __shared__ float common[32], least[8][32];
     __shared__ int some;
     pdl_enter();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = (int)blockIdx.x * 32 + lane;
-    if (threadIdx.x == 0) some = 0;
-    float top = 0.0f, sum = 0.0f, before = 0.0f;
-    bool unequal = false;
-    if (m < M) {
-        before = R.lift[m];
-        top = before;
-#pragma unroll 4
-        for (int i = warp; i < count; i += 8) {
-            const float2 s = stats[(size_t)i * M + m];
-            if (s.x == top) {
-                sum += s.y;
-            } else {
-                const float more = fmaxf(top, s.x);
-                sum = sum * exp2f(top - more) + s.y * exp2f(s.x - more);
-                top = more;
-                unequal = true;
-            }
-        }
-    }
-    shared[warp][lane] = make_float2(top, sum);
-    __syncthreads();
-    if (unequal) some = 1;
-    if (warp == 0) {
-        for (int w = 1; w < 8; ++w) {
-            const float2 s = shared[w][lane];
+    const float before = m < M && !first ? R.lift[m] : -INFINITY;
+    float top = before, sum = 0.0f, low = INFINITY;       // (halves of tiles without a word: minus infinity and zero)
+    auto join = [&](float2 s) {
+        if (s.x != -INFINITY && s.x != top) {
             const float more = fmaxf(top, s.x);
-            sum = sum * exp2f(top - more) + s.y * exp2f(s.x - more);
+            sum *= exp2f(top - more);
+            s.y *= exp2f(s.x - more);
             top = more;
         }
+        sum += s.y;
+    };
+    if (m < M)
+        for (int i0 = warp; i0 < count; i0 += 64) {
+            float2 s[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s[k] = i0 + 8 * k < count ? stats[(size_t)(i0 + 8 * k) * M + m] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                join(s[k]);
+                if (s[k].x != -INFINITY) low = fminf(low, s[k].x);
+            }
+        }
+    shared[warp][lane] = make_float2(top, sum);
+    least[warp][lane] = low;
+    __syncthreads();
+    if (warp == 0) {
+        for (int w = 1; w < 8; ++w) {
+            join(shared[w][lane]);
+            low = fminf(low, least[w][lane]);
+        }
         if (m < M) {
-            R.sum[m] = R.sum[m] * exp2f(before - top) + sum;
-            R.scale[m] = exp2f(before - top);
+            const float scale = before == -INFINITY ? 0.0f : exp2f(before - top);
+            R.sum[m] = first ? sum : R.sum[m] * scale + sum;
+            R.scale[m] = scale;
             R.lift[m] = top;
         }
         common[lane] = top;
+        const bool unequal = __any_sync(0xffffffffu, low < top);
+        if (lane == 0) some = unequal;
     }
     __syncthreads();
     if (some == 0) return;
@@ -426,8 +429,9 @@ __global__ void __launch_bounds__(256) lift_kernel(const float2* stats, int coun
     for (int r = 0; r < 32 && (int)blockIdx.x * 32 + r < M; ++r) {
         const int row = (int)blockIdx.x * 32 + r;
         for (int i = warp; i < count; i += 8) {
-            const float by = exp2f(stats[(size_t)i * M + row].x - common[r]);
-            if (by == 1.0f) continue;
+            const float under = stats[(size_t)i * M + row].x;
+            if (under == -INFINITY || under == common[r]) continue;
+            const float by = exp2f(under - common[r]);
             uint16_t* at = e + (size_t)row * ld_e + (size_t)(i >> 1) * width + (i & 1 ? wide : 0);
             for (int j = lane; j < (i & 1 ? narrow : wide); j += 32) at[j] = (uint16_t)pack_bf16x2(__uint_as_float((uint32_t)at[j] << 16) * by, 0.0f);
         }
@@ -445,9 +449,9 @@ __global__ void __launch_bounds__(256) finish_kernel(const float* O, int splits,
         uint4 out = make_uint4(0u, 0u, 0u, 0u);
         if (y != ignore) {
             const bool word = y >= 0 && y < V;
-            const float sum = R.sum[m], lift = R.lift[m], at = fmaf(R.logit[m], kLog2e, -R.ref[m]);      // (zero but for a rounding)
-            const float own = exp2f(at - lift), total = sum + own;
-            if (k == 0) loss[m] = lift == 0.0f ? log1pf(sum * exp2f(-at)) : logf(total) + (lift - at) * kLn2;
+            const float sum = word ? R.sum[m] : NAN, over = word ? fmaf(R.logit[m], kLog2e, -R.lift[m]) : 0.0f;      // (over: the label's logit above the lift, octaves)
+            const float own = exp2f(over), total = sum + own;
+            if (k == 0) loss[m] = sum == 0.0f ? 0.0f : over >= 0.0f ? log1pf(sum * exp2f(-over)) : logf(total) - over * kLn2;
             const float c = weights != nullptr ? scale * weights[m] : scale, a = c / total, b = a * sum;
             float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             for (int s = 0; s < splits; ++s) {
@@ -518,7 +522,7 @@ CePlan plan_of(int M, int V, int K, bool grad) {
         }
     }
     p.off_rows = 256;
-    p.off_stats = p.off_rows + 5 * up256((size_t)p.tokens * 4);
+    p.off_stats = p.off_rows + 4 * up256((size_t)p.tokens * 4);
     p.off_e = p.off_stats + up256((size_t)p.tiles * 2 * p.tokens * 8);
     p.off_out = p.off_e + (grad ? up256((size_t)p.tokens * p.tiles * p.width * 2) : 0);
     p.total = p.off_out + (grad ? up256((size_t)p.splits * p.tokens * K * 4) : 0);
@@ -531,8 +535,15 @@ template <int KIND>
 lowra_status launch_product(CeParams& P, cudaStream_t stream) {
     static SmemLimit limit = {};
     if (ensure_smem_limit(reinterpret_cast<const void*>(product_kernel<KIND>), kSmem, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
+    // (the warps' shares of the registers were added up for a kernel of this size)
+    static std::atomic<int> registers{0};
+    if (registers.load(std::memory_order_relaxed) == 0) {
+        cudaFuncAttributes of;
+        if (cudaFuncGetAttributes(&of, product_kernel<KIND>) != cudaSuccess) return LOWRA_ERR_CUDA;
+        registers.store(of.numRegs, std::memory_order_relaxed);
+    }
     const int sms = device_sm_count();
-    if (sms < 2) return LOWRA_ERR_CUDA;
+    if (sms < 2 || registers.load(std::memory_order_relaxed) != kLaunchRegisters) return LOWRA_ERR_CUDA;
     const int units = P.tiles_m * P.tiles_n * P.splits, pairs = units < sms / 2 ? units : sms / 2;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
@@ -581,7 +592,7 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
     uint32_t* status = reinterpret_cast<uint32_t*>(ws);
     const size_t row = up256((size_t)p.tokens * 4) / 4;
     float* rows = reinterpret_cast<float*>(ws + p.off_rows);
-    const CeRows R = {rows, rows + row, rows + 2 * row, rows + 3 * row, rows + 4 * row};
+    const CeRows R = {rows, rows + row, rows + 2 * row, rows + 3 * row};
     float2* stats = reinterpret_cast<float2*>(ws + p.off_stats);
     uint16_t* e = reinterpret_cast<uint16_t*>(ws + p.off_e);
     float* O = reinterpret_cast<float*>(ws + p.off_out);
@@ -601,7 +612,6 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
         P.splits = 1;
         P.blocks = (K + kDepth - 1) / kDepth;
         P.labels = labels;
-        P.ref = R.ref;
         P.lift = R.lift;
         P.label_logit = R.logit;
         P.stats = stats;
@@ -620,9 +630,6 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
                 return LOWRA_ERR_CUDA;
             continue;
         }
-        if (launch_pdl(label_kernel, (unsigned)((m + 7) / 8), 256, stream, X, W_dev, labels, m, (int)V, (int)K, (long long)ignore_index, R,
-                       pass == 0 ? status : reinterpret_cast<uint32_t*>(ws + 128)) != cudaSuccess)
-            return LOWRA_ERR_CUDA;
         CeParams G = P;
         G.N = K;
         G.width = kTile;
@@ -636,11 +643,12 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
             P.N = V - P.v0 < p.piece ? V - P.v0 : p.piece;
             P.tiles_n = (P.N + p.width - 1) / p.width;
             G.blocks = (P.N + kDepth - 1) / kDepth;
-            G.first = c == 0;
+            P.first = G.first = c == 0;
+            P.clear_status = pass == 0 && c == 0;
             // (columns that the first product does not write, in a last block that is not full, are past the end)
             if (!make_map(&G.a, e, (uint64_t)m, (uint64_t)P.tiles_n * p.width, (uint64_t)ld_e, 128)) return LOWRA_ERR_CUDA;
             if ((st = launch_product<kExponentials>(P, stream)) != LOWRA_OK) return st;
-            if (launch_pdl(lift_kernel, (unsigned)((m + 31) / 32), 256, stream, (const float2*)stats, 2 * P.tiles_n, m, p.width, e, ld_e, R) != cudaSuccess) return LOWRA_ERR_CUDA;
+            if (launch_pdl(lift_kernel, (unsigned)((m + 31) / 32), 256, stream, (const float2*)stats, 2 * P.tiles_n, m, p.width, P.first, e, ld_e, R) != cudaSuccess) return LOWRA_ERR_CUDA;
             if ((st = launch_product<kGradient>(G, stream)) != LOWRA_OK) return st;
         }
         const long long ctas = ((long long)m * (K / 8) + 255) / 256;
