@@ -23,8 +23,9 @@ namespace lowra {
 
 namespace {
 
+constexpr int kAdamResident = 4;                    // CTAs to an SM
 constexpr int kAdamThreads = 256, kAdamBlock = LOWRA_ADAMW_BLOCK;
-constexpr int kAdamMembers = 224;                   // of a launch: what kernel parameters have room for
+constexpr int kAdamFew = 16, kAdamMany = 224;       // members of a launch that its parameters have room for (24 KB of them take a launch 2 us more than 2 KB)
 static_assert(kAdamBlock == 32 * 8, "a warp's values");
 
 struct AdamMember {
@@ -38,9 +39,10 @@ struct AdamMember {
     float *m_scale_out, *v_scale_out;
     long long n;
 };
+template <int MEMBERS>
 struct AdamParams {
-    AdamMember f[kAdamMembers];
-    uint32_t first[kAdamMembers + 1];               // blocks before each factor's, and of all
+    AdamMember f[MEMBERS];
+    uint32_t first[MEMBERS + 1];                    // blocks before each factor's, and of all
     int count, grad_fp32;
     float b1, c1, b2, c2, decay, rate, root_scale, eps;
     // on the device, or null: the gradient's factor, the step and the learning rate
@@ -144,8 +146,8 @@ __device__ __forceinline__ float store_codes(uint8_t* p, int left, const float (
     return scale;
 }
 
-template <bool EIGHT>
-__global__ void __launch_bounds__(kAdamThreads, 3) adamw_kernel(const __grid_constant__ AdamParams P) {
+template <bool EIGHT, int MEMBERS>
+__global__ void __launch_bounds__(kAdamThreads, kAdamResident) adamw_kernel(const __grid_constant__ AdamParams<MEMBERS> P) {
     __shared__ float shared[3];
     pdl_enter();
     float decay = P.decay, rate = P.rate, root_scale = P.root_scale;
@@ -228,6 +230,40 @@ __global__ void __launch_bounds__(kAdamThreads, 3) adamw_kernel(const __grid_con
     }
 }
 
+template <bool EIGHT, int MEMBERS>
+lowra_status launch_adamw(const lowra_adamw_member* members, int count, const lowra_adamw_step& S, cudaStream_t stream) {
+    AdamParams<MEMBERS> P;
+    P.grad_fp32 = S.grad_fp32 != 0;
+    P.b1 = (float)S.beta1;
+    P.c1 = (float)(1.0 - S.beta1);
+    P.b2 = (float)S.beta2;
+    P.c2 = (float)(1.0 - S.beta2);
+    P.eps = (float)S.eps;
+    P.wd = S.weight_decay;
+    P.decay = (float)(1.0 - S.lr * S.weight_decay);
+    P.log_b1 = std::log(S.beta1);
+    P.log_b2 = std::log(S.beta2);
+    const double one = S.step_dev ? 1.0 : 1.0 - std::pow(S.beta1, (double)S.step);
+    P.rate = (float)((S.lr_dev ? 1.0 : S.lr) / one);
+    P.root_scale = S.step_dev ? 1.0f : (float)(1.0 / std::sqrt(1.0 - std::pow(S.beta2, (double)S.step)));
+    P.grad_scale = S.grad_scale_dev;
+    P.lr = S.lr_dev;
+    P.step = S.step_dev;
+    for (int i0 = 0; i0 < count; i0 += MEMBERS) {
+        P.count = std::min(count - i0, MEMBERS);
+        P.first[0] = 0;
+        for (int i = 0; i < P.count; ++i) {
+            const lowra_adamw_member& m = members[i0 + i];
+            P.f[i] = AdamMember{m.grad_dev, m.master_dev, m.master_out_dev, m.weight_dev, m.m_dev, m.v_dev, m.m_out_dev, m.v_out_dev,
+                                m.m_scale_dev, m.v_scale_dev, m.m_scale_out_dev, m.v_scale_out_dev, m.n};
+            P.first[i + 1] = P.first[i] + (uint32_t)((m.n + kAdamBlock - 1) / kAdamBlock);
+        }
+        const uint32_t wanted = (P.first[P.count] + kAdamThreads / 32 - 1) / (kAdamThreads / 32), most = (uint32_t)(kNumSMs * kAdamResident);
+        if (launch_pdl(adamw_kernel<EIGHT, MEMBERS>, std::min(wanted, most), kAdamThreads, stream, P) != cudaSuccess) return LOWRA_ERR_CUDA;
+    }
+    return LOWRA_OK;
+}
+
 // Something written that shares memory with anything else of the call.  In the order of their places, an array is in the way of one before it if it is in that of the one that reaches
 // furthest, among all if it is written, among the written if it is read.
 struct Place {
@@ -299,34 +335,8 @@ extern "C" lowra_status lowra_adamw(const lowra_adamw_member* members_host, int3
     if (blocks > 0x7fffffffull || any_clash(places.get(), n_places)) return LOWRA_ERR_SHAPE;
     const lowra_status st = check_device();
     if (st != LOWRA_OK) return st;
-    AdamParams P;
-    P.grad_fp32 = S.grad_fp32 != 0;
-    P.b1 = (float)S.beta1;
-    P.c1 = (float)(1.0 - S.beta1);
-    P.b2 = (float)S.beta2;
-    P.c2 = (float)(1.0 - S.beta2);
-    P.eps = (float)S.eps;
-    P.wd = S.weight_decay;
-    P.decay = (float)(1.0 - S.lr * S.weight_decay);
-    P.log_b1 = std::log(S.beta1);
-    P.log_b2 = std::log(S.beta2);
-    const double one = S.step_dev ? 1.0 : 1.0 - std::pow(S.beta1, (double)S.step);
-    P.rate = (float)((S.lr_dev ? 1.0 : S.lr) / one);
-    P.root_scale = S.step_dev ? 1.0f : (float)(1.0 / std::sqrt(1.0 - std::pow(S.beta2, (double)S.step)));
-    P.grad_scale = S.grad_scale_dev;
-    P.lr = S.lr_dev;
-    P.step = S.step_dev;
-    for (int i0 = 0; i0 < count; i0 += kAdamMembers) {
-        P.count = std::min(count - i0, kAdamMembers);
-        P.first[0] = 0;
-        for (int i = 0; i < P.count; ++i) {
-            const lowra_adamw_member& m = members_host[i0 + i];
-            P.f[i] = AdamMember{m.grad_dev, m.master_dev, m.master_out_dev, m.weight_dev, m.m_dev, m.v_dev, m.m_out_dev, m.v_out_dev,
-                                m.m_scale_dev, m.v_scale_dev, m.m_scale_out_dev, m.v_scale_out_dev, m.n};
-            P.first[i + 1] = P.first[i] + (uint32_t)((m.n + kAdamBlock - 1) / kAdamBlock);
-        }
-        const uint32_t wanted = (P.first[P.count] + kAdamThreads / 32 - 1) / (kAdamThreads / 32), most = (uint32_t)kNumSMs * 6;
-        if (launch_pdl(eight ? adamw_kernel<true> : adamw_kernel<false>, std::min(wanted, most), kAdamThreads, (cudaStream_t)stream_v, P) != cudaSuccess) return LOWRA_ERR_CUDA;
-    }
-    return LOWRA_OK;
+    const bool few = count <= kAdamFew;
+    cudaStream_t stream = (cudaStream_t)stream_v;
+    if (eight) return few ? launch_adamw<true, kAdamFew>(members_host, count, S, stream) : launch_adamw<true, kAdamMany>(members_host, count, S, stream);
+    return few ? launch_adamw<false, kAdamFew>(members_host, count, S, stream) : launch_adamw<false, kAdamMany>(members_host, count, S, stream);
 }

@@ -51,6 +51,29 @@ __device__ __forceinline__ void load_params(const void* p, int fp32, int n, floa
     }
 }
 
+// The same, read again for every row (volatile: kept over the rows, they would cost registers that the sums need).
+__device__ __forceinline__ void load_params_again(const void* p, int fp32, int n, float (&x)[8]) {
+    auto get = [](const char* from) {
+        uint4 v;
+        asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(from));
+        return v;
+    };
+    const char* from = static_cast<const char*>(p) + (size_t)n * (fp32 ? 4 : 2);
+    const uint4 a = get(from);
+    if (fp32) {
+        const uint4 b = get(from + 16);
+        x[0] = __uint_as_float(a.x); x[1] = __uint_as_float(a.y); x[2] = __uint_as_float(a.z); x[3] = __uint_as_float(a.w);
+        x[4] = __uint_as_float(b.x); x[5] = __uint_as_float(b.y); x[6] = __uint_as_float(b.z); x[7] = __uint_as_float(b.w);
+    } else {
+        unpack8(a, x);
+    }
+}
+
+// 16 bytes into shared memory, not waited for.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+
 // Sums over the threads of a group (whole warps, all of one CTA), the same in every thread.  Two places in shared memory in turn, so that one barrier does: a warp
 // that is a sum ahead writes into the other one.
 template <int COUNT>
@@ -153,66 +176,73 @@ __global__ void __launch_bounds__(kMostThreads) forward_kernel(const NormParams 
     }
 }
 
-// What a thread reads of a row.
-template <int VECTORS>
-struct Row {
-    uint4 dy[VECTORS], x[VECTORS], d[VECTORS];
-    float rstd, mean;
-};
-
-// A CTA to an SM, its groups walk over the rows, the next row's loads under way while this one's sums are formed.  The parameters' gradients are summed up by the threads
-// over their rows, in registers (in shared memory where a thread has sixteen channels), then over the groups of the CTA in their order, and, by another kernel, over the CTAs
-// in theirs: no atomics, so repeated calls agree bit for bit.
+// A CTA to an SM, its groups walk over the rows.  What a thread reads of a row it has asked for some rows ahead, into places in shared memory that are its own (cp.async: no barrier,
+// no registers; 4096 rows of 4096 with dsum 40.0 us with one row ahead in registers).  The parameters' gradients are summed up by the threads over their rows, in registers (in shared memory where
+// a thread has sixteen channels), then over the groups of the CTA in their order, and, by another kernel, over the CTAs in theirs: no atomics, so repeated calls agree bit for bit.
 template <int VECTORS, bool LAYER, bool BESIDE, bool SUMS>
-__global__ void __launch_bounds__(kMostThreads, 1) backward_kernel(const NormParams P) {
-    __shared__ float shared[2][kMostThreads / 32][LAYER ? 2 : 1];
-    extern __shared__ float4 kept[];                  // VECTORS > 1: [vector][weight's, bias's][half][thread]; else, at the end, one row of sums
-    const int groups = (int)blockDim.x / P.group, mine = (int)threadIdx.x / P.group, t = (int)threadIdx.x % P.group;
-    GroupSum<LAYER ? 2 : 1> add = {shared, mine * P.group / 32, P.group / 32, mine + 1, 0};
-    constexpr int kSums = LAYER ? 2 : 1;
+__global__ void __launch_bounds__(kMostThreads, 1) backward_kernel(const NormParams P, const int depth) {
+    constexpr int kSums = LAYER ? 2 : 1, kArrays = BESIDE ? 3 : 2;
+    __shared__ float shared[2][kMostThreads / 32][kSums];
+    extern __shared__ float4 kept[];                  // VECTORS > 1: [vector][weight's, bias's][half][thread]; else, at the end, one row of sums;  behind them the rows under way
+    const int groups = (int)blockDim.x / P.group, mine = (int)threadIdx.x / P.group, t = (int)threadIdx.x % P.group, threads = (int)blockDim.x;
+    GroupSum<kSums> add = {shared, mine * P.group / 32, P.group / 32, mine + 1, 0};
     const int step = (int)gridDim.x * groups;
     float dw[8], db[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[i] = db[i] = 0.0f;
     if (SUMS && VECTORS > 1)
-        for (int k = 0; k < VECTORS * kSums * 2; ++k) kept[k * (int)blockDim.x + (int)threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < VECTORS * kSums * 2; ++k) kept[k * threads + (int)threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
+    const uint4* ring = reinterpret_cast<const uint4*>(kept + (!SUMS ? 0 : VECTORS > 1 ? VECTORS * kSums * 2 * threads : kSums * 2 * P.group)) + threadIdx.x;   // [slot][vector][array][thread]
     pdl_enter();
-    auto read = [&](long long m, Row<VECTORS>& r) {
-        if (m >= P.M) return;
-        r.rstd = P.rstd[m];
-        r.mean = LAYER ? P.mean[m] : 0.0f;
+    auto ask = [&](long long m, int slot) {
+        if (m < P.M) {
 #pragma unroll
-        for (int v = 0; v < VECTORS; ++v) {
-            const int n = (t + v * P.group) * 8;
-            if (n >= P.N) continue;
-            r.dy[v] = load8(P.dY + m * P.N + n);
-            r.x[v] = load8(P.X + m * P.N + n);
-            if (BESIDE) r.d[v] = load8(P.residual + m * P.N + n);
+            for (int v = 0; v < VECTORS; ++v) {
+                const int n = (t + v * P.group) * 8;
+                if (n >= P.N) continue;
+                const uint32_t to = ptx::smem_u32(ring + (slot * VECTORS + v) * kArrays * threads);
+                const long long at = m * P.N + n;
+                copy16(to, P.dY + at);
+                copy16(to + 16u * threads, P.X + at);
+                if (BESIDE) copy16(to + 32u * threads, P.residual + at);
+            }
         }
+        ptx::cp_async_commit();
     };
-    float wf[8];
-    if (VECTORS == 1 && t * 8 < P.N) load_params(P.weight, P.fp32, t * 8, wf);
-    Row<VECTORS> now, next;
-    long long m = (long long)blockIdx.x * groups + mine;
-    read(m, now);
+    long long m = (long long)blockIdx.x * groups + mine, ahead = m;
+    for (int k = 0; k < depth; ++k, ahead += step) ask(ahead, k);
+    float rstd = 0.0f, mean = 0.0f;
+    auto statistics = [&](long long of) {
+        if (of >= P.M) return;
+        rstd = P.rstd[of];
+        if (LAYER) mean = P.mean[of];
+    };
+    statistics(m);
+    int slot = 0;
     for (; m < P.M; m += step) {
-        if (VECTORS == 1) read(m + step, next);
+        if (depth == 1) ptx::cp_async_wait<0>();
+        else if (depth == 2) ptx::cp_async_wait<1>();
+        else ptx::cp_async_wait<3>();
         float s[kSums];
 #pragma unroll
         for (int i = 0; i < kSums; ++i) s[i] = 0.0f;
         float g[VECTORS][8], xh[VECTORS][8];
+        uint4 beside[VECTORS];
 #pragma unroll
         for (int v = 0; v < VECTORS; ++v) {
             const int n = (t + v * P.group) * 8;
             if (n >= P.N) continue;
-            if (VECTORS > 1) load_params(P.weight, P.fp32, n, wf);
-            unpack8(now.dy[v], g[v]);
-            unpack8(now.x[v], xh[v]);
+            float wf[8];
+            load_params_again(P.weight, P.fp32, n, wf);
+            const uint4* row = ring + (slot * VECTORS + v) * kArrays * threads;
+            unpack8(row[0], g[v]);
+            unpack8(row[threads], xh[v]);
+            if (BESIDE) beside[v] = row[2 * threads];
             float pw[8], pb[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (LAYER) xh[v][i] -= now.mean;
-                xh[v][i] *= now.rstd;
+                if (LAYER) xh[v][i] -= mean;
+                xh[v][i] *= rstd;
                 pw[i] = g[v][i] * xh[v][i];
                 pb[i] = g[v][i];
                 g[v][i] *= wf[i];
@@ -226,16 +256,21 @@ __global__ void __launch_bounds__(kMostThreads, 1) backward_kernel(const NormPar
                     if (LAYER) db[i] += pb[i];
                 }
             } else if (SUMS) {
-                float4* at = kept + (size_t)v * kSums * 2 * blockDim.x + threadIdx.x;
+                float4* at = kept + (size_t)v * kSums * 2 * threads + threadIdx.x;
 #pragma unroll
                 for (int k = 0; k < kSums * 2; ++k) {
-                    float4 a = at[k * blockDim.x];
+                    float4 a = at[k * threads];
                     const float* p = k < 2 ? pw + 4 * k : pb + 4 * (k - 2);
                     a.x += p[0]; a.y += p[1]; a.z += p[2]; a.w += p[3];
-                    at[k * blockDim.x] = a;
+                    at[k * threads] = a;
                 }
             }
         }
+        ask(ahead, slot);                             // into the place that has just been read
+        ahead += step;
+        if (++slot == depth) slot = 0;
+        const float scale = rstd;
+        statistics(m + step);
         add(s);
         const float along = s[0] * P.over_n, level = LAYER ? s[kSums - 1] * P.over_n : 0.0f;
 #pragma unroll
@@ -243,18 +278,16 @@ __global__ void __launch_bounds__(kMostThreads, 1) backward_kernel(const NormPar
             const int n = (t + v * P.group) * 8;
             if (n >= P.N) continue;
             float d[8];
-            if (BESIDE) unpack8(now.d[v], d);
+            if (BESIDE) unpack8(beside[v], d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 float dx = g[v][i] - xh[v][i] * along;
                 if (LAYER) dx -= level;
-                dx *= now.rstd;
+                dx *= scale;
                 g[v][i] = BESIDE ? dx + d[i] : dx;
             }
             *reinterpret_cast<uint4*>(P.Y + m * P.N + n) = pack8(g[v]);
         }
-        if (VECTORS == 1) now = next;
-        else read(m + step, now);
     }
     if (!SUMS) return;
     float* out = P.parts + (size_t)blockIdx.x * kSums * P.N;
@@ -346,12 +379,15 @@ bool in_the_way(const Span* out, int outs, const Span* in, int ins, bool same_ma
 template <int VECTORS, bool LAYER, bool BESIDE, bool SUMS>
 lowra_status launch_backward(const NormParams& P, const NormShape& S, int ctas, cudaStream_t stream) {
     static SmemLimit limit = {};
-    const size_t bytes = !SUMS ? 0 : VECTORS > 1 ? (size_t)VECTORS * (LAYER ? 2 : 1) * 2 * S.threads * 16 : (size_t)(LAYER ? 2 : 1) * 2 * S.group * 16;
+    constexpr size_t kMost = 225 * 1024;
+    const size_t sums = !SUMS ? 0 : VECTORS > 1 ? (size_t)VECTORS * (LAYER ? 2 : 1) * 2 * S.threads * 16 : (size_t)(LAYER ? 2 : 1) * 2 * S.group * 16;
+    const size_t row = (size_t)VECTORS * (BESIDE ? 3 : 2) * S.threads * 16;
+    const int depth = sums + 4 * row <= kMost ? 4 : sums + 2 * row <= kMost ? 2 : 1;        // rows ahead
     const auto kernel = backward_kernel<VECTORS, LAYER, BESIDE, SUMS>;
-    if (bytes > 48 * 1024 - 1024 && ensure_smem_limit(reinterpret_cast<const void*>(kernel), bytes, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
+    if (ensure_smem_limit(reinterpret_cast<const void*>(kernel), sums + (size_t)depth * row, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
     cudaLaunchAttribute attr[1];
-    const cudaLaunchConfig_t cfg = config_of((unsigned)ctas, S.threads, bytes, stream, attr);
-    return cudaLaunchKernelEx(&cfg, kernel, P) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
+    const cudaLaunchConfig_t cfg = config_of((unsigned)ctas, S.threads, sums + (size_t)depth * row, stream, attr);
+    return cudaLaunchKernelEx(&cfg, kernel, P, depth) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
 }
 template <int VECTORS>
 lowra_status launch_backward(const NormParams& P, const NormShape& S, int ctas, bool layer, bool beside, bool sums, cudaStream_t stream) {

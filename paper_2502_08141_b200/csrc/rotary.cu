@@ -39,95 +39,100 @@ __device__ __forceinline__ uint4 load8(const uint16_t* p) {       // (not as rea
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// A piece of work of a thread: eight pairs of a head, or eight values to copy.
+// A head's work in pieces: eight pairs each, then eight values to copy each.  A thread keeps its place in the head and goes from head to head, so that it reads the cosines and sines of a token once
+// and divides nothing on the way.
 struct Piece {
     uint4 a, b;
-    uint16_t *to_a, *to_b;                          // null: nothing to do;  to_b null: a copy
-    int pair;                                       // in the table of cosines and sines
+    uint16_t* to;                                   // null: nothing to do
+    int token;
 };
 
 template <bool INTERLEAVED>
-__device__ __forceinline__ void load_piece(const RotaryParams& P, int token0, int tokens, int head0, int heads, int i, Piece& q) {
-    const int turned = P.R / 16, per_head = turned + (P.D - P.R) / 8;
-    const int head_of = i / per_head, u = i - head_of * per_head;
-    const int token = head_of / heads;
-    int head = head0 + head_of - token * heads;
-    q.to_a = q.to_b = nullptr;
-    if (token >= tokens) return;
-    const bool second = head >= P.part[0].heads;
-    const RotaryPart& part = P.part[second ? 1 : 0];
-    if (second) head -= P.part[0].heads;
-    const uint16_t* x = part.x + (token0 + token) * part.x_token + head * part.x_head;
-    uint16_t* out = part.out + (token0 + token) * part.out_token + head * part.out_head;
-    if (u < turned) {
-        const int at = INTERLEAVED ? u * 16 : u * 8, other = INTERLEAVED ? 8 : P.R / 2;
-        q.a = load8(x + at);
-        q.b = load8(x + at + other);
-        q.to_a = out + at;
-        q.to_b = out + at + other;
-        q.pair = token * (P.R / 2) + u * 8;
-    } else if (part.copies) {
-        const int at = P.R + (u - turned) * 8;
-        q.a = load8(x + at);
-        q.to_a = out + at;
-    }
-}
-
-// (cosine, sine) of eight pairs in `table`
-template <bool INTERLEAVED>
-__device__ __forceinline__ void turn_piece(const float2* table, Piece& q) {
-    if (q.to_a == nullptr) return;
-    if (q.to_b != nullptr) {
-        const float4* t = reinterpret_cast<const float4*>(table + q.pair);
-        const uint32_t a[4] = {q.a.x, q.a.y, q.a.z, q.a.w}, b[4] = {q.b.x, q.b.y, q.b.z, q.b.w};
-        uint32_t ra[4], rb[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 c = t[i];                  // two pairs
-            if (INTERLEAVED) {
-                const uint32_t v0 = i < 2 ? a[2 * i] : b[2 * i - 4], v1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
-                const uint32_t r0 = pack_bf16x2(low(v0) * c.x - high(v0) * c.y, high(v0) * c.x + low(v0) * c.y);
-                const uint32_t r1 = pack_bf16x2(low(v1) * c.z - high(v1) * c.w, high(v1) * c.z + low(v1) * c.w);
-                if (i < 2) { ra[2 * i] = r0; ra[2 * i + 1] = r1; }
-                else { rb[2 * i - 4] = r0; rb[2 * i - 3] = r1; }
-            } else {
-                ra[i] = pack_bf16x2(low(a[i]) * c.x - low(b[i]) * c.y, high(a[i]) * c.z - high(b[i]) * c.w);
-                rb[i] = pack_bf16x2(low(b[i]) * c.x + low(a[i]) * c.y, high(b[i]) * c.z + high(a[i]) * c.w);
-            }
-        }
-        q.a = make_uint4(ra[0], ra[1], ra[2], ra[3]);
-        *reinterpret_cast<uint4*>(q.to_b) = make_uint4(rb[0], rb[1], rb[2], rb[3]);
-    }
-    *reinterpret_cast<uint4*>(q.to_a) = q.a;
-}
-
-template <bool INTERLEAVED>
-__global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_constant__ RotaryParams P) {
-    __shared__ __align__(16) float2 table[kMostPairs];        // (tokens x pairs: a thread's worth, or one token's)
+__global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_constant__ RotaryParams P) {
+    __shared__ __align__(16) float4 table[kMostPairs / 2];      // [token][pair of the piece / 2][piece]: (cosine, sine) of two pairs
     pdl_enter();
     const int tile = (int)blockIdx.x / P.splits, split = (int)blockIdx.x - tile * P.splits;
     const int token0 = tile * P.tokens, tokens = min(P.tokens, P.M - token0);
     const int head0 = P.heads * split / P.splits, heads = P.heads * (split + 1) / P.splits - head0;
-    const int pieces = tokens * heads * (P.R / 16 + (P.D - P.R) / 8), pairs = P.R / 2;
-    constexpr int kAhead = 2;
+    const int turned = P.R / 16, per_head = turned + (P.D - P.R) / 8, pairs = P.R / 2;
+    const int lanes = max(1, kRotaryThreads / per_head);       // heads side by side (a head of more pieces than threads: one, its pieces in turns)
+    const int other = INTERLEAVED ? 8 : P.R / 2;
+    constexpr int kAhead = 4;
     Piece q[kAhead];
+    for (int u0 = (int)threadIdx.x % per_head, lane = (int)threadIdx.x / per_head, first = 1; first || u0 < per_head; u0 += kRotaryThreads, first = 0) {
+        const int u = u0;
+        const bool turns = u < turned;
+        const int at = turns ? (INTERLEAVED ? u * 16 : u * 8) : P.R + (u - turned) * 8;
+        int token = 0, head = lane;                 // of the next piece to load
+        auto load = [&](Piece& p) {
+            while (head >= heads) { head -= heads; ++token; }
+            p.to = nullptr;
+            p.token = token;
+            if (token < tokens && lane < lanes) {
+                const bool second = head0 + head >= P.part[0].heads;
+                const RotaryPart& part = P.part[second ? 1 : 0];
+                const int h = head0 + head - (second ? P.part[0].heads : 0);
+                if (turns || part.copies) {
+                    const uint16_t* x = part.x + (long long)(token0 + token) * part.x_token + (long long)h * part.x_head + at;
+                    p.a = load8(x);
+                    if (turns) p.b = load8(x + other);
+                    p.to = part.out + (long long)(token0 + token) * part.out_token + (long long)h * part.out_head + at;
+                }
+            }
+            head += lanes;
+        };
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) load_piece<INTERLEAVED>(P, token0, tokens, head0, heads, (int)threadIdx.x + k * kRotaryThreads, q[k]);
-    for (int i = threadIdx.x; i < tokens * pairs; i += kRotaryThreads) {
-        const int token = i / pairs;
-        // the turn's fraction, to the nearest 2^-32, as half turns from -1 to 1
-        const unsigned long long turn = (unsigned long long)(long long)P.positions[token0 + token] * P.turns[i - token * pairs] + 0x80000000ull;
-        float s, c;
-        sincospif((float)(int32_t)(uint32_t)(turn >> 32) * 0x1p-31f, &s, &c);
-        table[i] = make_float2(c * P.scale, (P.inverse ? -s : s) * P.scale);
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < pieces; i += kAhead * kRotaryThreads) {
+        for (int k = 0; k < kAhead; ++k) load(q[k]);
+        if (first) {
+            for (int i = threadIdx.x; i < tokens * pairs; i += kRotaryThreads) {
+                const int m = i / pairs, pair = i - m * pairs;
+                // the turn's fraction, to the nearest 2^-32, as half turns from -1 to 1
+                const unsigned long long turn = (unsigned long long)(long long)P.positions[token0 + m] * P.turns[pair] + 0x80000000ull;
+                float s, c;
+                sincospif((float)(int32_t)(uint32_t)(turn >> 32) * 0x1p-31f, &s, &c);
+                reinterpret_cast<float2*>(table + (m * 4 + (pair & 7) / 2) * turned + pair / 8)[pair & 1] = make_float2(c * P.scale, (P.inverse ? -s : s) * P.scale);
+            }
+            __syncthreads();
+        }
+        int have = -1;                              // the token whose cosines and sines are at hand
+        float4 cs[4];
+        auto finish = [&](Piece& p) {
+            if (p.to == nullptr) return;
+            if (turns) {
+                if (p.token != have) {
+                    have = p.token;
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) turn_piece<INTERLEAVED>(table, q[k]);
-        if (i + kAhead * kRotaryThreads < pieces)
+                    for (int i = 0; i < 4; ++i) cs[i] = table[(have * 4 + i) * turned + u];
+                }
+                const uint32_t a[4] = {p.a.x, p.a.y, p.a.z, p.a.w}, b[4] = {p.b.x, p.b.y, p.b.z, p.b.w};
+                uint32_t ra[4], rb[4];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) load_piece<INTERLEAVED>(P, token0, tokens, head0, heads, i + (kAhead + k) * kRotaryThreads, q[k]);
+                for (int i = 0; i < 4; ++i) {
+                    const float4 c = cs[i];         // two pairs
+                    if (INTERLEAVED) {
+                        const uint32_t v0 = i < 2 ? a[2 * i] : b[2 * i - 4], v1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
+                        const uint32_t r0 = pack_bf16x2(low(v0) * c.x - high(v0) * c.y, high(v0) * c.x + low(v0) * c.y);
+                        const uint32_t r1 = pack_bf16x2(low(v1) * c.z - high(v1) * c.w, high(v1) * c.z + low(v1) * c.w);
+                        if (i < 2) { ra[2 * i] = r0; ra[2 * i + 1] = r1; }
+                        else { rb[2 * i - 4] = r0; rb[2 * i - 3] = r1; }
+                    } else {
+                        ra[i] = pack_bf16x2(low(a[i]) * c.x - low(b[i]) * c.y, high(a[i]) * c.z - high(b[i]) * c.w);
+                        rb[i] = pack_bf16x2(low(b[i]) * c.x + low(a[i]) * c.y, high(b[i]) * c.z + high(a[i]) * c.w);
+                    }
+                }
+                *reinterpret_cast<uint4*>(p.to) = make_uint4(ra[0], ra[1], ra[2], ra[3]);
+                *reinterpret_cast<uint4*>(p.to + other) = make_uint4(rb[0], rb[1], rb[2], rb[3]);
+            } else {
+                *reinterpret_cast<uint4*>(p.to) = p.a;
+            }
+        };
+        while (q[0].token < tokens) {               // (pieces come in order: where the first of four is past the end, so are the others)
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                finish(q[k]);
+                load(q[k]);
+            }
+        }
     }
 }
 
