@@ -23,7 +23,10 @@ namespace lowra {
 
 namespace {
 
-constexpr int kAdamResident = 4;                    // CTAs to an SM
+// CTAs to an SM: with fp32 states the memory is bound by the number of streams that it serves (448 factors: 738 us with three, 815 with four, 926 with six); with 8-bit ones loads have to
+// hide more work
+template <bool EIGHT>
+constexpr int kAdamResident = EIGHT ? 5 : 3;
 constexpr int kAdamThreads = 256, kAdamBlock = LOWRA_ADAMW_BLOCK;
 constexpr int kAdamFew = 16, kAdamMany = 224;       // members of a launch that its parameters have room for (24 KB of them take a launch 2 us more than 2 KB)
 static_assert(kAdamBlock == 32 * 8, "a warp's values");
@@ -61,6 +64,10 @@ __device__ __forceinline__ T load(const void* p) {  // (not as read-only memory:
         asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
     return v;
 }
+
+__device__ __forceinline__ float2 mul2(float2 a, float b) { return lowra::mul2(a, make_float2(b, b)); }
+// Sums of two products each, every operation rounded by itself (an add.rn.f32x2 behind a mul.rn.f32x2 came out as one operation, rounded once; single additions do not).
+__device__ __forceinline__ float2 add_products(float2 a, float2 b) { return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y)); }
 
 // Eight values of a lane: `left` of them exist (eight but at a factor's end).
 __device__ __forceinline__ void load_floats(const float* p, int left, float (&x)[8]) {
@@ -113,23 +120,30 @@ __device__ __forceinline__ void load_codes(const uint8_t* p, int left, float sca
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3)));
-        x[2 * i] = __fmul_rn(f.x, scale);
-        x[2 * i + 1] = __fmul_rn(f.y, scale);
+        const float2 v = mul2(f, scale);
+        x[2 * i] = v.x;
+        x[2 * i + 1] = v.y;
     }
 }
-// The block's scale and the lane's codes.  Magnitudes are compared as integers: a NaN is above all, and its scale is NaN.
+// The larger magnitude; a NaN is above all.
+__device__ __forceinline__ float larger(float a, float b) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(fabsf(b)));
+    return m;
+}
+// The block's scale and the lane's codes.  Over the lanes magnitudes are compared as integers: a NaN is above all there too, and its scale is NaN.
 template <bool ROOT>
 __device__ __forceinline__ float store_codes(uint8_t* p, int left, const float (&x)[8]) {
-    uint32_t most = 0u;
+    float most = fabsf(x[0]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
-    float scale = __fmul_rn(__uint_as_float(__reduce_max_sync(0xffffffffu, most)), 1.0f / 448.0f);
+    for (int i = 1; i < 8; ++i) most = larger(most, x[i]);
+    float scale = __fmul_rn(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most))), 1.0f / 448.0f);
     if (scale < 0x1p-126f) scale = 0.0f;             // its reciprocal would be out of range: the block is zero
     const float over = scale > 0.0f ? __frcp_rn(scale) : 0.0f;
     uint32_t w[2] = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        float2 f = make_float2(__fmul_rn(x[2 * i], over), __fmul_rn(x[2 * i + 1], over));
+        float2 f = mul2(make_float2(x[2 * i], x[2 * i + 1]), over);
         if (ROOT) {
             if (f.x > 0.0f) f.x = fmaxf(f.x, 0x1p-9f);
             if (f.y > 0.0f) f.y = fmaxf(f.y, 0x1p-9f);
@@ -147,7 +161,7 @@ __device__ __forceinline__ float store_codes(uint8_t* p, int left, const float (
 }
 
 template <bool EIGHT, int MEMBERS>
-__global__ void __launch_bounds__(kAdamThreads, kAdamResident) adamw_kernel(const __grid_constant__ AdamParams<MEMBERS> P) {
+__global__ void __launch_bounds__(kAdamThreads, kAdamResident<EIGHT>) adamw_kernel(const __grid_constant__ AdamParams<MEMBERS> P) {
     __shared__ float shared[3];
     pdl_enter();
     float decay = P.decay, rate = P.rate, root_scale = P.root_scale;
@@ -174,14 +188,17 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamResident) adamw_kernel(cons
     }
     const float grad_scale = P.grad_scale != nullptr ? *P.grad_scale : 1.0f;
     const int lane = threadIdx.x & 31;
-    const uint32_t blocks = P.first[P.count], step = gridDim.x * (kAdamThreads / 32);
-    for (uint32_t block = blockIdx.x * (kAdamThreads / 32) + (threadIdx.x >> 5); block < blocks; block += step) {
-        int lo = 0, hi = P.count;                    // first[lo] <= block < first[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (P.first[mid] <= block) lo = mid;
-            else hi = mid;
-        }
+    // A run of blocks to a CTA, its warps one beside the other; the factor of the first one is searched for, the next ones follow.
+    const uint32_t blocks = P.first[P.count], end = (uint32_t)((unsigned long long)blocks * (blockIdx.x + 1) / gridDim.x);
+    uint32_t block = (uint32_t)((unsigned long long)blocks * blockIdx.x / gridDim.x) + (threadIdx.x >> 5);
+    int lo = 0;
+    for (int hi = P.count; hi - lo > 1;) {           // first[lo] <= block < first[hi]
+        const int mid = (lo + hi) >> 1;
+        if (P.first[mid] <= block) lo = mid;
+        else hi = mid;
+    }
+    for (; block < end; block += kAdamThreads / 32) {
+        while (P.first[lo + 1] <= block) ++lo;
         const AdamMember& F = P.f[lo];
         const uint32_t in = block - P.first[lo];
         const long long at = (long long)in * kAdamBlock + lane * 8;
@@ -199,13 +216,23 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamResident) adamw_kernel(cons
         }
         float root[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float gi = P.grad_scale != nullptr ? __fmul_rn(g[i], grad_scale) : g[i];
-            if (EIGHT) v[i] = __fmul_rn(v[i], v[i]);   // (what is kept is the root)
-            m[i] = __fadd_rn(__fmul_rn(P.b1, m[i]), __fmul_rn(P.c1, gi));
-            v[i] = __fadd_rn(__fmul_rn(P.b2, v[i]), __fmul_rn(__fmul_rn(P.c2, gi), gi));
-            root[i] = __fsqrt_rn(v[i]);
-            w[i] = w[i] * decay - rate * __fdividef(m[i], root[i] * root_scale + P.eps);
+        for (int i = 0; i < 8; i += 2) {
+            float2 gg = make_float2(g[i], g[i + 1]), vv = make_float2(v[i], v[i + 1]);
+            if (P.grad_scale != nullptr) gg = mul2(gg, grad_scale);
+            if (EIGHT) vv = lowra::mul2(vv, vv);        // (what is kept is the root)
+            const float2 mm = add_products(mul2(make_float2(m[i], m[i + 1]), P.b1), mul2(gg, P.c1));
+            vv = add_products(mul2(vv, P.b2), lowra::mul2(mul2(gg, P.c2), gg));
+            m[i] = mm.x;
+            m[i + 1] = mm.y;
+            v[i] = vv.x;
+            v[i + 1] = vv.y;
+            root[i] = __fsqrt_rn(vv.x);
+            root[i + 1] = __fsqrt_rn(vv.y);
+            const float2 under = fma2(make_float2(root[i], root[i + 1]), make_float2(root_scale, root_scale), make_float2(P.eps, P.eps));
+            const float2 step2 = make_float2(__fdividef(mm.x, under.x), __fdividef(mm.y, under.y));
+            const float2 ww = fma2(step2, make_float2(-rate, -rate), mul2(make_float2(w[i], w[i + 1]), decay));
+            w[i] = ww.x;
+            w[i + 1] = ww.y;
         }
         store_floats(F.master_out + at, left, w);
         if (F.weight != nullptr) {
@@ -258,7 +285,7 @@ lowra_status launch_adamw(const lowra_adamw_member* members, int count, const lo
                                 m.m_scale_dev, m.v_scale_dev, m.m_scale_out_dev, m.v_scale_out_dev, m.n};
             P.first[i + 1] = P.first[i] + (uint32_t)((m.n + kAdamBlock - 1) / kAdamBlock);
         }
-        const uint32_t wanted = (P.first[P.count] + kAdamThreads / 32 - 1) / (kAdamThreads / 32), most = (uint32_t)(kNumSMs * kAdamResident);
+        const uint32_t wanted = (P.first[P.count] + kAdamThreads / 32 - 1) / (kAdamThreads / 32), most = (uint32_t)(kNumSMs * kAdamResident<EIGHT>);
         if (launch_pdl(adamw_kernel<EIGHT, MEMBERS>, std::min(wanted, most), kAdamThreads, stream, P) != cudaSuccess) return LOWRA_ERR_CUDA;
     }
     return LOWRA_OK;

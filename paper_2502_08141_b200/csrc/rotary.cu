@@ -14,7 +14,8 @@ namespace {
 
 constexpr int kRotaryThreads = 256;
 constexpr int kMostPairs = 512;                     // R / 2
-constexpr int kMostTokens = 8;                      // of a CTA
+constexpr int kTablePairs = 2048;                   // tokens x pairs of a run (or one token's)
+constexpr int kRotaryResident = 4;                  // CTAs to an SM
 
 struct RotaryPart {
     const uint16_t* x;
@@ -26,7 +27,7 @@ struct RotaryParams {
     RotaryPart part[2];
     const int32_t* positions;
     const unsigned long long* turns;
-    int M, D, R, tokens, heads, splits;             // tokens of a CTA; heads of both parts; CTAs that share a token's heads
+    int M, D, R, tokens, heads, splits, ranges;     // tokens of a run; heads of both parts; CTAs that share a token's heads; ranges of tokens
     float scale;
     int interleaved, inverse;
 };
@@ -39,7 +40,7 @@ __device__ __forceinline__ uint4 load8(const uint16_t* p) {       // (not as rea
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// A head's work in pieces: eight pairs each, then eight values to copy each.  A thread keeps its place in the head and goes from head to head, so that it reads the cosines and sines of a token once
+// A head's work in pieces of sixteen values: eight pairs each, then values to copy.  A thread keeps its place in the head and goes from head to head, so that it reads the cosines and sines of a token once
 // and divides nothing on the way.
 struct Piece {
     uint4 a, b;
@@ -48,89 +49,95 @@ struct Piece {
 };
 
 template <bool INTERLEAVED>
-__global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_constant__ RotaryParams P) {
-    __shared__ __align__(16) float4 table[kMostPairs / 2];      // [token][pair of the piece / 2][piece]: (cosine, sine) of two pairs
+__global__ void __launch_bounds__(kRotaryThreads, kRotaryResident) rotary_kernel(const __grid_constant__ RotaryParams P) {
+    __shared__ __align__(16) float4 table[kTablePairs / 2];     // [token][pair of the piece / 2][piece]: (cosine, sine) of two pairs
     pdl_enter();
-    const int tile = (int)blockIdx.x / P.splits, split = (int)blockIdx.x - tile * P.splits;
-    const int token0 = tile * P.tokens, tokens = min(P.tokens, P.M - token0);
+    const int range = (int)blockIdx.x / P.splits, split = (int)blockIdx.x - range * P.splits;
+    const int begin = (int)((long long)P.M * range / P.ranges), end = (int)((long long)P.M * (range + 1) / P.ranges);
     const int head0 = P.heads * split / P.splits, heads = P.heads * (split + 1) / P.splits - head0;
-    const int turned = P.R / 16, per_head = turned + (P.D - P.R) / 8, pairs = P.R / 2;
+    const int turned = P.R / 16, per_head = turned + (P.D - P.R + 15) / 16, pairs = P.R / 2;
     const int lanes = max(1, kRotaryThreads / per_head);       // heads side by side (a head of more pieces than threads: one, its pieces in turns)
-    const int other = INTERLEAVED ? 8 : P.R / 2;
-    constexpr int kAhead = 4;
+    const int lane = (int)threadIdx.x / per_head;
+    constexpr int kAhead = 2;
     Piece q[kAhead];
-    for (int u0 = (int)threadIdx.x % per_head, lane = (int)threadIdx.x / per_head, first = 1; first || u0 < per_head; u0 += kRotaryThreads, first = 0) {
-        const int u = u0;
-        const bool turns = u < turned;
-        const int at = turns ? (INTERLEAVED ? u * 16 : u * 8) : P.R + (u - turned) * 8;
-        int token = 0, head = lane;                 // of the next piece to load
-        auto load = [&](Piece& p) {
-            while (head >= heads) { head -= heads; ++token; }
-            p.to = nullptr;
-            p.token = token;
-            if (token < tokens && lane < lanes) {
-                const bool second = head0 + head >= P.part[0].heads;
-                const RotaryPart& part = P.part[second ? 1 : 0];
-                const int h = head0 + head - (second ? P.part[0].heads : 0);
-                if (turns || part.copies) {
-                    const uint16_t* x = part.x + (long long)(token0 + token) * part.x_token + (long long)h * part.x_head + at;
-                    p.a = load8(x);
-                    if (turns) p.b = load8(x + other);
-                    p.to = part.out + (long long)(token0 + token) * part.out_token + (long long)h * part.out_head + at;
-                }
-            }
-            head += lanes;
-        };
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) load(q[k]);
-        if (first) {
-            for (int i = threadIdx.x; i < tokens * pairs; i += kRotaryThreads) {
-                const int m = i / pairs, pair = i - m * pairs;
-                // the turn's fraction, to the nearest 2^-32, as half turns from -1 to 1
-                const unsigned long long turn = (unsigned long long)(long long)P.positions[token0 + m] * P.turns[pair] + 0x80000000ull;
-                float s, c;
-                sincospif((float)(int32_t)(uint32_t)(turn >> 32) * 0x1p-31f, &s, &c);
-                reinterpret_cast<float2*>(table + (m * 4 + (pair & 7) / 2) * turned + pair / 8)[pair & 1] = make_float2(c * P.scale, (P.inverse ? -s : s) * P.scale);
-            }
-            __syncthreads();
-        }
-        int have = -1;                              // the token whose cosines and sines are at hand
-        float4 cs[4];
-        auto finish = [&](Piece& p) {
-            if (p.to == nullptr) return;
-            if (turns) {
-                if (p.token != have) {
-                    have = p.token;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) cs[i] = table[(have * 4 + i) * turned + u];
-                }
-                const uint32_t a[4] = {p.a.x, p.a.y, p.a.z, p.a.w}, b[4] = {p.b.x, p.b.y, p.b.z, p.b.w};
-                uint32_t ra[4], rb[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float4 c = cs[i];         // two pairs
-                    if (INTERLEAVED) {
-                        const uint32_t v0 = i < 2 ? a[2 * i] : b[2 * i - 4], v1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
-                        const uint32_t r0 = pack_bf16x2(low(v0) * c.x - high(v0) * c.y, high(v0) * c.x + low(v0) * c.y);
-                        const uint32_t r1 = pack_bf16x2(low(v1) * c.z - high(v1) * c.w, high(v1) * c.z + low(v1) * c.w);
-                        if (i < 2) { ra[2 * i] = r0; ra[2 * i + 1] = r1; }
-                        else { rb[2 * i - 4] = r0; rb[2 * i - 3] = r1; }
-                    } else {
-                        ra[i] = pack_bf16x2(low(a[i]) * c.x - low(b[i]) * c.y, high(a[i]) * c.z - high(b[i]) * c.w);
-                        rb[i] = pack_bf16x2(low(b[i]) * c.x + low(a[i]) * c.y, high(b[i]) * c.z + high(a[i]) * c.w);
+    for (int token0 = begin; token0 < end; token0 += P.tokens) {
+        const int tokens = min(P.tokens, end - token0);
+        if (token0 > begin) __syncthreads();            // the table has been read
+        bool made = false;
+        for (int u = (int)threadIdx.x % per_head; u < per_head; u += kRotaryThreads) {
+            const bool turns = u < turned;
+            const int at = turns ? (INTERLEAVED ? u * 16 : u * 8) : P.R + (u - turned) * 16, other = INTERLEAVED || !turns ? 8 : P.R / 2;
+            const bool both = turns || at + 8 < P.D;     // (the last piece to copy may have eight values)
+            int token = 0, head = lane;                 // of the next piece to load
+            auto load = [&](Piece& p) {
+                while (head >= heads) { head -= heads; ++token; }
+                p.to = nullptr;
+                p.token = token;
+                if (token < tokens && lane < lanes) {
+                    const bool second = head0 + head >= P.part[0].heads;
+                    const RotaryPart& part = P.part[second ? 1 : 0];
+                    const int h = head0 + head - (second ? P.part[0].heads : 0);
+                    if (turns || part.copies) {
+                        const uint16_t* x = part.x + (long long)(token0 + token) * part.x_token + (long long)h * part.x_head + at;
+                        p.a = load8(x);
+                        if (both) p.b = load8(x + other);
+                        p.to = part.out + (long long)(token0 + token) * part.out_token + (long long)h * part.out_head + at;
                     }
                 }
-                *reinterpret_cast<uint4*>(p.to) = make_uint4(ra[0], ra[1], ra[2], ra[3]);
-                *reinterpret_cast<uint4*>(p.to + other) = make_uint4(rb[0], rb[1], rb[2], rb[3]);
-            } else {
-                *reinterpret_cast<uint4*>(p.to) = p.a;
-            }
-        };
-        while (q[0].token < tokens) {               // (pieces come in order: where the first of four is past the end, so are the others)
+                head += lanes;
+            };
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                finish(q[k]);
-                load(q[k]);
+            for (int k = 0; k < kAhead; ++k) load(q[k]);
+            if (!made) {                                // (every thread comes by here once)
+                made = true;
+                for (int i = threadIdx.x; i < tokens * pairs; i += kRotaryThreads) {
+                    const int m = i / pairs, pair = i - m * pairs;
+                    // the turn's fraction, to the nearest 2^-32, as half turns from -1 to 1
+                    const unsigned long long turn = (unsigned long long)(long long)P.positions[token0 + m] * P.turns[pair] + 0x80000000ull;
+                    float s, c;
+                    sincospif((float)(int32_t)(uint32_t)(turn >> 32) * 0x1p-31f, &s, &c);
+                    reinterpret_cast<float2*>(table + (m * 4 + (pair & 7) / 2) * turned + pair / 8)[pair & 1] = make_float2(c * P.scale, (P.inverse ? -s : s) * P.scale);
+                }
+                __syncthreads();
+            }
+            int have = -1;                              // the token whose cosines and sines are at hand
+            float4 cs[4];
+            auto finish = [&](Piece& p) {
+                if (p.to == nullptr) return;
+                if (turns) {
+                    if (p.token != have) {
+                        have = p.token;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) cs[i] = table[(have * 4 + i) * turned + u];
+                    }
+                    const uint32_t a[4] = {p.a.x, p.a.y, p.a.z, p.a.w}, b[4] = {p.b.x, p.b.y, p.b.z, p.b.w};
+                    uint32_t ra[4], rb[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float4 c = cs[i];         // two pairs
+                        if (INTERLEAVED) {
+                            const uint32_t v0 = i < 2 ? a[2 * i] : b[2 * i - 4], v1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
+                            const uint32_t r0 = pack_bf16x2(low(v0) * c.x - high(v0) * c.y, high(v0) * c.x + low(v0) * c.y);
+                            const uint32_t r1 = pack_bf16x2(low(v1) * c.z - high(v1) * c.w, high(v1) * c.z + low(v1) * c.w);
+                            if (i < 2) { ra[2 * i] = r0; ra[2 * i + 1] = r1; }
+                            else { rb[2 * i - 4] = r0; rb[2 * i - 3] = r1; }
+                        } else {
+                            ra[i] = pack_bf16x2(low(a[i]) * c.x - low(b[i]) * c.y, high(a[i]) * c.z - high(b[i]) * c.w);
+                            rb[i] = pack_bf16x2(low(b[i]) * c.x + low(a[i]) * c.y, high(b[i]) * c.z + high(a[i]) * c.w);
+                        }
+                    }
+                    p.a = make_uint4(ra[0], ra[1], ra[2], ra[3]);
+                    p.b = make_uint4(rb[0], rb[1], rb[2], rb[3]);
+                }
+                *reinterpret_cast<uint4*>(p.to) = p.a;
+                if (both) *reinterpret_cast<uint4*>(p.to + other) = p.b;
+            };
+            while (q[0].token < tokens) {               // (pieces come in order: where the first is past the end, so is the other)
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    finish(q[k]);
+                    load(q[k]);
+                }
             }
         }
     }
@@ -258,14 +265,14 @@ extern "C" lowra_status lowra_rotary(const lowra_rotary_part* parts_host, int32_
     P.scale = scale;
     P.interleaved = interleaved != 0;
     P.inverse = inverse != 0;
-    // Where there are tokens for all SMs several times over, a CTA takes as many as give each of its threads a pair to work out; else one, its heads shared by several CTAs.
-    const int per_cta = kRotaryThreads / (dim / 2);
-    P.tokens = per_cta < 1 ? 1 : per_cta > kMostTokens ? kMostTokens : per_cta;
-    while (P.tokens > 1 && M < 4 * kNumSMs * P.tokens) --P.tokens;
-    const int tiles = (M + P.tokens - 1) / P.tokens;
-    const long long pieces = (long long)P.heads * (dim / 16 + (D - dim) / 8);
+    const int most = kTablePairs / (dim / 2), ctas = kNumSMs * kRotaryResident;
+    P.ranges = M < ctas ? M : ctas;
+    P.tokens = (M + P.ranges - 1) / P.ranges;
+    if (P.tokens > most) P.tokens = most;
+    // fewer tokens than CTAs: several share a token's heads, as long as each has a piece for every other thread
+    const long long pieces = (long long)P.heads * (dim / 16 + (D - dim + 15) / 16);
     P.splits = 1;
-    while (tiles * P.splits * 2 <= 2 * kNumSMs && P.splits * 2 <= P.heads && pieces > (long long)P.splits * kRotaryThreads / 2) P.splits *= 2;
+    while (P.ranges * P.splits * 2 <= ctas && P.splits * 2 <= P.heads && pieces > (long long)P.splits * kRotaryThreads / 2) P.splits *= 2;
     const auto kernel = P.interleaved ? rotary_kernel<true> : rotary_kernel<false>;
-    return launch_pdl(kernel, (unsigned)(tiles * P.splits), kRotaryThreads, (cudaStream_t)stream_v, P) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
+    return launch_pdl(kernel, (unsigned)(P.ranges * P.splits), kRotaryThreads, (cudaStream_t)stream_v, P) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
 }
