@@ -201,11 +201,10 @@ __global__ void __launch_bounds__(kMostThreads) forward_kernel(const NormParams 
 }
 
 // Rows that a thread has asked for ahead (cp.async: no registers), in places in shared memory that are its own, so that no barrier is needed: [slot][vector][array][thread].
-// Of kDepth rows under way half are worked on together, one barrier for their sums, and read again for the output: with one row at a time, in registers, the way through its barrier set the pace
-// (4096 rows of 4096, a residual beside: layer norm 39.9 us, gradient of the root mean square with dweight 32.3).
-template <int VECTORS, int ARRAYS>
+// DEPTH rows are under way, of which ROWS are worked on together, one barrier for their sums.
+template <int VECTORS, int ARRAYS, int ROWS, int DEPTH>
 struct Ring {
-    static constexpr int kRows = VECTORS == 1 ? 2 : 1, kDepth = 2 * kRows;
+    static constexpr int kRows = ROWS, kDepth = DEPTH;
     uint4* base;
     __device__ __forceinline__ uint4* place(int slot, int v, int array) const { return base + ((slot * VECTORS + v) * ARRAYS + array) * (int)blockDim.x + (int)threadIdx.x; }
     // one row (or nothing) into a slot: a group of copies each, so that they can be counted
@@ -215,8 +214,9 @@ struct Ring {
             for (int v = 0; v < VECTORS; ++v) {
                 const int n = (t + v * P.group) * 8;
                 if (n >= P.N) continue;
+                const long long at = m * P.N + n;
 #pragma unroll
-                for (int a = 0; a < ARRAYS; ++a) copy16(ptx::smem_u32(place(slot, v, a)), from[a] + m * P.N + n);
+                for (int a = 0; a < ARRAYS; ++a) copy16(ptx::smem_u32(place(slot, v, a)), from[a] + at);
             }
         }
         ptx::cp_async_commit();
@@ -224,6 +224,12 @@ struct Ring {
     static __device__ __forceinline__ void wait() { ptx::cp_async_wait<kDepth - kRows>(); }     // the oldest kRows are there
     static size_t bytes(int threads) { return (size_t)kDepth * VECTORS * ARRAYS * threads * 16; }
 };
+// Forward: a row's values are read again for its output, from shared memory; of two rows under way (four of short rows) half are worked on together.
+template <int VECTORS, bool RESIDUAL>
+using ForwardRing = Ring<VECTORS, RESIDUAL ? 2 : 1, VECTORS == 1 ? 2 : 1, VECTORS == 1 ? 4 : 2>;
+// Backward: with eight channels to a thread they are kept in registers, with sixteen read again.
+template <int VECTORS, bool BESIDE>
+using BackwardRing = Ring<VECTORS, BESIDE ? 3 : 2, 1, VECTORS == 1 ? 4 : 2>;
 
 // Eight bf16 as four pairs.
 __device__ __forceinline__ void unpack4(uint4 v, float2 (&x)[4]) {
@@ -259,7 +265,7 @@ __device__ __forceinline__ void load_params4(const void* p, int n, float2 (&x)[4
 // The forward pass over many rows: a CTA to an SM, its groups walk over the rows.
 template <int VECTORS, bool LAYER, bool RESIDUAL, bool FP32>
 __global__ void __launch_bounds__(kMostThreads, 1) forward_rows_kernel(const NormParams P) {
-    using Rows = Ring<VECTORS, RESIDUAL ? 2 : 1>;
+    using Rows = ForwardRing<VECTORS, RESIDUAL>;
     constexpr int R = Rows::kRows;
     __shared__ __align__(16) float shared[2 * R * kSumPlaces];
     extern __shared__ uint4 under_way[];
@@ -361,12 +367,12 @@ __global__ void __launch_bounds__(kMostThreads, 1) forward_rows_kernel(const Nor
 template <int VECTORS, bool LAYER, bool BESIDE, bool SUMS, bool FP32>
 __global__ void __launch_bounds__(kMostThreads, 1) backward_kernel(const NormParams P) {
     constexpr int kSums = LAYER ? 2 : 1;
-    using Rows = Ring<VECTORS, BESIDE ? 3 : 2>;
-    constexpr int R = Rows::kRows;
-    __shared__ __align__(16) float shared[2 * R * kSums * kSumPlaces];
+    constexpr bool kHold = VECTORS == 1;              // dY weight and xh, over the row's sums
+    using Rows = BackwardRing<VECTORS, BESIDE>;
+    __shared__ __align__(16) float shared[2 * kSums * kSumPlaces];
     extern __shared__ uint4 under_way[];
     const int groups = (int)blockDim.x / P.group, mine = (int)threadIdx.x / P.group, t = (int)threadIdx.x % P.group, step = (int)gridDim.x * groups;
-    RowSum<R * kSums> add(shared, P.group, mine);
+    RowSum<kSums> add(shared, P.group, mine);
     float2 dw[VECTORS][4], db[VECTORS][4];
 #pragma unroll
     for (int v = 0; v < VECTORS; ++v)
@@ -380,119 +386,114 @@ __global__ void __launch_bounds__(kMostThreads, 1) backward_kernel(const NormPar
     pdl_enter();
     const long long first = (long long)blockIdx.x * groups + mine;
     for (int k = 0; k < Rows::kDepth; ++k) ring.ask(P, from, first + (long long)k * step, t, k);
-    float rstd[R], mean[R];
-    auto statistics = [&](long long m0) {             // of the next rows, asked for before these ones' sums
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const long long m = m0 + (long long)r * step;
-            rstd[r] = m < P.M ? P.rstd[m] : 0.0f;
-            mean[r] = LAYER && m < P.M ? P.mean[m] : 0.0f;
-        }
+    float rstd = 0.0f, mean = 0.0f;
+    auto statistics = [&](long long m) {              // of the next row, asked for before this one's sums
+        if (m >= P.M) return;
+        rstd = P.rstd[m];
+        if (LAYER) mean = P.mean[m];
     };
     statistics(first);
-    int slot0 = 0;
-    for (long long m0 = first; m0 < P.M; m0 += (long long)R * step, slot0 ^= R) {
+    int slot = 0;
+    for (long long m = first; m < P.M; m += step) {
         Rows::wait();
-        float s[R * kSums], scale[R], level[R];
+        float2 along = both(0.0f), same = both(0.0f), g[4], xh[4];
+        uint4 beside = make_uint4(0u, 0u, 0u, 0u);
+        const float scale = rstd, level = -mean;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float2 along = both(0.0f), same = both(0.0f);
-            scale[r] = rstd[r];
-            level[r] = -mean[r];
-            if (m0 + (long long)r * step < P.M)
+        for (int v = 0; v < VECTORS; ++v) {
+            const int n = (t + v * P.group) * 8;
+            if (n >= P.N) continue;
+            float2 w[4];
+            load_params4<FP32>(P.weight, n, w);
+            unpack4(*ring.place(slot, v, 0), g);
+            unpack4(*ring.place(slot, v, 1), xh);
+            if (kHold && BESIDE) beside = *ring.place(slot, v, 2);
 #pragma unroll
-                for (int v = 0; v < VECTORS; ++v) {
-                    const int n = (t + v * P.group) * 8;
-                    if (n >= P.N) continue;
-                    float2 g[4], xh[4], w[4];
-                    load_params4<FP32>(P.weight, n, w);
-                    unpack4(*ring.place(slot0 + r, v, 0), g);
-                    unpack4(*ring.place(slot0 + r, v, 1), xh);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        xh[i] = mul2(LAYER ? add2(xh[i], both(level[r])) : xh[i], both(scale[r]));
-                        const float2 product = mul2(g[i], xh[i]);
-                        if (SUMS) {
-                            dw[v][i] = add2(dw[v][i], product);
-                            if (LAYER) db[v][i] = add2(db[v][i], g[i]);
-                        }
-                        along = fma2(product, w[i], along);
-                        if (LAYER) same = fma2(g[i], w[i], same);
-                    }
+            for (int i = 0; i < 4; ++i) {
+                xh[i] = mul2(LAYER ? add2(xh[i], both(level)) : xh[i], both(scale));
+                if (SUMS) {
+                    dw[v][i] = fma2(g[i], xh[i], dw[v][i]);
+                    if (LAYER) db[v][i] = add2(db[v][i], g[i]);
                 }
-            s[r * kSums] = along.x + along.y;
-            if (LAYER) s[r * kSums + kSums - 1] = same.x + same.y;
+                g[i] = mul2(g[i], w[i]);
+                along = fma2(g[i], xh[i], along);
+                if (LAYER) same = add2(g[i], same);
+            }
         }
-        statistics(m0 + (long long)R * step);
+        if (kHold) ring.ask(P, from, m + (long long)Rows::kDepth * step, t, slot);
+        statistics(m + step);
+        float s[kSums];
+        s[0] = along.x + along.y;
+        if (LAYER) s[kSums - 1] = same.x + same.y;
         add(s);
+        // dX = scale (g - same - xh along) + dsum
+        const float by = -s[0] * P.over_n, less = LAYER ? -s[kSums - 1] * P.over_n : 0.0f;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const long long m = m0 + (long long)r * step;
-            if (m < P.M) {
-                // dX = scale (g - same - (x + level) scale along) + dsum
-                const float by = -s[r * kSums] * P.over_n * scale[r], same = LAYER ? -s[r * kSums + kSums - 1] * P.over_n : 0.0f;
+        for (int v = 0; v < VECTORS; ++v) {
+            const int n = (t + v * P.group) * 8;
+            if (n >= P.N) continue;
+            float2 d[4];
+            if constexpr (!kHold) {
+                float2 w[4];
+                load_params4<FP32>(P.weight, n, w);
+                unpack4(*ring.place(slot, v, 0), g);
+                unpack4(*ring.place(slot, v, 1), xh);
+                if (BESIDE) beside = *ring.place(slot, v, 2);
 #pragma unroll
-                for (int v = 0; v < VECTORS; ++v) {
-                    const int n = (t + v * P.group) * 8;
-                    if (n >= P.N) continue;
-                    float2 g[4], x[4], w[4], d[4];
-                    load_params4<FP32>(P.weight, n, w);
-                    unpack4(*ring.place(slot0 + r, v, 0), g);
-                    unpack4(*ring.place(slot0 + r, v, 1), x);
-                    if constexpr (BESIDE) unpack4(*ring.place(slot0 + r, v, 2), d);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float2 dx = LAYER ? fma2(g[i], w[i], both(same)) : mul2(g[i], w[i]);
-                        dx = fma2(LAYER ? add2(x[i], both(level[r])) : x[i], both(by), dx);
-                        g[i] = BESIDE ? fma2(dx, both(scale[r]), d[i]) : mul2(dx, both(scale[r]));
-                    }
-                    *reinterpret_cast<uint4*>(P.Y + m * P.N + n) = pack4(g);
+                for (int i = 0; i < 4; ++i) {
+                    xh[i] = mul2(LAYER ? add2(xh[i], both(level)) : xh[i], both(scale));
+                    g[i] = mul2(g[i], w[i]);
                 }
             }
-            ring.ask(P, from, m + (long long)Rows::kDepth * step, t, slot0 + r);
+            if (BESIDE) unpack4(beside, d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float2 dx = fma2(xh[i], both(by), LAYER ? add2(g[i], both(less)) : g[i]);
+                g[i] = BESIDE ? fma2(dx, both(scale), d[i]) : mul2(dx, both(scale));
+            }
+            *reinterpret_cast<uint4*>(P.Y + m * P.N + n) = pack4(g);
         }
+        if (!kHold) ring.ask(P, from, m + (long long)Rows::kDepth * step, t, slot);
+        if (++slot == Rows::kDepth) slot = 0;
     }
     if (!SUMS) return;
+    // all groups' sums side by side, then added up in the order of the groups
     ptx::cp_async_wait<0>();
     __syncthreads();
-    float* out = P.parts + (size_t)blockIdx.x * kSums * P.N;
-    // group after group adds its sums to those of the ones before
     float4* kept = reinterpret_cast<float4*>(under_way);
-    for (int turn = 0; turn < groups; ++turn) {
-        if (mine == turn) {
 #pragma unroll
-            for (int v = 0; v < VECTORS; ++v) {
-                const int n = (t + v * P.group) * 8;
-                if (n >= P.N) continue;
+    for (int v = 0; v < VECTORS; ++v)
 #pragma unroll
-                for (int k = 0; k < kSums * 2; ++k) {
-                    const float2* p = k < 2 ? dw[v] + 2 * k : db[v] + 2 * (k - 2);
-                    float4 a = make_float4(p[0].x, p[0].y, p[1].x, p[1].y);
-                    float4* at = kept + (v * kSums * 2 + k) * P.group + t;
-                    if (turn > 0) {
-                        const float4 b = *at;
-                        a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
-                    }
-                    if (turn + 1 < groups) *at = a;
-                    else *reinterpret_cast<float4*>(out + (size_t)(k / 2) * P.N + n + 4 * (k & 1)) = a;
-                }
-            }
+        for (int k = 0; k < kSums * 2; ++k) {
+            const float2 a = k < 2 ? dw[v][2 * (k & 1)] : db[v][2 * (k & 1)], b = k < 2 ? dw[v][2 * (k & 1) + 1] : db[v][2 * (k & 1) + 1];
+            kept[((mine * VECTORS + v) * kSums * 2 + k) * P.group + t] = make_float4(a.x, a.y, b.x, b.y);
         }
-        __syncthreads();
+    __syncthreads();
+    float* out = P.parts + (size_t)blockIdx.x * kSums * P.N;
+    const int each = VECTORS * kSums * 2 * P.group;   // of a group
+    for (int i = threadIdx.x; i < each; i += (int)blockDim.x) {
+        const int k = i / P.group % (kSums * 2), n = (i % P.group + i / P.group / (kSums * 2) * P.group) * 8;
+        if (n >= P.N) continue;
+        float4 a = kept[i];
+        for (int other = 1; other < groups; ++other) {
+            const float4 b = kept[other * each + i];
+            a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+        }
+        *reinterpret_cast<float4*>(out + (size_t)(k / 2) * P.N + n + 4 * (k & 1)) = a;
     }
 }
 
-// The gradients of the parameters from the CTAs' sums, in the order of the CTAs: 32 channels to a CTA, an eighth of the sums to each of its warps.
+// The gradients of the parameters from the CTAs' sums, in a fixed order: 32 channels to a CTA, an eighth of the sums to each of its warps.
+constexpr int kMostParts = (kNumSMs + 7) / 8;
 __global__ void __launch_bounds__(256) add_parts_kernel(const float* parts, int count, int N, int sums, float* dweight, float* dbias) {
     __shared__ float shared[8][32];
     pdl_enter();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = (int)blockIdx.x * 32 + lane, which = (int)blockIdx.y;
-    const int first = count * warp / 8, end = count * (warp + 1) / 8;
-    float total = 0.0f;
-    if (n < N) {
-#pragma unroll 8
-        for (int i = first; i < end; ++i) total += parts[((size_t)i * sums + which) * N + n];
-    }
+    float total = 0.0f, v[kMostParts];                // all of a warp's under way at once
+#pragma unroll
+    for (int i = 0; i < kMostParts; ++i) v[i] = n < N && warp + 8 * i < count ? parts[((size_t)(warp + 8 * i) * sums + which) * N + n] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMostParts; ++i) total += v[i];
     shared[warp][lane] = total;
     __syncthreads();
     if (warp != 0 || n >= N) return;
@@ -516,6 +517,7 @@ NormShape shape_of(int N, int most, int longest) {
 }
 // Many rows: what a row costs beside its elements - its reduction, its addresses - is a third less with sixteen channels to a thread.  Few rows: the shorter way.
 NormShape shape_of_many(int N) { return shape_of(N, kMostThreads, 256); }
+NormShape shape_of_backward(int N) { return shape_of(N, kMostThreads, 8 * kMostThreads); }
 NormShape shape_of_few(int M, int N) { return shape_of(N, M > kNumSMs ? kForwardThreads : 0, 8 * kMostThreads); }      // (up to one for each SM: a CTA to each)
 
 cudaLaunchConfig_t config_of(unsigned grid, int threads, size_t bytes, cudaStream_t stream, cudaLaunchAttribute* attr) {
@@ -547,7 +549,7 @@ bool in_the_way(const Span* out, int outs, const Span* in, int ins, bool same_ma
 template <int VECTORS, bool LAYER, bool BESIDE, bool SUMS, bool FP32>
 lowra_status launch_backward(const NormParams& P, const NormShape& S, int ctas, cudaStream_t stream) {
     static SmemLimit limit = {};
-    const size_t bytes = Ring<VECTORS, BESIDE ? 3 : 2>::bytes(S.threads);        // (room for the sums too: groups of two or more, 64 bytes a thread at most)
+    const size_t bytes = BackwardRing<VECTORS, BESIDE>::bytes(S.threads);        // (room for the sums too, 128 bytes a thread at most)
     const auto kernel = backward_kernel<VECTORS, LAYER, BESIDE, SUMS, FP32>;
     if (ensure_smem_limit(reinterpret_cast<const void*>(kernel), bytes, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
     cudaLaunchAttribute attr[1];
@@ -573,7 +575,7 @@ int backward_ctas(int M, int N, const NormShape& S) {
 extern "C" size_t lowra_norm_workspace_bytes(int32_t M, int32_t N) {
     using namespace lowra;
     if (!good_shape(M, N)) return 0;
-    return ((size_t)backward_ctas(M, N, shape_of_many(N)) * 2 * (size_t)N * 4 + 255) / 256 * 256;
+    return ((size_t)backward_ctas(M, N, shape_of_backward(N)) * 2 * (size_t)N * 4 + 255) / 256 * 256;
 }
 
 extern "C" lowra_status lowra_norm_forward(const uint16_t* X_dev, const uint16_t* residual_dev, const void* weight_dev, const void* bias_dev, int32_t params_fp32,
@@ -600,7 +602,7 @@ extern "C" lowra_status lowra_norm_forward(const uint16_t* X_dev, const uint16_t
         return choose([&](auto two, auto is_layer, auto with_residual, auto fp32) {
             static SmemLimit limit = {};
             const auto kernel = forward_rows_kernel<two ? 2 : 1, is_layer, with_residual, fp32>;
-            const size_t bytes = Ring<two ? 2 : 1, with_residual ? 2 : 1>::bytes(many.threads);
+            const size_t bytes = ForwardRing<two ? 2 : 1, with_residual>::bytes(many.threads);
             if (ensure_smem_limit(reinterpret_cast<const void*>(kernel), bytes, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
             cudaLaunchAttribute attr[1];
             const cudaLaunchConfig_t cfg = config_of((unsigned)kNumSMs, many.threads, bytes, stream, attr);
@@ -642,7 +644,7 @@ extern "C" lowra_status lowra_norm_backward(const uint16_t* dY_dev, const uint16
         return LOWRA_ERR_SHAPE;
     lowra_status st = check_device();
     if (st != LOWRA_OK) return st;
-    const NormShape S = shape_of_many(N);
+    const NormShape S = shape_of_backward(N);
     const int ctas = backward_ctas(M, N, S);
     NormParams P = {X_dev, dsum_dev, dY_dev, weight_dev, nullptr, nullptr, dX_dev, const_cast<float*>(mean_dev), const_cast<float*>(rstd_dev),
                     static_cast<float*>(workspace_dev), M, N, S.group, params_fp32 != 0, 0.0f, 1.0f / (float)N};
