@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kMostThreads = 1024, kMostCols = 16384, kMostRows = 1 << 30;
 constexpr int kManyRows = 2;                      // of a group, from which on the forward pass asks for its rows ahead
+constexpr int kBackwardThreads = 512;               // of a CTA of the backward pass: 128 registers to each
 constexpr int kForwardThreads = 512;              // of a CTA, where rows are short enough for several groups
 
 struct NormParams {
@@ -227,9 +228,9 @@ struct Ring {
 // Forward: a row's values are read again for its output, from shared memory; of two rows under way (four of short rows) half are worked on together.
 template <int VECTORS, bool RESIDUAL>
 using ForwardRing = Ring<VECTORS, RESIDUAL ? 2 : 1, VECTORS == 1 ? 2 : 1, VECTORS == 1 ? 4 : 2>;
-// Backward: with eight channels to a thread they are kept in registers, with sixteen read again.
+// Backward: with up to sixteen channels to a thread they are kept in registers, with 32 read again.
 template <int VECTORS, bool BESIDE>
-using BackwardRing = Ring<VECTORS, BESIDE ? 3 : 2, 1, VECTORS == 1 ? 4 : 2>;
+using BackwardRing = Ring<VECTORS, BESIDE ? 3 : 2, 1, VECTORS <= 2 ? 4 : 2>;
 
 // Eight bf16 as four pairs.
 __device__ __forceinline__ void unpack4(uint4 v, float2 (&x)[4]) {
@@ -365,9 +366,9 @@ __global__ void __launch_bounds__(kMostThreads, 1) forward_rows_kernel(const Nor
 // A CTA to an SM, its groups walk over the rows.  The parameters' gradients are summed up by the threads over their rows, in registers, then over the groups of the CTA in their order, and, by another
 // kernel, over the CTAs in theirs: no atomics, so repeated calls agree bit for bit.
 template <int VECTORS, bool LAYER, bool BESIDE, bool SUMS, bool FP32>
-__global__ void __launch_bounds__(kMostThreads, 1) backward_kernel(const NormParams P) {
+__global__ void __launch_bounds__(kBackwardThreads, 1) backward_kernel(const NormParams P) {
     constexpr int kSums = LAYER ? 2 : 1;
-    constexpr bool kHold = VECTORS == 1;              // dY weight and xh, over the row's sums
+    constexpr bool kHold = VECTORS <= 2;              // dY weight and xh, over the row's sums
     using Rows = BackwardRing<VECTORS, BESIDE>;
     __shared__ __align__(16) float shared[2 * kSums * kSumPlaces];
     extern __shared__ uint4 under_way[];
@@ -396,18 +397,20 @@ __global__ void __launch_bounds__(kMostThreads, 1) backward_kernel(const NormPar
     int slot = 0;
     for (long long m = first; m < P.M; m += step) {
         Rows::wait();
-        float2 along = both(0.0f), same = both(0.0f), g[4], xh[4];
-        uint4 beside = make_uint4(0u, 0u, 0u, 0u);
+        constexpr int kKept = kHold ? VECTORS : 1;
+        float2 along = both(0.0f), same = both(0.0f), kept_g[kKept][4], kept_xh[kKept][4];
+        uint4 kept_beside[kKept];
         const float scale = rstd, level = -mean;
 #pragma unroll
         for (int v = 0; v < VECTORS; ++v) {
             const int n = (t + v * P.group) * 8;
             if (n >= P.N) continue;
             float2 w[4];
+            float2(&g)[4] = kept_g[kHold ? v : 0], (&xh)[4] = kept_xh[kHold ? v : 0];
             load_params4<FP32>(P.weight, n, w);
             unpack4(*ring.place(slot, v, 0), g);
             unpack4(*ring.place(slot, v, 1), xh);
-            if (kHold && BESIDE) beside = *ring.place(slot, v, 2);
+            if (kHold && BESIDE) kept_beside[kHold ? v : 0] = *ring.place(slot, v, 2);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 xh[i] = mul2(LAYER ? add2(xh[i], both(level)) : xh[i], both(scale));
@@ -433,19 +436,20 @@ __global__ void __launch_bounds__(kMostThreads, 1) backward_kernel(const NormPar
             const int n = (t + v * P.group) * 8;
             if (n >= P.N) continue;
             float2 d[4];
+            float2(&g)[4] = kept_g[kHold ? v : 0], (&xh)[4] = kept_xh[kHold ? v : 0];
             if constexpr (!kHold) {
                 float2 w[4];
                 load_params4<FP32>(P.weight, n, w);
                 unpack4(*ring.place(slot, v, 0), g);
                 unpack4(*ring.place(slot, v, 1), xh);
-                if (BESIDE) beside = *ring.place(slot, v, 2);
+                if (BESIDE) kept_beside[0] = *ring.place(slot, v, 2);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     xh[i] = mul2(LAYER ? add2(xh[i], both(level)) : xh[i], both(scale));
                     g[i] = mul2(g[i], w[i]);
                 }
             }
-            if (BESIDE) unpack4(beside, d);
+            if (BESIDE) unpack4(kept_beside[kHold ? v : 0], d);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float2 dx = fma2(xh[i], both(by), LAYER ? add2(g[i], both(less)) : g[i]);
@@ -508,7 +512,7 @@ struct NormShape {
 // Rows of up to `longest` channels by eight to a thread, longer ones by sixteen; as many rows side by side in a CTA as `most` threads have room for (a named barrier to a group of
 // several warps: fifteen at most).
 NormShape shape_of(int N, int most, int longest) {
-    const int vectors = N <= longest ? 1 : 2;
+    const int vectors = N <= longest ? 1 : N <= 16 * most ? 2 : 4;
     const int group = (N / 8 + 32 * vectors - 1) / (32 * vectors) * 32;
     int groups = most / group;
     if (groups < 1) groups = 1;
@@ -517,8 +521,13 @@ NormShape shape_of(int N, int most, int longest) {
 }
 // Many rows: what a row costs beside its elements - its reduction, its addresses - is a third less with sixteen channels to a thread.  Few rows: the shorter way.
 NormShape shape_of_many(int N) { return shape_of(N, kMostThreads, 256); }
-NormShape shape_of_backward(int N) { return shape_of(N, kMostThreads, 8 * kMostThreads); }
-NormShape shape_of_few(int M, int N) { return shape_of(N, M > kNumSMs ? kForwardThreads : 0, 8 * kMostThreads); }      // (up to one for each SM: a CTA to each)
+NormShape shape_of_backward(int N) { return shape_of(N, kBackwardThreads, 2048); }
+NormShape shape_of_few(int M, int N) {      // (up to one for each SM: a CTA to each)
+    NormShape S = shape_of(N, kMostThreads, 8 * kMostThreads);
+    const int groups = M > kNumSMs && S.group < kForwardThreads ? kForwardThreads / S.group : 1;
+    S.threads = S.group * (S.group > 32 && groups > 15 ? 15 : groups);
+    return S;
+}
 
 cudaLaunchConfig_t config_of(unsigned grid, int threads, size_t bytes, cudaStream_t stream, cudaLaunchAttribute* attr) {
     cudaLaunchConfig_t cfg = {};
@@ -649,9 +658,9 @@ extern "C" lowra_status lowra_norm_backward(const uint16_t* dY_dev, const uint16
     NormParams P = {X_dev, dsum_dev, dY_dev, weight_dev, nullptr, nullptr, dX_dev, const_cast<float*>(mean_dev), const_cast<float*>(rstd_dev),
                     static_cast<float*>(workspace_dev), M, N, S.group, params_fp32 != 0, 0.0f, 1.0f / (float)N};
     cudaStream_t stream = (cudaStream_t)stream_v;
-    st = choose([&](auto two, auto is_layer, auto beside, auto with_sums, auto fp32) {
-        return launch_backward<two ? 2 : 1, is_layer, beside, with_sums, fp32>(P, S, ctas, stream);
-    }, std::tuple<>(), S.vectors == 2, layer, dsum_dev != nullptr, sums, params_fp32 != 0);
+    st = choose([&](auto four, auto two, auto is_layer, auto beside, auto with_sums, auto fp32) {
+        return launch_backward<four ? 4 : two ? 2 : 1, is_layer, beside, with_sums, fp32>(P, S, ctas, stream);
+    }, std::tuple<>(), S.vectors == 4, S.vectors == 2, layer, dsum_dev != nullptr, sums, params_fp32 != 0);
     if (st != LOWRA_OK || !sums) return st;
     cudaLaunchAttribute attr[1];
     cudaLaunchConfig_t cfg = config_of((unsigned)((N + 31) / 32), 256, 0, stream, attr);
