@@ -348,87 +348,97 @@ struct CeRows {
     float *logit, *lift, *sum, *scale;
 };
 
-// Loss without a gradient: from the halves of tiles, (largest in octaves, sum) each.  32 tokens to a CTA, an eighth of the halves to a warp.
-__global__ void __launch_bounds__(256) loss_kernel(const float2* stats, int count, const float* logit, const long long* labels, int M, int V, long long ignore, float* loss) {
-    __shared__ float2 shared[8][32];
-    pdl_enter();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = (int)blockIdx.x * 32 + lane;
-    float top = -INFINITY, sum = 0.0f;
-    auto join = [&](float2 s) {      // (empty halves: minus infinity and zero)
-        if (s.x == -INFINITY) { sum += s.y; return; }
-        const float more = fmaxf(top, s.x);
-        sum = sum * exp2f(top - more) + s.y * exp2f(s.x - more);
-        top = more;
-    };
-    if (m < M)
-#pragma unroll 4
-        for (int i = warp; i < count; i += 8) join(stats[(size_t)i * M + m]);
-    shared[warp][lane] = make_float2(top, sum);
-    __syncthreads();
-    if (warp != 0 || m >= M) return;
-    for (int w = 1; w < 8; ++w) join(shared[w][lane]);
-    const long long y = labels[m];
-    if (y == ignore || y < 0 || y >= V) {
-        loss[m] = y == ignore ? 0.0f : NAN;
-        return;
-    }
-    const float over = fmaf(logit[m], kLog2e, -top);      // the label's logit above the largest of the others, octaves
-    loss[m] = top == -INFINITY ? sum : over >= 0.0f ? log1pf(sum * exp2f(-over)) : logf(sum + exp2f(over)) - over * kLn2;
-}
-
-// Between a piece's two products: the largest lift of each token, its sum, the factor for O; exponentials that were formed under a smaller lift are brought to it.
-__global__ void __launch_bounds__(256) lift_kernel(const float2* stats, int count, int M, int width, int first, uint16_t* e, long long ld_e, CeRows R) {
-    __shared__ float2 shared[8][32];
-    __shared__ float common[32], least[8][32];
-    __shared__ int some;
-    pdl_enter();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = (int)blockIdx.x * 32 + lane;
-    const float before = m < M && !first ? R.lift[m] : -INFINITY;
-    float top = before, sum = 0.0f, low = INFINITY;       // (halves of tiles without a word: minus infinity and zero)
-    auto join = [&](float2 s) {
+// A token's halves of tiles, (octaves that the exponentials were taken under, sum of them) each, joined: eight tokens to a CTA, 32 threads to a token, eight of their loads under way at once.
+// (Halves without a word: minus infinity and zero.)  Empty in the end where no half had one.
+constexpr int kTokens = 8, kLanes = 32;
+struct Joined {
+    float top, sum, low;      // the largest of the octaves, the sum under it, the least
+    __device__ __forceinline__ void add(float2 s) {
         if (s.x != -INFINITY && s.x != top) {
             const float more = fmaxf(top, s.x);
             sum *= exp2f(top - more);
             s.y *= exp2f(s.x - more);
             top = more;
         }
+        if (s.x != -INFINITY) low = fminf(low, s.x);
         sum += s.y;
-    };
-    if (m < M)
-        for (int i0 = warp; i0 < count; i0 += 64) {
-            float2 s[8];
+    }
+    // the token's, in the threads of the first warp (all of which are there)
+    __device__ __forceinline__ void collect(const float2* stats, int count, int M, int m, float (*shared)[kTokens][3]) {
+        const int lane = (int)threadIdx.x / kTokens;
+        if (m < M)
+            for (int i0 = lane; i0 < count; i0 += 8 * kLanes) {
+                float2 s[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s[k] = i0 + 8 * k < count ? stats[(size_t)(i0 + 8 * k) * M + m] : make_float2(-INFINITY, 0.0f);
+                for (int k = 0; k < 8; ++k) s[k] = i0 + k * kLanes < count ? stats[(size_t)(i0 + k * kLanes) * M + m] : make_float2(-INFINITY, 0.0f);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                join(s[k]);
-                if (s[k].x != -INFINITY) low = fminf(low, s[k].x);
+                for (int k = 0; k < 8; ++k) add(s[k]);
             }
+        auto join = [&](float other_top, float other_sum, float other_low) {
+            low = fminf(low, other_low);
+            add(make_float2(other_top, other_sum));
+        };
+#pragma unroll
+        for (int d = 8; d < 32; d *= 2) {
+            const float a = __shfl_xor_sync(0xffffffffu, top, d), b = __shfl_xor_sync(0xffffffffu, sum, d), c = __shfl_xor_sync(0xffffffffu, low, d);
+            join(a, b, c);
         }
-    shared[warp][lane] = make_float2(top, sum);
-    least[warp][lane] = low;
-    __syncthreads();
-    if (warp == 0) {
-        for (int w = 1; w < 8; ++w) {
-            join(shared[w][lane]);
-            low = fminf(low, least[w][lane]);
+        const int warp = (int)threadIdx.x >> 5, token = (int)threadIdx.x % kTokens;
+        if ((threadIdx.x & 31) < kTokens) {
+            shared[warp][token][0] = top;
+            shared[warp][token][1] = sum;
+            shared[warp][token][2] = low;
         }
-        if (m < M) {
-            const float scale = before == -INFINITY ? 0.0f : exp2f(before - top);
-            R.sum[m] = first ? sum : R.sum[m] * scale + sum;
+        __syncthreads();
+        if (warp == 0)
+            for (int w = 1; w < kTokens * kLanes / 32; ++w) join(shared[w][token][0], shared[w][token][1], shared[w][token][2]);
+    }
+};
+
+// Loss without a gradient.
+__global__ void __launch_bounds__(kTokens * kLanes) loss_kernel(const float2* stats, int count, const float* logit, const long long* labels, int M, int V, long long ignore, float* loss) {
+    __shared__ float shared[kTokens * kLanes / 32][kTokens][3];
+    pdl_enter();
+    const int m = (int)blockIdx.x * kTokens + (int)threadIdx.x % kTokens;
+    Joined all = {-INFINITY, 0.0f, INFINITY};
+    all.collect(stats, count, M, m, shared);
+    if (threadIdx.x >= kTokens || m >= M) return;
+    const long long y = labels[m];
+    if (y == ignore || y < 0 || y >= V) {
+        loss[m] = y == ignore ? 0.0f : NAN;
+        return;
+    }
+    const float over = fmaf(logit[m], kLog2e, -all.top);      // the label's logit above the largest of the others, octaves
+    loss[m] = all.top == -INFINITY ? all.sum : over >= 0.0f ? log1pf(all.sum * exp2f(-over)) : logf(all.sum + exp2f(over)) - over * kLn2;
+}
+
+// Between a piece's two products: the largest lift of each token, its sum, the factor for O; exponentials that were formed under a smaller lift are brought to it.
+__global__ void __launch_bounds__(kTokens * kLanes) lift_kernel(const float2* stats, int count, int M, int width, int first, uint16_t* e, long long ld_e, CeRows R) {
+    __shared__ float shared[kTokens * kLanes / 32][kTokens][3];
+    __shared__ float common[kTokens];
+    __shared__ int some;
+    pdl_enter();
+    const int m0 = (int)blockIdx.x * kTokens, m = m0 + (int)threadIdx.x % kTokens;
+    const float before = m < M && !first ? R.lift[m] : -INFINITY;
+    Joined all = {before, 0.0f, INFINITY};
+    all.collect(stats, count, M, m, shared);
+    if (threadIdx.x < 32) {
+        if (threadIdx.x < kTokens && m < M) {
+            const float scale = before == -INFINITY ? 0.0f : exp2f(before - all.top);
+            R.sum[m] = first ? all.sum : R.sum[m] * scale + all.sum;
             R.scale[m] = scale;
-            R.lift[m] = top;
+            R.lift[m] = all.top;
         }
-        common[lane] = top;
-        const bool unequal = __any_sync(0xffffffffu, low < top);
-        if (lane == 0) some = unequal;
+        if (threadIdx.x < kTokens) common[threadIdx.x] = all.top;
+        const bool unequal = __any_sync(0xffffffffu, threadIdx.x < kTokens && all.low < all.top);
+        if (threadIdx.x == 0) some = unequal;
     }
     __syncthreads();
     if (some == 0) return;
-    const int chunks = width / 32, wide = (chunks + 1) / 2 * 32, narrow = chunks / 2 * 32;
-    for (int r = 0; r < 32 && (int)blockIdx.x * 32 + r < M; ++r) {
-        const int row = (int)blockIdx.x * 32 + r;
-        for (int i = warp; i < count; i += 8) {
+    const int chunks = width / 32, wide = (chunks + 1) / 2 * 32, narrow = chunks / 2 * 32, lane = threadIdx.x & 31;
+    for (int r = 0; r < kTokens && m0 + r < M; ++r) {
+        const int row = m0 + r;
+        for (int i = (int)threadIdx.x >> 5; i < count; i += kTokens * kLanes / 32) {
             const float under = stats[(size_t)i * M + row].x;
             if (under == -INFINITY || under == common[r]) continue;
             const float by = exp2f(under - common[r]);
@@ -625,7 +635,7 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
             P.tiles_n = p.tiles;
             P.clear_status = pass == 0;
             if ((st = launch_product<kSums>(P, stream)) != LOWRA_OK) return st;
-            if (launch_pdl(loss_kernel, (unsigned)((m + 31) / 32), 256, stream, (const float2*)stats, 2 * p.tiles, (const float*)R.logit, labels, m, (int)V, (long long)ignore_index,
+            if (launch_pdl(loss_kernel, (unsigned)((m + kTokens - 1) / kTokens), kTokens * kLanes, stream, (const float2*)stats, 2 * p.tiles, (const float*)R.logit, labels, m, (int)V, (long long)ignore_index,
                            loss_dev + m0) != cudaSuccess)
                 return LOWRA_ERR_CUDA;
             continue;
@@ -648,7 +658,7 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
             // (columns that the first product does not write, in a last block that is not full, are past the end)
             if (!make_map(&G.a, e, (uint64_t)m, (uint64_t)P.tiles_n * p.width, (uint64_t)ld_e, 128)) return LOWRA_ERR_CUDA;
             if ((st = launch_product<kExponentials>(P, stream)) != LOWRA_OK) return st;
-            if (launch_pdl(lift_kernel, (unsigned)((m + 31) / 32), 256, stream, (const float2*)stats, 2 * P.tiles_n, m, p.width, P.first, e, ld_e, R) != cudaSuccess) return LOWRA_ERR_CUDA;
+            if (launch_pdl(lift_kernel, (unsigned)((m + kTokens - 1) / kTokens), kTokens * kLanes, stream, (const float2*)stats, 2 * P.tiles_n, m, p.width, P.first, e, ld_e, R) != cudaSuccess) return LOWRA_ERR_CUDA;
             if ((st = launch_product<kGradient>(G, stream)) != LOWRA_OK) return st;
         }
         const long long ctas = ((long long)m * (K / 8) + 255) / 256;
