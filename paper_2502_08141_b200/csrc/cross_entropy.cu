@@ -44,13 +44,31 @@ struct CeBarriers {
 };
 static_assert(sizeof(CeBarriers) <= 1024, "barrier block");
 
+// Of a token: the label's logit, lift and sum so far, 2^-(lift added by the last piece).
+struct CeRows {
+    float *logit, *lift, *sum, *scale;
+};
+
+// What the end of a token's gradient takes: dX = c (O - S W_y) / (S + E).
+struct CeEnd {
+    CeRows rows;
+    const uint16_t* W;
+    const long long* labels;
+    const float* weights;
+    uint16_t* dX;
+    long long ignore;
+    int V, K;
+    float scale;
+};
+
 struct CeParams {
     CUtensorMap a, b;                             // X, or the exponentials [M, piece];  W as [V, K], in boxes of words or of 64 words x 64 features
     int M, N, V;                                  // tokens; words of the piece or features; words in all
     int v0;                                       // the piece's first word
-    int width, tiles_m, tiles_n, splits;          // columns of a tile; tiles; (gradient) parts of the contraction
+    int width, tiles_m, tiles_n;                  // columns of a tile; tiles
+    int whole, splits;                            // the first tiles are whole, the contraction of the others is cut into so many parts (all whole: splits 1)
     int blocks;                                   // contraction blocks in all
-    int first;                                    // the first piece: lift and O have no value yet
+    int first, last;                              // the first piece: lift and O have no value yet; (gradient) the last one: whole tiles are finished
     const long long* labels;
     const float* lift;                            // (exponentials) a token's lift so far, in octaves
     float* label_logit;                           // l_y (out)
@@ -58,11 +76,43 @@ struct CeParams {
     uint16_t* e;                                  // [M, ld_e]
     long long ld_e;
     const float* scale;                           // (gradient) 2^-(lift added by the piece)
-    float* out;                                   // (gradient) O [splits][M, N]
+    float *out, *parts;                           // (gradient) O [M, N] of whole tiles; of the others' parts, [part][tile][256 tokens][256 features]
+    CeEnd end;                                    // (gradient)
     uint32_t* status;
     unsigned long long wait_ns;
     int clear_status;
 };
+
+// The factors of a token's O and of its label's row of W in dX.
+struct Factors {
+    float o, w;
+    const uint16_t* row;      // null: the token does not count, or has no word (and o, w are NaN)
+};
+__device__ __forceinline__ Factors factors_of(const CeEnd& E, int m) {
+    const long long y = E.labels[m];
+    if (y < 0 || y >= E.V) {
+        const float none = y == E.ignore ? 0.0f : NAN;
+        return {none, none, nullptr};
+    }
+    if (y == E.ignore) return {0.0f, 0.0f, nullptr};
+    const float sum = E.rows.sum[m], own = exp2f(fmaf(E.rows.logit[m], kLog2e, -E.rows.lift[m])), c = E.weights != nullptr ? E.scale * E.weights[m] : E.scale;
+    const float a = c / (sum + own);
+    return {a, -a * sum, E.W + (size_t)y * E.K};
+}
+// Eight features of dX from those of O, at feature k.
+__device__ __forceinline__ uint4 end_of(const Factors& f, const float (&o)[8], int k) {
+    if (f.row == nullptr) {
+        const uint32_t v = pack_bf16x2(f.o, f.o);     // (zero or NaN, whatever O holds)
+        return make_uint4(v, v, v, v);
+    }
+    const uint4 w = __ldg(reinterpret_cast<const uint4*>(f.row + k));
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    uint32_t r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        r[j] = pack_bf16x2(fmaf(f.w, __uint_as_float(x[j] << 16), f.o * o[2 * j]), fmaf(f.w, __uint_as_float(x[j] & 0xffff0000u), f.o * o[2 * j + 1]));
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -82,7 +132,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t crank = blockIdx.x & 1u;
     const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
-    const int tiles = P.tiles_m * P.tiles_n, units = tiles * P.splits;
+    const int rest = P.tiles_m * P.tiles_n - P.whole, units = P.whole + rest * P.splits;
     const bool mn = KIND == kGradient;              // W's features are the contiguous ones of its tiles
 
     if (threadIdx.x == 0) {
@@ -103,9 +153,12 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     if (P.clear_status && blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0u;
     bool failed = false;
 
-    // Unit u: tokens fastest, so that the pairs at work share the words or features of their tiles; a part of the contraction after the other.
+    // Unit u: its tile (tokens fastest, so that the pairs at work share the words or features of their tiles), and which of its parts (none: the whole contraction).
+    auto tile_of = [&](int u) { return u < P.whole ? u : P.whole + (u - P.whole) % rest; };
     auto blocks_of = [&](int u, int* kb0) {
-        const int s = u / tiles;
+        *kb0 = 0;
+        if (u < P.whole) return P.blocks;
+        const int s = (u - P.whole) / rest;
         *kb0 = (int)((long long)P.blocks * s / P.splits);
         return (int)((long long)P.blocks * (s + 1) / P.splits) - *kb0;
     };
@@ -120,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         int s = 0;
         uint32_t ph = 0;
         for (int u = pair; u < units && !failed; u += pairs) {
-            const int t = u % tiles, m0 = t % P.tiles_m * kTile + (int)crank * 128, n0 = t / P.tiles_m * P.width + (int)crank * (P.width / 2);
+            const int t = tile_of(u), m0 = t % P.tiles_m * kTile + (int)crank * 128, n0 = t / P.tiles_m * P.width + (int)crank * (P.width / 2);
             int kb0;
             const int n = blocks_of(u, &kb0);
             for (int kb = kb0; kb < kb0 + n; ++kb) {
@@ -187,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         const uint32_t empty0 = ptx::map_to_cta(ptx::smem_u32(&bars->tmem_empty[0]), 0u);
         int i = 0;
         for (int u = pair; u < units && !failed; u += pairs) {
-            const int t = u % tiles, tn = t / P.tiles_m, row = t % P.tiles_m * kTile + (int)crank * 128 + q * 32 + lane;
+            const int t = tile_of(u), tn = t / P.tiles_m, row = t % P.tiles_m * kTile + (int)crank * 128 + q * 32 + lane;
             const bool mine = row < P.M;
             int kb0;
             const int segments = segments_of(blocks_of(u, &kb0));
@@ -245,12 +298,16 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             if (failed) break;
             const int n0 = tn * P.width + c_first * 32;      // the first column, in the piece
             if constexpr (KIND == kGradient) {
-                float* out = P.out + (size_t)(u / tiles) * P.M * P.N + (size_t)row * P.N + n0;
+                const bool is_whole = u < P.whole, ends = is_whole && P.last != 0;
+                float* out = is_whole ? P.out + (size_t)row * P.N + n0
+                                      : P.parts + (size_t)(u - P.whole) * (kTile * kTile) + ((int)crank * 128 + q * 32 + lane) * kTile + c_first * 32;
+                Factors f = {0.0f, 0.0f, nullptr};
+                if (ends && mine) f = factors_of(P.end, row);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        if (!mine || c >= c_count || n0 + c * 32 + j * 8 >= P.N) continue;
+                        if (!mine || n0 + c * 32 + j * 8 >= P.N) continue;
                         float* at = out + c * 32 + j * 8;
                         uint32_t* w = &v[c][j * 8];
                         if (!P.first) {
@@ -259,7 +316,15 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 #pragma unroll
                             for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(fmaf(old[k], scale, __uint_as_float(w[k])));
                         }
-                        ptx::st_global_v8(at, w);
+                        if (ends) {
+                            float o[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) o[k] = __uint_as_float(w[k]);
+                            const int k0 = n0 + c * 32 + j * 8;
+                            *reinterpret_cast<uint4*>(P.end.dX + (size_t)row * P.N + k0) = end_of(f, o, k0);
+                        } else {
+                            ptx::st_global_v8(at, w);
+                        }
                     }
                 }
             } else {
@@ -343,11 +408,6 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 }
 
 // ------------------------------------------------------------------------------------------------ the tokens' own numbers
-// Of a token: the label's logit, lift and sum so far, 2^-(lift added by the last piece).
-struct CeRows {
-    float *logit, *lift, *sum, *scale;
-};
-
 // A token's halves of tiles, (octaves that the exponentials were taken under, sum of them) each, joined: eight tokens to a CTA, 32 threads to a token, eight of their loads under way at once.
 // (Halves without a word: minus infinity and zero.)  Empty in the end where no half had one.
 constexpr int kTokens = 8, kLanes = 32;
@@ -448,47 +508,39 @@ __global__ void __launch_bounds__(kTokens * kLanes) lift_kernel(const float2* st
     }
 }
 
-// dX = c (O - S W_y) / (S + E), and the loss; eight features to a thread.
-__global__ void __launch_bounds__(256) finish_kernel(const float* O, int splits, const uint16_t* W, const long long* labels, const float* weights, int M, int V, int K, long long ignore,
-                                                     float scale, CeRows R, uint16_t* dX, float* loss) {
+// The losses, and dX where the contraction was cut: the parts in their order, eight features to a thread.
+__global__ void __launch_bounds__(256) finish_kernel(const CeEnd E, const float* parts, int whole, int rest, int splits, int tiles_m, int M, float* loss) {
     pdl_enter();
-    const long long vectors = (long long)M * (K / 8), step = (long long)gridDim.x * 256;
+    const long long step = (long long)gridDim.x * 256, vectors = (long long)rest * kTile * (kTile / 8);
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < vectors; i += step) {
-        const int m = (int)(i / (K / 8)), k = (int)(i - (long long)m * (K / 8)) * 8;
-        const long long y = labels[m];
-        uint4 out = make_uint4(0u, 0u, 0u, 0u);
-        if (y != ignore) {
-            const bool word = y >= 0 && y < V;
-            const float sum = word ? R.sum[m] : NAN, over = word ? fmaf(R.logit[m], kLog2e, -R.lift[m]) : 0.0f;      // (over: the label's logit above the lift, octaves)
-            const float own = exp2f(over), total = sum + own;
-            if (k == 0) loss[m] = sum == 0.0f ? 0.0f : over >= 0.0f ? log1pf(sum * exp2f(-over)) : logf(total) - over * kLn2;
-            const float c = weights != nullptr ? scale * weights[m] : scale, a = c / total, b = a * sum;
-            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            for (int s = 0; s < splits; ++s) {
-                const float4* o = reinterpret_cast<const float4*>(O + ((size_t)s * M + m) * K + k);
-                const float4 p = __ldcs(o), q = __ldcs(o + 1);
-                x[0] += p.x; x[1] += p.y; x[2] += p.z; x[3] += p.w; x[4] += q.x; x[5] += q.y; x[6] += q.z; x[7] += q.w;
-            }
-            const uint4 w = word ? __ldg(reinterpret_cast<const uint4*>(W + (size_t)y * K + k)) : make_uint4(0u, 0u, 0u, 0u);
-            const uint32_t wv[4] = {w.x, w.y, w.z, w.w};
-            uint32_t r[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float lo = a * x[2 * j] - b * __uint_as_float(wv[j] << 16), hi = a * x[2 * j + 1] - b * __uint_as_float(wv[j] & 0xffff0000u);
-                r[j] = pack_bf16x2(lo, hi);
-            }
-            out = make_uint4(r[0], r[1], r[2], r[3]);
-        } else if (k == 0) {
-            loss[m] = 0.0f;
+        const int r = (int)(i / (kTile * kTile / 8)), in = (int)(i % (kTile * kTile / 8)), t = whole + r;
+        const int m = t % tiles_m * kTile + in / (kTile / 8), k = t / tiles_m * kTile + in % (kTile / 8) * 8;
+        if (m >= M || k >= E.K) continue;
+        float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < splits; ++s) {
+            const float4* from = reinterpret_cast<const float4*>(parts + ((size_t)s * rest + r) * (kTile * kTile) + (size_t)in * 8);
+            const float4 p = __ldcs(from), q = __ldcs(from + 1);
+            o[0] += p.x; o[1] += p.y; o[2] += p.z; o[3] += p.w; o[4] += q.x; o[5] += q.y; o[6] += q.z; o[7] += q.w;
         }
-        *reinterpret_cast<uint4*>(dX + (size_t)m * K + k) = out;
+        *reinterpret_cast<uint4*>(E.dX + (size_t)m * E.K + k) = end_of(factors_of(E, m), o, k);
+    }
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < M; i += step) {
+        const int m = (int)i;
+        const long long y = E.labels[m];
+        float value = 0.0f;
+        if (y != E.ignore) {
+            const bool word = y >= 0 && y < E.V;
+            const float sum = word ? E.rows.sum[m] : NAN, over = word ? fmaf(E.rows.logit[m], kLog2e, -E.rows.lift[m]) : 0.0f;      // (over: the label's logit above the lift, octaves)
+            value = sum == 0.0f ? 0.0f : over >= 0.0f ? log1pf(sum * exp2f(-over)) : logf(sum + exp2f(over)) - over * kLn2;
+        }
+        loss[m] = value;
     }
 }
 
 // ------------------------------------------------------------------------------------------------ host
 constexpr int kMostTokens = 4096;                          // of a pass; more go in several passes
 constexpr size_t kPieceBytes = (size_t)128 << 20;          // of a piece's exponentials
-constexpr int kMostV = 1 << 24, kMostK = 1 << 16, kMostM = 1 << 30, kMostSplits = 16;
+constexpr int kMostV = 1 << 24, kMostK = 1 << 16, kMostM = 1 << 30, kMostSplits = 64;
 constexpr int kPairs = kNumSMs / 2;
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -498,9 +550,25 @@ struct CePlan {
     int passes, tokens;                 // passes over the tokens, tokens of one
     int width, tiles;                   // columns of a tile of logits, and tiles of a piece
     int pieces, piece;                  // pieces of the vocabulary, their words (the last may have fewer)
-    int splits;                         // parts of the gradient's contraction
-    size_t off_rows, off_stats, off_e, off_out, total;
+    size_t off_rows, off_stats, off_e, off_out, off_parts, total;
 };
+// The gradient's tiles: as many whole ones as fill all pairs, the contraction of the rest cut into parts that do.
+struct CeCut {
+    int whole, rest, splits;
+};
+CeCut cut_of(int tokens, int K, int blocks) {
+    const int tiles = ((tokens + kTile - 1) / kTile) * ((K + kTile - 1) / kTile), rest = tiles % kPairs;
+    CeCut c = {tiles - rest, rest, 1};
+    // rounds of blocks, six more for filling and draining, and what a part costs in memory and at the end (1.5 blocks' time for each of a round)
+    double least = -1.0;
+    for (int s = 1; rest > 0 && s <= kMostSplits && s <= blocks && (s == 1 || rest * s <= 2 * kPairs); ++s) {
+        const double cost = (double)((rest * s + kPairs - 1) / kPairs) * ((blocks + s - 1) / s + 6) + 1.5 * s * rest / kPairs;
+        if (least < 0.0 || cost < least) { least = cost; c.splits = s; }
+    }
+    if (c.splits == 1) c = {tiles, 0, 1};
+    return c;
+}
+int blocks_of_piece(int words) { return (words + kDepth - 1) / kDepth; }
 CePlan plan_of(int M, int V, int K, bool grad) {
     CePlan p;
     p.passes = (M + kMostTokens - 1) / kMostTokens;
@@ -521,21 +589,21 @@ CePlan plan_of(int M, int V, int K, bool grad) {
     p.tiles = (words + p.width - 1) / p.width;
     p.piece = p.pieces > 1 ? p.tiles * p.width : V;
     p.pieces = (V + p.piece - 1) / p.piece;
-    p.splits = 1;
-    if (grad) {
-        // parts of the contraction: rounds of blocks, six more for filling and draining, and what O costs in memory (in blocks' time, 0.3 us)
-        const long units = (long)tiles_m * ((K + kTile - 1) / kTile), blocks = (p.tiles * p.width + kDepth - 1) / kDepth;
-        double least = -1.0;
-        for (int s = 1; s <= kMostSplits && s <= blocks; ++s) {
-            const double cost = (double)((units * s + kPairs - 1) / kPairs) * ((blocks + s - 1) / s + 6) * p.pieces + s * ((double)p.tokens * K * 8.0 / 6.4e12 / 0.3e-6);
-            if (least < 0.0 || cost < least) { least = cost; p.splits = s; }
-        }
-    }
     p.off_rows = 256;
     p.off_stats = p.off_rows + 4 * up256((size_t)p.tokens * 4);
     p.off_e = p.off_stats + up256((size_t)p.tiles * 2 * p.tokens * 8);
     p.off_out = p.off_e + (grad ? up256((size_t)p.tokens * p.tiles * p.width * 2) : 0);
-    p.total = p.off_out + (grad ? up256((size_t)p.splits * p.tokens * K * 4) : 0);
+    p.off_parts = p.off_out + (grad && p.pieces > 1 ? up256((size_t)p.tokens * K * 4) : 0);
+    size_t parts = 0;
+    auto room = [&](int m) {
+        const CeCut c = cut_of(m, K, blocks_of_piece(p.piece));
+        const size_t bytes = (size_t)c.rest * c.splits * kTile * kTile * 4;
+        if (bytes > parts) parts = bytes;
+    };
+    if (grad) room(p.tokens);
+    const int left = M - (p.passes - 1) * p.tokens;      // (the last pass may have fewer tokens)
+    if (grad && left > 0) room(left);
+    p.total = p.off_parts + parts;
     return p;
 }
 
@@ -554,7 +622,7 @@ lowra_status launch_product(CeParams& P, cudaStream_t stream) {
     }
     const int sms = device_sm_count();
     if (sms < 2 || registers.load(std::memory_order_relaxed) != kLaunchRegisters) return LOWRA_ERR_CUDA;
-    const int units = P.tiles_m * P.tiles_n * P.splits, pairs = units < sms / 2 ? units : sms / 2;
+    const int units = P.whole + (P.tiles_m * P.tiles_n - P.whole) * P.splits, pairs = units < sms / 2 ? units : sms / 2;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -605,7 +673,7 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
     const CeRows R = {rows, rows + row, rows + 2 * row, rows + 3 * row};
     float2* stats = reinterpret_cast<float2*>(ws + p.off_stats);
     uint16_t* e = reinterpret_cast<uint16_t*>(ws + p.off_e);
-    float* O = reinterpret_cast<float*>(ws + p.off_out);
+    float *O = reinterpret_cast<float*>(ws + p.off_out), *parts = reinterpret_cast<float*>(ws + p.off_parts);
     const long long ld_e = (long long)p.tiles * p.width;
     for (int pass = 0; pass < p.passes; ++pass) {
         const long long m0 = (long long)pass * p.tokens;
@@ -633,6 +701,7 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
         if (!dX_dev) {
             P.N = V;
             P.tiles_n = p.tiles;
+            P.whole = P.tiles_m * P.tiles_n;
             P.clear_status = pass == 0;
             if ((st = launch_product<kSums>(P, stream)) != LOWRA_OK) return st;
             if (launch_pdl(loss_kernel, (unsigned)((m + kTokens - 1) / kTokens), kTokens * kLanes, stream, (const float2*)stats, 2 * p.tiles, (const float*)R.logit, labels, m, (int)V, (long long)ignore_index,
@@ -644,15 +713,21 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
         G.N = K;
         G.width = kTile;
         G.tiles_n = (K + kTile - 1) / kTile;
-        G.splits = p.splits;
+        const CeCut cut = cut_of(m, K, blocks_of_piece(p.piece));
+        G.whole = cut.whole;
+        G.splits = cut.splits;
         G.scale = R.scale;
         G.out = O;
+        G.parts = parts;
+        G.end = CeEnd{R, W_dev, labels, weights, dX_dev + m0 * K, (long long)ignore_index, (int)V, (int)K, scale};
         if (!make_map(&G.b, W_dev, (uint64_t)V, (uint64_t)K, (uint64_t)K, 64)) return LOWRA_ERR_CUDA;
         for (int c = 0; c < p.pieces; ++c) {
             P.v0 = G.v0 = c * p.piece;
             P.N = V - P.v0 < p.piece ? V - P.v0 : p.piece;
             P.tiles_n = (P.N + p.width - 1) / p.width;
-            G.blocks = (P.N + kDepth - 1) / kDepth;
+            P.whole = P.tiles_m * P.tiles_n;
+            G.blocks = blocks_of_piece(P.N);
+            G.last = c + 1 == p.pieces;
             P.first = G.first = c == 0;
             P.clear_status = pass == 0 && c == 0;
             // (columns that the first product does not write, in a last block that is not full, are past the end)
@@ -661,9 +736,10 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
             if (launch_pdl(lift_kernel, (unsigned)((m + kTokens - 1) / kTokens), kTokens * kLanes, stream, (const float2*)stats, 2 * P.tiles_n, m, p.width, P.first, e, ld_e, R) != cudaSuccess) return LOWRA_ERR_CUDA;
             if ((st = launch_product<kGradient>(G, stream)) != LOWRA_OK) return st;
         }
-        const long long ctas = ((long long)m * (K / 8) + 255) / 256;
-        if (launch_pdl(finish_kernel, (unsigned)(ctas < 8 * kNumSMs ? ctas : 8 * kNumSMs), 256, stream, (const float*)O, p.splits, W_dev, labels, weights, m, (int)V, (int)K,
-                       (long long)ignore_index, scale, R, dX_dev + m0 * K, loss_dev + m0) != cudaSuccess)
+        long long ctas = ((long long)cut.rest * (kTile * kTile / 8) + 255) / 256;
+        if (ctas < (m + 255) / 256) ctas = (m + 255) / 256;
+        if (launch_pdl(finish_kernel, (unsigned)(ctas < 8 * kNumSMs ? ctas : 8 * kNumSMs), 256, stream, G.end, (const float*)parts, cut.whole, cut.rest, cut.splits, P.tiles_m, m, loss_dev + m0) !=
+            cudaSuccess)
             return LOWRA_ERR_CUDA;
     }
     return LOWRA_OK;
