@@ -724,15 +724,14 @@ PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
         for (int i = 0; i < kNames; ++i) names[i] = PyUnicode_InternFromString(kText[i]);
     }
     try {
-        // the members' arrays: their dicts are the caller's, and other threads run during the call
-        std::vector<at::Tensor> held;
-        held.reserve((size_t)count * kNames + 3);
+        // (The members' arrays are not held: no other Python thread runs before the call is made.  Its host side takes 0.2 us a factor.)
         std::vector<lowra_adamw_member> members((size_t)count);
         const int64_t dev = c10::cuda::current_device();
+        const at::Device here(at::kCUDA, (c10::DeviceIndex)dev);
         auto scalar = [&](PyObject* o, at::ScalarType type, const void** p) {
-            held.push_back(THPVariable_Unpack(o));
-            *p = held.back().data_ptr();
-            return array(held.back(), type, 1, dev) && held.back().numel() == 1;
+            const at::Tensor& t = THPVariable_Unpack(o);
+            *p = t.data_ptr();
+            return array(t, type, 1, dev) && t.numel() == 1;
         };
         const void *lr = nullptr, *at_step = nullptr, *factor = nullptr;
         if ((!lr_here && !scalar(args[1], at::kFloat, &lr)) || (!step_here && !scalar(args[5], at::kInt, &at_step)) || (args[6] != Py_None && !scalar(args[6], at::kFloat, &factor)))
@@ -744,31 +743,36 @@ PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
         for (Py_ssize_t i = 0; i < count; ++i) {
             PyObject* m = PyList_GET_ITEM(args[0], i);
             if (!PyDict_CheckExact(m)) Py_RETURN_NONE;
+            PyObject *of[kNames] = {}, *key = nullptr, *value = nullptr;
+            Py_ssize_t place = 0;
+            while (PyDict_Next(m, &place, &key, &value)) {      // (one walk; a name is mostly the same object as ours)
+                int k = 0;
+                while (k < kNames && key != names[k]) ++k;
+                for (int j = 0; k == kNames && j < kNames; ++j)
+                    if (PyUnicode_CheckExact(key) && PyUnicode_Compare(key, names[j]) == 0) k = j + 2 * kNames;
+                if (k == kNames || value == Py_None) continue;
+                of[k >= 2 * kNames ? k - 2 * kNames : k] = value;
+            }
+            if (PyErr_Occurred() != nullptr || of[kGrad] == nullptr || of[kMaster] == nullptr || of[kM] == nullptr || of[kV] == nullptr || !plain(of[kGrad]) || !plain(of[kM])) {
+                PyErr_Clear();
+                Py_RETURN_NONE;
+            }
+            const at::Tensor& grad = THPVariable_Unpack(of[kGrad]);
+            if (i == 0) {
+                grad_type = grad.scalar_type();
+                state_type = THPVariable_Unpack(of[kM]).scalar_type();
+            }
+            const int64_t elements = grad.numel(), blocks = (elements + LOWRA_ADAMW_BLOCK - 1) / LOWRA_ADAMW_BLOCK;
+            if (state_type != at::kFloat && (of[kMScale] == nullptr || of[kVScale] == nullptr)) Py_RETURN_NONE;
             void* at[kNames] = {};
-            const at::Tensor* grad = nullptr;
-            int64_t elements = 0, blocks = 0;
             for (int k = 0; k < kNames; ++k) {
-                PyObject* o = PyDict_GetItemWithError(m, names[k]);
-                if (o == nullptr || o == Py_None) {
-                    if (PyErr_Occurred() != nullptr || k < kMScale || ((k == kMScale || k == kVScale) && state_type != at::kFloat)) {
-                        PyErr_Clear();
-                        Py_RETURN_NONE;
-                    }
-                    continue;
-                }
-                if (!plain(o)) Py_RETURN_NONE;
-                held.push_back(THPVariable_Unpack(o));
-                const at::Tensor& a = held.back();
+                if (of[k] == nullptr) continue;
+                if (!plain(of[k])) Py_RETURN_NONE;
+                const at::Tensor& a = THPVariable_Unpack(of[k]);
                 const bool scales = k == kMScale || k == kVScale || k == kMScaleOut || k == kVScaleOut, states = k == kM || k == kV || k == kMOut || k == kVOut;
-                if (k == kGrad) {
-                    grad = &a;
-                    elements = a.numel();
-                    blocks = (elements + LOWRA_ADAMW_BLOCK - 1) / LOWRA_ADAMW_BLOCK;
-                    if (i == 0) grad_type = a.scalar_type();
-                }
-                if (k == kM && i == 0) state_type = a.scalar_type();
                 const at::ScalarType type = k == kGrad ? grad_type : k == kWeight ? at::kBFloat16 : states ? state_type : at::kFloat;
-                if (!on(a, dev) || a.scalar_type() != type || (scales && state_type == at::kFloat) || (scales ? a.dim() != 1 || a.size(0) != blocks : !a.sizes().equals(grad->sizes())))
+                if (a.device() != here || !a.is_contiguous() || a.scalar_type() != type || (scales && state_type == at::kFloat) ||
+                    (scales ? a.dim() != 1 || a.size(0) != blocks : !a.sizes().equals(grad.sizes())))
                     Py_RETURN_NONE;
                 at[k] = a.data_ptr();
             }
@@ -780,11 +784,7 @@ PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if ((grad_type != at::kFloat && grad_type != at::kBFloat16) || (state_type != at::kFloat && state_type != at::kFloat8_e4m3fn)) Py_RETURN_NONE;
         step.bits = state_type == at::kFloat ? 32 : 8;
         step.grad_fp32 = grad_type == at::kFloat;
-        lowra_status st;
-        {
-            Released released;
-            st = library.adamw(members.data(), (int32_t)count, &step, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream());
-        }
+        const lowra_status st = library.adamw(members.data(), (int32_t)count, &step, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream());
         if (st != LOWRA_OK) return PyLong_FromLong(st);
         return Py_NewRef(args[0]);
     } catch (...) {
