@@ -23,12 +23,17 @@ namespace lowra {
 
 namespace {
 
-// CTAs to an SM: with fp32 states the memory is bound by the number of streams that it serves (448 factors: 738 us with three, 815 with four, 926 with six); with 8-bit ones loads have to
-// hide more work
+// CTAs to an SM that the registers are shared out for, and that a launch has: with fp32 states the memory is bound by the number of streams that it serves (448 factors: 738 us with three, 815 with
+// four, 926 with six; with fp32 gradients, one stream more in wider pieces, the other way: 8 layers 218 us with four, 241 with three); with 8-bit ones loads have to hide more work (8 layers 118 us with five, 124 with four; with fp32
+// gradients 137, 125).
 template <bool EIGHT>
-constexpr int kAdamResident = EIGHT ? 5 : 3;
+constexpr int kAdamResident = EIGHT ? 5 : 4;
+int resident_of(bool eight, bool grad_fp32) { return eight ? (grad_fp32 ? 4 : 5) : grad_fp32 ? 4 : 3; }
+// Blocks from which on a launch waits for the one before to have ended, as launches do: CTAs that come in as the others leave crowd on the SMs that are done first (448 factors, two
+// launches a step, step after step: 840 us when they may come in from the start, 777 when this launch is nearly done, 716 so; a layer's fourteen, 8 bits: 19.7, 17.8, 19.8).
+constexpr uint32_t kAdamMany = 1 << 16;
 constexpr int kAdamThreads = 256, kAdamBlock = LOWRA_ADAMW_BLOCK;
-constexpr int kAdamFew = 16, kAdamMany = 224;       // members of a launch that its parameters have room for (24 KB of them take a launch 2 us more than 2 KB)
+constexpr int kFewMembers = 16, kManyMembers = 224;       // members of a launch that its parameters have room for (24 KB of them take a launch 2 us more than 2 KB)
 static_assert(kAdamBlock == 32 * 8, "a warp's values");
 
 struct AdamMember {
@@ -163,7 +168,8 @@ __device__ __forceinline__ float store_codes(uint8_t* p, int left, const float (
 template <bool EIGHT, int MEMBERS>
 __global__ void __launch_bounds__(kAdamThreads, kAdamResident<EIGHT>) adamw_kernel(const __grid_constant__ AdamParams<MEMBERS> P) {
     __shared__ float shared[3];
-    pdl_enter();
+    if (gridDim.x <= kNumSMs) pdl_release();          // (few blocks: there is room for the next launch's)
+    pdl_wait();
     float decay = P.decay, rate = P.rate, root_scale = P.root_scale;
     if (P.step != nullptr || P.lr != nullptr) {      // a captured step reads them when it runs
         if (threadIdx.x == 0) {
@@ -255,6 +261,7 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamResident<EIGHT>) adamw_kern
             store_floats(static_cast<float*>(F.v_out) + at, left, v);
         }
     }
+    pdl_release();
 }
 
 template <bool EIGHT, int MEMBERS>
@@ -285,8 +292,17 @@ lowra_status launch_adamw(const lowra_adamw_member* members, int count, const lo
                                 m.m_scale_dev, m.v_scale_dev, m.m_scale_out_dev, m.v_scale_out_dev, m.n};
             P.first[i + 1] = P.first[i] + (uint32_t)((m.n + kAdamBlock - 1) / kAdamBlock);
         }
-        const uint32_t wanted = (P.first[P.count] + kAdamThreads / 32 - 1) / (kAdamThreads / 32), most = (uint32_t)(kNumSMs * kAdamResident<EIGHT>);
-        if (launch_pdl(adamw_kernel<EIGHT, MEMBERS>, std::min(wanted, most), kAdamThreads, stream, P) != cudaSuccess) return LOWRA_ERR_CUDA;
+        const uint32_t wanted = (P.first[P.count] + kAdamThreads / 32 - 1) / (kAdamThreads / 32), most = (uint32_t)(kNumSMs * resident_of(EIGHT, P.grad_fp32 != 0));
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.gridDim = dim3(std::min(wanted, most), 1, 1);
+        cfg.blockDim = dim3(kAdamThreads, 1, 1);
+        cfg.stream = stream;
+        cfg.attrs = attr;
+        cfg.numAttrs = P.first[P.count] < kAdamMany ? 1 : 0;
+        if (cudaLaunchKernelEx(&cfg, adamw_kernel<EIGHT, MEMBERS>, P) != cudaSuccess) return LOWRA_ERR_CUDA;
     }
     return LOWRA_OK;
 }
@@ -395,8 +411,8 @@ extern "C" lowra_status lowra_adamw(const lowra_adamw_member* members_host, int3
     if (any_clash(places.get(), n_places)) return LOWRA_ERR_SHAPE;
     const lowra_status st = check_device();
     if (st != LOWRA_OK) return st;
-    const bool few = count <= kAdamFew;
+    const bool few = count <= kFewMembers;
     cudaStream_t stream = (cudaStream_t)stream_v;
-    if (eight) return few ? launch_adamw<true, kAdamFew>(members_host, count, S, stream) : launch_adamw<true, kAdamMany>(members_host, count, S, stream);
-    return few ? launch_adamw<false, kAdamFew>(members_host, count, S, stream) : launch_adamw<false, kAdamMany>(members_host, count, S, stream);
+    if (eight) return few ? launch_adamw<true, kFewMembers>(members_host, count, S, stream) : launch_adamw<true, kManyMembers>(members_host, count, S, stream);
+    return few ? launch_adamw<false, kFewMembers>(members_host, count, S, stream) : launch_adamw<false, kManyMembers>(members_host, count, S, stream);
 }

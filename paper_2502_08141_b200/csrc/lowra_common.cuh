@@ -52,9 +52,11 @@ static inline bool overlap(Span a, Span b) {
 // right away (so the successor's launch latency and set-up overlap this kernel) and itself waits, before it
 // touches global memory, until its predecessor has completed and flushed - stream order is preserved.
 // -------------------------------------------------------------------------------------------
+__device__ __forceinline__ void pdl_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_enter() {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    pdl_release();
+    pdl_wait();
 }
 template <typename... KArgs, typename... Args>
 static inline cudaError_t launch_pdl(void (*kernel)(KArgs...), unsigned grid, unsigned block, cudaStream_t stream, Args&&... args) {
