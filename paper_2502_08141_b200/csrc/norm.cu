@@ -523,8 +523,10 @@ NormShape shape_of(int N, int most, int longest) {
 NormShape shape_of_many(int N) { return shape_of(N, kMostThreads, 256); }
 // Backward, us with eight channels to a thread and with sixteen: root mean square 8192 x 1024 18.1, 20.6; layer norm, twice the sums, 1001 x 1024 9.7, 7.3, 4096 x 4096 40.4, 34.9.
 NormShape shape_of_backward(int N, bool layer) { return shape_of(N, kBackwardThreads, layer ? 256 : 2048); }
-NormShape shape_of_few(int M, int N) {      // (up to one for each SM: a CTA to each)
-    NormShape S = shape_of(N, kMostThreads, 8 * kMostThreads);
+// Up to one for each SM: a CTA to each.  Layer norm over more than two for each: sixteen channels to a thread, and so more rows at once on an SM (333 x 5120 6.8 -> 5.0 us, 149 x 4096 3.3 -> 4.1;
+// root mean square 600 x 4096 6.3 -> 7.1).
+NormShape shape_of_few(int M, int N, bool layer) {
+    NormShape S = shape_of(N, kMostThreads, layer && M > 2 * kNumSMs ? 2048 : 8 * kMostThreads);
     const int groups = M > kNumSMs && S.group < kForwardThreads ? kForwardThreads / S.group : 1;
     S.threads = S.group * (S.group > 32 && groups > 15 ? 15 : groups);
     return S;
@@ -620,7 +622,7 @@ extern "C" lowra_status lowra_norm_forward(const uint16_t* X_dev, const uint16_t
             return cudaLaunchKernelEx(&cfg, kernel, P) == cudaSuccess ? LOWRA_OK : LOWRA_ERR_CUDA;
         }, std::tuple<>(), many.vectors == 2, layer, residual_dev != nullptr, params_fp32 != 0);
     }
-    const NormShape S = shape_of_few(M, N);
+    const NormShape S = shape_of_few(M, N, layer);
     const int groups = S.threads / S.group;
     P.group = S.group;
     cudaLaunchAttribute attr[1];
