@@ -1292,8 +1292,8 @@ def lowra_rotary(q: torch.Tensor, positions: torch.Tensor, turns: torch.Tensor, 
     parts = [(q, out, "q", "out")] if k is None else [(q, out, "q", "out"), (k, k_out, "k", "k_out")]
     if k is None and k_out is not None:
         raise ValueError("k_out without k")
-    if turns.dim() != 1 or turns.element_size() != 8 or turns.is_floating_point():
-        raise ValueError("turns must be a vector of 64-bit numbers")
+    if turns.dim() != 1 or turns.dtype not in (torch.int64, torch.uint64):
+        raise ValueError(f"turns must be a vector of {torch.int64} or {torch.uint64}, got {turns.dtype} {list(turns.shape)}")
     _extent(turns, 0, "turns")
     _dev(positions, torch.int32, "positions")
     if positions.shape != (M,):

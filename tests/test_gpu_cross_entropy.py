@@ -192,3 +192,21 @@ def test_refusals():
                 dict(X=X[:, :32].contiguous(), W=W[:, :32].contiguous())):
         with pytest.raises(lw.LowraError):
             lw.lowra_cross_entropy(**{**dict(X=X, W=W, labels=labels, want_grad=True), **bad})
+
+
+def test_waits_that_may_run_out():
+    """With a limit of a microsecond a wait may run out: the call then says so by its status word, and the next one, with the usual limit, is right."""
+    X, W, labels, weights = make(300, 20000, 2048)
+    good, good_dX = lw.lowra_cross_entropy(X, W, labels, want_grad=True)
+    ws = torch.empty(lw.lowra_cross_entropy_workspace_bytes(300, 20000, 2048, True), dtype=torch.uint8, device="cuda")
+    lw.lowra_set_wait_limit(1000)
+    try:
+        loss, dX = lw.lowra_cross_entropy(X, W, labels, want_grad=True, workspace=ws)
+        status = lw.lowra_device_status(ws)
+    finally:
+        lw.lowra_set_wait_limit(0)
+    assert status in (lw.LOWRA_OK, lw.LOWRA_ERR_TIMEOUT)
+    if status == lw.LOWRA_OK:
+        assert torch.equal(loss, good) and torch.equal(dX, good_dX)
+    loss, dX = lw.lowra_cross_entropy(X, W, labels, want_grad=True, workspace=ws)
+    assert lw.lowra_device_status(ws) == lw.LOWRA_OK and torch.equal(loss, good) and torch.equal(dX, good_dX)

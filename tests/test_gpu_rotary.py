@@ -123,11 +123,17 @@ def test_graph_with_positions_that_change():
     assert torch.equal(out, other)
 
 
+def test_unsigned_table():
+    turns, _ = table(64)
+    x, positions = heads(8, 4, 64), torch.arange(8, device="cuda", dtype=torch.int32)
+    assert torch.equal(lw.lowra_rotary(x, positions, turns.view(torch.uint64)), lw.lowra_rotary(x, positions, turns))
+
+
 def test_refusals():
     turns, _ = table(64)
     x, positions = heads(8, 4, 64), torch.arange(8, device="cuda", dtype=torch.int32)
     for bad in (dict(q=x.float()), dict(q=x[0]), dict(q=x.transpose(1, 2)), dict(q=x.cpu()), dict(positions=positions.long()), dict(positions=positions[:7]), dict(turns=turns.int()),
-                dict(turns=turns.double()), dict(turns=turns.cpu()), dict(k=x[:, :, :32]), dict(k=x[:7]), dict(out=x[:, :3]), dict(k_out=x)):
+                dict(turns=turns.double()), dict(turns=turns.view(torch.complex64)), dict(turns=turns.cpu()), dict(k=x[:, :, :32]), dict(k=x[:7]), dict(out=x[:, :3]), dict(k_out=x)):
         with pytest.raises(ValueError):
             lw.lowra_rotary(**{**dict(q=x, positions=positions, turns=turns), **bad})
     both = heads(8, 5, 64)
