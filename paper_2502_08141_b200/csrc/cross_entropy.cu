@@ -13,6 +13,7 @@
 //
 // The products: CTA pairs (clusters of two) walk over tiles of 256 tokens x up to 256 words (features), tcgen05.mma with cta_group::2, both operands by TMA, 64 contraction indices
 // (32 KB a CTA) to a stage, six stages; two accumulators in turn, so the epilogue's eight warps work on one tile while the next is formed.
+// Up to 64 tokens and no gradient, bound by reading W: the other way round, 256 words by 32 or 64 tokens, ten stages; a pair's MMAs then take an eighth or a quarter of the time that its words do.
 // warp 0 = TMA, 1 = MMA (of the CTA of rank 0) and TMEM, 4-11 = epilogue.  The 128 columns that an epilogue's thread holds, and 32 more on their way, do not fit into the 168 registers that
 // twelve warps get: the first four give some to the others.  All waits are bounded (lowra_set_wait_limit); no CTA waits for another cluster.
 #include <atomic>
@@ -25,20 +26,28 @@ namespace lowra {
 namespace {
 
 constexpr int kTile = 256;                        // tokens, and at most so many words or features, of a pair's tile
-constexpr int kStages = 6, kDepth = 64;           // contraction indices of a stage
-constexpr uint32_t kHalfBytes = 128 * kDepth * 2, kStageBytes = 2 * kHalfBytes;
+constexpr int kDepth = 64;                        // contraction indices of a stage
+constexpr uint32_t kHalfBytes = 128 * kDepth * 2;
+constexpr int kFewTokens = 64;                    // up to so many, the words are the tile's rows and the tokens its columns
 constexpr int kThreads = 384, kEpilogue = 8, kFirstEpilogue = 4;      // threads; epilogue warps, behind four others
 constexpr int kLaunchRegisters = 168, kFewRegisters = 40, kManyRegisters = 232;   // a thread: at the launch, of the first four warps, of the others
 static_assert(128 * kFewRegisters + 256 * kManyRegisters <= kThreads * kLaunchRegisters, "what the others take, the first four have given (a larger share would be waited for without end)");
-constexpr uint32_t kSmem = kStages * kStageBytes + 1024;
 constexpr uint64_t kGrace = 50ull * 1000ull;      // after a failure: time for copies and MMAs still in flight to land
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kHeadroom = 64.0f;                // octaves that the largest exponentials may be from one
 constexpr int kSegment = 16;                      // contraction blocks of a logit that are added up in the tensor memory
-constexpr int kSums = 0, kExponentials = 1, kGradient = 2;
+constexpr int kSums = 0, kExponentials = 1, kGradient = 2, kFew = 3;
+// Stages of the ring: 128 rows of either operand, or, for few tokens, 128 words and 32 tokens.
+template <int KIND>
+constexpr uint32_t kStageBytes = kHalfBytes + (KIND == kFew ? kHalfBytes / 4 : kHalfBytes);
+template <int KIND>
+constexpr int kStages = KIND == kFew ? 10 : 6;
+constexpr int kMostStages = 10;
+template <int KIND>
+constexpr uint32_t kSmem = kStages<KIND> * kStageBytes<KIND> + 1024;
 
 struct CeBarriers {
-    uint64_t full[kStages], empty[kStages];
+    uint64_t full[kMostStages], empty[kMostStages];
     uint64_t tmem_full[2], tmem_empty[2];
     uint32_t tmem_base, abort;
 };
@@ -62,10 +71,11 @@ struct CeEnd {
 };
 
 struct CeParams {
-    CUtensorMap a, b;                             // X, or the exponentials [M, piece];  W as [V, K], in boxes of words or of 64 words x 64 features
+    CUtensorMap a, b;                             // X, or the exponentials [M, piece];  W as [V, K], in boxes of words or of 64 words x 64 features  (few tokens: W; X)
     int M, N, V;                                  // tokens; words of the piece or features; words in all
     int v0;                                       // the piece's first word
-    int width, tiles_m, tiles_n;                  // columns of a tile; tiles
+    int width, tiles_m, tiles_n;                  // columns of a tile; tiles  (few tokens: words of a tile, its rows; tiles_m 1)
+    int columns;                                  // (few tokens) of a tile: the tokens, filled up to a multiple of 32
     int whole, splits;                            // the first tiles are whole, the contraction of the others is cut into so many parts (all whole: splits 1)
     int blocks;                                   // contraction blocks in all
     int first, last;                              // the first piece: lift and O have no value yet; (gradient) the last one: whole tiles are finished
@@ -123,7 +133,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
 template <int KIND>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CeParams P) {
     extern __shared__ __align__(1024) unsigned char smem[];
-    CeBarriers* bars = reinterpret_cast<CeBarriers*>(smem + kStages * kStageBytes);
+    constexpr int kRing = kStages<KIND>;
+    constexpr uint32_t kStage = kStageBytes<KIND>;
+    CeBarriers* bars = reinterpret_cast<CeBarriers*>(smem + kRing * kStage);
     volatile uint32_t* abort_flag = &bars->abort;
     if ((ptx::smem_u32(smem) & 1023u) != 0u) {      // never seen; without it the operand descriptors would be wrong
         if (threadIdx.x == 0) atomicExch(P.status, (uint32_t)LOWRA_ERR_CUDA);
@@ -136,7 +148,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     const bool mn = KIND == kGradient;              // W's features are the contiguous ones of its tiles
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) { ptx::mbar_init(&bars->full[s], 1); ptx::mbar_init(&bars->empty[s], 1); }
+        for (int s = 0; s < kRing; ++s) { ptx::mbar_init(&bars->full[s], 1); ptx::mbar_init(&bars->empty[s], 1); }
         for (int a = 0; a < 2; ++a) { ptx::mbar_init(&bars->tmem_full[a], 1); ptx::mbar_init(&bars->tmem_empty[a], 2 * kEpilogue); }
         bars->abort = 0u;
         ptx::fence_barrier_init();
@@ -164,74 +176,77 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     };
     auto segments_of = [&](int n) { return KIND == kGradient ? (n > 0 ? 1 : 0) : (n + kSegment - 1) / kSegment; };
     if (warp < kFirstEpilogue) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
-    if (warp == 0) {
-        const bool leader = ptx::elect_one();
-        ptx::fence_proxy_async_all();               // (the exponentials were written by ordinary stores)
-        const uint32_t full0 = ptx::map_to_cta(ptx::smem_u32(&bars->full[0]), 0u);
-        const uint32_t b_bytes = (uint32_t)P.width * kDepth;      // half the tile's columns x 64 x 2 bytes
-        int s = 0;
-        uint32_t ph = 0;
-        for (int u = pair; u < units && !failed; u += pairs) {
-            const int t = tile_of(u), m0 = t % P.tiles_m * kTile + (int)crank * 128, n0 = t / P.tiles_m * P.width + (int)crank * (P.width / 2);
-            int kb0;
-            const int n = blocks_of(u, &kb0);
-            for (int kb = kb0; kb < kb0 + n; ++kb) {
-                if (!ptx::mbar_wait_lanes(&bars->empty[s], ph ^ 1u, abort_flag, P.wait_ns)) { failed = true; break; }
-                unsigned char* a_s = smem + s * kStageBytes;
-                const uint32_t bar = full0 + (uint32_t)s * 8u;
-                if (leader) {
-                    if (crank == 0u) ptx::mbar_arrive_expect_tx(&bars->full[s], 2u * (kHalfBytes + b_bytes));
-                    ptx::tma_load_2d_pair(a_s, &P.a, kb * kDepth, m0, bar);
-                    if (mn) {
-                        ptx::tma_load_2d_pair(a_s + kHalfBytes, &P.b, n0, P.v0 + kb * kDepth, bar);
-                        ptx::tma_load_2d_pair(a_s + kHalfBytes + 8192, &P.b, n0 + 64, P.v0 + kb * kDepth, bar);
-                    } else {
-                        ptx::tma_load_2d_pair(a_s + kHalfBytes, &P.b, kb * kDepth, P.v0 + n0, bar);
-                    }
-                }
-                __syncwarp();
-                if (++s == kStages) { s = 0; ph ^= 1u; }
-            }
-        }
-        if (failed) bars->abort = 1u;
-    } else if (warp == 1) {
-        if (crank == 0u) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
+        if (warp == 0) {
             const bool leader = ptx::elect_one();
-            const uint32_t idesc = ptx::umma_idesc_bf16(kTile, P.width) | (mn ? 1u << 16 : 0u), b_step = mn ? 128u : 2u;
-            const uint64_t a0 = ptx::umma_desc_k_sw128(ptx::smem_u32(smem));
-            const uint64_t b0 = mn ? ptx::umma_desc_mn_sw128(ptx::smem_u32(smem) + kHalfBytes, 8192u) : ptx::umma_desc_k_sw128(ptx::smem_u32(smem) + kHalfBytes);
-            int s = 0, i = 0;
+            ptx::fence_proxy_async_all();               // (the exponentials were written by ordinary stores)
+            const uint32_t full0 = ptx::map_to_cta(ptx::smem_u32(&bars->full[0]), 0u);
+            // half the tile's rows and columns x 64 x 2 bytes
+            const uint32_t a_bytes = KIND == kFew ? (uint32_t)P.width * kDepth : kHalfBytes, b_bytes = (uint32_t)(KIND == kFew ? P.columns : P.width) * kDepth;
+            int s = 0;
             uint32_t ph = 0;
-            bool ready = false;
             for (int u = pair; u < units && !failed; u += pairs) {
+                const int t = tile_of(u);
+                const int m0 = KIND == kFew ? P.v0 + t * P.width + (int)crank * (P.width / 2) : t % P.tiles_m * kTile + (int)crank * 128;
+                const int n0 = KIND == kFew ? (int)crank * (P.columns / 2) : t / P.tiles_m * P.width + (int)crank * (P.width / 2);
                 int kb0;
-                const int n = blocks_of(u, &kb0), segments = segments_of(n);      // (none in a part without blocks: a short last piece)
-                for (int g = 0; g < segments && !failed; ++g, ++i) {
-                    const uint32_t acc = (uint32_t)i & 1u, d = tmem_base + acc * kTile;
-                    if (!ptx::mbar_wait_lanes(&bars->tmem_empty[acc], (((uint32_t)i >> 1) & 1u) ^ 1u, abort_flag, P.wait_ns)) { failed = true; break; }
-                    ptx::tc_fence_after();
-                    const int first = n * g / segments, last = n * (g + 1) / segments - 1;
-                    for (int kb = first; kb <= last; ++kb) {
-                        if (!ready && !ptx::mbar_wait_lanes(&bars->full[s], ph, abort_flag, P.wait_ns)) { failed = true; break; }
-                        ptx::tc_fence_after();
-                        const uint64_t a = a0 + (uint64_t)s * (kStageBytes >> 4), b = b0 + (uint64_t)s * (kStageBytes >> 4);
-                        const int here = s;
-                        if (++s == kStages) { s = 0; ph ^= 1u; }
-                        ready = __all_sync(0xffffffffu, ptx::mbar_test_wait(&bars->full[s], ph));      // (asked for ahead of its use)
-                        if (leader) {
-#pragma unroll
-                            for (uint32_t k = 0; k < kDepth / 16; ++k) ptx::umma_bf16_pair(d, a + 2u * k, b + b_step * k, idesc, (kb != first || k != 0) ? 1u : 0u);
-                            ptx::umma_commit_pair(&bars->empty[here]);
-                            if (kb == last) ptx::umma_commit_pair(&bars->tmem_full[acc]);
+                const int n = blocks_of(u, &kb0);
+                for (int kb = kb0; kb < kb0 + n; ++kb) {
+                    if (!ptx::mbar_wait_lanes(&bars->empty[s], ph ^ 1u, abort_flag, P.wait_ns)) { failed = true; break; }
+                    unsigned char* a_s = smem + s * kStage;
+                    const uint32_t bar = full0 + (uint32_t)s * 8u;
+                    if (leader) {
+                        if (crank == 0u) ptx::mbar_arrive_expect_tx(&bars->full[s], 2u * (a_bytes + b_bytes));
+                        ptx::tma_load_2d_pair(a_s, &P.a, kb * kDepth, m0, bar);
+                        if (mn) {
+                            ptx::tma_load_2d_pair(a_s + kHalfBytes, &P.b, n0, P.v0 + kb * kDepth, bar);
+                            ptx::tma_load_2d_pair(a_s + kHalfBytes + 8192, &P.b, n0 + 64, P.v0 + kb * kDepth, bar);
+                        } else {
+                            ptx::tma_load_2d_pair(a_s + kHalfBytes, &P.b, kb * kDepth, KIND == kFew ? n0 : P.v0 + n0, bar);
                         }
-                        __syncwarp();
                     }
+                    __syncwarp();
+                    if (++s == kRing) { s = 0; ph ^= 1u; }
                 }
             }
             if (failed) bars->abort = 1u;
+        } else if (warp == 1) {
+            if (crank == 0u) {
+                const bool leader = ptx::elect_one();
+                const uint32_t idesc = ptx::umma_idesc_bf16(kTile, KIND == kFew ? P.columns : P.width) | (mn ? 1u << 16 : 0u), b_step = mn ? 128u : 2u;
+                const uint64_t a0 = ptx::umma_desc_k_sw128(ptx::smem_u32(smem));
+                const uint64_t b0 = mn ? ptx::umma_desc_mn_sw128(ptx::smem_u32(smem) + kHalfBytes, 8192u) : ptx::umma_desc_k_sw128(ptx::smem_u32(smem) + kHalfBytes);
+                int s = 0, i = 0;
+                uint32_t ph = 0;
+                bool ready = false;
+                for (int u = pair; u < units && !failed; u += pairs) {
+                    int kb0;
+                    const int n = blocks_of(u, &kb0), segments = segments_of(n);      // (none in a part without blocks: a short last piece)
+                    for (int g = 0; g < segments && !failed; ++g, ++i) {
+                        const uint32_t acc = (uint32_t)i & 1u, d = tmem_base + acc * kTile;
+                        if (!ptx::mbar_wait_lanes(&bars->tmem_empty[acc], (((uint32_t)i >> 1) & 1u) ^ 1u, abort_flag, P.wait_ns)) { failed = true; break; }
+                        ptx::tc_fence_after();
+                        const int first = n * g / segments, last = n * (g + 1) / segments - 1;
+                        for (int kb = first; kb <= last; ++kb) {
+                            if (!ready && !ptx::mbar_wait_lanes(&bars->full[s], ph, abort_flag, P.wait_ns)) { failed = true; break; }
+                            ptx::tc_fence_after();
+                            const uint64_t a = a0 + (uint64_t)s * (kStage >> 4), b = b0 + (uint64_t)s * (kStage >> 4);
+                            const int here = s;
+                            if (++s == kRing) { s = 0; ph ^= 1u; }
+                            ready = __all_sync(0xffffffffu, ptx::mbar_test_wait(&bars->full[s], ph));      // (asked for ahead of its use)
+                            if (leader) {
+#pragma unroll
+                                for (uint32_t k = 0; k < kDepth / 16; ++k) ptx::umma_bf16_pair(d, a + 2u * k, b + b_step * k, idesc, (kb != first || k != 0) ? 1u : 0u);
+                                ptx::umma_commit_pair(&bars->empty[here]);
+                                if (kb == last) ptx::umma_commit_pair(&bars->tmem_full[acc]);
+                            }
+                            __syncwarp();
+                        }
+                    }
+                }
+                if (failed) bars->abort = 1u;
+            }
         }
-    }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
         // ------------------------------------------------------------------ epilogue: a lane is a token, a warp takes half of the tile's columns, 32 at a time
@@ -239,143 +254,181 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         const int chunks = P.width / 32, c_first = ch == 0 ? 0 : (chunks + 1) / 2, c_count = ch == 0 ? (chunks + 1) / 2 : chunks / 2;
         const uint32_t empty0 = ptx::map_to_cta(ptx::smem_u32(&bars->tmem_empty[0]), 0u);
         int i = 0;
-        for (int u = pair; u < units && !failed; u += pairs) {
-            const int t = tile_of(u), tn = t / P.tiles_m, row = t % P.tiles_m * kTile + (int)crank * 128 + q * 32 + lane;
-            const bool mine = row < P.M;
-            int kb0;
-            const int segments = segments_of(blocks_of(u, &kb0));
+        // an accumulator's columns from `first` on: `take` reads them, then it is free
+        auto drain = [&](int first, auto take) {
+            const uint32_t acc = (uint32_t)i & 1u;
+            if (!ptx::mbar_wait_warp(&bars->tmem_full[acc], ((uint32_t)i >> 1) & 1u, abort_flag, P.wait_ns)) { failed = true; return; }
+            ptx::tc_fence_after();
+            take(tmem_base + acc * kTile + ((uint32_t)(q * 32) << 16) + (uint32_t)first);
+            ptx::tc_fence_before();
             __syncwarp();
-            // what belongs to the token is asked for ahead of the tile
-            float lift = -INFINITY, scale = 1.0f;
-            int label = -1;
-            if (mine) {
-                if (KIND == kExponentials && !P.first) lift = P.lift[row];
-                if (KIND != kGradient) {
-                    const long long y = P.labels[row];
-                    label = y >= 0 && y < P.V ? (int)y : -1;
-                }
-                if (KIND == kGradient && !P.first) scale = P.scale[row];
+            if (lane == 0) {
+                if (crank == 0u) ptx::mbar_arrive(&bars->tmem_empty[acc]);
+                else ptx::mbar_arrive_cluster(empty0 + acc * 8u);
             }
-            uint32_t v[4][32];
-            // the next accumulator's columns: `take` reads them, then it is free
-            auto drain = [&](auto take) {
-                const uint32_t acc = (uint32_t)i & 1u;
-                if (!ptx::mbar_wait_warp(&bars->tmem_full[acc], ((uint32_t)i >> 1) & 1u, abort_flag, P.wait_ns)) { failed = true; return; }
-                ptx::tc_fence_after();
-                take(tmem_base + acc * kTile + ((uint32_t)(q * 32) << 16) + (uint32_t)c_first * 32u);
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (crank == 0u) ptx::mbar_arrive(&bars->tmem_empty[acc]);
-                    else ptx::mbar_arrive_cluster(empty0 + acc * 8u);
-                }
-                ++i;
-            };
-            if (KIND != kGradient || segments > 0) {
-                drain([&](uint32_t from) {
+            ++i;
+        };
+        if constexpr (KIND == kFew) {
+            // a lane is a word, a column a token: a token's largest and sum are the warp's, by shuffles; half of the tokens to a warp
+            const int first = ch * 32, place = q * 32 + lane, half = P.width / 2;
+            for (int u = pair; u < units && !failed; u += pairs) {
+                const int word = P.v0 + u * P.width + (int)crank * half + place, segments = segments_of(P.blocks);
+                const bool is_word = place < half && word < P.V;
+                float v[32];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(from + (uint32_t)c * 32u, v[c]);
-                    ptx::tmem_ld_wait();
-                });
-            } else {
+                for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+                for (int g = 0; g < segments && !failed; ++g)
+                    drain(first, [&](uint32_t from) {
+                        if (first >= P.columns) return;
+                        uint32_t w[32];
+                        ptx::tmem_ld_32x32(from, w);
+                        ptx::tmem_ld_wait();
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[c][j] = 0u;
-            }
-            if constexpr (KIND != kGradient)
-                for (int g = 1; g < segments && !failed; ++g)
-                    drain([&](uint32_t from) {
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t w[32];
-                            ptx::tmem_ld_32x32(from + (uint32_t)c * 32u, w);
-                            ptx::tmem_ld_wait();
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) v[c][j] = __float_as_uint(__uint_as_float(v[c][j]) + __uint_as_float(w[j]));
-                        }
+                        for (int j = 0; j < 32; ++j) v[j] += __uint_as_float(w[j]);
                     });
-            if (failed) break;
-            const int n0 = tn * P.width + c_first * 32;      // the first column, in the piece
-            if constexpr (KIND == kGradient) {
-                const bool is_whole = u < P.whole, ends = is_whole && P.last != 0;
-                float* out = is_whole ? P.out + (size_t)row * P.N + n0
-                                      : P.parts + (size_t)(u - P.whole) * (kTile * kTile) + ((int)crank * 128 + q * 32 + lane) * kTile + c_first * 32;
-                Factors f = {0.0f, 0.0f, nullptr};
-                if (ends && mine) f = factors_of(P.end, row);
+                if (failed) break;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int j = 0; j < 32; ++j) {
+                    const int token = first + j;
+                    if (token >= P.M) continue;      // (the same in all lanes)
+                    const bool own = P.labels[token] == (long long)word && is_word;
+                    if (own) P.label_logit[token] = v[j];
+                    const float x = is_word && !own ? v[j] : -INFINITY;
+                    float most = x;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (!mine || n0 + c * 32 + j * 8 >= P.N) continue;
-                        float* at = out + c * 32 + j * 8;
-                        uint32_t* w = &v[c][j * 8];
-                        if (!P.first) {
-                            const float4 a = reinterpret_cast<const float4*>(at)[0], b = reinterpret_cast<const float4*>(at)[1];
-                            const float old[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                    for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+                    const float under = most == -INFINITY ? 0.0f : most * kLog2e;
+                    float sum = exp2_fast(fmaf(x, kLog2e, -under));
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(fmaf(old[k], scale, __uint_as_float(w[k])));
-                        }
-                        if (ends) {
-                            float o[8];
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) o[k] = __uint_as_float(w[k]);
-                            const int k0 = n0 + c * 32 + j * 8;
-                            *reinterpret_cast<uint4*>(P.end.dX + (size_t)row * P.N + k0) = end_of(f, o, k0);
-                        } else {
-                            ptx::st_global_v8(at, w);
-                        }
-                    }
+                    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                    if (lane == 0) P.stats[(size_t)((u * 2 + (int)crank) * 4 + q) * P.M + token] = make_float2(most == -INFINITY ? -INFINITY : under, sum);
                 }
-            } else {
-                // the label's word and those past the last do not take part, nor do columns that a narrower tile does not have
-                const int at = label - (P.v0 + n0), last = min(P.V - (P.v0 + n0), c_count * 32);
-                if (__any_sync(0xffffffffu, (at >= 0 && at < last) || last < 128)) {
+            }
+        } else {
+            for (int u = pair; u < units && !failed; u += pairs) {
+                const int t = tile_of(u), tn = t / P.tiles_m, row = t % P.tiles_m * kTile + (int)crank * 128 + q * 32 + lane;
+                const bool mine = row < P.M;
+                int kb0;
+                const int segments = segments_of(blocks_of(u, &kb0));
+                __syncwarp();
+                // what belongs to the token is asked for ahead of the tile
+                float lift = -INFINITY, scale = 1.0f;
+                int label = -1;
+                if (mine) {
+                    if (KIND == kExponentials && !P.first) lift = P.lift[row];
+                    if (KIND != kGradient) {
+                        const long long y = P.labels[row];
+                        label = y >= 0 && y < P.V ? (int)y : -1;
+                    }
+                    if (KIND == kGradient && !P.first) scale = P.scale[row];
+                }
+                uint32_t v[4][32];
+                if (KIND != kGradient || segments > 0) {
+                    drain(c_first * 32, [&](uint32_t from) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(from + (uint32_t)c * 32u, v[c]);
+                        ptx::tmem_ld_wait();
+                    });
+                } else {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            if (c * 32 + j == at && at < last) P.label_logit[row] = __uint_as_float(v[c][j]);
-                            if (c * 32 + j == at || c * 32 + j >= last) v[c][j] = 0xff800000u;
+                        for (int j = 0; j < 32; ++j) v[c][j] = 0u;
+                }
+                if constexpr (KIND != kGradient)
+                    for (int g = 1; g < segments && !failed; ++g)
+                        drain(c_first * 32, [&](uint32_t from) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t w[32];
+                                ptx::tmem_ld_32x32(from + (uint32_t)c * 32u, w);
+                                ptx::tmem_ld_wait();
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) v[c][j] = __float_as_uint(__uint_as_float(v[c][j]) + __uint_as_float(w[j]));
+                            }
+                        });
+                if (failed) break;
+                const int n0 = tn * P.width + c_first * 32;      // the first column, in the piece
+                if constexpr (KIND == kGradient) {
+                    const bool is_whole = u < P.whole, ends = is_whole && P.last != 0;
+                    float* out = is_whole ? P.out + (size_t)row * P.N + n0
+                                          : P.parts + (size_t)(u - P.whole) * (kTile * kTile) + ((int)crank * 128 + q * 32 + lane) * kTile + c_first * 32;
+                    Factors f = {0.0f, 0.0f, nullptr};
+                    if (ends && mine) f = factors_of(P.end, row);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (!mine || n0 + c * 32 + j * 8 >= P.N) continue;
+                            float* at = out + c * 32 + j * 8;
+                            uint32_t* w = &v[c][j * 8];
+                            if (!P.first) {
+                                const float4 a = reinterpret_cast<const float4*>(at)[0], b = reinterpret_cast<const float4*>(at)[1];
+                                const float old[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(fmaf(old[k], scale, __uint_as_float(w[k])));
+                            }
+                            if (ends) {
+                                float o[8];
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) o[k] = __uint_as_float(w[k]);
+                                const int k0 = n0 + c * 32 + j * 8;
+                                *reinterpret_cast<uint4*>(P.end.dX + (size_t)row * P.N + k0) = end_of(f, o, k0);
+                            } else {
+                                ptx::st_global_v8(at, w);
+                            }
                         }
-                }
-                float most = -INFINITY, sum = 0.0f;
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) most = fmaxf(most, __uint_as_float(v[c][j]));
-                // under which the exponentials are taken, in octaves: the largest, or the token's lift
-                const float octaves = most * kLog2e;
-                float under = 0.0f;
-                if (KIND == kSums) {
-                    if (most != -INFINITY) under = octaves;
-                } else {
-                    if (lift != -INFINITY) under = lift;
-                    if (octaves - under > kHeadroom || (lift == -INFINITY && octaves - under < -kHeadroom)) under = most == -INFINITY ? under : ceilf(octaves);
-                }
-                float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const float y = exp2_fast(fmaf(__uint_as_float(v[c][j]), kLog2e, -under));
-                        v[c][j] = __float_as_uint(y);
-                        part[j & 3] += y;
                     }
-                }
-                sum = (part[0] + part[1]) + (part[2] + part[3]);
-                if (mine) {
-                    P.stats[(size_t)(tn * 2 + ch) * P.M + row] = make_float2(most == -INFINITY ? -INFINITY : under, sum);
-                    if constexpr (KIND == kExponentials) {
-                        uint16_t* e = P.e + (size_t)row * P.ld_e + n0;
+                } else {
+                    // the label's word and those past the last do not take part, nor do columns that a narrower tile does not have
+                    const int at = label - (P.v0 + n0), last = min(P.V - (P.v0 + n0), c_count * 32);
+                    if (__any_sync(0xffffffffu, (at >= 0 && at < last) || last < 128)) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            if (c >= c_count) continue;
-                            uint32_t w[16];
+                        for (int c = 0; c < 4; ++c)
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) w[j] = pack_bf16x2(__uint_as_float(v[c][2 * j]), __uint_as_float(v[c][2 * j + 1]));
-                            ptx::st_global_v8(e + c * 32, w);
-                            ptx::st_global_v8(e + c * 32 + 16, w + 8);
+                            for (int j = 0; j < 32; ++j) {
+                                if (c * 32 + j == at && at < last) P.label_logit[row] = __uint_as_float(v[c][j]);
+                                if (c * 32 + j == at || c * 32 + j >= last) v[c][j] = 0xff800000u;
+                            }
+                    }
+                    float most = -INFINITY, sum = 0.0f;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) most = fmaxf(most, __uint_as_float(v[c][j]));
+                    // under which the exponentials are taken, in octaves: the largest, or the token's lift
+                    const float octaves = most * kLog2e;
+                    float under = 0.0f;
+                    if (KIND == kSums) {
+                        if (most != -INFINITY) under = octaves;
+                    } else {
+                        if (lift != -INFINITY) under = lift;
+                        if (octaves - under > kHeadroom || (lift == -INFINITY && octaves - under < -kHeadroom)) under = most == -INFINITY ? under : ceilf(octaves);
+                    }
+                    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float y = exp2_fast(fmaf(__uint_as_float(v[c][j]), kLog2e, -under));
+                            v[c][j] = __float_as_uint(y);
+                            part[j & 3] += y;
+                        }
+                    }
+                    sum = (part[0] + part[1]) + (part[2] + part[3]);
+                    if (mine) {
+                        P.stats[(size_t)(tn * 2 + ch) * P.M + row] = make_float2(most == -INFINITY ? -INFINITY : under, sum);
+                        if constexpr (KIND == kExponentials) {
+                            uint16_t* e = P.e + (size_t)row * P.ld_e + n0;
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                if (c >= c_count) continue;
+                                uint32_t w[16];
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) w[j] = pack_bf16x2(__uint_as_float(v[c][2 * j]), __uint_as_float(v[c][2 * j + 1]));
+                                ptx::st_global_v8(e + c * 32, w);
+                                ptx::st_global_v8(e + c * 32 + 16, w + 8);
+                            }
                         }
                     }
                 }
@@ -548,7 +601,8 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 // How a call is cut: by rules on its sizes alone, so that the scratch can be asked for beforehand.
 struct CePlan {
     int passes, tokens;                 // passes over the tokens, tokens of one
-    int width, tiles;                   // columns of a tile of logits, and tiles of a piece
+    int width, tiles;                   // columns of a tile of logits (few tokens: rows), and tiles of a piece
+    int few, entries;                   // few tokens, no gradient: columns of the tile; parts of a token's sum that a tile leaves
     int pieces, piece;                  // pieces of the vocabulary, their words (the last may have fewer)
     size_t off_rows, off_stats, off_e, off_out, off_parts, total;
 };
@@ -589,9 +643,11 @@ CePlan plan_of(int M, int V, int K, bool grad) {
     p.tiles = (words + p.width - 1) / p.width;
     p.piece = p.pieces > 1 ? p.tiles * p.width : V;
     p.pieces = (V + p.piece - 1) / p.piece;
+    p.few = !grad && M <= kFewTokens ? (M + 31) / 32 * 32 : 0;
+    p.entries = p.few ? 8 : 2;
     p.off_rows = 256;
     p.off_stats = p.off_rows + 4 * up256((size_t)p.tokens * 4);
-    p.off_e = p.off_stats + up256((size_t)p.tiles * 2 * p.tokens * 8);
+    p.off_e = p.off_stats + up256((size_t)p.tiles * p.entries * p.tokens * 8);
     p.off_out = p.off_e + (grad ? up256((size_t)p.tokens * p.tiles * p.width * 2) : 0);
     p.off_parts = p.off_out + (grad && p.pieces > 1 ? up256((size_t)p.tokens * K * 4) : 0);
     size_t parts = 0;
@@ -612,7 +668,7 @@ bool good_sizes(int M, int V, int K) { return M >= 1 && M <= kMostM && V >= 1 &&
 template <int KIND>
 lowra_status launch_product(CeParams& P, cudaStream_t stream) {
     static SmemLimit limit = {};
-    if (ensure_smem_limit(reinterpret_cast<const void*>(product_kernel<KIND>), kSmem, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
+    if (ensure_smem_limit(reinterpret_cast<const void*>(product_kernel<KIND>), kSmem<KIND>, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
     // (the warps' shares of the registers were added up for a kernel of this size)
     static std::atomic<int> registers{0};
     if (registers.load(std::memory_order_relaxed) == 0) {
@@ -632,7 +688,7 @@ lowra_status launch_product(CeParams& P, cudaStream_t stream) {
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3((unsigned)pairs * 2, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = kSmem;
+    cfg.dynamicSmemBytes = kSmem<KIND>;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
@@ -703,8 +759,13 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
             P.tiles_n = p.tiles;
             P.whole = P.tiles_m * P.tiles_n;
             P.clear_status = pass == 0;
-            if ((st = launch_product<kSums>(P, stream)) != LOWRA_OK) return st;
-            if (launch_pdl(loss_kernel, (unsigned)((m + kTokens - 1) / kTokens), kTokens * kLanes, stream, (const float2*)stats, 2 * p.tiles, (const float*)R.logit, labels, m, (int)V, (long long)ignore_index,
+            if (p.few) {
+                P.columns = p.few;
+                if (!make_map(&P.a, W_dev, (uint64_t)V, (uint64_t)K, (uint64_t)K, (uint32_t)p.width / 2) || !make_map(&P.b, X, (uint64_t)m, (uint64_t)K, (uint64_t)K, (uint32_t)p.few / 2))
+                    return LOWRA_ERR_CUDA;
+            }
+            if ((st = p.few ? launch_product<kFew>(P, stream) : launch_product<kSums>(P, stream)) != LOWRA_OK) return st;
+            if (launch_pdl(loss_kernel, (unsigned)((m + kTokens - 1) / kTokens), kTokens * kLanes, stream, (const float2*)stats, p.entries * p.tiles, (const float*)R.logit, labels, m, (int)V, (long long)ignore_index,
                            loss_dev + m0) != cudaSuccess)
                 return LOWRA_ERR_CUDA;
             continue;

@@ -63,7 +63,7 @@ def check(X, W, labels, weights=None, scale=1.0, **kw):
 
 
 @pytest.mark.parametrize("M, V, K", [(1, 1, 64), (1, 2, 64), (2, 31, 64), (3, 129, 72), (16, 32000, 512), (130, 257, 4096), (257, 1000, 264), (777, 5003, 1024), (256, 256, 256),
-                                     (1000, 300, 5120), (64, 100003, 128)])
+                                     (1000, 300, 5120), (64, 100003, 128), (33, 777, 1096), (17, 5000, 4096), (65, 5000, 512)])
 @pytest.mark.parametrize("known", [0.0, 14.0])
 def test_loss_and_gradient(M, V, K, known):
     X, W, labels, weights = make(M, V, K, known=known, ignored=0.0 if M == 1 else 0.2)
