@@ -44,7 +44,7 @@ template <int KIND>
 constexpr int kStages = KIND == kFew ? 10 : 6;
 constexpr int kMostStages = 10;
 template <int KIND>
-constexpr uint32_t kSmem = kStages<KIND> * kStageBytes<KIND> + 1024;
+constexpr uint32_t kSmem = kStages<KIND> * kStageBytes<KIND> + 1024 + (KIND == kFew ? 8 * 32 * 8 : 0);
 
 struct CeBarriers {
     uint64_t full[kMostStages], empty[kMostStages];
@@ -82,7 +82,7 @@ struct CeParams {
     const long long* labels;
     const float* lift;                            // (exponentials) a token's lift so far, in octaves
     float* label_logit;                           // l_y (out)
-    float2* stats;                                // [2 tiles_n][M]: of half a tile, (largest in octaves, or lift; sum)
+    float2* stats;                                // [2 tiles_n][M]: of half a tile (few tokens: [CTAs][M]), (largest in octaves, or lift; sum)
     uint16_t* e;                                  // [M, ld_e]
     long long ld_e;
     const float* scale;                           // (gradient) 2^-(lift added by the piece)
@@ -130,12 +130,28 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
+// Of 32 values a lane, each joined over the lanes: lane l gets the one numbered l.  Halves of the values change places, so that it takes 31 shuffles in all.
+template <typename F>
+__device__ __forceinline__ float over_lanes(float (&v)[32], F join) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < d; ++i) {
+            const bool upper = (lane & d) != 0;
+            const float keep = upper ? v[i + d] : v[i], give = upper ? v[i] : v[i + d];
+            v[i] = join(keep, __shfl_xor_sync(0xffffffffu, give, d));
+        }
+    return v[0];
+}
+
 template <int KIND>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CeParams P) {
     extern __shared__ __align__(1024) unsigned char smem[];
     constexpr int kRing = kStages<KIND>;
     constexpr uint32_t kStage = kStageBytes<KIND>;
     CeBarriers* bars = reinterpret_cast<CeBarriers*>(smem + kRing * kStage);
+    [[maybe_unused]] float2* const parts = reinterpret_cast<float2*>(smem + kRing * kStage + 1024);      // (few tokens) [half of the tokens][quarter of the words][token]
     volatile uint32_t* abort_flag = &bars->abort;
     if ((ptx::smem_u32(smem) & 1023u) != 0u) {      // never seen; without it the operand descriptors would be wrong
         if (threadIdx.x == 0) atomicExch(P.status, (uint32_t)LOWRA_ERR_CUDA);
@@ -269,12 +285,15 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             ++i;
         };
         if constexpr (KIND == kFew) {
-            // a lane is a word, a column a token: a token's largest and sum are the warp's, by shuffles; half of the tokens to a warp
-            const int first = ch * 32, place = q * 32 + lane, half = P.width / 2;
+            // A lane is a word, a column a token, half of the tokens to a warp.  Lane l keeps the largest and the sum of its token l, over all of the CTA's tiles.
+            const int first = ch * 32, place = q * 32 + lane, half = P.width / 2, token = first + lane;
+            long long label = -1;
+            if (token < P.M) label = P.labels[token];
+            float top = -INFINITY, total = 0.0f;
             for (int u = pair; u < units && !failed; u += pairs) {
-                const int word = P.v0 + u * P.width + (int)crank * half + place, segments = segments_of(P.blocks);
-                const bool is_word = place < half && word < P.V;
-                float v[32];
+                const int word0 = P.v0 + u * P.width + (int)crank * half + q * 32, segments = segments_of(P.blocks);
+                const bool is_word = place < half && word0 + lane < P.V;
+                float v[32], e[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = 0.0f;
                 for (int g = 0; g < segments && !failed; ++g)
@@ -287,23 +306,37 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                         for (int j = 0; j < 32; ++j) v[j] += __uint_as_float(w[j]);
                     });
                 if (failed) break;
+                // the labels' own words do not take part, nor do lanes without one
+                const uint32_t near = __ballot_sync(0xffffffffu, label >= word0 && label < word0 + 32 && label < P.V);
+                if (near != 0u) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const long long l = __shfl_sync(0xffffffffu, label, j);
+                        if ((near >> j & 1u) != 0u && l == word0 + lane && is_word) {
+                            P.label_logit[first + j] = v[j];
+                            v[j] = -INFINITY;
+                        }
+                    }
+                }
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
-                    const int token = first + j;
-                    if (token >= P.M) continue;      // (the same in all lanes)
-                    const bool own = P.labels[token] == (long long)word && is_word;
-                    if (own) P.label_logit[token] = v[j];
-                    const float x = is_word && !own ? v[j] : -INFINITY;
-                    float most = x;
+                    if (!is_word) v[j] = -INFINITY;
+                    e[j] = v[j];
+                }
+                const float most = over_lanes(e, [](float a, float b) { return fmaxf(a, b); });
+                const float under = most == -INFINITY ? 0.0f : most * kLog2e;
 #pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-                    const float under = most == -INFINITY ? 0.0f : most * kLog2e;
-                    float sum = exp2_fast(fmaf(x, kLog2e, -under));
-#pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                    if (lane == 0) P.stats[(size_t)((u * 2 + (int)crank) * 4 + q) * P.M + token] = make_float2(most == -INFINITY ? -INFINITY : under, sum);
+                for (int j = 0; j < 32; ++j) e[j] = exp2_fast(fmaf(v[j], kLog2e, -__shfl_sync(0xffffffffu, under, j)));
+                const float sum = over_lanes(e, [](float a, float b) { return a + b; });
+                if (most != -INFINITY) {
+                    const float more = fmaxf(top, under);
+                    total = total * exp2_fast(top - more) + sum * exp2_fast(under - more);
+                    top = more;
+                } else {
+                    total += sum;                     // (zero, or NaN)
                 }
             }
+            parts[(ch * 4 + q) * 32 + lane] = make_float2(top, total);
         } else {
             for (int u = pair; u < units && !failed; u += pairs) {
                 const int t = tile_of(u), tn = t / P.tiles_m, row = t % P.tiles_m * kTile + (int)crank * 128 + q * 32 + lane;
@@ -444,6 +477,22 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     __syncwarp();
     ptx::tc_fence_before();
     __syncthreads();
+    if constexpr (KIND == kFew) {
+        const int token = threadIdx.x;
+        if (token < P.M) {                            // (up to 64; after a failure the numbers mean nothing, and the status says so)
+            float2 all = parts[token / 32 * 128 + token % 32];
+            for (int w = 1; w < 4; ++w) {
+                const float2 part = parts[token / 32 * 128 + w * 32 + token % 32];
+                if (part.x != -INFINITY) {
+                    const float more = fmaxf(all.x, part.x);
+                    all = make_float2(more, all.y * exp2_fast(all.x - more) + part.y * exp2_fast(part.x - more));
+                } else {
+                    all.y += part.y;
+                }
+            }
+            P.stats[(size_t)blockIdx.x * P.M + token] = all;
+        }
+    }
     ptx::cluster_sync();   // the peer's copies, arrivals and MMAs no longer touch this CTA
     if (*abort_flag != 0u) {
         // somebody gave up, and roles that did not wait may have left copies or MMAs in flight (the same answer in both CTAs)
@@ -461,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 }
 
 // ------------------------------------------------------------------------------------------------ the tokens' own numbers
-// A token's halves of tiles, (octaves that the exponentials were taken under, sum of them) each, joined: eight tokens to a CTA, 32 threads to a token, eight of their loads under way at once.
+// A token's halves of tiles, or of a CTA's words, (octaves that the exponentials were taken under, sum of them) each, joined: eight tokens to a CTA, 32 threads to a token, eight of their loads under way at once.
 // (Halves without a word: minus infinity and zero.)  Empty in the end where no half had one.
 constexpr int kTokens = 8, kLanes = 32;
 struct Joined {
@@ -602,7 +651,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 struct CePlan {
     int passes, tokens;                 // passes over the tokens, tokens of one
     int width, tiles;                   // columns of a tile of logits (few tokens: rows), and tiles of a piece
-    int few, entries;                   // few tokens, no gradient: columns of the tile; parts of a token's sum that a tile leaves
+    int few;                            // few tokens, no gradient: columns of the tile
     int pieces, piece;                  // pieces of the vocabulary, their words (the last may have fewer)
     size_t off_rows, off_stats, off_e, off_out, off_parts, total;
 };
@@ -644,10 +693,9 @@ CePlan plan_of(int M, int V, int K, bool grad) {
     p.piece = p.pieces > 1 ? p.tiles * p.width : V;
     p.pieces = (V + p.piece - 1) / p.piece;
     p.few = !grad && M <= kFewTokens ? (M + 31) / 32 * 32 : 0;
-    p.entries = p.few ? 8 : 2;
     p.off_rows = 256;
     p.off_stats = p.off_rows + 4 * up256((size_t)p.tokens * 4);
-    p.off_e = p.off_stats + up256((size_t)p.tiles * p.entries * p.tokens * 8);
+    p.off_e = p.off_stats + up256((size_t)(p.few ? 2 * kPairs : 2 * p.tiles) * p.tokens * 8);
     p.off_out = p.off_e + (grad ? up256((size_t)p.tokens * p.tiles * p.width * 2) : 0);
     p.off_parts = p.off_out + (grad && p.pieces > 1 ? up256((size_t)p.tokens * K * 4) : 0);
     size_t parts = 0;
@@ -665,6 +713,11 @@ CePlan plan_of(int M, int V, int K, bool grad) {
 
 bool good_sizes(int M, int V, int K) { return M >= 1 && M <= kMostM && V >= 1 && V <= kMostV && K >= 64 && K <= kMostK && K % 8 == 0; }
 
+// Pairs that a launch has: a unit each at least.
+int pairs_of(const CeParams& P) {
+    const int units = P.whole + (P.tiles_m * P.tiles_n - P.whole) * P.splits, sms = device_sm_count();
+    return units < sms / 2 ? units : sms / 2;
+}
 template <int KIND>
 lowra_status launch_product(CeParams& P, cudaStream_t stream) {
     static SmemLimit limit = {};
@@ -676,9 +729,8 @@ lowra_status launch_product(CeParams& P, cudaStream_t stream) {
         if (cudaFuncGetAttributes(&of, product_kernel<KIND>) != cudaSuccess) return LOWRA_ERR_CUDA;
         registers.store(of.numRegs, std::memory_order_relaxed);
     }
-    const int sms = device_sm_count();
-    if (sms < 2 || registers.load(std::memory_order_relaxed) != kLaunchRegisters) return LOWRA_ERR_CUDA;
-    const int units = P.whole + (P.tiles_m * P.tiles_n - P.whole) * P.splits, pairs = units < sms / 2 ? units : sms / 2;
+    const int pairs = pairs_of(P);
+    if (pairs < 1 || registers.load(std::memory_order_relaxed) != kLaunchRegisters) return LOWRA_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -765,7 +817,7 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
                     return LOWRA_ERR_CUDA;
             }
             if ((st = p.few ? launch_product<kFew>(P, stream) : launch_product<kSums>(P, stream)) != LOWRA_OK) return st;
-            if (launch_pdl(loss_kernel, (unsigned)((m + kTokens - 1) / kTokens), kTokens * kLanes, stream, (const float2*)stats, p.entries * p.tiles, (const float*)R.logit, labels, m, (int)V, (long long)ignore_index,
+            if (launch_pdl(loss_kernel, (unsigned)((m + kTokens - 1) / kTokens), kTokens * kLanes, stream, (const float2*)stats, p.few ? 2 * pairs_of(P) : 2 * p.tiles, (const float*)R.logit, labels, m, (int)V, (long long)ignore_index,
                            loss_dev + m0) != cudaSuccess)
                 return LOWRA_ERR_CUDA;
             continue;
