@@ -105,7 +105,8 @@ __device__ __forceinline__ Factors factors_of(const CeEnd& E, int m) {
         return {none, none, nullptr};
     }
     if (y == E.ignore) return {0.0f, 0.0f, nullptr};
-    const float sum = E.rows.sum[m], own = exp2f(fmaf(E.rows.logit[m], kLog2e, -E.rows.lift[m])), c = E.weights != nullptr ? E.scale * E.weights[m] : E.scale;
+    const float logit = E.rows.logit[m], sum = E.rows.sum[m], c = E.weights != nullptr ? E.scale * E.weights[m] : E.scale;
+    const float own = logit < INFINITY ? exp2f(fmaf(logit, kLog2e, -E.rows.lift[m])) : NAN;
     const float a = c / (sum + own);
     return {a, -a * sum, E.W + (size_t)y * E.K};
 }
@@ -557,6 +558,14 @@ struct Joined {
     }
 };
 
+// -log of the label's share, from its logit and the sum of the others' exponentials, taken under `top` octaves (minus infinity: none has one).
+__device__ __forceinline__ float loss_of(float logit, float top, float sum) {
+    if (!(logit < INFINITY) || (top == -INFINITY && logit == -INFINITY)) return NAN;
+    if (top == -INFINITY) return sum;                         // (zero, or NaN)
+    const float over = fmaf(logit, kLog2e, -top);             // the label's logit above the others', octaves
+    return over >= 0.0f ? log1pf(sum * exp2f(-over)) : logf(sum + exp2f(over)) - over * kLn2;
+}
+
 // Loss without a gradient.
 __global__ void __launch_bounds__(kTokens * kLanes) loss_kernel(const float2* stats, int count, const float* logit, const long long* labels, int M, int V, long long ignore, float* loss) {
     __shared__ float shared[kTokens * kLanes / 32][kTokens][3];
@@ -570,8 +579,7 @@ __global__ void __launch_bounds__(kTokens * kLanes) loss_kernel(const float2* st
         loss[m] = y == ignore ? 0.0f : NAN;
         return;
     }
-    const float over = fmaf(logit[m], kLog2e, -all.top);      // the label's logit above the largest of the others, octaves
-    loss[m] = all.top == -INFINITY ? all.sum : over >= 0.0f ? log1pf(all.sum * exp2f(-over)) : logf(all.sum + exp2f(over)) - over * kLn2;
+    loss[m] = loss_of(logit[m], all.top, all.sum);
 }
 
 // Between a piece's two products: the largest lift of each token, its sum, the factor for O; exponentials that were formed under a smaller lift are brought to it.
@@ -629,13 +637,7 @@ __global__ void __launch_bounds__(256) finish_kernel(const CeEnd E, const float*
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < M; i += step) {
         const int m = (int)i;
         const long long y = E.labels[m];
-        float value = 0.0f;
-        if (y != E.ignore) {
-            const bool word = y >= 0 && y < E.V;
-            const float sum = word ? E.rows.sum[m] : NAN, over = word ? fmaf(E.rows.logit[m], kLog2e, -E.rows.lift[m]) : 0.0f;      // (over: the label's logit above the lift, octaves)
-            value = sum == 0.0f ? 0.0f : over >= 0.0f ? log1pf(sum * exp2f(-over)) : logf(sum + exp2f(over)) - over * kLn2;
-        }
-        loss[m] = value;
+        loss[m] = y == E.ignore ? 0.0f : y >= 0 && y < E.V ? loss_of(E.rows.logit[m], E.rows.lift[m], E.rows.sum[m]) : NAN;
     }
 }
 

@@ -210,3 +210,18 @@ def test_waits_that_may_run_out():
         assert torch.equal(loss, good) and torch.equal(dX, good_dX)
     loss, dX = lw.lowra_cross_entropy(X, W, labels, want_grad=True, workspace=ws)
     assert lw.lowra_device_status(ws) == lw.LOWRA_OK and torch.equal(loss, good) and torch.equal(dX, good_dX)
+
+
+@pytest.mark.parametrize("M, V", [(5, 900), (300, 900), (3, 1), (257, 1)])
+def test_labels_whose_logit_is_no_number(M, V):
+    """The label's own logit NaN or +infinity: NaN, although the label's word is left out of the sums; -infinity: the loss is infinite, or NaN where there is no other word."""
+    for value, beside in ((float("inf"), True), (float("nan"), True), (float("-inf"), V == 1)):
+        X, W, labels, _ = make(M, V, 128, ignored=0.0)
+        X[:, 3] = 1.0
+        labels[:] = V // 2
+        W[V // 2, 3] = value
+        loss, dX = lw.lowra_cross_entropy(X, W, labels, want_grad=True)
+        only, _ = lw.lowra_cross_entropy(X, W, labels)
+        for got in (loss, only):
+            assert got.isnan().all() if beside else (got == float("inf")).all()
+        assert dX.isnan().any(1).all()
