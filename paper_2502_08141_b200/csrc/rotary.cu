@@ -56,88 +56,82 @@ __global__ void __launch_bounds__(kRotaryThreads, kRotaryResident) rotary_kernel
     const int begin = (int)((long long)P.M * range / P.ranges), end = (int)((long long)P.M * (range + 1) / P.ranges);
     const int head0 = P.heads * split / P.splits, heads = P.heads * (split + 1) / P.splits - head0;
     const int turned = P.R / 16, per_head = turned + (P.D - P.R + 15) / 16, pairs = P.R / 2;
-    const int lanes = max(1, kRotaryThreads / per_head);       // heads side by side (a head of more pieces than threads: one, its pieces in turns)
-    const int lane = (int)threadIdx.x / per_head;
+    const int lanes = kRotaryThreads / per_head;       // heads side by side (a head has 256 pieces at most)
+    const int lane = (int)threadIdx.x / per_head, u = (int)threadIdx.x % per_head;     // a thread's head and piece
     constexpr int kAhead = 2;
     Piece q[kAhead];
     for (int token0 = begin; token0 < end; token0 += P.tokens) {
         const int tokens = min(P.tokens, end - token0);
         if (token0 > begin) __syncthreads();            // the table has been read
-        bool made = false;
-        for (int u = (int)threadIdx.x % per_head; u < per_head; u += kRotaryThreads) {
-            const bool turns = u < turned;
-            const int at = turns ? (INTERLEAVED ? u * 16 : u * 8) : P.R + (u - turned) * 16, other = INTERLEAVED || !turns ? 8 : P.R / 2;
-            const bool both = turns || at + 8 < P.D;     // (the last piece to copy may have eight values)
-            int token = 0, head = lane;                 // of the next piece to load
-            auto load = [&](Piece& p) {
-                while (head >= heads) { head -= heads; ++token; }
-                p.to = nullptr;
-                p.token = token;
-                if (token < tokens && lane < lanes) {
-                    const bool second = head0 + head >= P.part[0].heads;
-                    const RotaryPart& part = P.part[second ? 1 : 0];
-                    const int h = head0 + head - (second ? P.part[0].heads : 0);
-                    if (turns || part.copies) {
-                        const uint16_t* x = part.x + (long long)(token0 + token) * part.x_token + (long long)h * part.x_head + at;
-                        p.a = load8(x);
-                        if (both) p.b = load8(x + other);
-                        p.to = part.out + (long long)(token0 + token) * part.out_token + (long long)h * part.out_head + at;
-                    }
+        const bool turns = u < turned;
+        const int at = turns ? (INTERLEAVED ? u * 16 : u * 8) : P.R + (u - turned) * 16, other = INTERLEAVED || !turns ? 8 : P.R / 2;
+        const bool both = turns || at + 8 < P.D;     // (the last piece to copy may have eight values)
+        int token = 0, head = lane;                 // of the next piece to load
+        auto load = [&](Piece& p) {
+            while (head >= heads) { head -= heads; ++token; }
+            p.to = nullptr;
+            p.token = token;
+            if (token < tokens && lane < lanes) {
+                const bool second = head0 + head >= P.part[0].heads;
+                const RotaryPart& part = P.part[second ? 1 : 0];
+                const int h = head0 + head - (second ? P.part[0].heads : 0);
+                if (turns || part.copies) {
+                    const uint16_t* x = part.x + (long long)(token0 + token) * part.x_token + (long long)h * part.x_head + at;
+                    p.a = load8(x);
+                    if (both) p.b = load8(x + other);
+                    p.to = part.out + (long long)(token0 + token) * part.out_token + (long long)h * part.out_head + at;
                 }
-                head += lanes;
-            };
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) load(q[k]);
-            if (!made) {                                // (every thread comes by here once)
-                made = true;
-                for (int i = threadIdx.x; i < tokens * pairs; i += kRotaryThreads) {
-                    const int m = i / pairs, pair = i - m * pairs;
-                    // the turn's fraction, to the nearest 2^-32, as half turns from -1 to 1
-                    const unsigned long long turn = (unsigned long long)(long long)P.positions[token0 + m] * P.turns[pair] + 0x80000000ull;
-                    float s, c;
-                    sincospif((float)(int32_t)(uint32_t)(turn >> 32) * 0x1p-31f, &s, &c);
-                    reinterpret_cast<float2*>(table + (m * 4 + (pair & 7) / 2) * turned + pair / 8)[pair & 1] = make_float2(c * P.scale, (P.inverse ? -s : s) * P.scale);
-                }
-                __syncthreads();
             }
-            int have = -1;                              // the token whose cosines and sines are at hand
-            float4 cs[4];
-            auto finish = [&](Piece& p) {
-                if (p.to == nullptr) return;
-                if (turns) {
-                    if (p.token != have) {
-                        have = p.token;
+            head += lanes;
+        };
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) cs[i] = table[(have * 4 + i) * turned + u];
-                    }
-                    const uint32_t a[4] = {p.a.x, p.a.y, p.a.z, p.a.w}, b[4] = {p.b.x, p.b.y, p.b.z, p.b.w};
-                    uint32_t ra[4], rb[4];
+        for (int k = 0; k < kAhead; ++k) load(q[k]);
+        for (int i = threadIdx.x; i < tokens * pairs; i += kRotaryThreads) {
+            const int m = i / pairs, pair = i - m * pairs;
+            // the turn's fraction, to the nearest 2^-32, as half turns from -1 to 1
+            const unsigned long long turn = (unsigned long long)(long long)P.positions[token0 + m] * P.turns[pair] + 0x80000000ull;
+            float s, c;
+            sincospif((float)(int32_t)(uint32_t)(turn >> 32) * 0x1p-31f, &s, &c);
+            reinterpret_cast<float2*>(table + (m * 4 + (pair & 7) / 2) * turned + pair / 8)[pair & 1] = make_float2(c * P.scale, (P.inverse ? -s : s) * P.scale);
+        }
+        __syncthreads();
+        int have = -1;                              // the token whose cosines and sines are at hand
+        float4 cs[4];
+        auto finish = [&](Piece& p) {
+            if (p.to == nullptr) return;
+            if (turns) {
+                if (p.token != have) {
+                    have = p.token;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float4 c = cs[i];         // two pairs
-                        if (INTERLEAVED) {
-                            const uint32_t v0 = i < 2 ? a[2 * i] : b[2 * i - 4], v1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
-                            const uint32_t r0 = pack_bf16x2(low(v0) * c.x - high(v0) * c.y, high(v0) * c.x + low(v0) * c.y);
-                            const uint32_t r1 = pack_bf16x2(low(v1) * c.z - high(v1) * c.w, high(v1) * c.z + low(v1) * c.w);
-                            if (i < 2) { ra[2 * i] = r0; ra[2 * i + 1] = r1; }
-                            else { rb[2 * i - 4] = r0; rb[2 * i - 3] = r1; }
-                        } else {
-                            ra[i] = pack_bf16x2(low(a[i]) * c.x - low(b[i]) * c.y, high(a[i]) * c.z - high(b[i]) * c.w);
-                            rb[i] = pack_bf16x2(low(b[i]) * c.x + low(a[i]) * c.y, high(b[i]) * c.z + high(a[i]) * c.w);
-                        }
-                    }
-                    p.a = make_uint4(ra[0], ra[1], ra[2], ra[3]);
-                    p.b = make_uint4(rb[0], rb[1], rb[2], rb[3]);
+                    for (int i = 0; i < 4; ++i) cs[i] = table[(have * 4 + i) * turned + u];
                 }
-                *reinterpret_cast<uint4*>(p.to) = p.a;
-                if (both) *reinterpret_cast<uint4*>(p.to + other) = p.b;
-            };
-            while (q[0].token < tokens) {               // (pieces come in order: where the first is past the end, so is the other)
+                const uint32_t a[4] = {p.a.x, p.a.y, p.a.z, p.a.w}, b[4] = {p.b.x, p.b.y, p.b.z, p.b.w};
+                uint32_t ra[4], rb[4];
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k) {
-                    finish(q[k]);
-                    load(q[k]);
+                for (int i = 0; i < 4; ++i) {
+                    const float4 c = cs[i];         // two pairs
+                    if (INTERLEAVED) {
+                        const uint32_t v0 = i < 2 ? a[2 * i] : b[2 * i - 4], v1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
+                        const uint32_t r0 = pack_bf16x2(low(v0) * c.x - high(v0) * c.y, high(v0) * c.x + low(v0) * c.y);
+                        const uint32_t r1 = pack_bf16x2(low(v1) * c.z - high(v1) * c.w, high(v1) * c.z + low(v1) * c.w);
+                        if (i < 2) { ra[2 * i] = r0; ra[2 * i + 1] = r1; }
+                        else { rb[2 * i - 4] = r0; rb[2 * i - 3] = r1; }
+                    } else {
+                        ra[i] = pack_bf16x2(low(a[i]) * c.x - low(b[i]) * c.y, high(a[i]) * c.z - high(b[i]) * c.w);
+                        rb[i] = pack_bf16x2(low(b[i]) * c.x + low(a[i]) * c.y, high(b[i]) * c.z + high(a[i]) * c.w);
+                    }
                 }
+                p.a = make_uint4(ra[0], ra[1], ra[2], ra[3]);
+                p.b = make_uint4(rb[0], rb[1], rb[2], rb[3]);
+            }
+            *reinterpret_cast<uint4*>(p.to) = p.a;
+            if (both) *reinterpret_cast<uint4*>(p.to + other) = p.b;
+        };
+        while (q[0].token < tokens) {               // (pieces come in order: where the first is past the end, so is the other)
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                finish(q[k]);
+                load(q[k]);
             }
         }
     }
