@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(kRotaryThreads, kRotaryResident) rotary_kernel
     const int turned = P.R / 16, per_head = turned + (P.D - P.R + 15) / 16, pairs = P.R / 2;
     const int lanes = kRotaryThreads / per_head;       // heads side by side (a head has 256 pieces at most)
     const int lane = (int)threadIdx.x / per_head, u = (int)threadIdx.x % per_head;     // a thread's head and piece
+    const int first = lane / heads, tokens_on = lanes / heads, heads_on = lanes - tokens_on * heads;      // from a thread's piece to its next
     constexpr int kAhead = 2;
     Piece q[kAhead];
     for (int token0 = begin; token0 < end; token0 += P.tokens) {
@@ -66,9 +67,8 @@ __global__ void __launch_bounds__(kRotaryThreads, kRotaryResident) rotary_kernel
         const bool turns = u < turned;
         const int at = turns ? (INTERLEAVED ? u * 16 : u * 8) : P.R + (u - turned) * 16, other = INTERLEAVED || !turns ? 8 : P.R / 2;
         const bool both = turns || at + 8 < P.D;     // (the last piece to copy may have eight values)
-        int token = 0, head = lane;                 // of the next piece to load
+        int token = first, head = lane - first * heads;                 // of the next piece to load
         auto load = [&](Piece& p) {
-            while (head >= heads) { head -= heads; ++token; }
             p.to = nullptr;
             p.token = token;
             if (token < tokens && lane < lanes) {
@@ -82,7 +82,9 @@ __global__ void __launch_bounds__(kRotaryThreads, kRotaryResident) rotary_kernel
                     p.to = part.out + (long long)(token0 + token) * part.out_token + (long long)h * part.out_head + at;
                 }
             }
-            head += lanes;
+            token += tokens_on;
+            head += heads_on;
+            if (head >= heads) { head -= heads; ++token; }
         };
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) load(q[k]);
