@@ -76,6 +76,7 @@ struct CeParams {
     int v0;                                       // the piece's first word
     int width, tiles_m, tiles_n;                  // columns of a tile; tiles  (few tokens: words of a tile, its rows; tiles_m 1)
     int columns;                                  // (few tokens) of a tile: the tokens, filled up to a multiple of 32
+    int a_rows, a_halves;                         // (not of few tokens) rows that a CTA loads of its half of a tile's tokens, and CTAs of a pair that do
     int whole, splits;                            // the first tiles are whole, the contraction of the others is cut into so many parts (all whole: splits 1)
     int blocks;                                   // contraction blocks in all
     int first, last;                              // the first piece: lift and O have no value yet; (gradient) the last one: whole tiles are finished
@@ -198,8 +199,10 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             const bool leader = ptx::elect_one();
             ptx::fence_proxy_async_all();               // (the exponentials were written by ordinary stores)
             const uint32_t full0 = ptx::map_to_cta(ptx::smem_u32(&bars->full[0]), 0u);
-            // half the tile's rows and columns x 64 x 2 bytes
-            const uint32_t a_bytes = KIND == kFew ? (uint32_t)P.width * kDepth : kHalfBytes, b_bytes = (uint32_t)(KIND == kFew ? P.columns : P.width) * kDepth;
+            // of the pair: rows and columns x 64 x 2 bytes
+            const uint32_t a_bytes = KIND == kFew ? (uint32_t)P.width * (kDepth * 2) : (uint32_t)(P.a_rows * P.a_halves) * (kDepth * 2);
+            const uint32_t bytes = a_bytes + (uint32_t)(KIND == kFew ? P.columns : P.width) * (kDepth * 2);
+            const bool has_a = KIND == kFew || (int)crank < P.a_halves;
             int s = 0;
             uint32_t ph = 0;
             for (int u = pair; u < units && !failed; u += pairs) {
@@ -213,8 +216,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                     unsigned char* a_s = smem + s * kStage;
                     const uint32_t bar = full0 + (uint32_t)s * 8u;
                     if (leader) {
-                        if (crank == 0u) ptx::mbar_arrive_expect_tx(&bars->full[s], 2u * (a_bytes + b_bytes));
-                        ptx::tma_load_2d_pair(a_s, &P.a, kb * kDepth, m0, bar);
+                        if (crank == 0u) ptx::mbar_arrive_expect_tx(&bars->full[s], bytes);
+                        if (has_a) ptx::tma_load_2d_pair(a_s, &P.a, kb * kDepth, m0, bar);
                         if (mn) {
                             ptx::tma_load_2d_pair(a_s + kHalfBytes, &P.b, n0, P.v0 + kb * kDepth, bar);
                             ptx::tma_load_2d_pair(a_s + kHalfBytes + 8192, &P.b, n0 + 64, P.v0 + kb * kDepth, bar);
@@ -807,7 +810,11 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
         P.ld_e = ld_e;
         P.status = status;
         P.wait_ns = wait_limit_ns();
-        if (!make_map(&P.a, X, (uint64_t)m, (uint64_t)K, (uint64_t)K, 128) || !make_map(&P.b, W_dev, (uint64_t)V, (uint64_t)K, (uint64_t)K, (uint32_t)p.width / 2)) return LOWRA_ERR_CUDA;
+        // Up to 128 tokens: the second CTA of a pair has none, and the first loads its own only.  What the tile's other rows hold of earlier kernels comes out in rows that are not looked at.
+        // (35006 words, 3672 features, us with all 128 rows of either CTA, past the end filled with zeros, and so: 157, 117 for 12 tokens)
+        P.a_halves = m <= 128 ? 1 : 2;
+        P.a_rows = m < 128 ? (m + 7) / 8 * 8 : 128;
+        if (!make_map(&P.a, X, (uint64_t)m, (uint64_t)K, (uint64_t)K, (uint32_t)P.a_rows) || !make_map(&P.b, W_dev, (uint64_t)V, (uint64_t)K, (uint64_t)K, (uint32_t)p.width / 2)) return LOWRA_ERR_CUDA;
         if (!dX_dev) {
             P.N = V;
             P.tiles_n = p.tiles;
@@ -846,7 +853,7 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
             P.first = G.first = c == 0;
             P.clear_status = pass == 0 && c == 0;
             // (columns that the first product does not write, in a last block that is not full, are past the end)
-            if (!make_map(&G.a, e, (uint64_t)m, (uint64_t)P.tiles_n * p.width, (uint64_t)ld_e, 128)) return LOWRA_ERR_CUDA;
+            if (!make_map(&G.a, e, (uint64_t)m, (uint64_t)P.tiles_n * p.width, (uint64_t)ld_e, (uint32_t)P.a_rows)) return LOWRA_ERR_CUDA;
             if ((st = launch_product<kExponentials>(P, stream)) != LOWRA_OK) return st;
             if (launch_pdl(lift_kernel, (unsigned)((m + kTokens - 1) / kTokens), kTokens * kLanes, stream, (const float2*)stats, 2 * P.tiles_n, m, p.width, P.first, e, ld_e, R) != cudaSuccess) return LOWRA_ERR_CUDA;
             if ((st = launch_product<kGradient>(G, stream)) != LOWRA_OK) return st;
