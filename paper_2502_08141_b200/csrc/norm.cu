@@ -2,9 +2,10 @@
 //     h = bf16(X + residual);   Y = (h - mu) rstd weight + bias,   rstd = 1 / sqrt(mean (h - mu)^2 + eps)          (root mean square: mu = 0, no bias)
 // and its gradient, with g = dY weight and xh = (h - mu) rstd,
 //     dX = rstd (g - mean g - xh mean(g xh)) + dsum;    dweight = sum over the rows of dY xh;    dbias = sum over the rows of dY
-// Bound by memory.  A row is taken by one group of threads, eight neighbouring channels (16 bytes) to a thread, sixteen above 8192 channels, and stays in their
-// registers between its statistics and its output: every array is read or written once.  The statistics are sums in fp32 over the registers; the variance is that of the
+// Bound by memory.  A row is taken by one group of threads, eight neighbouring channels (16 bytes) to a thread or two or four times as many, and stays in their
+// registers, or in shared memory, between its statistics and its output: every array is read or written once.  The statistics are sums in fp32 over the registers; the variance is that of the
 // differences from the mean, a second sum, so that a mean far from zero costs no digits.
+#include <algorithm>
 #include <tuple>
 #include <type_traits>
 
@@ -506,6 +507,140 @@ __global__ void __launch_bounds__(256) add_parts_kernel(const float* parts, int 
     if (out != nullptr) out[n] = total;
 }
 
+// Few rows, where the CTAs' sums would be more than the rows themselves: the parameters' gradients are formed by CTAs of their own, beside those of the rows, from the same inputs (from L2, as a
+// rule: the rows' CTAs read them at the same time).  One launch; where dX takes the place of dY or X, the columns' CTAs go ahead in a launch of their own.
+// Columns: 32 channels to a CTA, four lanes to a row's 64 bytes, every warp eight rows at a time (of long rows twice the channels, half the rows), joined by shuffles, then over the warps in
+// their order; two rows to a lane under way (four: 600 x 4096 7.8 -> 8.2 us).
+template <int LANES>
+constexpr int kColumns = 8 * LANES;
+constexpr int kWideColumns = 2048;                    // channels above which they are 64 to a CTA (256 x 4096 5.2 -> 4.6 us, 128 x 8192 5.6 -> 4.2)
+struct BackwardFew {
+    int first, columns;                               // CTA that the launch begins with; CTAs of the columns, before those of the rows
+    float *dweight, *dbias;
+};
+template <bool LAYER, int LANES>
+__device__ __forceinline__ void columns_of(const NormParams& P, const BackwardFew& C, int strip) {
+    constexpr int kSums = LAYER ? 2 : 1, kUnder = 2;
+    constexpr int kCols = kColumns<LANES>, kRowsOfWarp = 32 / LANES;
+    __shared__ float shared[kMostThreads / 32][kSums][kCols];
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, warps = (int)blockDim.x >> 5, n = strip * kCols + lane % LANES * 8;
+    float2 dw[4], db[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dw[i] = db[i] = both(0.0f);
+    const int step = warps * kRowsOfWarp;
+    if (n < P.N)
+        for (int m0 = warp * kRowsOfWarp + lane / LANES; m0 < P.M; m0 += kUnder * step) {
+            uint4 y[kUnder], x[kUnder];
+            float rstd[kUnder], mean[kUnder];
+#pragma unroll
+            for (int k = 0; k < kUnder; ++k) {
+                const int m = m0 + k * step;
+                y[k] = x[k] = make_uint4(0u, 0u, 0u, 0u);
+                rstd[k] = mean[k] = 0.0f;
+                if (m >= P.M) continue;
+                y[k] = *reinterpret_cast<const uint4*>(P.dY + (size_t)m * P.N + n);
+                x[k] = *reinterpret_cast<const uint4*>(P.X + (size_t)m * P.N + n);
+                rstd[k] = P.rstd[m];
+                if (LAYER) mean[k] = P.mean[m];
+            }
+#pragma unroll
+            for (int k = 0; k < kUnder; ++k) {
+                if (m0 + k * step >= P.M) continue;
+                float2 g[4], xh[4];
+                unpack4(y[k], g);
+                unpack4(x[k], xh);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    xh[i] = mul2(LAYER ? add2(xh[i], both(-mean[k])) : xh[i], both(rstd[k]));
+                    dw[i] = fma2(g[i], xh[i], dw[i]);
+                    if (LAYER) db[i] = add2(db[i], g[i]);
+                }
+            }
+        }
+#pragma unroll
+    for (int d = LANES; d < 32; d *= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            dw[i] = add2(dw[i], make_float2(__shfl_xor_sync(0xffffffffu, dw[i].x, d), __shfl_xor_sync(0xffffffffu, dw[i].y, d)));
+            if (LAYER) db[i] = add2(db[i], make_float2(__shfl_xor_sync(0xffffffffu, db[i].x, d), __shfl_xor_sync(0xffffffffu, db[i].y, d)));
+        }
+    if (lane < LANES)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            *reinterpret_cast<float2*>(&shared[warp][0][lane * 8 + 2 * i]) = dw[i];
+            if (LAYER) *reinterpret_cast<float2*>(&shared[warp][kSums - 1][lane * 8 + 2 * i]) = db[i];
+        }
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < kSums * kCols; i += (int)blockDim.x) {
+        const int which = i / kCols, at = i % kCols;
+        float total = 0.0f;
+        for (int w = 0; w < warps; ++w) total += shared[w][which][at];
+        float* out = which == 0 ? C.dweight : C.dbias;
+        if (out != nullptr && strip * kCols + at < P.N) out[strip * kCols + at] = total;
+    }
+}
+
+template <int VECTORS, bool LAYER, bool BESIDE, int LANES>
+__global__ void __launch_bounds__(kMostThreads) backward_few_kernel(const NormParams P, const BackwardFew C) {
+    constexpr int kSums = LAYER ? 2 : 1;
+    __shared__ float shared[2][kMostThreads / 32][kSums];
+    pdl_enter();
+    const int cta = C.first + (int)blockIdx.x;
+    if (cta < C.columns) {
+        columns_of<LAYER, LANES>(P, C, cta);
+        return;
+    }
+    const int mine = (int)threadIdx.x / P.group, t = (int)threadIdx.x % P.group;
+    GroupSum<kSums> add = {shared, mine * P.group / 32, P.group / 32, mine + 1, 0};
+    const long long m = (long long)(cta - C.columns) * (int)(blockDim.x / P.group) + mine;
+    if (m >= P.M) return;                             // (a whole group)
+    uint4 y[VECTORS], x[VECTORS], beside[VECTORS];
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v) {
+        const int n = (t + v * P.group) * 8;
+        if (n >= P.N) continue;
+        y[v] = load8(P.dY + m * P.N + n);
+        x[v] = load8(P.X + m * P.N + n);
+        if (BESIDE) beside[v] = load8(P.residual + m * P.N + n);
+    }
+    const float scale = P.rstd[m], level = LAYER ? -P.mean[m] : 0.0f;
+    float2 along = both(0.0f), same = both(0.0f), g[VECTORS][4], xh[VECTORS][4];
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v) {
+        const int n = (t + v * P.group) * 8;
+        if (n >= P.N) continue;
+        float w[8];
+        load_params(P.weight, P.fp32, n, w);
+        unpack4(y[v], g[v]);
+        unpack4(x[v], xh[v]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            xh[v][i] = mul2(LAYER ? add2(xh[v][i], both(level)) : xh[v][i], both(scale));
+            g[v][i] = mul2(g[v][i], make_float2(w[2 * i], w[2 * i + 1]));
+            along = fma2(g[v][i], xh[v][i], along);
+            if (LAYER) same = add2(g[v][i], same);
+        }
+    }
+    float s[kSums];
+    s[0] = along.x + along.y;
+    if (LAYER) s[kSums - 1] = same.x + same.y;
+    add(s);
+    const float by = -s[0] * P.over_n, less = LAYER ? -s[kSums - 1] * P.over_n : 0.0f;
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v) {
+        const int n = (t + v * P.group) * 8;
+        if (n >= P.N) continue;
+        float2 d[4];
+        if (BESIDE) unpack4(beside[v], d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 dx = fma2(xh[v][i], both(by), LAYER ? add2(g[v][i], both(less)) : g[v][i]);
+            d[i] = BESIDE ? fma2(dx, both(scale), d[i]) : mul2(dx, both(scale));
+        }
+        *reinterpret_cast<uint4*>(P.Y + m * P.N + n) = pack4(d);
+    }
+}
+
 struct NormShape {
     int vectors, group, threads;     // vectors to a thread, threads to a row and to a CTA
 };
@@ -523,14 +658,23 @@ NormShape shape_of(int N, int most, int longest) {
 NormShape shape_of_many(int N) { return shape_of(N, kMostThreads, 256); }
 // Backward, us with eight channels to a thread and with sixteen: root mean square 8192 x 1024 18.1, 20.6; layer norm, twice the sums, 1001 x 1024 9.7, 7.3, 4096 x 4096 40.4, 34.9.
 NormShape shape_of_backward(int N, bool layer) { return shape_of(N, kBackwardThreads, layer ? 256 : 2048); }
+// A CTA of so many threads, or of one row.
+NormShape with_threads(NormShape S, int threads) {
+    const int groups = std::max(threads / S.group, 1);
+    S.threads = S.group * (S.group > 32 ? std::min(groups, 15) : groups);
+    return S;
+}
 // Up to one for each SM: a CTA to each.  Layer norm over more than two for each: sixteen channels to a thread, and so more rows at once on an SM (333 x 5120 6.8 -> 5.0 us, 149 x 4096 3.3 -> 4.1;
 // root mean square 600 x 4096 6.3 -> 7.1).
 NormShape shape_of_few(int M, int N, bool layer) {
     NormShape S = shape_of(N, kMostThreads, layer && M > 2 * kNumSMs ? 2048 : 8 * kMostThreads);
-    const int groups = M > kNumSMs && S.group < kForwardThreads ? kForwardThreads / S.group : 1;
-    S.threads = S.group * (S.group > 32 && groups > 15 ? 15 : groups);
-    return S;
+    return with_threads(S, M > kNumSMs ? kForwardThreads : 32);
 }
+// Backward, rows up to which their CTAs and those of the columns are one launch (us with two launches, a CTA to an SM, and so; layer norm / root mean square: 1 x 4096 5.1 / 3.9, 2.0 / 1.8;
+// 256 x 4096 10.5 / 9.4, 4.6 / 4.6; 1001 x 1024 7.3 / 6.0, 6.2 / 6.0; 600 x 256 3.7 / 3.4, 3.0 / 2.7, 1001 x 256 3.7 / 3.5, 4.3 / 4.1; 1500 x 13824 55.7 / 49.1, 51.9 / 49.9).
+int few_rows_of(int N) { return std::min(768 + N / 4, 1536); }
+// Sixteen channels to a thread above 4096, for two CTAs to an SM (600 x 8192 19.1 -> 12.3); few warps would go over the columns' rows for long (128 x 256 with one warp 4.0 us, with eight 1.7).
+NormShape shape_of_few_backward(int M, int N) { return with_threads(shape_of(N, kMostThreads, 4096), M > kNumSMs ? kForwardThreads : 256); }
 
 cudaLaunchConfig_t config_of(unsigned grid, int threads, size_t bytes, cudaStream_t stream, cudaLaunchAttribute* attr) {
     cudaLaunchConfig_t cfg = {};
@@ -561,7 +705,7 @@ bool in_the_way(const Span* out, int outs, const Span* in, int ins, bool same_ma
 template <int VECTORS, bool LAYER, bool BESIDE, bool SUMS, bool FP32>
 lowra_status launch_backward(const NormParams& P, const NormShape& S, int ctas, cudaStream_t stream) {
     static SmemLimit limit = {};
-    const size_t bytes = BackwardRing<VECTORS, BESIDE>::bytes(S.threads);        // (room for the sums too, 128 bytes a thread at most)
+    const size_t bytes = BackwardRing<VECTORS, BESIDE>::bytes(S.threads);        // (room for the sums too: 32 or 64 bytes for eight channels, where the rows take 64 or more)
     const auto kernel = backward_kernel<VECTORS, LAYER, BESIDE, SUMS, FP32>;
     if (ensure_smem_limit(reinterpret_cast<const void*>(kernel), bytes, &limit) != LOWRA_OK) return LOWRA_ERR_CUDA;
     cudaLaunchAttribute attr[1];
@@ -657,11 +801,27 @@ extern "C" lowra_status lowra_norm_backward(const uint16_t* dY_dev, const uint16
         return LOWRA_ERR_SHAPE;
     lowra_status st = check_device();
     if (st != LOWRA_OK) return st;
-    const NormShape S = shape_of_backward(N, layer);
+    const bool in_place = sums && (dX_dev == dY_dev || dX_dev == X_dev);      // (two launches either way: 600 x 1024 6.3 us as columns and rows, 5.3 a CTA to an SM)
+    const bool few = M <= (in_place ? few_rows_of(N) / 2 : few_rows_of(N));
+    const NormShape S = few ? shape_of_few_backward(M, N) : shape_of_backward(N, layer);
     const int ctas = backward_ctas(M, N, S);
     NormParams P = {X_dev, dsum_dev, dY_dev, weight_dev, nullptr, nullptr, dX_dev, const_cast<float*>(mean_dev), const_cast<float*>(rstd_dev),
                     static_cast<float*>(workspace_dev), M, N, S.group, params_fp32 != 0, 0.0f, 1.0f / (float)N};
     cudaStream_t stream = (cudaStream_t)stream_v;
+    if (few) {
+        const bool wide = N > kWideColumns;
+        const int columns = !sums ? 0 : wide ? (N + kColumns<8> - 1) / kColumns<8> : (N + kColumns<4> - 1) / kColumns<4>, groups = S.threads / S.group, rows_ctas = (M + groups - 1) / groups;
+        auto launch = [&](int first, int count) {
+            return choose([&](auto two, auto is_layer, auto beside, auto is_wide) {
+                cudaLaunchAttribute attr[1];
+                const cudaLaunchConfig_t cfg = config_of((unsigned)count, S.threads, 0, stream, attr);
+                return cudaLaunchKernelEx(&cfg, backward_few_kernel<two ? 2 : 1, is_layer, beside, is_wide ? 8 : 4>, P, BackwardFew{first, columns, dweight_dev, dbias_dev}) == cudaSuccess ? LOWRA_OK
+                                                                                                                                                                           : LOWRA_ERR_CUDA;
+            }, std::tuple<>(), S.vectors == 2, layer, dsum_dev != nullptr, wide);
+        };
+        if (in_place) st = launch(0, columns);
+        return st != LOWRA_OK ? st : in_place ? launch(columns, rows_ctas) : launch(0, columns + rows_ctas);
+    }
     st = choose([&](auto four, auto two, auto is_layer, auto beside, auto with_sums, auto fp32) {
         return launch_backward<four ? 4 : two ? 2 : 1, is_layer, beside, with_sums, fp32>(P, S, ctas, stream);
     }, std::tuple<>(), S.vectors == 4, S.vectors == 2, layer, dsum_dev != nullptr, sums, params_fp32 != 0);

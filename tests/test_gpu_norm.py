@@ -190,3 +190,22 @@ def test_refusals():
                  lambda: lw.lowra_norm_backward(c["dY"], c["X"], c["weight"], rstd, dbias=torch.empty(64, device="cuda"))):
         with pytest.raises((lw.LowraError, ValueError)):
             call()
+
+
+@pytest.mark.parametrize("M, N", [(1, 8), (3, 40), (832, 256), (833, 256), (1024, 1024), (1025, 1024), (513, 1024), (149, 2056), (300, 4104), (1536, 8200), (1537, 8200), (77, 16384)])
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+def test_backward_of_few_rows_and_of_more(M, N, kind):
+    """Sizes about which columns and rows become CTAs of one launch, of two where dX takes an input's place, or of none; odd ends of the columns; one gradient of the two."""
+    c = make(M, N, kind, torch.float32, True, seed=6)
+    mean, rstd = statistics32(c["X"], kind == "layer")
+    dX, dw, db = lw.lowra_norm_backward(c["dY"], c["X"], c["weight"], rstd, mean=mean, dsum=c["dsum"], want_params=True)
+    check_backward(c, kind, mean, rstd, dX, dw, db)
+    alone = lw.lowra_norm_backward(c["dY"], c["X"], c["weight"], rstd, mean=mean, dsum=c["dsum"])
+    check_backward(c, kind, mean, rstd, *alone)
+    for place in ("dY", "X", "dsum"):
+        a = {k: c[k].clone() for k in ("dY", "X", "dsum")}
+        only = torch.full((N,), 7.0, device="cuda")
+        out = lw.lowra_norm_backward(a["dY"], a["X"], c["weight"], rstd, mean=mean, dsum=a["dsum"], dX=a[place], dweight=only)
+        assert out[0] is a[place] and out[1] is only and out[2] is None
+        check_backward(c, kind, mean, rstd, *out)
+        assert all(torch.equal(a[k], c[k]) for k in a if k != place)
