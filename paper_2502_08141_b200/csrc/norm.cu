@@ -513,7 +513,6 @@ __global__ void __launch_bounds__(256) add_parts_kernel(const float* parts, int 
 // their order; two rows to a lane under way (four: 600 x 4096 7.8 -> 8.2 us).
 template <int LANES>
 constexpr int kColumns = 8 * LANES;
-constexpr int kWideColumns = 2048;                    // channels above which they are 64 to a CTA (256 x 4096 5.2 -> 4.6 us, 128 x 8192 5.6 -> 4.2)
 struct BackwardFew {
     int first, columns;                               // CTA that the launch begins with; CTAs of the columns, before those of the rows
     float *dweight, *dbias;
@@ -671,10 +670,15 @@ NormShape shape_of_few(int M, int N, bool layer) {
     return with_threads(S, M > kNumSMs ? kForwardThreads : 32);
 }
 // Backward, rows up to which their CTAs and those of the columns are one launch (us with two launches, a CTA to an SM, and so; layer norm / root mean square: 1 x 4096 5.1 / 3.9, 2.0 / 1.8;
-// 256 x 4096 10.5 / 9.4, 4.6 / 4.6; 1001 x 1024 7.3 / 6.0, 6.2 / 6.0; 600 x 256 3.7 / 3.4, 3.0 / 2.7, 1001 x 256 3.7 / 3.5, 4.3 / 4.1; 1500 x 13824 55.7 / 49.1, 51.9 / 49.9).
-int few_rows_of(int N) { return std::min(768 + N / 4, 1536); }
-// Sixteen channels to a thread above 4096, for two CTAs to an SM (600 x 8192 19.1 -> 12.3); few warps would go over the columns' rows for long (128 x 256 with one warp 4.0 us, with eight 1.7).
-NormShape shape_of_few_backward(int M, int N) { return with_threads(shape_of(N, kMostThreads, 4096), M > kNumSMs ? kForwardThreads : 256); }
+// 256 x 4096 10.5 / 9.4, 4.6 / 4.6; 800 x 264 4.5 / 3.8, 3.7 / 3.5, 1001 x 264 4.5 / 3.9, 4.9 / 4.6; 1001 x 1024 7.3 / 6.0, 6.2 / 6.0, 2048 x 1024 11.7 / 8.3, 9.6 / 9.8; 2048 x 2056 17.3 / 15.8,
+// 12.4 / 11.3; 3000 x 4096 29.3 / 26.8, 28.6 / 27.9; 1500 x 13824 55.6 / 49.3, 51.7 / 49.9, 2048 x 13824 67.5 / 60.2, 70.2 / 67.5).
+int few_rows_of(int N, bool layer) { return N <= (layer ? 640 : 1280) ? 768 + N / 4 : N <= 8192 ? 2048 : 1536; }
+// Sixteen channels to a thread above 4096, for two CTAs to an SM (600 x 8192 19.1 -> 11.2); few warps would go over the columns' rows for long (128 x 256 with one warp 4.0 us, with eight 1.7;
+// 2048 x 2056 with nine 16.1, with eighteen 12.4; 2048 x 2552, of ten warps a row, twenty 18.6, ten 14.3).
+NormShape shape_of_few_backward(int M, int N) { return with_threads(shape_of(N, kMostThreads, 4096), M > kNumSMs ? kForwardThreads + kForwardThreads / 8 : 256); }
+// Whether the columns are 64 to a CTA: where 32 would be more CTAs than the SMs have room for beside the rows' (256 x 4096 5.2 -> 4.6 us, 128 x 8192 5.6 -> 4.2; 1001 x 5120, 160 CTAs of ten warps,
+// 11.9 -> 15.8).
+bool wide_columns(int N, const NormShape& S) { return (N + 31) / 32 * S.threads > 360 * kNumSMs; }
 
 cudaLaunchConfig_t config_of(unsigned grid, int threads, size_t bytes, cudaStream_t stream, cudaLaunchAttribute* attr) {
     cudaLaunchConfig_t cfg = {};
@@ -802,14 +806,14 @@ extern "C" lowra_status lowra_norm_backward(const uint16_t* dY_dev, const uint16
     lowra_status st = check_device();
     if (st != LOWRA_OK) return st;
     const bool in_place = sums && (dX_dev == dY_dev || dX_dev == X_dev);      // (two launches either way: 600 x 1024 6.3 us as columns and rows, 5.3 a CTA to an SM)
-    const bool few = M <= (in_place ? few_rows_of(N) / 2 : few_rows_of(N));
+    const bool few = M <= (in_place ? few_rows_of(N, layer) / 4 : few_rows_of(N, layer));
     const NormShape S = few ? shape_of_few_backward(M, N) : shape_of_backward(N, layer);
     const int ctas = backward_ctas(M, N, S);
     NormParams P = {X_dev, dsum_dev, dY_dev, weight_dev, nullptr, nullptr, dX_dev, const_cast<float*>(mean_dev), const_cast<float*>(rstd_dev),
                     static_cast<float*>(workspace_dev), M, N, S.group, params_fp32 != 0, 0.0f, 1.0f / (float)N};
     cudaStream_t stream = (cudaStream_t)stream_v;
     if (few) {
-        const bool wide = N > kWideColumns;
+        const bool wide = wide_columns(N, S);
         const int columns = !sums ? 0 : wide ? (N + kColumns<8> - 1) / kColumns<8> : (N + kColumns<4> - 1) / kColumns<4>, groups = S.threads / S.group, rows_ctas = (M + groups - 1) / groups;
         auto launch = [&](int first, int count) {
             return choose([&](auto two, auto is_layer, auto beside, auto is_wide) {
