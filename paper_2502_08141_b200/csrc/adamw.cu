@@ -6,8 +6,10 @@
 // The states' arithmetic is fp32 with every operation rounded by itself, in the order above ((1 - b2) g first, then times g): what is rounded to 8 bits does not depend on
 // how a compiler joins operations.
 // Bound by memory: gradient, weights and states each read once and written once, 28 bytes a weight (bf16 gradient, fp32 states) or 16 (8 bits).  A warp takes 256 values at a
-// time, eight to a lane, so that a scale is two warp reductions and all accesses are 16 bytes wide (8 for codes); the factors' descriptions are kernel parameters, found by
-// a binary search over their first blocks (some 10 steps, behind 48 warps' loads).
+// time, eight to a lane, so that a scale is a warp reduction and all accesses are 16 bytes wide (8 for codes); the factors' descriptions are kernel parameters: a warp looks for
+// the one of its first block by bisection and then goes on from one to the next.
+// Measured: 448 factors of rank 64 (160 M weights, fp32 states) 720 us, one reading and writing 693 at the copy rate; fourteen of them in 8 bits 17.8 us (12.4), of which a launch with nothing to do is 2;
+// two of 1024 x 16 and 16 x 4096 3.1 us.
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <string.h>

@@ -14,6 +14,9 @@
 // The products: CTA pairs (clusters of two) walk over tiles of 256 tokens x up to 256 words (features), tcgen05.mma with cta_group::2, both operands by TMA, 64 contraction indices
 // (32 KB a CTA) to a stage, six stages; two accumulators in turn, so the epilogue's eight warps work on one tile while the next is formed.
 // Up to 64 tokens and no gradient, bound by reading W: the other way round, 256 words by 32 or 64 tokens, ten stages; a pair's MMAs then take an eighth or a quarter of the time that its words do.
+// Measured: 4096 tokens, 32000 words, 4096 features with the gradient 1400 us at full clock and 1650 under the power cap (at the rate of two library products 1262 and 1509), the tensor pipe 88 to 91 %
+// busy; 777 tokens, 50265 words, 1024 features 188 us (94: nine tokens are all that the fourth tile of them holds, and the pipe is 75 % busy); 16 tokens, 32000 words, 4096 features, loss alone 46 us (W
+// once: 40.6).
 // warp 0 = TMA, 1 = MMA (of the CTA of rank 0) and TMEM, 4-11 = epilogue.  The 128 columns that an epilogue's thread holds, and 32 more on their way, do not fit into the 168 registers that
 // twelve warps get: the first four give some to the others.  All waits are bounded (lowra_set_wait_limit); no CTA waits for another cluster.
 #include <atomic>

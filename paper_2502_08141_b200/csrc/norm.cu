@@ -5,6 +5,8 @@
 // Bound by memory.  A row is taken by one group of threads, eight neighbouring channels (16 bytes) to a thread or two or four times as many, and stays in their
 // registers, or in shared memory, between its statistics and its output: every array is read or written once.  The statistics are sums in fp32 over the registers; the variance is that of the
 // differences from the mean, a second sum, so that a mean far from zero costs no digits.
+// Measured, us, in brackets at the copy rate: forward 333 x 5120 with a residual 5.0 (2.1), one token of 4096 2.0; backward with the weight's gradient 4096 x 4096, residual, 32.6 (20.8: the rows 26, their
+// CTAs' sums 5), layer norm 1001 x 1024 6.2 (1.0: a chain of loads, two sums over a row, and a thousand rows for every column), 256 x 4096 4.6.
 #include <algorithm>
 #include <tuple>
 #include <type_traits>

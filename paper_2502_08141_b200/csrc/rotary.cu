@@ -4,6 +4,7 @@
 // 2^64, which is modulo one turn, so an angle at any 32-bit position is right to 2^-33 of a turn without a wide multiplication or a reduction.
 // Bound by memory, 4 bytes for every value.  A CTA takes the heads of a few tokens: its threads first work out the tokens' cosines and sines into shared memory, one pair each,
 // with their first loads already under way, then go over the heads, sixteen values (eight pairs) of a head at a time.
+// Measured: 4096 tokens, 32 + 32 heads of 128 25.4 us (20.8 at the copy rate; at 134 MB filling and draining the memory takes some 3 us), 16 tokens 2.4, one head of 64 for 1346 tokens 3.6.
 #include <math.h>
 
 #include "lowra_common.cuh"
