@@ -6,7 +6,7 @@
 // registers, or in shared memory, between its statistics and its output: every array is read or written once.  The statistics are sums in fp32 over the registers; the variance is that of the
 // differences from the mean, a second sum, so that a mean far from zero costs no digits.
 // Measured, us, in brackets at the copy rate: forward 333 x 5120 with a residual 5.0 (2.1), one token of 4096 2.0; backward with the weight's gradient 4096 x 4096, residual, 32.6 (20.8: the rows 26, their
-// CTAs' sums 5), layer norm 1001 x 1024 6.2 (1.0: a chain of loads, two sums over a row, and a thousand rows for every column), 256 x 4096 4.6.
+// CTAs' sums 5), layer norm 1001 x 1024 5.6 (1.0: a chain of loads, two sums over a row, and a thousand rows for every column), 256 x 4096 4.6.
 #include <algorithm>
 #include <tuple>
 #include <type_traits>
@@ -511,10 +511,7 @@ __global__ void __launch_bounds__(256) add_parts_kernel(const float* parts, int 
 
 // Few rows, where the CTAs' sums would be more than the rows themselves: the parameters' gradients are formed by CTAs of their own, beside those of the rows, from the same inputs (from L2, as a
 // rule: the rows' CTAs read them at the same time).  One launch; where dX takes the place of dY or X, the columns' CTAs go ahead in a launch of their own.
-// Columns: 32 channels to a CTA, four lanes to a row's 64 bytes, every warp eight rows at a time (of long rows twice the channels, half the rows), joined by shuffles, then over the warps in
-// their order; two rows to a lane under way (four: 600 x 4096 7.8 -> 8.2 us).
-template <int LANES>
-constexpr int kColumns = 8 * LANES;
+// Columns: 16, 32 or 64 channels to a CTA, LANES lanes to a row's part of them, a warp 32 / LANES rows at a time, joined by shuffles, then over the warps in their order; two rows to a lane under way (four: 600 x 4096 7.8 -> 8.2 us).
 struct BackwardFew {
     int first, columns;                               // CTA that the launch begins with; CTAs of the columns, before those of the rows
     float *dweight, *dbias;
@@ -522,7 +519,7 @@ struct BackwardFew {
 template <bool LAYER, int LANES>
 __device__ __forceinline__ void columns_of(const NormParams& P, const BackwardFew& C, int strip) {
     constexpr int kSums = LAYER ? 2 : 1, kUnder = 2;
-    constexpr int kCols = kColumns<LANES>, kRowsOfWarp = 32 / LANES;
+    constexpr int kCols = 8 * LANES, kRowsOfWarp = 32 / LANES;
     __shared__ float shared[kMostThreads / 32][kSums][kCols];
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, warps = (int)blockDim.x >> 5, n = strip * kCols + lane % LANES * 8;
     float2 dw[4], db[4];
@@ -672,15 +669,20 @@ NormShape shape_of_few(int M, int N, bool layer) {
     return with_threads(S, M > kNumSMs ? kForwardThreads : 32);
 }
 // Backward, rows up to which their CTAs and those of the columns are one launch (us with two launches, a CTA to an SM, and so; layer norm / root mean square: 1 x 4096 5.1 / 3.9, 2.0 / 1.8;
-// 256 x 4096 10.5 / 9.4, 4.6 / 4.6; 800 x 264 4.5 / 3.8, 3.7 / 3.5, 1001 x 264 4.5 / 3.9, 4.9 / 4.6; 1001 x 1024 7.3 / 6.0, 6.2 / 6.0, 2048 x 1024 11.7 / 8.3, 9.6 / 9.8; 2048 x 2056 17.3 / 15.8,
-// 12.4 / 11.3; 3000 x 4096 29.3 / 26.8, 28.6 / 27.9; 1500 x 13824 55.6 / 49.3, 51.7 / 49.9, 2048 x 13824 67.5 / 60.2, 70.2 / 67.5).
-int few_rows_of(int N, bool layer) { return N <= (layer ? 640 : 1280) ? 768 + N / 4 : N <= 8192 ? 2048 : 1536; }
+// 256 x 4096 10.5 / 9.4, 4.6 / 4.6; 800 x 264 4.5 / 3.8, 3.4 / 3.3, 1500 x 264 4.9 / 5.0, 4.8 / 4.5, 2000 x 392 6.3 / 5.8, 7.9 / 7.2; 1001 x 1024 7.3 / 6.0, 5.6 / 5.0, 2000 x 1024 11.6 / 8.2, 8.3 / 7.7;
+// 2048 x 2056 17.3 / 15.8, 12.4 / 11.3; 3000 x 4096 29.3 / 26.8, 28.6 / 27.9; 1500 x 13824 55.6 / 49.3, 51.7 / 49.9, 2048 x 13824 67.5 / 60.2, 70.2 / 67.5).
+int few_rows_of(int N) { return N <= 8192 ? std::min(1024 + N, 2048) : 1536; }
 // Sixteen channels to a thread above 4096, for two CTAs to an SM (600 x 8192 19.1 -> 11.2); few warps would go over the columns' rows for long (128 x 256 with one warp 4.0 us, with eight 1.7;
 // 2048 x 2056 with nine 16.1, with eighteen 12.4; 2048 x 2552, of ten warps a row, twenty 18.6, ten 14.3).
 NormShape shape_of_few_backward(int M, int N) { return with_threads(shape_of(N, kMostThreads, 4096), M > kNumSMs ? kForwardThreads + kForwardThreads / 8 : 256); }
-// Whether the columns are 64 to a CTA: where 32 would be more CTAs than the SMs have room for beside the rows' (256 x 4096 5.2 -> 4.6 us, 128 x 8192 5.6 -> 4.2; 1001 x 5120, 160 CTAs of ten warps,
-// 11.9 -> 15.8).
-bool wide_columns(int N, const NormShape& S) { return (N + 31) / 32 * S.threads > 360 * kNumSMs; }
+// Lanes to a row of the columns (8 channels each): as few as leave the SMs room for the columns' CTAs beside the rows' (four and eight: 256 x 4096 5.2 -> 4.6 us, 128 x 8192 5.6 -> 4.2, 1001 x 5120, 160 CTAs of
+// ten warps, 11.9 -> 15.8; four and two, which takes hold with more than a few
+// rows to a lane: 1001 x 1024 6.2 -> 5.6, 1500 x 1288 8.0 -> 7.4, 300 x 1024 3.0 -> 3.3).
+int lanes_of_columns(int M, int N, const NormShape& S) {
+    for (int lanes = M > 512 ? 2 : 4; lanes < 8; lanes *= 2)
+        if ((N + 8 * lanes - 1) / (8 * lanes) * S.threads <= 360 * kNumSMs) return lanes;
+    return 8;
+}
 
 cudaLaunchConfig_t config_of(unsigned grid, int threads, size_t bytes, cudaStream_t stream, cudaLaunchAttribute* attr) {
     cudaLaunchConfig_t cfg = {};
@@ -808,22 +810,22 @@ extern "C" lowra_status lowra_norm_backward(const uint16_t* dY_dev, const uint16
     lowra_status st = check_device();
     if (st != LOWRA_OK) return st;
     const bool in_place = sums && (dX_dev == dY_dev || dX_dev == X_dev);      // (two launches either way: 600 x 1024 6.3 us as columns and rows, 5.3 a CTA to an SM)
-    const bool few = M <= (in_place ? few_rows_of(N, layer) / 4 : few_rows_of(N, layer));
+    const bool few = M <= (in_place ? few_rows_of(N) / 4 : few_rows_of(N));
     const NormShape S = few ? shape_of_few_backward(M, N) : shape_of_backward(N, layer);
     const int ctas = backward_ctas(M, N, S);
     NormParams P = {X_dev, dsum_dev, dY_dev, weight_dev, nullptr, nullptr, dX_dev, const_cast<float*>(mean_dev), const_cast<float*>(rstd_dev),
                     static_cast<float*>(workspace_dev), M, N, S.group, params_fp32 != 0, 0.0f, 1.0f / (float)N};
     cudaStream_t stream = (cudaStream_t)stream_v;
     if (few) {
-        const bool wide = wide_columns(N, S);
-        const int columns = !sums ? 0 : wide ? (N + kColumns<8> - 1) / kColumns<8> : (N + kColumns<4> - 1) / kColumns<4>, groups = S.threads / S.group, rows_ctas = (M + groups - 1) / groups;
+        const int lanes = lanes_of_columns(M, N, S);
+        const int columns = sums ? (N + 8 * lanes - 1) / (8 * lanes) : 0, groups = S.threads / S.group, rows_ctas = (M + groups - 1) / groups;
         auto launch = [&](int first, int count) {
-            return choose([&](auto two, auto is_layer, auto beside, auto is_wide) {
+            return choose([&](auto two, auto is_layer, auto beside, auto two_lanes, auto four_lanes) {
                 cudaLaunchAttribute attr[1];
                 const cudaLaunchConfig_t cfg = config_of((unsigned)count, S.threads, 0, stream, attr);
-                return cudaLaunchKernelEx(&cfg, backward_few_kernel<two ? 2 : 1, is_layer, beside, is_wide ? 8 : 4>, P, BackwardFew{first, columns, dweight_dev, dbias_dev}) == cudaSuccess ? LOWRA_OK
+                return cudaLaunchKernelEx(&cfg, backward_few_kernel<two ? 2 : 1, is_layer, beside, two_lanes ? 2 : four_lanes ? 4 : 8>, P, BackwardFew{first, columns, dweight_dev, dbias_dev}) == cudaSuccess ? LOWRA_OK
                                                                                                                                                                            : LOWRA_ERR_CUDA;
-            }, std::tuple<>(), S.vectors == 2, layer, dsum_dev != nullptr, wide);
+            }, std::tuple<>(), S.vectors == 2, layer, dsum_dev != nullptr, lanes == 2, lanes == 4);
         };
         if (in_place) st = launch(0, columns);
         return st != LOWRA_OK ? st : in_place ? launch(columns, rows_ctas) : launch(0, columns + rows_ctas);

@@ -192,7 +192,7 @@ def test_refusals():
             call()
 
 
-@pytest.mark.parametrize("M, N", [(1, 8), (3, 40), (832, 256), (833, 256), (208, 256), (209, 256), (1024, 1024), (1025, 1024), (513, 1024), (2048, 1288), (2049, 1288), (149, 2056), (300, 4104), (1536, 8200), (1537, 8200), (77, 16384)])
+@pytest.mark.parametrize("M, N", [(1, 8), (3, 40), (832, 256), (833, 256), (208, 256), (209, 256), (320, 256), (321, 256), (1280, 256), (1281, 256), (700, 504), (1024, 1024), (1025, 1024), (513, 1024), (2048, 1288), (2049, 1288), (149, 2056), (300, 4104), (1536, 8200), (1537, 8200), (77, 16384)])
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 def test_backward_of_few_rows_and_of_more(M, N, kind):
     """Sizes about which columns and rows become CTAs of one launch, of two where dX takes an input's place, or of none; odd ends of the columns; one gradient of the two."""
