@@ -225,3 +225,13 @@ def test_labels_whose_logit_is_no_number(M, V):
         for got in (loss, only):
             assert got.isnan().all() if beside else (got == float("inf")).all()
         assert dX.isnan().any(1).all()
+
+
+@pytest.mark.parametrize("M", [2, 9, 40, 65, 100, 121, 127, 128, 129, 136, 255])
+def test_tiles_of_few_tokens(M):
+    """A tile's rows without a token are not loaded: after a call whose numbers are all NaN, what it left in their places changes nothing.  Widths of tiles from 128 to 256, a short last one."""
+    for V, K in ((1000, 200), (9473, 72), (18945, 136)):
+        X, W, labels, weights = make(M, V, K)
+        big = torch.full((512, K), float("nan"), dtype=torch.bfloat16, device="cuda")
+        lw.lowra_cross_entropy(big, W, torch.zeros(512, dtype=torch.int64, device="cuda"), want_grad=True)
+        check(X, W, labels, weights)
