@@ -174,21 +174,14 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamResident<EIGHT>) adamw_kern
     pdl_wait();
     float decay = P.decay, rate = P.rate, root_scale = P.root_scale;
     if (P.step != nullptr || P.lr != nullptr) {      // a captured step reads them when it runs
-        if (threadIdx.x == 0) {
-            float lr = P.lr != nullptr ? *P.lr : 0.0f;
-            if (P.lr != nullptr) decay = (float)(1.0 - (double)lr * P.wd);
-            double one = 1.0;                        // 1 - b1^t, which rate holds already where the step is the host's
-            if (P.step != nullptr) {
-                const double t = (double)*P.step;
-                one = -expm1(t * P.log_b1);
-                root_scale = (float)(1.0 / sqrt(-expm1(t * P.log_b2)));
-            }
+        if (threadIdx.x == 0) {                      // (fp64, a chain of its own for each of the two powers: a captured step of two factors 3.9 -> 3.6 us, with the host's step 3.2)
+            const float lr = P.lr != nullptr ? *P.lr : 1.0f;
             // rate: lr / (1 - b1^t) as far as the host knows it, else lr, 1 / (1 - b1^t) or 1
-            rate = (float)((double)rate * (P.lr != nullptr ? (double)lr : 1.0) / one);
-            shared[0] = decay;
-            shared[1] = rate;
-            shared[2] = root_scale;
+            const double one = P.step != nullptr ? -expm1((double)*P.step * P.log_b1) : 1.0;
+            shared[0] = P.lr != nullptr ? (float)(1.0 - (double)lr * P.wd) : decay;
+            shared[1] = (float)((double)rate * (double)lr / one);
         }
+        if (threadIdx.x == 32) shared[2] = P.step != nullptr ? (float)(1.0 / sqrt(-expm1((double)*P.step * P.log_b2))) : root_scale;
         __syncthreads();
         decay = shared[0];
         rate = shared[1];
