@@ -567,12 +567,16 @@ struct Joined {
     }
 };
 
-// -log of the label's share, from its logit and the sum of the others' exponentials, taken under `top` octaves (minus infinity: none has one).
+// -log of the label's share, from its logit and the sum of the others' exponentials, taken under `top` octaves (minus infinity: none has one).  `top` is the largest of the others' or, with a gradient, the
+// token's lift, from which both may be far: so the label is set against the others' sum, and not against `top`, whose octaves cancel in fp64.  Neither way has a difference of large numbers: with the
+// larger share of the two the loss is log(1 + their ratio), else both of its terms are positive.
 __device__ __forceinline__ float loss_of(float logit, float top, float sum) {
     if (!(logit < INFINITY) || (top == -INFINITY && logit == -INFINITY)) return NAN;
     if (top == -INFINITY) return sum;                         // (zero, or NaN)
-    const float over = fmaf(logit, kLog2e, -top);             // the label's logit above the others', octaves
-    return over >= 0.0f ? log1pf(sum * exp2f(-over)) : logf(sum + exp2f(over)) - over * kLn2;
+    int octaves = 0;
+    const float others = 2.0f * frexpf(sum, &octaves);        // sum = others 2^(octaves - 1), others in [1, 2)
+    const float over = (float)((double)logit * (double)kLog2e - ((double)top + (double)(octaves - 1)));
+    return over >= 0.0f ? log1pf(others * exp2f(-over)) : logf(others + exp2f(over)) - over * kLn2;
 }
 
 // Loss without a gradient.
