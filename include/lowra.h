@@ -539,6 +539,9 @@ lowra_status lowra_rotary(const lowra_rotary_part* parts_host, int32_t count, in
  * one behind the other (the last block may be short) s = (largest magnitude) / 448, fp32, in m_scale, v_scale [ceil(n / LOWRA_ADAMW_BLOCK)], and in m and v, one byte each, m' / s and
  * sqrt(v') / s as e4m3 (to nearest, ties to even; a root that is not zero becomes at least 2^-9; a block with s < 2^-126 is zero).  A block that meets a NaN or an infinity
  * stays NaN.  w' is formed before m' and v' are rounded.
+ * To nearest, a step that moves a kept value by less than half the distance of two codes (3 to 6 %) leaves it as it was: with beta2 = 0.999 a root hardly ever falls, and grows only under gradients some ten times as
+ * large, so that the second moment is that of the first steps.  bits = 8 | LOWRA_ADAMW_DITHER: m' / s and sqrt(v') / s each go to one of the two codes about them, the upper one with the chance that their place between
+ * them gives it, so that over the steps the moments follow those in fp32 (a root to some 15 %); which one depends on the step's number t and the value's place in the call alone, so repeated and captured calls agree.
  *   lowra_adamw_member: arrays on the device, 16-byte aligned (scales 4), of n elements without gaps: grad bf16 or, with grad_fp32 != 0, fp32 (all members alike); master fp32 w;
  *     each *_out may be its input itself (in place); weight bf16, or NULL; what is written overlaps nothing else in the call (members may read one gradient)
  *   members_host: HOST array of 1 .. LOWRA_MAX_ADAMW members, read before the call returns
@@ -548,6 +551,7 @@ lowra_status lowra_rotary(const lowra_rotary_part* parts_host, int32_t count, in
  */
 #define LOWRA_MAX_ADAMW 4096
 #define LOWRA_ADAMW_BLOCK 256
+#define LOWRA_ADAMW_DITHER 0x100
 typedef struct {
     const void* grad_dev;
     const float* master_dev;

@@ -1319,6 +1319,7 @@ def lowra_rotary(q: torch.Tensor, positions: torch.Tensor, turns: torch.Tensor, 
 
 
 LOWRA_ADAMW_BLOCK = 256
+_ADAMW_DITHER = 0x100
 _E4M3 = torch.float8_e4m3fn
 
 
@@ -1329,14 +1330,16 @@ def _scalar(t: torch.Tensor, dtype, name: str) -> int:
     return t.data_ptr()
 
 
-def lowra_adamw(members, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, step=1, grad_scale: Optional[torch.Tensor] = None, stream=None):
+def lowra_adamw(members, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, step=1, grad_scale: Optional[torch.Tensor] = None, stream=None,
+                dither: bool = False):
     """A step of adaptive moments with decoupled weight decay over the factors of a model, in one call.  `members`: dicts with grad (bf16 or fp32, all alike), master (fp32), m and v (fp32,
     or torch.float8_e4m3fn with m_scale and v_scale, fp32 [ceil(n / LOWRA_ADAMW_BLOCK)]: v then holds the second moment's root) and, optionally, weight (bf16, receives the
     rounded weights); all of one shape.  States and master are updated in place unless master_out, m_out, v_out, m_scale_out, v_scale_out are given; a state begins as zeros.
     `step`, counted from 1, and lr: numbers, or CUDA tensors of one int32 or fp32 (what a captured call that is replayed needs); grad_scale: a CUDA tensor of one fp32 that
-    multiplies the gradients.  Returns the members."""
+    multiplies the gradients.  dither, for states in 8 bits: they are rounded up or down by their place between two codes and the step's number, not to nearest, which loses what changes a state by less than
+    3 to 6 % (with betas[1] = 0.999: every fall of the second moment); a training run wants it.  Returns the members."""
     if stream is None and _py_calls is not None:
-        done = _py_calls.adamw(members, lr, betas, eps, weight_decay, step, grad_scale)
+        done = _py_calls.adamw(members, lr, betas, eps, weight_decay, step, grad_scale, dither)
         if done is not None:
             if done.__class__ is int:
                 _check(done, "lowra_adamw")
@@ -1376,7 +1379,7 @@ def lowra_adamw(members, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay
             setattr(c, name + "_dev", t.data_ptr())
             if name not in ("grad", "weight"):
                 setattr(c, name + "_out_dev", (t if new is None else new).data_ptr())
-    s = _CAdamwStep(0.0, float(betas[0]), float(betas[1]), float(eps), float(weight_decay), 0, None, None, None, 8 if eight else 32, int(fp32))
+    s = _CAdamwStep(0.0, float(betas[0]), float(betas[1]), float(eps), float(weight_decay), 0, None, None, None, (8 if eight else 32) | (_ADAMW_DITHER if dither else 0), int(fp32))
     if isinstance(lr, torch.Tensor):
         s.lr_dev = _scalar(lr, torch.float32, "lr")
     else:

@@ -18,7 +18,7 @@
 //   norm_backward(dY, X, weight, rstd, mean, dsum, dX, dweight, dbias, whether these are wanted, workspace: the first four given, the others may be None)   dX, dweight, dbias
 //   rotary(q, positions, turns, k or None, interleaved, inverse, scale, out or None, k_out or None)                                                out, or the pair
 //   cross_entropy(X, W, labels, scale, weights, ignore_index, loss, dX, whether dX is wanted, workspace: tensors but the first three may be None)   loss, dX
-//   adamw(members, lr, betas, eps, weight_decay, step, grad_scale or None)                                                                          the members
+//   adamw(members, lr, betas, eps, weight_decay, step, grad_scale or None, dither)                                                                          the members
 //   update_factors(members, lr, momentum, nesterov, weight_decay, steps, coefficients, eps, rank or None, workspace or None)                                     the members
 #include <torch/extension.h>
 
@@ -706,7 +706,7 @@ PyObject* cross_entropy(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
     lowra_adamw_step step = {};
-    if (n != 7 || library.forward == nullptr || !PyList_CheckExact(args[0]) || !PyTuple_CheckExact(args[2]) || PyTuple_GET_SIZE(args[2]) != 2 ||
+    if (n != 8 || library.forward == nullptr || !PyBool_Check(args[7]) || !PyList_CheckExact(args[0]) || !PyTuple_CheckExact(args[2]) || PyTuple_GET_SIZE(args[2]) != 2 ||
         !number(PyTuple_GET_ITEM(args[2], 0), &step.beta1) || !number(PyTuple_GET_ITEM(args[2], 1), &step.beta2) || !number(args[3], &step.eps) ||
         !number(args[4], &step.weight_decay))
         Py_RETURN_NONE;
@@ -782,7 +782,7 @@ PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
                                                     in(kMScale), out(kMScaleOut, kMScale), in(kVScale), out(kVScaleOut, kVScale), elements};
         }
         if ((grad_type != at::kFloat && grad_type != at::kBFloat16) || (state_type != at::kFloat && state_type != at::kFloat8_e4m3fn)) Py_RETURN_NONE;
-        step.bits = state_type == at::kFloat ? 32 : 8;
+        step.bits = (state_type == at::kFloat ? 32 : 8) | (args[7] == Py_True ? LOWRA_ADAMW_DITHER : 0);
         step.grad_fp32 = grad_type == at::kFloat;
         const lowra_status st = library.adamw(members.data(), (int32_t)count, &step, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream());
         if (st != LOWRA_OK) return PyLong_FromLong(st);
