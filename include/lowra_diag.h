@@ -50,6 +50,15 @@ lowra_status lowra_diag_wait_expiry(void* workspace_dev, size_t workspace_bytes,
 lowra_status lowra_diag_drop_t_flags(int32_t calls);
 
 /*
+ * (No counterpart in the paper.)  The same for lowra_cross_entropy, which has no flags: in the next `calls` calls the products named (1: those that form the logits, 2: those
+ * of the gradient, 3: both) load the first 64 contraction indices of every pair of SMs and nothing behind them.  The tensor core's warp waits for tiles that never come, gives up
+ * after the limit set by lowra_set_wait_limit, and both CTAs of the pair leave through their failure path: status word LOWRA_ERR_TIMEOUT, loss and gradient not valid, GPU and
+ * workspace usable afterwards.  (A product whose pairs have no more than 64 indices each is not affected.)  Set the limit to a few milliseconds first.  calls: 0 .. 1000 (0 disarms).
+ * Errors: calls or products out of range -> LOWRA_ERR_SHAPE.
+ */
+lowra_status lowra_diag_drop_tiles(int32_t calls, int32_t products);
+
+/*
  * (No counterpart in the paper.)  What a launch of the forward (backward == 0) or the backward-input pass runs on a whole GPU for `count` members of
  * this layout with tokens_host[i] tokens each: a plain call (count 1), the members of a batch call, or (one_weight != 0) the token groups of
  * lowra_lora_forward_adapters that go into one launch, all of them.  Host only: no device is needed, nothing is launched, and layout's device arrays may be NULL.

@@ -42,7 +42,7 @@ EXPORTS = (
     "lowra_encode_group", "lowra_decode_group", "lowra_diag_choose", "lowra_lora_forward_epilogue",
     "lowra_lora_forward_batch_epilogue", "lowra_lora_forward_adapters_epilogue", "lowra_epilogue_workspace_bytes", "lowra_epilogue_backward",
     "lowra_update_workspace_bytes", "lowra_update_factors", "lowra_norm_workspace_bytes", "lowra_norm_forward", "lowra_norm_backward", "lowra_rotary_turns", "lowra_rotary",
-    "lowra_adamw", "lowra_cross_entropy_workspace_bytes", "lowra_cross_entropy",
+    "lowra_adamw", "lowra_cross_entropy_workspace_bytes", "lowra_cross_entropy", "lowra_diag_drop_tiles",
 )
 
 
@@ -248,6 +248,8 @@ def lib() -> ctypes.CDLL:
         L.lowra_diag_wait_expiry.restype = ctypes.c_int
         L.lowra_diag_drop_t_flags.argtypes = [i32]
         L.lowra_diag_drop_t_flags.restype = ctypes.c_int
+        L.lowra_diag_drop_tiles.argtypes = [i32, i32]
+        L.lowra_diag_drop_tiles.restype = ctypes.c_int
         L.lowra_diag_choose.argtypes = [lp, i32, vp, i32, i32, i32, ctypes.POINTER(_CChoice)]
         L.lowra_diag_choose.restype = ctypes.c_int
         _py_calls = _load_py_calls(L)
@@ -1456,6 +1458,11 @@ def lowra_diag_wait_expiry(workspace: torch.Tensor, limit_ns: int, stream=None) 
 def lowra_diag_drop_t_flags(calls: int) -> None:
     """Self test: the next `calls` fused calls do not publish their "down-projection ready" flags and time out."""
     _check(lib().lowra_diag_drop_t_flags(int(calls)), "lowra_diag_drop_t_flags")
+
+
+def lowra_diag_drop_tiles(calls: int, products: int = 3) -> None:
+    """Self test: in the next `calls` calls of lowra_cross_entropy the products named (1: the logits', 2: the gradient's, 3: both) load no tiles behind their first ones and time out."""
+    _check(lib().lowra_diag_drop_tiles(int(calls), int(products)), "lowra_diag_drop_tiles")
 
 
 def lowra_diag_choose(layout: Layout, backward: bool, tokens, r: int, one_weight: bool = False) -> dict:

@@ -22,6 +22,7 @@
 #include <atomic>
 
 #include "gemm_params.cuh"
+#include "lowra_diag.h"
 #include "ptx.cuh"
 
 namespace lowra {
@@ -95,6 +96,7 @@ struct CeParams {
     uint32_t* status;
     unsigned long long wait_ns;
     int clear_status;
+    int withheld;                                 // diagnostic (lowra_diag_drop_tiles): nothing is loaded behind a pair's first block, so the waits run out
 };
 
 // The factors of a token's O and of its label's row of W in dX.
@@ -208,12 +210,14 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             const bool has_a = KIND == kFew || (int)crank < P.a_halves;
             int s = 0;
             uint32_t ph = 0;
-            for (int u = pair; u < units && !failed; u += pairs) {
+            const int loaded = P.withheld ? pair + 1 : units;
+            for (int u = pair; u < loaded && !failed; u += pairs) {
                 const int t = tile_of(u);
                 const int m0 = KIND == kFew ? P.v0 + t * P.width + (int)crank * (P.width / 2) : t % P.tiles_m * kTile + (int)crank * 128;
                 const int n0 = KIND == kFew ? (int)crank * (P.columns / 2) : t / P.tiles_m * P.width + (int)crank * (P.width / 2);
                 int kb0;
-                const int n = blocks_of(u, &kb0);
+                int n = blocks_of(u, &kb0);
+                if (P.withheld && n > 1) n = 1;
                 for (int kb = kb0; kb < kb0 + n; ++kb) {
                     if (!ptx::mbar_wait_lanes(&bars->empty[s], ph ^ 1u, abort_flag, P.wait_ns)) { failed = true; break; }
                     unsigned char* a_s = smem + s * kStage;
@@ -726,6 +730,8 @@ CePlan plan_of(int M, int V, int K, bool grad) {
     return p;
 }
 
+std::atomic<int> g_dropping{0};     // diagnostic: calls to come, times four, and which of their products (1: the logits', 2: the gradient's) load no more than a first block
+
 bool good_sizes(int M, int V, int K) { return M >= 1 && M <= kMostM && V >= 1 && V <= kMostV && K >= 64 && K <= kMostK && K % 8 == 0; }
 
 // Pairs that a launch has: a unit each at least.
@@ -765,6 +771,12 @@ lowra_status launch_product(CeParams& P, cudaStream_t stream) {
 }  // namespace
 }  // namespace lowra
 
+extern "C" lowra_status lowra_diag_drop_tiles(int32_t calls, int32_t products) {
+    if (calls < 0 || calls > 1000 || products < 1 || products > 3) return LOWRA_ERR_SHAPE;
+    lowra::g_dropping.store(calls > 0 ? calls * 4 + products : 0, std::memory_order_relaxed);
+    return LOWRA_OK;
+}
+
 extern "C" size_t lowra_cross_entropy_workspace_bytes(int32_t M, int32_t V, int32_t K, int32_t grad) {
     using namespace lowra;
     return good_sizes(M, V, K) ? plan_of(M, V, K, grad != 0).total : 0;
@@ -788,6 +800,9 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
     }
     lowra_status st = check_device();
     if (st != LOWRA_OK) return st;
+    int dropping = g_dropping.load(std::memory_order_relaxed);
+    while (dropping >= 4 && !g_dropping.compare_exchange_weak(dropping, dropping - 4, std::memory_order_relaxed)) {}
+    if (dropping < 4) dropping = 0;
     cudaStream_t stream = (cudaStream_t)stream_v;
     unsigned char* ws = static_cast<unsigned char*>(workspace_dev);
     uint32_t* status = reinterpret_cast<uint32_t*>(ws);
@@ -820,6 +835,7 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
         P.ld_e = ld_e;
         P.status = status;
         P.wait_ns = wait_limit_ns();
+        P.withheld = dropping & 1;
         // Up to 128 tokens: the second CTA of a pair has none, and the first loads its own only.  What the tile's other rows hold of earlier kernels comes out in rows that are not looked at.
         // (35006 words, 3672 features, us with all 128 rows of either CTA, past the end filled with zeros, and so: 157, 117 for 12 tokens)
         P.a_halves = m <= 128 ? 1 : 2;
@@ -844,6 +860,7 @@ extern "C" lowra_status lowra_cross_entropy(const uint16_t* X_dev, const uint16_
         CeParams G = P;
         G.N = K;
         G.width = kTile;
+        G.withheld = dropping >> 1 & 1;
         G.tiles_n = (K + kTile - 1) / kTile;
         const CeCut cut = cut_of(m, K, blocks_of_piece(p.piece));
         G.whole = cut.whole;
