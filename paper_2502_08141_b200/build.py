@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import glob
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -21,6 +22,17 @@ NVCC_FLAGS = [
     "--ftz=false", "--prec-div=true", "--prec-sqrt=true", "--fmad=true",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "-Xptxas", "-v",
 ]
+
+# Kernels whose warps give registers to one another: what each is launched with, for which the shares were added up.  With fewer, a warp would wait for registers without end.
+LAUNCH_REGISTERS = {"product_kernel": 168, "gram_kernel": 168, "apply_kernel": 128}
+
+
+def wrong_registers(report: str) -> list:
+    """What ptxas reports (-v) of the kernels of LAUNCH_REGISTERS and is not what they need: (mangled name, registers)."""
+    wrong = []
+    for name, used in re.findall(r"Compiling entry function '(\S+)'.*?Used (\d+) registers", report, re.S):
+        wrong += [(name, int(used)) for kernel, n in LAUNCH_REGISTERS.items() if re.search(rf"\d{kernel}(?![a-z_])", name) and int(used) != n]
+    return wrong
 
 
 def sources():
@@ -68,7 +80,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
         out, _ = p.communicate()
         if verbose or p.returncode != 0:
             sys.stderr.write(f"--- {os.path.basename(src)}\n{out}\n")
-        return p.returncode == 0
+        wrong = wrong_registers(out)
+        if wrong:
+            sys.stderr.write(f"--- {os.path.basename(src)}: registers at launch are not those that the kernels' warps share out: {wrong}\n")
+        return p.returncode == 0 and not wrong
 
     done = [finished(src, p) for src, p in procs]
     if all(done):
