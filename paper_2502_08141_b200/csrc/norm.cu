@@ -520,7 +520,7 @@ template <bool LAYER, int LANES>
 __device__ __forceinline__ void columns_of(const NormParams& P, const BackwardFew& C, int strip) {
     constexpr int kSums = LAYER ? 2 : 1, kUnder = 2;
     constexpr int kCols = 8 * LANES, kRowsOfWarp = 32 / LANES;
-    __shared__ float shared[kMostThreads / 32][kSums][kCols];
+    __shared__ __align__(8) float shared[kMostThreads / 32][kSums][kCols];      // (written in pairs)
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, warps = (int)blockDim.x >> 5, n = strip * kCols + lane % LANES * 8;
     float2 dw[4], db[4];
 #pragma unroll
