@@ -99,22 +99,25 @@ struct CeParams {
     int withheld;                                 // diagnostic (lowra_diag_drop_tiles): nothing is loaded behind a pair's first block, so the waits run out
 };
 
-// The factors of a token's O and of its label's row of W in dX.
+// The factors of a token's O and of its label's row of W in dX.  S and O are brought to S in [1/2, 1) first: the label may be so far above the lift that its own exponential under it is no fp32 number,
+// while the others are as far above it too.
 struct Factors {
-    float o, w;
+    float o, w, scale;        // of O scale, a power of two, with it; of W
     const uint16_t* row;      // null: the token does not count, or has no word (and o, w are NaN)
 };
 __device__ __forceinline__ Factors factors_of(const CeEnd& E, int m) {
     const long long y = E.labels[m];
     if (y < 0 || y >= E.V) {
         const float none = y == E.ignore ? 0.0f : NAN;
-        return {none, none, nullptr};
+        return {none, none, 1.0f, nullptr};
     }
-    if (y == E.ignore) return {0.0f, 0.0f, nullptr};
+    if (y == E.ignore) return {0.0f, 0.0f, 1.0f, nullptr};
     const float logit = E.rows.logit[m], sum = E.rows.sum[m], c = E.weights != nullptr ? E.scale * E.weights[m] : E.scale;
-    const float own = logit < INFINITY ? exp2f(fmaf(logit, kLog2e, -E.rows.lift[m])) : NAN;
-    const float a = c / (sum + own);
-    return {a, -a * sum, E.W + (size_t)y * E.K};
+    int octaves = 0;
+    const float others = frexpf(sum, &octaves);               // sum = others 2^octaves, others in [1/2, 1), or both zero
+    const float own = logit < INFINITY ? exp2f(fmaf(logit, kLog2e, -(E.rows.lift[m] + (float)octaves))) : NAN;
+    const float a = c / (others + own);
+    return {a, -a * others, exp2f((float)-octaves), E.W + (size_t)y * E.K};
 }
 // Eight features of dX from those of O, at feature k.
 __device__ __forceinline__ uint4 end_of(const Factors& f, const float (&o)[8], int k) {
@@ -127,7 +130,7 @@ __device__ __forceinline__ uint4 end_of(const Factors& f, const float (&o)[8], i
     uint32_t r[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        r[j] = pack_bf16x2(fmaf(f.w, __uint_as_float(x[j] << 16), f.o * o[2 * j]), fmaf(f.w, __uint_as_float(x[j] & 0xffff0000u), f.o * o[2 * j + 1]));
+        r[j] = pack_bf16x2(fmaf(f.w, __uint_as_float(x[j] << 16), f.o * (f.scale * o[2 * j])), fmaf(f.w, __uint_as_float(x[j] & 0xffff0000u), f.o * (f.scale * o[2 * j + 1])));
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
@@ -397,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                     const bool is_whole = u < P.whole, ends = is_whole && P.last != 0;
                     float* out = is_whole ? P.out + (size_t)row * P.N + n0
                                           : P.parts + (size_t)(u - P.whole) * (kTile * kTile) + ((int)crank * 128 + q * 32 + lane) * kTile + c_first * 32;
-                    Factors f = {0.0f, 0.0f, nullptr};
+                    Factors f = {0.0f, 0.0f, 1.0f, nullptr};
                     if (ends && mine) f = factors_of(P.end, row);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
