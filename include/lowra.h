@@ -502,8 +502,8 @@ lowra_status lowra_norm_backward(const uint16_t* dY_dev, const uint16_t* X_dev, 
  * first `dim` values of every head of token m become
  *     scale * (a cos t - b sin t, b cos t + a sin t),     t = positions[m] * frequency of the pair          (inverse != 0: -t, the gradient's turn)
  * in fp32, rounded to bf16 once; the values behind them stay as they are.  Pair i of a head is (value i, value dim/2 + i), or, interleaved, (2i, 2i + 1).
- *   lowra_rotary_turns (host only) writes the pairs' frequencies, in turns a position as fractions of 2^64 (angles at every 32-bit position are then right to 2^-33 of a
- *   turn), and the factor that the turned values get.  frequency_i = base^(-2i/dim), and by kind, for contexts longer than those trained on:
+ *   lowra_rotary_turns (host only) writes the pairs' frequencies, in turns a position as fractions of 2^64 (what is left of a turn at any 32-bit position is then right to 2^-33
+ *   of one; the angle that is used is that as an fp32 number, right to 2^-26), and the factor that the turned values get.  frequency_i = base^(-2i/dim), and by kind, for contexts longer than those trained on:
  *     LOWRA_ROTARY_NONE    as it is;      LOWRA_ROTARY_LINEAR  divided by `factor`;      LOWRA_ROTARY_NTK   base * factor^(dim / (dim - 2)) in the place of base
  *     LOWRA_ROTARY_YARN    pairs that turn more than `high` times in `original` positions as they are, those under `low` divided by `factor`, a ramp over the pairs between;
  *                          turned values times 0.1 ln(factor) + 1

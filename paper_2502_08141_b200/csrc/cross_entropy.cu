@@ -9,13 +9,15 @@
 // so that 1 - p_y = S / (S + E) and a small loss have no cancellation (with e_y among the others, a token known to 0.99 got its gradient to 2^-9 / 0.01).
 // That is two products of 2 M V K operations, where forming the sums first and the exponentials again would be three.
 // The tensor core adds up in fp32 without rounding to nearest, which over 256 additions takes some 2^-18 off a logit; so a logit's sum is formed in segments of 1024 features, which the epilogue
-// adds (losses over 4096 features: error against fp64 2.0e-6 -> 5e-7).
+// adds (losses over 4096 features: error against fp64 2.0e-6 -> 5e-7).  The second product is not cut: over 16000 words that leaves some 4e-6 of dX, which is rounded to bf16 in the end.
+// The exponentials are bf16 in the second product because its operands are of one type and W is bf16 (as two such numbers each they would double that product): 1.4e-4 to 1.5e-4 of the gradient's norm
+// over a vocabulary of 32000 to 50265 words, beside 1.66e-3 for the rounding of dX itself; 2^-9 at most, where one word has all that the label has not.  S is the sum of the unrounded ones.
 //
 // The products: CTA pairs (clusters of two) walk over tiles of 256 tokens x up to 256 words (features), tcgen05.mma with cta_group::2, both operands by TMA, 64 contraction indices
 // (32 KB a CTA) to a stage, six stages; two accumulators in turn, so the epilogue's eight warps work on one tile while the next is formed.
 // Up to 64 tokens and no gradient, bound by reading W: the other way round, 256 words by 32 or 64 tokens, ten stages; a pair's MMAs then take an eighth or a quarter of the time that its words do.
 // Measured: 4096 tokens, 32000 words, 4096 features with the gradient 1400 us at full clock and 1650 under the power cap (at the rate of two library products 1262 and 1509), the tensor pipe 88 to 91 %
-// busy; 777 tokens, 50265 words, 1024 features 188 us (94: nine tokens are all that the fourth tile of them holds, and the pipe is 75 % busy); 16 tokens, 32000 words, 4096 features, loss alone 46 us (W
+// busy; 777 tokens, 50265 words, 1024 features 189 to 193 us (94: nine tokens are all that the fourth tile of them holds, and the pipe is 75 % busy); 16 tokens, 32000 words, 4096 features, loss alone 46 to 48 us (W
 // once: 40.6).
 // warp 0 = TMA, 1 = MMA (of the CTA of rank 0) and TMEM, 4-11 = epilogue.  The 128 columns that an epilogue's thread holds, and 32 more on their way, do not fit into the 168 registers that
 // twelve warps get: the first four give some to the others.  All waits are bounded (lowra_set_wait_limit); no CTA waits for another cluster.

@@ -5,8 +5,9 @@
 // Bound by memory.  A row is taken by one group of threads, eight neighbouring channels (16 bytes) to a thread or two or four times as many, and stays in their
 // registers, or in shared memory, between its statistics and its output: every array is read or written once.  The statistics are sums in fp32 over the registers; the variance is that of the
 // differences from the mean, a second sum, so that a mean far from zero costs no digits.
-// Measured, us, in brackets at the copy rate: forward 333 x 5120 with a residual 5.0 (2.1), one token of 4096 2.0; backward with the weight's gradient 4096 x 4096, residual, 32.6 (20.8: the rows 26, their
-// CTAs' sums 5), layer norm 1001 x 1024 5.6 (1.0: a chain of loads, two sums over a row, and a thousand rows for every column), 256 x 4096 4.6.
+// Measured, us, in brackets at the copy rate: kernels one behind the other on inputs from memory: forward with a residual, layer norm 333 x 5120 5.5 (2.1), 4096 x 4096 25.3 (20.8; root mean square 24.6), one token of 4096 2.0;
+// without one, layer norm 3039 x 3968 15.1 (7.5), 1673 x 10024 25.5 (10.4: one row at work on an SM, two barriers to it); backward with the weight's gradient, root mean square 4096 x 4096, residual, 31.5 to 32.6
+// (20.8: the rows 26, their CTAs' sums 5), layer norm 1001 x 1024 5.4 (1.0: a chain of loads, two sums over a row, and a thousand rows for every column), 256 x 4096 4.1 (1.0), 2048 x 13824 54.4 (26.3).
 #include <algorithm>
 #include <tuple>
 #include <type_traits>
@@ -670,7 +671,8 @@ NormShape shape_of_few(int M, int N, bool layer) {
 }
 // Backward, rows up to which their CTAs and those of the columns are one launch (us with two launches, a CTA to an SM, and so; layer norm / root mean square: 1 x 4096 5.1 / 3.9, 2.0 / 1.8;
 // 256 x 4096 10.5 / 9.4, 4.6 / 4.6; 800 x 264 4.5 / 3.8, 3.4 / 3.3, 1500 x 264 4.9 / 5.0, 4.8 / 4.5, 2000 x 392 6.3 / 5.8, 7.9 / 7.2; 1001 x 1024 7.3 / 6.0, 5.6 / 5.0, 2000 x 1024 11.6 / 8.2, 8.3 / 7.7;
-// 2048 x 2056 17.3 / 15.8, 12.4 / 11.3; 3000 x 4096 29.3 / 26.8, 28.6 / 27.9; 1500 x 13824 55.6 / 49.3, 51.7 / 49.9, 2048 x 13824 67.5 / 60.2, 70.2 / 67.5).
+// 2048 x 2056 17.3 / 15.8, 12.4 / 11.3; 3000 x 4096 29.3 / 26.8, 28.6 / 27.9; 1500 x 13824 55.6 / 49.3, 51.7 / 49.9, 2048 x 13824 67.5 / 60.2, 70.2 / 67.5.  What three arrays take at the copy rate: 256 x 4096 1.0, 1500 x 264 0.4, 2000 x 392 0.7, 1001 x 1024 1.0, 2000 x 1024 1.9, 2048 x 2056 3.9,
+// 3000 x 4096 11.4, 1500 x 13824 19.3, 2048 x 13824 26.3: about the border both ways are two to three times that, as large sums or as inputs read twice).
 int few_rows_of(int N) { return N <= 8192 ? std::min(1024 + N, 2048) : 1536; }
 // Sixteen channels to a thread above 4096, for two CTAs to an SM (600 x 8192 19.1 -> 11.2); few warps would go over the columns' rows for long (128 x 256 with one warp 4.0 us, with eight 1.7;
 // 2048 x 2056 with nine 16.1, with eighteen 12.4; 2048 x 2552, of ten warps a row, twenty 18.6, ten 14.3).

@@ -1,7 +1,8 @@
 // lowra_rotary: positions turned into the heads of queries and keys.  A pair (a, b) of a head's first R values at position p becomes
 //     scale * (a cos t - b sin t, b cos t + a sin t),   t = p * frequency of the pair;   the gradient turns the other way.
 // Pairs lie side by side (interleaved) or half of the R values apart.  The frequencies come in turns (of 2 pi), as fractions of 2^64: the product with a position is taken modulo
-// 2^64, which is modulo one turn, so an angle at any 32-bit position is right to 2^-33 of a turn without a wide multiplication or a reduction.
+// 2^64, which is modulo one turn, so that at any 32-bit position what is left of a turn is right to 2^-33 of one, without a wide multiplication or a
+// reduction.  As an fp32 number, half turns from -1 to 1, it is right to 2^-26 of a turn, 9e-8 radians: cosines and sines are off by 2e-7 at most, absolutely (an output's rounding to bf16 is 2^-9 of it).
 // Bound by memory, 4 bytes for every value.  A CTA takes the heads of a few tokens: its threads first work out the tokens' cosines and sines into shared memory, one pair each,
 // with their first loads already under way, then go over the heads, sixteen values (eight pairs) of a head at a time.
 // Measured: 4096 tokens, 32 + 32 heads of 128 25.4 us (20.8 at the copy rate; at 134 MB filling and draining the memory takes some 3 us), 16 tokens 2.4, one head of 64 for 1346 tokens 3.6.
